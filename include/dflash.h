@@ -50,6 +50,9 @@ extern "C" {
 #define DFLASH_DEV_BAD_PAGE          2   /* page index outside the pool: tile skipped            */
 #define DFLASH_DEV_CTX_OVERFLOW      4   /* position beyond page table capacity: row skipped     */
 #define DFLASH_DEV_TIMEOUT           8   /* a bounded on-chip wait expired: output invalid       */
+#define DFLASH_DEV_BAD_ROW          16   /* page-table row that a page operation cannot take: request left out */
+#define DFLASH_DEV_POOL_FULL        32   /* not enough free pages: request left out             */
+#define DFLASH_DEV_BAD_GROUP        64   /* group bounds not rising or outside the batch: prefixes read unshared */
 
 #define DFLASH_F32   0
 #define DFLASH_BF16  1
@@ -391,6 +394,149 @@ typedef struct {
 } dflash_attn_bwd_args;
 int32_t dflash_block_attention_bwd(dflash_handle* h, const dflash_attn_bwd_args* a /*[host]*/, void* stream);
 
+/* ---- block attention of a batch that shares long prefixes ----
+ * (The paper serves independent sequences; its block attention, App. A.3, is computed here with the keys that several
+ * sequences have in common read and multiplied once for all of them.)
+ * The same result as dflash_block_attention: row r of sequence b attends over the ctx_len[b] cached positions and the
+ * block rows (all of them, or those <= r in mode CAUSAL). Sequences group_start[g] .. group_start[g+1]-1 form group g and
+ * share their first prefix_len[g] positions: these are read from the page-table row of the group's FIRST sequence, the
+ * rest of a sequence from its own row (the own row's entries below the prefix are not looked at, nor does the prefix have to
+ * end on a page border). A sequence with ctx_len[b] < prefix_len[g], and one outside every group, reads its own row only.
+ * All K/V of a prefix are read once per group (and kv head); the rows of all its sequences are the rows of ONE
+ * product with them.
+ * Any rows 1..32, any Hq/Hkv up to 128. bf16 with 8- to 256-token pages runs on the tensor cores (head_dim 64 and
+ * 128); fp32 and smaller pages take a CUDA-core kernel. Two launches (the second merges the partial results of the key ranges in a
+ * fixed order: bit-reproducible). Lengths and groups are device data: a captured call may be replayed with others, as
+ * long as max_ctx_len bounds every ctx_len and prefix_len (longer ones are clamped and set DFLASH_DEV_CTX_OVERFLOW).
+ * group_start must not fall and must lie in 0..batch, else DFLASH_DEV_BAD_GROUP is set and every sequence reads its
+ * own row. A page index outside the pool sets DFLASH_DEV_BAD_PAGE and its keys are left out.
+ * Errors: DFLASH_ERR_INVALID_ARG, DFLASH_ERR_UNSUPPORTED (more than 65535 sequences or groups, Hq/Hkv > 128),
+ * DFLASH_ERR_WORKSPACE. Calls must not overlap in time if they share a workspace. */
+typedef struct {
+    int32_t        mode;         /* DFLASH_ATTN_FULL | DFLASH_ATTN_CAUSAL                     */
+    const void*    q;            /* [device] [batch, rows, Hq, hd], position-encoded          */
+    const void*    k_blk;        /* [device] [batch, rows, Hkv, hd]                           */
+    const void*    v_blk;        /* [device] [batch, rows, Hkv, hd]                           */
+    int32_t        batch, rows;  /* rows <= 32                                                */
+    int32_t        n_groups;     /* >= 0; 0: nothing is shared                                */
+    const int32_t* group_start;  /* [device] [n_groups + 1]                                   */
+    const int32_t* prefix_len;   /* [device] [n_groups]; negative = 0                         */
+    const int32_t* ctx_len;      /* [device] [batch] cached positions, the prefix among them  */
+    int32_t        max_ctx_len;  /* [host value] upper bound of ctx_len and prefix_len        */
+    const int32_t* page_table;   /* [device] [batch, max_pages]                               */
+    int32_t        max_pages;
+    const void*    kv_pool;      /* [device] pool with the layout above                       */
+    int32_t        n_pool_pages;
+    int32_t        layer;        /* which pool layer to read                                  */
+    void*          out;          /* [device] out [batch, rows, Hq, hd]                        */
+    float*         lse_out;      /* [device] out [batch, rows, Hq] fp32, natural log of the sum of exponentials; may be NULL */
+    void*          workspace;    /* [device] >= dflash_prefix_attention_workspace_bytes(...), 256-byte aligned */
+    int64_t        workspace_bytes;
+    int32_t*       dev_status;   /* [device] may be NULL                                      */
+} dflash_prefix_attn_args;
+int32_t dflash_prefix_attention(dflash_handle* h, const dflash_prefix_attn_args* a /*[host]*/, void* stream);
+/* Bytes for up to max_batch sequences of up to max_rows rows each in up to max_groups groups. */
+int64_t dflash_prefix_attention_workspace_bytes(const dflash_handle* h, int32_t max_batch, int32_t max_rows, int32_t max_groups);
+
+/* ---- pages of a cache: copy, fork, resize, compact ----
+ * (No counterpart in the paper, which assumes a serving stack around it: these calls make and keep the page tables that every
+ * other call reads.) The state is the page table [n_rows, max_pages] (an entry is a physical page, or negative: none) and
+ * ref_count [n_pool_pages], the number of table entries that hold each page; a page is free when its count is not
+ * positive. All of it lives in device memory, so that the calls chain with the decode cycle without a host round trip.
+ * Fresh pages are the free ones of lowest index, handed out in list order, then in order of position: results do not depend on
+ * timing. Pages that a call releases can be handed out by the NEXT call. Requests are judged by the state at the
+ * call's start and are independent of each other, except that they share the free pages: the requests of a list
+ * are given their pages in list order, and one that does not fit is left out as a whole (DFLASH_DEV_POOL_FULL), as are
+ * those behind it that need a page. A list entry that cannot be carried out is left out as a whole, its row untouched:
+ * row outside the table, a row listed before, a fork whose child row is not empty or whose parent is the child of an entry
+ * of the list (DFLASH_DEV_BAD_ROW); a page index outside the pool or a missing page in what has to be read
+ * (DFLASH_DEV_BAD_PAGE); more positions than a row has entries for (DFLASH_DEV_CTX_OVERFLOW).
+ * kv_pool is the pool of the handle's shape (all layers are copied). Where a second pool is kept under the same
+ * table (a drafter's beside its target's), hand the page copies that a call reports to dflash_pages_copy with the
+ * other handle. Lists hold at most 65535 entries (DFLASH_ERR_UNSUPPORTED). Two launches each (copy: one).
+ * Workspace: dflash_pages_workspace_bytes(n, max_pages, n_pool_pages), 256-byte aligned; calls must not overlap in time. */
+typedef struct {
+    int32_t        n;            /* list entries                                              */
+    const int32_t* count;        /* [device] [1] entries that hold something, if fewer than n; may be NULL */
+    const int32_t* src;          /* [device] [n] page to copy from; negative: nothing to do   */
+    const int32_t* dst;          /* [device] [n] page to copy to                              */
+    const int32_t* n_slots;      /* [device] [n] slots copied, from slot 0 (clamped to 0..page_size); NULL: whole pages */
+    void*          kv_pool;      /* [device]                                                  */
+    int32_t        n_pool_pages;
+    int32_t*       dev_status;   /* [device] may be NULL                                      */
+} dflash_pages_copy_args;
+/* Copies the first n_slots[i] slots of page src[i] onto those of page dst[i]: every layer, K and V, every head. A page
+ * may be the source of several entries. An entry is left out, and DFLASH_DEV_BAD_PAGE set, if a page index lies
+ * outside the pool, if its destination is that of an earlier entry, or if its destination is the source of an entry (a
+ * copy of a page onto itself among them): what is copied never depends on the order. */
+int32_t dflash_pages_copy(dflash_handle* h, const dflash_pages_copy_args* a /*[host]*/, void* stream);
+
+typedef struct {
+    int32_t        n;            /* list entries                                              */
+    const int32_t* parent;       /* [device] [n] rows of the page table                       */
+    const int32_t* child;        /* [device] [n] rows that hold no page yet                   */
+    const int32_t* fork_len;     /* [device] [n] positions that the child takes over (negative = 0) */
+    int32_t*       page_table;   /* [device] in/out [n_rows, max_pages]                       */
+    int32_t        n_rows, max_pages;
+    int32_t*       ref_count;    /* [device] in/out [n_pool_pages]                            */
+    void*          kv_pool;      /* [device] in/out                                           */
+    int32_t        n_pool_pages;
+    int32_t*       copy_src;     /* [device] out [n] the page copies made (one per entry at most; -1: none), for   */
+    int32_t*       copy_dst;     /* [device] out [n] dflash_pages_copy on another pool; all three may be NULL      */
+    int32_t*       copy_slots;   /* [device] out [n]                                          */
+    void*          workspace;    /* [device]                                                  */
+    int64_t        workspace_bytes;
+    int32_t*       dev_status;   /* [device] may be NULL                                      */
+} dflash_pages_fork_args;
+/* The child's row takes over the parent's pages of its first fork_len positions: pages that these fill are shared (their
+ * count rises by one), a last page that they fill in part is copied into a fresh one, so that parent and child
+ * can both go on writing behind them. */
+int32_t dflash_pages_fork(dflash_handle* h, const dflash_pages_fork_args* a /*[host]*/, void* stream);
+
+typedef struct {
+    int32_t        n;            /* list entries                                              */
+    const int32_t* rows;         /* [device] [n] rows of the page table                       */
+    const int32_t* keep_len;     /* [device] [n] positions whose contents stay (clamped to 0..capacity) */
+    const int32_t* capacity;     /* [device] [n] positions that the row has pages for afterwards; <= 0 releases the row */
+    int32_t*       page_table;   /* [device] in/out [n_rows, max_pages]                       */
+    int32_t        n_rows, max_pages;
+    int32_t*       ref_count;    /* [device] in/out [n_pool_pages]                            */
+    void*          kv_pool;      /* [device] in/out                                           */
+    int32_t        n_pool_pages;
+    int32_t*       copy_src;     /* [device] out [n], as for dflash_pages_fork; all three may be NULL */
+    int32_t*       copy_dst;
+    int32_t*       copy_slots;
+    void*          workspace;    /* [device]                                                  */
+    int64_t        workspace_bytes;
+    int32_t*       dev_status;   /* [device] may be NULL                                      */
+} dflash_pages_resize_args;
+/* Gives a row pages for exactly `capacity` positions: entries behind them are released (count falls by one, entry
+ * becomes -1), missing ones are filled with fresh pages. A page that a position in [keep_len, capacity) falls into and that
+ * another entry of the table holds too is replaced by a fresh one (copy on write: its first keep_len % page_size
+ * slots are copied where it holds kept positions), so those positions can be written without touching another sequence. If two listed rows share such a page, each
+ * gets its own and the old one is free afterwards. */
+int32_t dflash_pages_resize(dflash_handle* h, const dflash_pages_resize_args* a /*[host]*/, void* stream);
+
+typedef struct {
+    int32_t*       page_table;   /* [device] in/out [n_rows, max_pages]                       */
+    int32_t        n_rows, max_pages;
+    int32_t*       ref_count;    /* [device] in/out [n_pool_pages]                            */
+    void*          kv_pool;      /* [device] in/out                                           */
+    int32_t        n_pool_pages;
+    int32_t*       n_live;       /* [device] out [1] pages in use; may be NULL                */
+    int32_t*       copy_src;     /* [device] out [n_pool_pages / 2] the moves, entries past *n_copies are -1;      */
+    int32_t*       copy_dst;     /* [device] out [n_pool_pages / 2] all three may be NULL                          */
+    int32_t*       n_copies;     /* [device] out [1]                                          */
+    void*          workspace;    /* [device]                                                  */
+    int64_t        workspace_bytes;
+    int32_t*       dev_status;   /* [device] may be NULL                                      */
+} dflash_pages_compact_args;
+/* Moves the pages in use to the front of the pool: with n of them, the i-th free page below n takes the contents, the
+ * count and the table entries of the i-th used page at or behind n. Afterwards pages 0..n-1 are in use, the others free. A table
+ * entry at or behind n whose page is not in use is left as it is and sets DFLASH_DEV_BAD_PAGE. */
+int32_t dflash_pages_compact(dflash_handle* h, const dflash_pages_compact_args* a /*[host]*/, void* stream);
+int64_t dflash_pages_workspace_bytes(int32_t max_n, int32_t max_pages, int32_t n_pool_pages);
+
 /* ---- building block: LM head fused with row-wise argmax (Sec. 4.2: LM head shared with the
  * target). ids[m] = argmax_v (W_lm z_m)_v with z = hidden (apply_norm = 0) or
  * z = g_f * hidden / rms(hidden) (apply_norm = 1). */
@@ -479,6 +625,14 @@ int32_t dflash_attention_plan(const dflash_handle* h, int32_t batch, int32_t max
  * K-split cluster, tiles split across CTAs, K-split-cluster phase (0/1). The paper has no counterpart: a test aid. */
 int32_t dflash_gemm_plan_check(int32_t M, int32_t N, int32_t K, int32_t n_groups, int32_t sm_count, int32_t pair_cap,
                                int32_t cluster_cap, int32_t* info /*[host] [6] or NULL*/);
+
+/* How dflash_prefix_attention cuts up a call, walked on the host with the kernels' own arithmetic (no CUDA work; the arrays
+ * are host memory, group_start rising within 0..batch). Returns 0 when every CTA's stretch continues the one before
+ * it, all key tiles are taken once and the partial results fit the workspace; a positive code names the first check that failed, a
+ * negative one bad arguments. info (may be NULL): items, items of groups, key tiles, segments, smallest and largest cost of
+ * a CTA. The paper has no counterpart: a test aid. */
+int32_t dflash_prefix_plan_check(const dflash_handle* h, int32_t batch, int32_t rows, int32_t n_groups, const int32_t* group_start,
+                                 const int32_t* prefix_len, const int32_t* ctx_len, int32_t max_ctx_len, int64_t* info /*[host] [6] or NULL*/);
 
 /* Static description of a return code. */
 const char* dflash_status_string(int32_t code);

@@ -21,6 +21,7 @@ F32, BF16 = 0, 1
 ATTN_FULL, ATTN_CAUSAL = 0, 1
 VERIFY_LOGITS, VERIFY_IDS = 0, 1
 DEV_BAD_TOKEN, DEV_BAD_PAGE, DEV_CTX_OVERFLOW, DEV_TIMEOUT = 1, 2, 4, 8
+DEV_BAD_ROW, DEV_POOL_FULL, DEV_BAD_GROUP = 16, 32, 64
 
 EXPORTS = (
     "dflash_create", "dflash_destroy", "dflash_set_weights", "dflash_workspace_bytes",
@@ -29,7 +30,9 @@ EXPORTS = (
     "dflash_profile_read", "dflash_family_name", "dflash_trace_enable", "dflash_trace_read",
     "dflash_verify_accept_static", "dflash_sample_rows", "dflash_verify_accept_sample",
     "dflash_sample_workspace_bytes", "dflash_target_verify", "dflash_block_loss", "dflash_attention_plan",
-    "dflash_block_attention_bwd", "dflash_gemm_plan_check",
+    "dflash_block_attention_bwd", "dflash_gemm_plan_check", "dflash_prefix_attention",
+    "dflash_prefix_attention_workspace_bytes", "dflash_prefix_plan_check", "dflash_pages_copy", "dflash_pages_fork",
+    "dflash_pages_resize", "dflash_pages_compact", "dflash_pages_workspace_bytes",
 )
 N_FAMILIES = 15
 
@@ -129,6 +132,40 @@ class AttnBwdArgs(C.Structure):
                 ("workspace_bytes", C.c_int64), ("dev_status", C.c_void_p)]
 
 
+class PrefixAttnArgs(C.Structure):
+    _fields_ = [("mode", C.c_int32), ("q", C.c_void_p), ("k_blk", C.c_void_p), ("v_blk", C.c_void_p), ("batch", C.c_int32),
+                ("rows", C.c_int32), ("n_groups", C.c_int32), ("group_start", C.c_void_p), ("prefix_len", C.c_void_p),
+                ("ctx_len", C.c_void_p), ("max_ctx_len", C.c_int32), ("page_table", C.c_void_p), ("max_pages", C.c_int32),
+                ("kv_pool", C.c_void_p), ("n_pool_pages", C.c_int32), ("layer", C.c_int32), ("out", C.c_void_p),
+                ("lse_out", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64), ("dev_status", C.c_void_p)]
+
+
+class PagesCopyArgs(C.Structure):
+    _fields_ = [("n", C.c_int32), ("count", C.c_void_p), ("src", C.c_void_p), ("dst", C.c_void_p), ("n_slots", C.c_void_p),
+                ("kv_pool", C.c_void_p), ("n_pool_pages", C.c_int32), ("dev_status", C.c_void_p)]
+
+
+class PagesForkArgs(C.Structure):
+    _fields_ = [("n", C.c_int32), ("parent", C.c_void_p), ("child", C.c_void_p), ("fork_len", C.c_void_p),
+                ("page_table", C.c_void_p), ("n_rows", C.c_int32), ("max_pages", C.c_int32), ("ref_count", C.c_void_p),
+                ("kv_pool", C.c_void_p), ("n_pool_pages", C.c_int32), ("copy_src", C.c_void_p), ("copy_dst", C.c_void_p),
+                ("copy_slots", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64), ("dev_status", C.c_void_p)]
+
+
+class PagesResizeArgs(C.Structure):
+    _fields_ = [("n", C.c_int32), ("rows", C.c_void_p), ("keep_len", C.c_void_p), ("capacity", C.c_void_p),
+                ("page_table", C.c_void_p), ("n_rows", C.c_int32), ("max_pages", C.c_int32), ("ref_count", C.c_void_p),
+                ("kv_pool", C.c_void_p), ("n_pool_pages", C.c_int32), ("copy_src", C.c_void_p), ("copy_dst", C.c_void_p),
+                ("copy_slots", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64), ("dev_status", C.c_void_p)]
+
+
+class PagesCompactArgs(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("n_rows", C.c_int32), ("max_pages", C.c_int32), ("ref_count", C.c_void_p),
+                ("kv_pool", C.c_void_p), ("n_pool_pages", C.c_int32), ("n_live", C.c_void_p), ("copy_src", C.c_void_p),
+                ("copy_dst", C.c_void_p), ("n_copies", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
+                ("dev_status", C.c_void_p)]
+
+
 class LmHeadArgs(C.Structure):
     _fields_ = [("hidden", C.c_void_p), ("hidden_is_f32", C.c_int32), ("n_rows", C.c_int32),
                 ("apply_norm", C.c_int32), ("ids", C.c_void_p), ("top1", C.c_void_p), ("margin", C.c_void_p),
@@ -156,7 +193,9 @@ def load():
                      ("dflash_verify_accept", VerifyArgs), ("dflash_verify_accept_static", VerifyArgs), ("dflash_block_attention", AttnArgs),
                      ("dflash_lmhead_argmax", LmHeadArgs), ("dflash_sample_rows", SampleArgs),
                      ("dflash_verify_accept_sample", VerifySampleArgs), ("dflash_target_verify", TargetArgs),
-                     ("dflash_block_loss", BlockLossArgs), ("dflash_block_attention_bwd", AttnBwdArgs)):
+                     ("dflash_block_loss", BlockLossArgs), ("dflash_block_attention_bwd", AttnBwdArgs),
+                     ("dflash_prefix_attention", PrefixAttnArgs), ("dflash_pages_copy", PagesCopyArgs), ("dflash_pages_fork", PagesForkArgs),
+                     ("dflash_pages_resize", PagesResizeArgs), ("dflash_pages_compact", PagesCompactArgs)):
         fn = getattr(lib, name)
         fn.argtypes = [C.c_void_p, C.POINTER(st), C.c_void_p]
         fn.restype = C.c_int32
@@ -166,6 +205,13 @@ def load():
     lib.dflash_attention_plan.restype = C.c_int32
     lib.dflash_gemm_plan_check.argtypes = [C.c_int32] * 7 + [C.POINTER(C.c_int32)]
     lib.dflash_gemm_plan_check.restype = C.c_int32
+    lib.dflash_prefix_attention_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32]
+    lib.dflash_prefix_attention_workspace_bytes.restype = C.c_int64
+    lib.dflash_pages_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+    lib.dflash_pages_workspace_bytes.restype = C.c_int64
+    i32p = C.POINTER(C.c_int32)
+    lib.dflash_prefix_plan_check.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, i32p, i32p, i32p, C.c_int32, C.POINTER(C.c_int64)]
+    lib.dflash_prefix_plan_check.restype = C.c_int32
     lib.dflash_status_string.argtypes = [C.c_int32]
     lib.dflash_status_string.restype = C.c_char_p
     lib.dflash_launch_count.argtypes = []
@@ -202,6 +248,15 @@ def _ptr(t: Optional[torch.Tensor]):
     return C.c_void_p(t.data_ptr())
 
 
+def _ints(t: Optional[torch.Tensor], shape=None):
+    """Pointer of an int32 device tensor (of the given shape)."""
+    if t is None:
+        return None
+    assert t.dtype == torch.int32, "int32 tensor expected"
+    assert shape is None or tuple(t.shape) == tuple(shape), f"shape {tuple(shape)} expected, got {tuple(t.shape)}"
+    return _ptr(t)
+
+
 def _stream(stream) -> C.c_void_p:
     s = stream if stream is not None else torch.cuda.current_stream()
     return C.c_void_p(s.cuda_stream)
@@ -227,6 +282,7 @@ class DFlash:
         self.h = hp
         self._keep = {}
         self._ws = None
+        self._scratches = {}
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
 
     def close(self):
@@ -453,6 +509,99 @@ class DFlash:
                         1 if shared_page_row else 0, _ptr(dq), _ptr(dk_blk), _ptr(dv_blk), _ptr(dkv_ctx), _ptr(ws), ws.numel(),
                         _ptr(self.status))
         _check(self.lib.dflash_block_attention_bwd(self.h, C.byref(a), _stream(stream)))
+
+    # ---- a batch over a shared cache --------------------------------------------------------
+    def _scratch(self, name, need, stream):
+        """Workspace of the calls below: grown on demand, on the stream that asks for it. A smaller one stays alive, because
+        a captured graph may still write to it."""
+        if need < 0:
+            raise DFlashError(int(need))
+        kept = self._scratches.setdefault(name, [])
+        if not kept or kept[-1].numel() < need:
+            with torch.cuda.stream(stream):
+                kept.append(torch.empty(max(int(need), 256), dtype=torch.uint8, device=self.device))
+        return kept[-1]
+
+    def _on(self, stream):
+        return stream if stream is not None else torch.cuda.current_stream(self.device)
+
+    def _pool(self, kv_pool):
+        c = self.cfg
+        assert kv_pool.dtype == c.torch_dtype, "pool of the handle's dtype expected"
+        assert tuple(kv_pool.shape) == (c.n_layers, kv_pool.shape[1], 2, c.n_kv_heads, c.page_size, c.head_dim), "pool layout of the handle expected"
+        return _ptr(kv_pool)
+
+    def dflash_prefix_attention(self, mode, q, k_blk, v_blk, group_start, prefix_len, ctx_len, max_ctx_len, page_table, kv_pool, layer,
+                                out, stream=None, lse_out=None):
+        """dflash_block_attention of a batch in which sequences group_start[g] .. group_start[g+1]-1 share their first
+        prefix_len[g] positions (read from the page-table row of the first of them, once for all). group_start int32 [n+1] and
+        prefix_len int32 [n], or both None: nothing is shared."""
+        c = self.cfg
+        S, R = q.shape[0], q.shape[1]
+        for t, heads in ((q, c.n_q_heads), (k_blk, c.n_kv_heads), (v_blk, c.n_kv_heads), (out, c.n_q_heads)):
+            assert t.dtype == c.torch_dtype and tuple(t.shape) == (S, R, heads, c.head_dim), "[batch, rows, heads, head_dim] of the handle's dtype expected"
+        assert lse_out is None or (lse_out.dtype == torch.float32 and tuple(lse_out.shape) == (S, R, c.n_q_heads)), "lse_out [batch, rows, Hq] fp32 expected"
+        n = 0 if prefix_len is None else prefix_len.shape[0]
+        st = self._on(stream)
+        with torch.cuda.device(self.device):
+            ws = self._scratch("prefix_attention", self.lib.dflash_prefix_attention_workspace_bytes(self.h, S, R, n), st)
+            a = PrefixAttnArgs(mode, _ptr(q), _ptr(k_blk), _ptr(v_blk), S, R, n, _ints(group_start, (n + 1,)) if n else None,
+                               _ints(prefix_len, (n,)) if n else None, _ints(ctx_len, (S,)), int(max_ctx_len),
+                               _ints(page_table, (S, page_table.shape[1])), page_table.shape[1], self._pool(kv_pool), kv_pool.shape[1], layer,
+                               _ptr(out), _ptr(lse_out), _ptr(ws), ws.numel(), _ptr(self.status))
+            _check(self.lib.dflash_prefix_attention(self.h, C.byref(a), _stream(st)))
+
+    def dflash_pages_copy(self, src, dst, kv_pool, n_slots=None, count=None, stream=None):
+        """Page src[i] -> dst[i] in every layer (its first n_slots[i] slots); entries with a negative source do nothing,
+        nor do those from count[0] on."""
+        n = src.shape[0]
+        with torch.cuda.device(self.device):
+            a = PagesCopyArgs(n, _ints(count, (1,)), _ints(src, (n,)), _ints(dst, (n,)), _ints(n_slots, (n,)), self._pool(kv_pool), kv_pool.shape[1],
+                              _ptr(self.status))
+            _check(self.lib.dflash_pages_copy(self.h, C.byref(a), _stream(self._on(stream))))
+
+    def _pages_ws(self, n, page_table, ref_count, stream):
+        return self._scratch("pages", self.lib.dflash_pages_workspace_bytes(n, page_table.shape[1], ref_count.shape[0]), stream)
+
+    def dflash_pages_fork(self, parent, child, fork_len, page_table, ref_count, kv_pool, copies=None, stream=None):
+        """Row child[i] takes over the first fork_len[i] positions of row parent[i]: whole pages shared, a last partial one
+        copied. copies = (src, dst, n_slots), int32 [n] each, receives the page copies made."""
+        n = parent.shape[0]
+        rows, width = page_table.shape
+        st = self._on(stream)
+        cs, cd, cn = copies if copies is not None else (None, None, None)
+        with torch.cuda.device(self.device):
+            ws = self._pages_ws(n, page_table, ref_count, st)
+            a = PagesForkArgs(n, _ints(parent, (n,)), _ints(child, (n,)), _ints(fork_len, (n,)), _ints(page_table), rows, width,
+                              _ints(ref_count, (kv_pool.shape[1],)), self._pool(kv_pool), kv_pool.shape[1], _ints(cs, (n,)), _ints(cd, (n,)),
+                              _ints(cn, (n,)), _ptr(ws), ws.numel(), _ptr(self.status))
+            _check(self.lib.dflash_pages_fork(self.h, C.byref(a), _stream(st)))
+
+    def dflash_pages_resize(self, rows, keep_len, capacity, page_table, ref_count, kv_pool, copies=None, stream=None):
+        """Row rows[i] gets pages for capacity[i] positions (0 releases it), its own ones from position keep_len[i] on."""
+        n = rows.shape[0]
+        n_rows, width = page_table.shape
+        st = self._on(stream)
+        cs, cd, cn = copies if copies is not None else (None, None, None)
+        with torch.cuda.device(self.device):
+            ws = self._pages_ws(n, page_table, ref_count, st)
+            a = PagesResizeArgs(n, _ints(rows, (n,)), _ints(keep_len, (n,)), _ints(capacity, (n,)), _ints(page_table), n_rows, width,
+                                _ints(ref_count, (kv_pool.shape[1],)), self._pool(kv_pool), kv_pool.shape[1], _ints(cs, (n,)), _ints(cd, (n,)),
+                                _ints(cn, (n,)), _ptr(ws), ws.numel(), _ptr(self.status))
+            _check(self.lib.dflash_pages_resize(self.h, C.byref(a), _stream(st)))
+
+    def dflash_pages_compact(self, page_table, ref_count, kv_pool, n_live=None, copies=None, stream=None):
+        """Moves the pages in use to the front of the pool. n_live int32 [1] receives their number; copies = (src, dst, count),
+        int32 [n_pool_pages // 2], the same, and [1], the moves made."""
+        n_rows, width = page_table.shape
+        pages = kv_pool.shape[1]
+        st = self._on(stream)
+        cs, cd, cn = copies if copies is not None else (None, None, None)
+        with torch.cuda.device(self.device):
+            ws = self._pages_ws(0, page_table, ref_count, st)
+            a = PagesCompactArgs(_ints(page_table), n_rows, width, _ints(ref_count, (pages,)), self._pool(kv_pool), pages, _ints(n_live, (1,)),
+                                 _ints(cs, (pages // 2,)), _ints(cd, (pages // 2,)), _ints(cn, (1,)), _ptr(ws), ws.numel(), _ptr(self.status))
+            _check(self.lib.dflash_pages_compact(self.h, C.byref(a), _stream(st)))
 
     def dflash_lmhead_argmax(self, hidden, apply_norm, ids, top1=None, margin=None, logits_out=None, stream=None):
         M = hidden.shape[0]

@@ -2,6 +2,8 @@
 #include "dflash_internal.h"
 #include "gemm_tc.cuh"
 #include "attn_tc.cuh"
+#include "pages.cuh"
+#include "prefix_attn.cuh"
 
 #include <algorithm>
 #include <cstring>
@@ -677,6 +679,97 @@ int32_t dflash_block_attention(dflash_handle* h, const dflash_attn_args* a, void
     } else {
         RUN(FAM_ATTENTION, launch_attention_simt(L, *a));
     }
+    return DFLASH_OK;
+}
+
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+int64_t dflash_prefix_attention_workspace_bytes(const dflash_handle* h, int32_t max_batch, int32_t max_rows, int32_t max_groups) {
+    if (!h || max_batch < 0 || max_rows < 0 || max_rows > 32 || max_groups < 0) return DFLASH_ERR_INVALID_ARG;
+    if (max_batch > 65535 || max_groups > 65535 || !prefix_attn_supported(h->cfg)) return DFLASH_ERR_UNSUPPORTED;
+    return prefix_attn_workspace_bytes(h, max_batch, max_rows, max_groups);
+}
+
+int32_t dflash_prefix_attention(dflash_handle* h, const dflash_prefix_attn_args* a, void* stream) {
+    if (!h || !a) return DFLASH_ERR_INVALID_ARG;
+    if (a->batch < 0 || a->rows < 0 || a->rows > 32 || a->n_groups < 0 || a->max_pages < 1 || a->n_pool_pages < 1 || a->layer < 0 ||
+        a->layer >= h->cfg.n_layers || a->max_ctx_len < 0)
+        return DFLASH_ERR_INVALID_ARG;
+    if (a->mode != DFLASH_ATTN_FULL && a->mode != DFLASH_ATTN_CAUSAL) return DFLASH_ERR_INVALID_ARG;
+    if (a->batch > 65535 || a->n_groups > 65535 || a->max_ctx_len > INT32_MAX - 512 || !prefix_attn_supported(h->cfg)) return DFLASH_ERR_UNSUPPORTED;
+    if (a->batch == 0 || a->rows == 0) return DFLASH_OK;
+    if (!a->q || !a->k_blk || !a->v_blk || !a->ctx_len || !a->page_table || !a->kv_pool || !a->out || (a->n_groups > 0 && (!a->group_start || !a->prefix_len)))
+        return DFLASH_ERR_INVALID_ARG;
+    if (!aligned16(a->q) || !aligned16(a->k_blk) || !aligned16(a->v_blk) || !aligned16(a->kv_pool) || !aligned16(a->out)) return DFLASH_ERR_INVALID_ARG;
+    if (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 255) ||
+        prefix_attn_workspace_bytes(h, a->batch, a->rows, a->n_groups) > a->workspace_bytes)
+        return DFLASH_ERR_WORKSPACE;
+    Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
+    RUN(FAM_ATTENTION, launch_prefix_attention(L, *a));
+    return DFLASH_OK;
+}
+
+int32_t dflash_prefix_plan_check(const dflash_handle* h, int32_t batch, int32_t rows, int32_t n_groups, const int32_t* group_start,
+                                 const int32_t* prefix_len, const int32_t* ctx_len, int32_t max_ctx_len, int64_t* info) {
+    if (!h || batch < 1 || batch > 65535 || rows < 1 || rows > 32 || n_groups < 0 || n_groups > 65535 || max_ctx_len < 0 || !ctx_len ||
+        (n_groups > 0 && (!group_start || !prefix_len)))
+        return DFLASH_ERR_INVALID_ARG;
+    for (int g = 0; g <= n_groups && n_groups > 0; ++g)
+        if (group_start[g] < 0 || group_start[g] > batch || (g > 0 && group_start[g - 1] > group_start[g])) return DFLASH_ERR_INVALID_ARG;
+    return prefix_plan_check(h->cfg, h->sm_count, batch, rows, n_groups, group_start, prefix_len, ctx_len, max_ctx_len, info);
+}
+
+// ---- pages ----
+int64_t dflash_pages_workspace_bytes(int32_t max_n, int32_t max_pages, int32_t n_pool_pages) {
+    if (max_n < 0 || max_pages < 1 || n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
+    if (max_n > 65535) return DFLASH_ERR_UNSUPPORTED;
+    return pages_workspace_bytes(max_n, max_pages, n_pool_pages);
+}
+static int check_pages_ws(void* ws, int64_t bytes, int n, int max_pages, int n_pages) {
+    return (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) || pages_workspace_bytes(n, max_pages, n_pages) > bytes) ? DFLASH_ERR_WORKSPACE : DFLASH_OK;
+}
+
+int32_t dflash_pages_copy(dflash_handle* h, const dflash_pages_copy_args* a, void* stream) {
+    if (!h || !a || a->n < 0 || a->n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
+    if (a->n > 65535) return DFLASH_ERR_UNSUPPORTED;
+    if (a->n == 0) return DFLASH_OK;
+    if (!a->src || !a->dst || !a->kv_pool || !aligned16(a->kv_pool)) return DFLASH_ERR_INVALID_ARG;
+    Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
+    RUN(FAM_MISC, launch_pages_copy(L, *a));
+    return DFLASH_OK;
+}
+
+int32_t dflash_pages_fork(dflash_handle* h, const dflash_pages_fork_args* a, void* stream) {
+    if (!h || !a || a->n < 0 || a->n_rows < 1 || a->max_pages < 1 || a->n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
+    if (a->n > 65535) return DFLASH_ERR_UNSUPPORTED;
+    if (a->n == 0) return DFLASH_OK;
+    if (!a->parent || !a->child || !a->fork_len || !a->page_table || !a->ref_count || !a->kv_pool || !aligned16(a->kv_pool)) return DFLASH_ERR_INVALID_ARG;
+    if ((a->copy_src != nullptr) != (a->copy_dst != nullptr) || (a->copy_src != nullptr) != (a->copy_slots != nullptr)) return DFLASH_ERR_INVALID_ARG;
+    DFLASH_TRY(check_pages_ws(a->workspace, a->workspace_bytes, a->n, a->max_pages, a->n_pool_pages));
+    Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
+    RUN(FAM_MISC, launch_pages_fork(L, *a));
+    return DFLASH_OK;
+}
+
+int32_t dflash_pages_resize(dflash_handle* h, const dflash_pages_resize_args* a, void* stream) {
+    if (!h || !a || a->n < 0 || a->n_rows < 1 || a->max_pages < 1 || a->n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
+    if (a->n > 65535) return DFLASH_ERR_UNSUPPORTED;
+    if (a->n == 0) return DFLASH_OK;
+    if (!a->rows || !a->keep_len || !a->capacity || !a->page_table || !a->ref_count || !a->kv_pool || !aligned16(a->kv_pool)) return DFLASH_ERR_INVALID_ARG;
+    if ((a->copy_src != nullptr) != (a->copy_dst != nullptr) || (a->copy_src != nullptr) != (a->copy_slots != nullptr)) return DFLASH_ERR_INVALID_ARG;
+    DFLASH_TRY(check_pages_ws(a->workspace, a->workspace_bytes, a->n, a->max_pages, a->n_pool_pages));
+    Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
+    RUN(FAM_MISC, launch_pages_resize(L, *a));
+    return DFLASH_OK;
+}
+
+int32_t dflash_pages_compact(dflash_handle* h, const dflash_pages_compact_args* a, void* stream) {
+    if (!h || !a || a->n_rows < 1 || a->max_pages < 1 || a->n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
+    if (!a->page_table || !a->ref_count || !a->kv_pool || !aligned16(a->kv_pool)) return DFLASH_ERR_INVALID_ARG;
+    if ((a->copy_src != nullptr) != (a->copy_dst != nullptr) || (a->copy_src != nullptr) != (a->n_copies != nullptr)) return DFLASH_ERR_INVALID_ARG;
+    DFLASH_TRY(check_pages_ws(a->workspace, a->workspace_bytes, 0, a->max_pages, a->n_pool_pages));
+    Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
+    RUN(FAM_MISC, launch_pages_compact(L, *a));
     return DFLASH_OK;
 }
 
