@@ -1,0 +1,688 @@
+// Tensor-core kernel of the shared-prefix attention (see prefix_attn.cu), and what it shares with the other kernels there.
+#pragma once
+
+#include "prefix_plan.cuh"
+#include "ptx_sm100.cuh"
+
+#include <math_constants.h>
+
+namespace dflash {
+namespace {
+
+using namespace ptx;
+
+constexpr float GAP = 8.f;               // log2 units by which a tile has to top the running maximum to raise it
+
+struct Params {
+    PlanParams plan;
+    int32_t Hq, page_size, max_pages, n_pages, layer, causal;
+    int32_t box;                         // keys per copy: min(page_size, 64)
+    int32_t rows_per_tile;               // (sequence, row) pairs per query tile
+    int32_t group_slots;                 // partial results of group items come first
+    int32_t own_rows;                    // packed rows of a partial result of a sequence item (a multiple of 8)
+    float scale_log2;
+    const int32_t* page_table;
+    const void *q, *k_blk, *v_blk, *pool;
+    void* out;
+    float* lse;
+    float* part;                         // [group_slots][2][128] rows, then [own slots][2][own_rows]
+    float2* ml;                          // (running maximum in log2 units, sum) of the same rows
+    PlanOut po;
+    int32_t* status;
+    unsigned long long* trace;
+};
+// Partial results are kept in groups of 8 rows x hd: [row / 8][hd / 4][row % 8][4], so that neighbouring threads (rows) write,
+// and the merge's lanes read, whole 128-byte lines.
+__device__ __forceinline__ int64_t slot_row(const Params& p, bool group, int slot, int sub, int row) {
+    return group ? ((int64_t)slot * 2 + sub) * 128 + row : (int64_t)p.group_slots * 256 + ((int64_t)slot * 2 + sub) * p.own_rows + row;
+}
+__device__ __forceinline__ int64_t part_offset(int64_t row, int hd, int c4) { return (row >> 3) * 8 * hd + c4 * 32 + (row & 7) * 4; }
+
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&t);
+}
+
+// ---- tensor-core kernel -----------------------------------------------------------------------------------------
+constexpr int N_THREADS = 384;           // warps 0-3, 4-7: softmax; 8, 11: copies; 9, 10: products of one softmax warpgroup each
+// A softmax thread holds a row of 128 scores. The block is launched with 168 registers a thread (65536 / 384); the third
+// warpgroup gives up 80 of its own: 2 * 208 + 88 = 3 * 168.
+constexpr int REGS_SOFTMAX = 208, REGS_OTHER = 88;
+constexpr int KT = 128;                  // keys per tile
+constexpr uint32_t TMEM_COLS = 512;      // S0 | S1 | O0 | O1, 128 columns each
+constexpr int NI = 16;                   // ring of tile masks: more tiles than the K/V ring can hold (checked below)
+
+struct TileInfo {
+    unsigned long long mask[2];          // keys of each chunk that exist
+    int32_t causal_chunk;                // chunk (0 or 1) that holds the block in causal mode, else 2
+    int32_t full;                        // all 128 keys exist and nothing is causal
+};
+// Shared memory as offsets from a 1024-byte boundary. The roles work with 32-bit addresses that each of them forms anew
+// (role_base): anything they share is spilled for the sake of the softmax threads' registers, and a reload from local memory, which has next to
+// no L1 beside 227 KB of shared memory, cost the MMA warp 0.3 us at every step.
+template <int HD>
+struct Shape {
+    static constexpr int HALVES = HD / 64;                    // 64-element (128-byte) column halves of an operand
+    static constexpr int Q_BYTES = 128 * HD * 2;
+    static constexpr int STAGE = KT * HD * 2;
+    // K and V tiles have a ring each, filled by a warp each: with one ring for both, a warp could come to a stage whose last two uses were
+    // the other warp's and still open, and the wait for a phase's parity would let it pass. A K tile is used up a softmax earlier than its V tile.
+    static constexpr int NK = HD == 128 ? 2 : 5, NV = HD == 128 ? 3 : 5;
+    static constexpr uint32_t RING_K = 2 * Q_BYTES, RING_V = RING_K + NK * STAGE;
+    static constexpr uint32_t Q_FULL = RING_V + NV * STAGE;   // queries and the segment they belong to are there
+    static constexpr uint32_t Q_EMPTY = Q_FULL + 8;           // queries used up, segment read by every softmax warp
+    static constexpr uint32_t FULL_K = Q_EMPTY + 8, FULL_V = FULL_K + 8 * NK;          // [NK], [NV]
+    static constexpr uint32_t EMPTY_K = FULL_V + 8 * NV, EMPTY_V = EMPTY_K + 8 * NK;   // [NK], [NV]
+    static constexpr uint32_t DRAIN = EMPTY_V + 8 * NV;       // [2] all products of an MMA thread that gives up
+    static constexpr uint32_t S_FULL = DRAIN + 16;            // [2] S_t written (and all earlier products done)
+    static constexpr uint32_t P_HALF = S_FULL + 16;           // [2] first 64 keys of P_t written, O_t rescaled, missing V rows zeroed
+    static constexpr uint32_t P_FULL = P_HALF + 16;           // [2] all of P_t written
+    static constexpr uint32_t O_FULL = P_FULL + 16;           // [2] the segment's last product into O_t done
+    static constexpr uint32_t INFO = O_FULL + 16;             // [NI] TileInfo
+    static constexpr uint32_t CUR = INFO + NI * sizeof(TileInfo);       // [2] the segment whose queries are in shared memory, and the one before
+    static constexpr uint32_t TMEM_SLOT = CUR + 2 * sizeof(Segment);
+    static constexpr uint32_t ABORT = TMEM_SLOT + 4;
+    static constexpr int SMEM = 1024 + ABORT + 4;
+    static_assert(SMEM <= 227 * 1024, "shared memory of one CTA");
+    static_assert(NI >= NK + NV + 2, "a tile's mask outlives its K and V stages");
+};
+
+// ---- 32-bit shared-memory addresses ----
+extern __shared__ uint8_t prefix_smem[];
+__device__ __forceinline__ uint32_t role_base() {
+    uint32_t a;
+    asm volatile("mov.u32 %0, %1;" : "=r"(a) : "r"(smem_u32(prefix_smem)));
+    return (a + 1023) & ~1023u;
+}
+__device__ __forceinline__ int lds(uint32_t a) {
+    int v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ unsigned long long lds64(uint32_t a) {
+    unsigned long long v;
+    asm volatile("ld.shared.b64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts(uint32_t a, int v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
+__device__ __forceinline__ void sts64(uint32_t a, unsigned long long v) { asm volatile("st.shared.b64 [%0], %1;" ::"r"(a), "l"(v) : "memory"); }
+__device__ __forceinline__ void zero16(uint32_t a) { asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a), "r"(0) : "memory"); }
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded wait; false if the limit ran out or another role gave up. The loop stays a loop: unrolled at some thirty places it
+// was most of the kernel's code, which then missed the instruction cache.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t abort_at, long long limit = SPIN_LIMIT) {
+    if (bar_try(bar, parity)) return true;
+    const long long t0 = clock64();
+#pragma unroll 1
+    while (!bar_try(bar, parity)) {
+        if ((abort_at && lds(abort_at)) || clock64() - t0 > limit) return false;
+    }
+    return true;
+}
+// lane 0 waits, the warp learns the outcome
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t abort_at) {
+    int ok = 0;
+    if ((threadIdx.x & 31) == 0) ok = bar_wait(bar, parity, abort_at);
+    ok = __shfl_sync(0xffffffffu, ok, 0);
+    __syncwarp();
+    return ok != 0;
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar, uint64_t policy) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar), "l"(policy)
+                 : "memory");
+}
+__device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar, uint64_t policy) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar), "l"(policy)
+                 : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+template <int N> __device__ __forceinline__ void reg_alloc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void reg_dealloc() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// two fp32 operations an instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Low words: K-major operand (leading offset unused); V tile as MN-major operand, [key][64 elements] halves `half_bytes` apart.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_lo_mn(uint32_t addr, uint32_t half_bytes) { return ((addr & 0x3FFFFu) >> 4) | ((half_bytes >> 4) << 16); }
+// D (+)= A B with A in shared memory, or (bf16, M rows in the TMEM lanes, two K elements a column) in TMEM. The high words of the descriptors are the same for every tile here:
+// stride 1024 bytes, version 1, 128-byte swizzle.
+constexpr uint32_t DESC_HI = (1024 >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(DESC_HI)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(DESC_HI)
+        : "memory");
+}
+
+// 2^x for two values of at most 127 without the special-function unit, which at 4 results a clock and SM sub-partition would take as long
+// for a tile's exponentials as the tensor core takes for its products: x = n + f with |f| <= 1/2 by adding and subtracting 1.5 * 2^23, 2^f by a
+// polynomial fitted on Chebyshev nodes (relative error 2.1e-7, as good as ex2.approx), times 2^n put together from its bits.
+// Values below -126 count as -126, NaN stays NaN.
+__device__ __forceinline__ float2 poly_exp2(float2 x) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
+    const float2 big = make_float2(12582912.f, 12582912.f);
+    const float2 t = add2(x, big), n = add2(t, make_float2(-12582912.f, -12582912.f));
+    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
+    float2 y = fma2(f, make_float2(0.0013276468962f, 0.0013276468962f), make_float2(0.0096755409613f, 0.0096755409613f));
+    y = fma2(y, f, make_float2(0.0555071346462f, 0.0555071346462f));
+    y = fma2(y, f, make_float2(0.2402212023735f, 0.2402212023735f));
+    y = fma2(y, f, make_float2(0.6931469440460f, 0.6931469440460f));
+    y = fma2(y, f, make_float2(1.0000001192093f, 1.0000001192093f));
+    const float2 s = make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3f800000), __int_as_float((__float_as_int(t.y) << 23) + 0x3f800000));
+    return mul2(y, s);
+}
+
+// ---- copies: warp 8 K tiles, queries and tile masks; warp 11 V tiles ----
+// A copy instruction costs its warp about 0.1 us and a tile of two 64-token pages takes four, hence two warps. The lanes
+// look 32 boxes (64 keys, or a page if that is less) up at a time, so that a tile costs two shuffles besides its copies.
+template <int HD>
+__device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensorMap& tmPool, const CUtensorMap& tmKb, const CUtensorMap& tmVb, const Params& p) {
+    using Sh = Shape<HD>;
+    const uint32_t sb = role_base();
+    const int lane = threadIdx.x & 31;
+    const int vs = threadIdx.x >> 5 == 11;               // V tiles (one copy of the code for both warps: it stays in the instruction cache)
+    const CUtensorMap* tmBlock = vs ? &tmVb : &tmKb;
+    const uint32_t ring = sb + (vs ? Sh::RING_V : Sh::RING_K), full_at = sb + (vs ? Sh::FULL_V : Sh::FULL_K), empty_at = sb + (vs ? Sh::EMPTY_V : Sh::EMPTY_K);
+    const int n_stages = vs ? Sh::NV : Sh::NK;
+    int st = 0;                                          // next stage, and parity of the wait for it
+    uint32_t phase = 1;
+    const uint64_t keep = policy_evict_last(), once = policy_evict_first();
+    const int shift = 31 - __clz(p.box), per_tile = KT >> shift, page_shift = 31 - __clz(p.page_size);
+    const int2 list = __ldcg(p.po.list + blockIdx.x);
+    auto fetch = [&](int k) { return k < list.y && lane < (int)sizeof(Segment) / 4 ? __ldcg(reinterpret_cast<const int*>(p.po.segs + list.x + k) + lane) : 0; };
+    int next = fetch(0);                                 // a word of the next segment per lane
+    int tile0 = 0, n_seg = 0;                            // key tiles of the segments before
+    bool ok = true;
+#pragma unroll 1
+    while (n_seg < list.y) {
+        const int cur = next;
+        next = fetch(n_seg + 1);
+        auto seg = [&](int word) { return __shfl_sync(0xffffffffu, cur, word); };
+#define SEG(field) seg(offsetof(Segment, field) / 4)
+        const int n_chunks = SEG(n_chunks), n = (n_chunks + 1) >> 1;
+        const int ctx_chunks = SEG(ctx_chunks), two = SEG(two), seq = SEG(seq), kvh = SEG(kvh), key0 = SEG(chunk) * CHUNK_KEYS, key_lo = SEG(lo), key_hi = SEG(hi), row0 = SEG(row0);
+        const uint64_t pol = SEG(prefix) ? keep : once;
+        int win = -32, row = -1;                         // boxes win .. win + 31 of the segment: each lane's first pool row, or -1
+        uint32_t there = 0, whole = 0;                   // of these: copied at all, all keys exist
+        auto issue = [&](int j) {                        // this warp's copies of the segment's j-th tile
+            const int box0 = j * per_tile, n_box = min(per_tile, (ctx_chunks * CHUNK_KEYS >> shift) - box0);     // boxes of cached keys
+            if (n_box > 0 && box0 >= win + 32) {
+                win = box0;
+                const int key = key0 + ((box0 + lane) << shift), pg = key >> page_shift;
+                const bool in = key < key_hi && key + p.box > key_lo && box0 + lane < (ctx_chunks * CHUNK_KEYS >> shift);
+                int page = -1;
+                if (in && pg < p.max_pages) page = __ldg(p.page_table + (int64_t)seq * p.max_pages + pg);
+                const bool good = page >= 0 && page < p.n_pages;
+                if (in && !good && !vs && p.status) atomicOr(p.status, DFLASH_DEV_BAD_PAGE);
+                row = good ? (int)(((((int64_t)p.layer * p.n_pages + page) * 2 + vs) * p.plan.Hkv + kvh) * p.page_size) + (key & (p.page_size - 1)) : -1;
+                there = __ballot_sync(0xffffffffu, good);
+                whole = __ballot_sync(0xffffffffu, good && key >= key_lo && key + p.box <= key_hi);
+            }
+            const bool block = ctx_chunks < n_chunks && 2 * j + 2 >= n_chunks;      // the block's chunk is in this tile
+            const int bc = ctx_chunks - 2 * j;           // and which of its two that is
+            const uint32_t sel = n_box > 0 ? (uint32_t)((1ull << n_box) - 1) << (box0 - win) : 0u;
+            if (!vs && lane == 0) {
+                const uint32_t ti = sb + Sh::INFO + ((tile0 + j) % NI) * (uint32_t)sizeof(TileInfo);
+                const bool full = n_box == per_tile && (whole & sel) == sel;
+                if (!full) {
+                    unsigned long long m0 = 0, m1 = 0;
+#pragma unroll 1
+                    for (int x = 0; x < n_box; ++x) {
+                        if (!(there >> (box0 - win + x) & 1)) continue;
+                        const int at = x << shift, key = key0 + j * KT + at;        // column of the tile, key
+                        const int c0 = max(0, key_lo - key), c1 = min(p.box, key_hi - key);
+                        const unsigned long long bits = (c1 >= 64 ? ~0ull : (1ull << c1) - 1) & ~((1ull << c0) - 1);
+                        if (at < 64) m0 |= bits << at;
+                        else m1 |= bits << (at - 64);
+                    }
+                    const unsigned long long rows = (1ull << p.plan.R) - 1;
+                    if (block && bc == 0) m0 = rows;
+                    if (block && bc == 1) m1 = rows;
+                    sts64(ti, m0);
+                    sts64(ti + 8, m1);
+                    sts(ti + offsetof(TileInfo, causal_chunk), block && p.causal ? bc : 2);
+                }
+                sts(ti + offsetof(TileInfo, full), full);
+            }
+            if (!warp_wait(empty_at + 8 * st, phase, sb + Sh::ABORT)) return false;
+            const uint32_t dst = ring + st * Sh::STAGE, bar = full_at + 8 * st;
+            if (lane == 0) bar_expect(bar, (uint32_t)(__popc(there & sel) * p.box + (block ? 32 : 0)) * (HD * 2));
+#pragma unroll 1
+            for (int x = 0; x < n_box; ++x) {
+                const int y = __shfl_sync(0xffffffffu, row, box0 - win + x);
+                if (lane == 0 && y >= 0) {
+#pragma unroll
+                    for (int h = 0; h < Sh::HALVES; ++h) load_2d(dst + h * (KT * 128) + (x << shift) * 128, &tmPool, h * 64, y, bar, pol);
+                }
+            }
+            if (block && lane == 0) {                    // a box of 32 rows: the block, and others that the masks hide
+#pragma unroll
+                for (int h = 0; h < Sh::HALVES; ++h) load_2d(dst + h * (KT * 128) + bc * 8192, tmBlock, kvh * HD + h * 64, seq * p.plan.R, bar, once);
+            }
+            if (++st == n_stages) { st = 0; phase ^= 1; }
+            return true;
+        };
+        // K tiles that do not need a stage the previous segment's last product still reads go ahead of the queries
+        int j = 0;
+        if (!vs) {
+#pragma unroll 1
+            for (; j < min(n, 2) && ok; ++j) ok = issue(j);
+            if (!ok) break;
+            if (n_seg > 0 && !warp_wait(sb + Sh::Q_EMPTY, (n_seg - 1) & 1, sb + Sh::ABORT)) { ok = false; break; }
+            if (lane < (int)sizeof(Segment) / 4) sts(sb + Sh::CUR + (n_seg & 1) * (uint32_t)sizeof(Segment) + 4 * lane, cur);
+            __syncwarp();
+            if (lane == 0) {
+                const int q_row = seq * p.plan.R + row0 / p.plan.G;        // a tile begins with a whole (sequence, row)
+                const uint32_t bytes = (uint32_t)p.plan.row_tile * HD * 2;
+                bar_expect(sb + Sh::Q_FULL, two ? 2 * bytes : bytes);
+#pragma unroll 1
+                for (int t = 0; t <= two; ++t)
+#pragma unroll
+                    for (int h = 0; h < Sh::HALVES; ++h)
+                        load_4d(sb + t * Sh::Q_BYTES + h * (128 * 128), &tmQ, h * 64, 0, kvh, q_row + t * p.rows_per_tile, sb + Sh::Q_FULL, keep);
+            }
+            __syncwarp();
+        }
+#undef SEG
+        ++n_seg;
+#pragma unroll 1
+        for (; j < n && ok; ++j) ok = issue(j);
+        if (!ok) break;
+        tile0 += n;
+    }
+    if (ok && !vs && lane == 0) {                        // an empty segment ends the other roles
+        if (n_seg > 0 && !bar_wait(sb + Sh::Q_EMPTY, (n_seg - 1) & 1, sb + Sh::ABORT)) ok = false;
+        if (ok) {
+            sts(sb + Sh::CUR + (n_seg & 1) * (uint32_t)sizeof(Segment) + offsetof(Segment, n_chunks), 0);
+            bar_arrive(sb + Sh::Q_FULL);
+        }
+    }
+    if (lane == 0 && !ok) {
+        sts(sb + Sh::ABORT, 1);
+        if (p.status) atomicOr(p.status, DFLASH_DEV_TIMEOUT);
+        // copies in flight have to land before the CTA's shared memory is given up
+#pragma unroll 1
+        for (int k = 0; k < n_stages; ++k) bar_wait(full_at + 8 * k, (k < st ? phase : phase ^ 1) ^ 1, 0, DRAIN_LIMIT);      // the last copies into each stage
+        if (!vs && n_seg > 0) bar_wait(sb + Sh::Q_FULL, (n_seg - 1) & 1, 0, DRAIN_LIMIT);
+    }
+}
+
+// ---- products: one thread for each softmax warpgroup (a wait on a barrier takes 0.1 us and more beside two busy softmax warps, even if it has
+// nothing to wait for; one thread for both warpgroups was what bound the kernel) ----
+template <int HD>
+__device__ __forceinline__ void mma_role(const Params& p, int t) {
+    using Sh = Shape<HD>;
+    const uint32_t sb = role_base(), tmem = lds(sb + Sh::TMEM_SLOT);
+    const uint32_t q_desc = desc_lo(sb), k_desc = desc_lo(sb + Sh::RING_K), v_desc = desc_lo_mn(sb + Sh::RING_V, KT * 128);
+    uint32_t tile0 = 0;                                  // key tiles of the segments before
+    uint32_t p_phase = 0;                                // parity of the next waits for P_t
+    bool ok = true;
+#pragma unroll 1
+    for (int k = 0;; ++k) {
+        if (!bar_wait(sb + Sh::Q_FULL, k & 1, sb + Sh::ABORT)) { ok = false; break; }
+        const uint32_t cur = sb + Sh::CUR + (k & 1) * (uint32_t)sizeof(Segment);
+        const int two = lds(cur + offsetof(Segment, two)), n_chunks = lds(cur + offsetof(Segment, n_chunks)), n = (n_chunks + 1) >> 1;
+        if (n == 0) break;
+        // Both threads say when they are done with a stage; with one query tile its only user does so twice.
+        auto release = [&](uint32_t bar) {
+            commit(bar);
+            if (!two) commit(bar);
+        };
+        // descriptors differ in their address field alone (14 bits of 16-byte units, far from its end)
+        auto scores = [&](int j) {                // S_t = Q K_j^T
+            const uint32_t st = (tile0 + j) % Sh::NK, kd = k_desc + st * (Sh::STAGE >> 4);
+            if (!bar_wait(sb + Sh::FULL_K + 8 * st, (tile0 + j) / Sh::NK & 1, sb + Sh::ABORT)) return false;
+            tc_fence_after();
+            const uint32_t qd = q_desc + (two ? t * (Sh::Q_BYTES >> 4) : 0), d = tmem + t * 128;
+            const uint32_t idesc = instr_desc_bf16(128, 64 * min(2, n_chunks - 2 * j));
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk)
+                mma_ss(d, qd + (kk >> 2) * (128 * 128 >> 4) + (kk & 3) * 2, kd + (kk >> 2) * (KT * 128 >> 4) + (kk & 3) * 2, idesc, kk > 0 ? 1u : 0u);
+            commit(sb + Sh::S_FULL + 8 * t);
+            release(sb + Sh::EMPTY_K + 8 * st);
+            return true;
+        };
+        auto values = [&](int j, bool fresh) {    // O_t (+)= P_t V_j, the first 64 keys as soon as their part of P_t is there
+            const uint32_t st = (tile0 + j) % Sh::NV, vd = v_desc + st * (Sh::STAGE >> 4);
+            constexpr uint32_t idesc = instr_desc_bf16(128, HD) | (1u << 16);     // B is MN-major
+            const uint32_t d = tmem + 256 + t * 128, a = tmem + t * 128, ph = p_phase;
+            p_phase ^= 1;
+            if (!bar_wait(sb + Sh::FULL_V + 8 * st, (tile0 + j) / Sh::NV & 1, sb + Sh::ABORT) || !bar_wait(sb + Sh::P_HALF + 8 * t, ph, sb + Sh::ABORT)) return false;
+            tc_fence_after();
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) mma_ts(d, a + kk * 8, vd + kk * (2048 >> 4), idesc, (!fresh || kk > 0) ? 1u : 0u);
+            if (!bar_wait(sb + Sh::P_FULL + 8 * t, ph, sb + Sh::ABORT)) return false;
+            tc_fence_after();
+            if (n_chunks - 2 * j > 1) {
+#pragma unroll
+                for (int kk = 4; kk < 8; ++kk) mma_ts(d, a + kk * 8, vd + kk * (2048 >> 4), idesc, 1u);
+            }
+            release(sb + Sh::EMPTY_V + 8 * st);
+            return true;
+        };
+        const int first = two ? 0 : t, step = two ? 1 : 2;      // this thread's key tiles; scores run one ahead of values
+        if (first >= n) commit(sb + Sh::Q_EMPTY);
+#pragma unroll 1
+        for (int j = first; j < n + step; j += step) {
+            if (j > first) {
+                if (!(ok = values(j - step, j - step == first))) break;
+                if (j >= n) commit(sb + Sh::O_FULL + 8 * t);
+            }
+            if (j < n) {
+                if (!(ok = scores(j))) break;
+                if (j + step >= n) commit(sb + Sh::Q_EMPTY);
+            }
+        }
+        if (!ok) break;
+        tile0 += n;
+    }
+    if (!ok) {
+        sts(sb + Sh::ABORT, 1);
+        if (p.status) atomicOr(p.status, DFLASH_DEV_TIMEOUT);
+        commit(sb + Sh::DRAIN + 8 * t);                  // TMEM is given back below: no product may still be running
+        bar_wait(sb + Sh::DRAIN + 8 * t, 0, 0, DRAIN_LIMIT);
+    }
+}
+
+// ---- softmax: thread = query row ----
+// P of 32 keys (16 columns), its part of the row sum. FAST: every fourth pair takes the polynomial.
+template <bool FAST>
+__device__ __forceinline__ void softmax_32(const float* s, float scale, float m, float2* sum, uint32_t* pk) {
+    const float2 scale2 = make_float2(scale, scale), neg2 = make_float2(-m, -m);
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+        float2 x = fma2(make_float2(s[2 * c], s[2 * c + 1]), scale2, neg2);
+        if (FAST && (c & 3) == 3) {
+            x = poly_exp2(x);
+        } else {
+            x.x = fast_exp2(x.x);
+            x.y = fast_exp2(x.y);
+        }
+        sum[c & 1] = add2(sum[c & 1], x);
+        pk[c] = pack_bf16(x.x, x.y);                     // P in bf16: as coarse as the operands V and K
+    }
+}
+
+template <int HD>
+__device__ __forceinline__ void softmax_role(const Params& p) {
+    using Sh = Shape<HD>;
+    const uint32_t sb = role_base();
+    const int t = (threadIdx.x >> 7) & 1, ew = (threadIdx.x >> 5) & 3, row = threadIdx.x & 127, lane = threadIdx.x & 31;
+    const uint32_t tS = lds(sb + Sh::TMEM_SLOT) + t * 128 + ((uint32_t)(ew * 32) << 16), tO = tS + 256;
+    uint32_t tile0 = 0;                                  // key tiles of the segments before
+    uint32_t s_phase = 0, o_phase = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (int k = 0;; ++k) {
+        if (!bar_wait(sb + Sh::Q_FULL, k & 1, sb + Sh::ABORT)) { ok = false; break; }
+        const uint32_t cur = sb + Sh::CUR + (k & 1) * (uint32_t)sizeof(Segment);     // stays until this warp, one segment on, arrives on Q_EMPTY
+        const int two = lds(cur + offsetof(Segment, two)), n_chunks = lds(cur + offsetof(Segment, n_chunks)), n = (n_chunks + 1) >> 1;
+        if (n == 0) break;
+        __syncwarp();
+        if (lane == 0) bar_arrive(sb + Sh::Q_EMPTY);
+        auto first_row = [&] { return lds(cur + offsetof(Segment, row0)) + (two ? t * p.plan.row_tile : 0); };
+        const bool busy = ew * 32 < min(p.plan.row_tile, lds(cur + offsetof(Segment, n_rows)) - first_row());       // this warp has rows
+        float m_run = -CUDART_INF_F, l_run = 0.f;
+        const int step = two ? 1 : 2, first = two ? 0 : t;
+#pragma unroll 1
+        for (int j = first; j < n; j += step) {
+            if (!bar_wait(sb + Sh::S_FULL + 8 * t, s_phase, sb + Sh::ABORT)) { ok = false; break; }
+            s_phase ^= 1;
+            tc_fence_after();
+            const uint32_t ti = sb + Sh::INFO + ((tile0 + j) % NI) * (uint32_t)sizeof(TileInfo);
+            const bool all = lds(ti + offsetof(TileInfo, full));
+            if (!all) {
+                // V rows that do not exist must not poison P V: 0 x whatever the page holds there
+                const uint32_t st = (tile0 + j) % Sh::NV;
+                if (!bar_wait(sb + Sh::FULL_V + 8 * st, (tile0 + j) / Sh::NV & 1, sb + Sh::ABORT)) { ok = false; break; }
+                if (!(lds64(ti + 8 * (row >> 6)) >> (row & 63) & 1)) {
+                    const uint32_t v = sb + Sh::RING_V + st * Sh::STAGE + row * 128;
+#pragma unroll
+                    for (int h = 0; h < Sh::HALVES; ++h)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) zero16(v + h * (KT * 128) + c * 16);
+                }
+                fence_proxy_async();
+            }
+            float s[128];
+            float m_use = 0.f, alpha = 1.f;
+            float2 sum[2] = {};
+            if (busy) {
+                tmem_ld32_nowait(tS, s);
+                tmem_ld32_nowait(tS + 32, s + 32);
+                tmem_ld32_nowait(tS + 64, s + 64);
+                tmem_ld32_nowait(tS + 96, s + 96);
+                tmem_ld_wait();
+                if (!all) {
+                    unsigned long long m0 = lds64(ti), m1 = lds64(ti + 8);
+                    const int cc = lds(ti + offsetof(TileInfo, causal_chunk)), r = (first_row() + row) / p.plan.G;      // block row, in a sequence's item
+                    const unsigned long long seen = r >= 63 ? ~0ull : (2ull << r) - 1;
+                    if (cc == 0) m0 &= seen;
+                    if (cc == 1) m1 &= seen;
+                    const uint32_t w4[4] = {(uint32_t)m0, (uint32_t)(m0 >> 32), (uint32_t)m1, (uint32_t)(m1 >> 32)};
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (!(w4[g] >> c & 1)) s[g * 32 + c] = -CUDART_INF_F;
+                }
+                float mx4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+                for (int c = 0; c < 128; c += 2) mx4[(c >> 1) & 3] = max3(mx4[(c >> 1) & 3], s[c], s[c + 1]);
+                const float mx = max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * p.scale_log2;      // scale > 0
+                const bool raise = mx > m_run + GAP || (m_run == -CUDART_INF_F && mx > -CUDART_INF_F);
+                const float m_new = raise ? mx : m_run;
+                alpha = (raise && m_run > -CUDART_INF_F) ? fast_exp2(m_run - m_new) : 1.f;
+                m_use = m_new > -CUDART_INF_F ? m_new : 0.f;
+                m_run = m_new;
+                // every earlier product into O_t is done (S_t was issued behind it)
+                if (j > first && __any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll 1
+                    for (int c = 0; c < HD; c += 16) {
+                        float o[16];
+                        tmem_ld16(tO + c, o);
+#pragma unroll
+                        for (int d = 0; d < 16; ++d) o[d] *= alpha;
+                        tmem_st16(tO + c, reinterpret_cast<const uint32_t*>(o));
+                    }
+                }
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    uint32_t pk[16];
+                    if (all) softmax_32<true>(s + 32 * g, p.scale_log2, m_use, sum, pk);
+                    else softmax_32<false>(s + 32 * g, p.scale_log2, m_use, sum, pk);
+                    tmem_st16(tS + g * 16, pk);
+                }
+                tmem_st_wait();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(sb + Sh::P_HALF + 8 * t);
+            if (busy) {
+#pragma unroll
+                for (int g = 2; g < 4; ++g) {
+                    uint32_t pk[16];
+                    if (all) softmax_32<true>(s + 32 * g, p.scale_log2, m_use, sum, pk);
+                    else softmax_32<false>(s + 32 * g, p.scale_log2, m_use, sum, pk);
+                    tmem_st16(tS + g * 16, pk);
+                }
+                tmem_st_wait();
+                sum[0] = add2(sum[0], sum[1]);
+                l_run = l_run * alpha + (sum[0].x + sum[0].y);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(sb + Sh::P_FULL + 8 * t);
+        }
+        if (!ok) break;
+        // ---- the segment's partial result ----
+        const bool any = n > first;
+        if (any) {
+            if (!bar_wait(sb + Sh::O_FULL + 8 * t, o_phase, sb + Sh::ABORT)) { ok = false; break; }
+            o_phase ^= 1;
+            tc_fence_after();
+        }
+        if (busy) {
+            const int rows_here = min(p.plan.row_tile, lds(cur + offsetof(Segment, n_rows)) - first_row());
+            const int64_t at = slot_row(p, lds(cur + offsetof(Segment, prefix)) != 0, lds(cur + offsetof(Segment, slot)), t, row);
+            if (row < rows_here) p.ml[at] = make_float2(m_run, l_run);
+            if (any) {
+#pragma unroll
+                for (int c4 = 0; c4 < HD / 32; ++c4) {
+                    float o[32];
+                    tmem_ld32_nowait(tO + c4 * 32, o);
+                    tmem_ld_wait();
+                    if (row < rows_here) {
+#pragma unroll
+                        for (int d = 0; d < 32; d += 4)
+                            *reinterpret_cast<float4*>(p.part + part_offset(at, HD, c4 * 8 + d / 4)) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
+                    }
+                }
+            }
+        }
+        tc_fence_before();                               // O_t is read: the next segment's first P_HALF lets it be overwritten
+        tile0 += n;
+    }
+    if (threadIdx.x == 0) trace_max(p.trace, 2);
+    if (!ok) {
+        sts(sb + Sh::ABORT, 1);
+        if (lane == 0 && p.status) atomicOr(p.status, DFLASH_DEV_TIMEOUT);
+    }
+}
+
+template <int HD>
+__global__ void __launch_bounds__(N_THREADS, 1)
+prefix_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmPool, const __grid_constant__ CUtensorMap tmKb,
+                      const __grid_constant__ CUtensorMap tmVb, const __grid_constant__ Params p) {
+    using Sh = Shape<HD>;
+    const uint32_t sb = role_base();
+    const int warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        trace_min(p.trace, 0);
+        bar_init(sb + Sh::Q_FULL, 1);
+        bar_init(sb + Sh::Q_EMPTY, 10);                  // a commit of each MMA warp and one arrival of each softmax warp
+#pragma unroll 1
+        for (int s = 0; s < Sh::NK + Sh::NV; ++s) {
+            bar_init(sb + Sh::FULL_K + 8 * s, 1);
+            bar_init(sb + Sh::EMPTY_K + 8 * s, 2);
+        }
+        for (int t = 0; t < 2; ++t) bar_init(sb + Sh::DRAIN + 8 * t, 1);
+        for (int t = 0; t < 2; ++t) {
+            bar_init(sb + Sh::S_FULL + 8 * t, 1);
+            bar_init(sb + Sh::P_HALF + 8 * t, 4);
+            bar_init(sb + Sh::P_FULL + 8 * t, 4);
+            bar_init(sb + Sh::O_FULL + 8 * t, 1);
+        }
+        sts(sb + Sh::ABORT, 0);
+        fence_barrier_init();
+        fence_proxy_async();
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sb + Sh::TMEM_SLOT), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_trigger();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();
+    if (threadIdx.x == 0) trace_min(p.trace, 1);
+    if (__ldcg(&p.po.list[blockIdx.x].y) == 0) {
+        // nothing to do: on to the end
+    } else if (warp >= 8) {
+        reg_dealloc<REGS_OTHER>();
+        if (warp == 8 || warp == 11) copy_role<HD>(tmQ, tmPool, tmKb, tmVb, p);
+        else if ((threadIdx.x & 31) == 0) mma_role<HD>(p, warp - 9);
+        __syncwarp();
+    } else {
+        reg_alloc<REGS_SOFTMAX>();
+        softmax_role<HD>(p);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x >> 5 == 9) {
+        tc_fence_after();
+        tmem_dealloc(lds(role_base() + Sh::TMEM_SLOT), TMEM_COLS);
+    }
+    if (threadIdx.x == 0) trace_max(p.trace, 3);
+}
+
+}  // namespace
+}  // namespace dflash

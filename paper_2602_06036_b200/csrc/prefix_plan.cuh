@@ -1,14 +1,15 @@
 // How the work of the shared-prefix attention is cut up: one chain of key tiles over all (rows, kv head) items, of which
-// every CTA takes an equal stretch by cost. Shared by the tensor-core kernel, the CUDA-core kernel and the merge.
+// every CTA takes an equal stretch by cost. A small kernel writes each CTA's segments down (the arithmetic inlined into the
+// attention kernel itself made its code 231 KB long and its instruction cache miss all the time: 567 us for what now takes a third).
 //
 // Entries: the groups (rows of all their sequences against the prefix), then the sequences (their rows against what is
 // their own: cached keys behind the prefix, and the block). The query rows of an entry and kv head are "packed":
 // row (b, r, j) of the Hq/Hkv heads j that share the kv head, in this order. An item is one kv head of an entry, up to two tiles
-// of packed rows, and a range of key tiles. Lengths and groups are device data, so each CTA works the chain out itself
-// (one pass of the CTA over groups and sequences).
+// of packed rows, and a range of key tiles.
 #pragma once
 
 #include "dflash_internal.h"
+#include "ptx_sm100.cuh"
 
 namespace dflash {
 namespace {
@@ -31,7 +32,7 @@ struct Entry {
     int32_t chunk0, n_chunks, n_tiles;   // chunks of 64 keys from chunk0 * 64 on, the block's chunk last
     int32_t items, blocks;               // items of row tiles per kv head and key block; key blocks
     int32_t single;                      // 1: the last of these items has one row tile
-    int64_t cost;                        // of all kv heads
+    int32_t cost;                        // of all kv heads
 };
 
 // Clamped length; one that max_ctx_len does not cover is flagged (by `tell`).
@@ -62,27 +63,20 @@ __host__ __device__ __forceinline__ int plan_shared(const PlanParams& p, int g, 
     return len >= P ? P : 0;
 }
 
+// Costs are 32-bit numbers: the host refuses a call whose bound of them is higher (plan_fits).
+//
 // A call of few key tiles is cut into single ones: no cost for an item's start then, which would leave CTAs idle.
-__host__ __device__ __forceinline__ int64_t plan_cost(PlanParams& p, int64_t tiles, int64_t cost, int n_cta) {
-    if (tiles > 2 * (int64_t)n_cta) return cost;
-    p.cost_item = 0;
-    return 0;                            // to be summed up again
-}
-// How many CTAs share a chain of this cost: each stretch is at least as long as the largest distance between the starts of
-// neighbouring key tiles, so that every CTA below this number has one (the merge reads the results of all CTAs from an
-// item's first to its last).
-__host__ __device__ __forceinline__ int plan_ctas(const PlanParams& p, int64_t total, int n_cta) {
-    const int64_t most = total / (p.cost_item + (p.cost_one > p.cost_two ? p.cost_one : p.cost_two));
-    return most < 1 ? 1 : most < n_cta ? (int)most : n_cta;
-}
-
-__host__ __device__ __forceinline__ int64_t plan_lo(int64_t total, int cta, int n_cta) {     // where a CTA's stretch begins
-    return cta < n_cta ? (total * cta + n_cta - 1) / n_cta : total;
+__host__ __device__ __forceinline__ bool plan_few(const PlanParams& p, int tiles, int n_cta) { return tiles <= 2 * n_cta; }
+// Length of a CTA's stretch of costs: its share, and at least the largest distance between the starts of neighbouring key
+// tiles, so that every CTA up to the last used one has a tile (the merge reads the results of all CTAs from an item's first to its last).
+__host__ __device__ __forceinline__ int plan_stretch(const PlanParams& p, int total, int n_cta) {
+    const int share = (total + n_cta - 1) / n_cta, gap = p.cost_item + (p.cost_one > p.cost_two ? p.cost_one : p.cost_two);
+    return share > gap ? share : gap;
 }
 
 // `share`: costs a CTA takes (0: not known yet, key blocks are left at 1). Long prefixes are cut into blocks of about one CTA's
 // share, ordered before the row tiles: CTAs that run side by side then read the same keys, which come out of L2.
-__host__ __device__ __forceinline__ Entry plan_entry(const PlanParams& p, int e, bool groups_ok, int64_t share, bool tell) {
+__host__ __device__ __forceinline__ Entry plan_entry(const PlanParams& p, int e, bool groups_ok, int32_t share, bool tell) {
     Entry x{};
     x.blocks = 1;
     if (e < p.n_groups) {
@@ -106,13 +100,12 @@ __host__ __device__ __forceinline__ Entry plan_entry(const PlanParams& p, int e,
     const int row_tiles = (x.n_rows + p.row_tile - 1) / p.row_tile;
     x.items = (row_tiles + p.tiles_per_item - 1) / p.tiles_per_item;
     x.single = row_tiles % p.tiles_per_item != 0 || p.tiles_per_item == 1;
-    const int64_t one = p.tiles_per_item == 1 ? (int64_t)x.items * p.cost_one : (int64_t)(x.items - x.single) * p.cost_two + x.single * p.cost_one;
+    const int one = p.tiles_per_item == 1 ? x.items * p.cost_one : (x.items - x.single) * p.cost_two + x.single * p.cost_one;
     if (share > 0 && x.items > 1) {
-        const int64_t per = (int64_t)x.n_tiles * p.cost_two;
-        const int64_t blocks = (per + share / 2) / share;
-        x.blocks = blocks < 1 ? 1 : blocks > x.n_tiles ? x.n_tiles : (int)blocks;
+        const int blocks = (x.n_tiles * p.cost_two + share / 2) / share;
+        x.blocks = blocks < 1 ? 1 : blocks > x.n_tiles ? x.n_tiles : blocks;
     }
-    x.cost = (int64_t)p.Hkv * ((int64_t)x.items * x.blocks * p.cost_item + x.n_tiles * one);
+    x.cost = p.Hkv * (x.items * x.blocks * p.cost_item + x.n_tiles * one);
     return x;
 }
 __host__ __device__ __forceinline__ int entry_items(const PlanParams& p, const Entry& x) { return x.n_tiles ? p.Hkv * x.items * x.blocks : 0; }
@@ -124,209 +117,198 @@ struct Segment {
     int32_t lo, hi, block;               // as in Entry
     int32_t chunk, n_chunks;             // first chunk (as 64-key index into the cache) and number; the block's chunk is
     int32_t ctx_chunks;                  //   the one behind ctx_chunks chunks of the segment (block = 1) or absent
-    int32_t item;                        // number among the items of groups, or among those of sequences
     int32_t prefix;                      // an item of a group
-    int32_t first, last;                 // holds the item's first / last key tile
+    int32_t slot;                        // where its partial result goes (group items and sequence items apart)
+    int32_t pad[3];
 };
+static_assert(sizeof(Segment) == 64, "copied by 16 lanes");
 
-// Walks the segments of one CTA. Every thread that walks holds the same state.
-struct Walker {
-    Entry x;
-    int32_t e, kvh, kb, it;              // entry, kv head, key block, item of row tiles
-    int32_t item;                        // number of that item
-    int32_t n_group_items;
-    int64_t start;                       // cost at which it starts
-    int64_t lo, hi;                      // the CTA's stretch of costs
-    int64_t share;
-    bool groups_ok, done;                // done: the item has been looked at
-};
-__host__ __device__ __forceinline__ int block_lo(const Entry& x, int kb) { return (int)((int64_t)x.n_tiles * kb / x.blocks); }
+__host__ __device__ __forceinline__ int block_lo(const Entry& x, int kb) {      // even blocks, the first ones a tile longer
+    const int q = x.n_tiles / x.blocks, r = x.n_tiles % x.blocks;
+    return kb * q + (kb < r ? kb : r);
+}
 __host__ __device__ __forceinline__ int item_cost_tile(const PlanParams& p, const Entry& x, int it) {
     return (p.tiles_per_item == 1 || (x.single && it == x.items - 1)) ? p.cost_one : p.cost_two;
 }
 // first key tile of an item of n tiles that starts at cost `at` or later; tile 0 starts with the item
-__host__ __device__ __forceinline__ int tile_at(const PlanParams& p, int64_t start, int n, int cost, int64_t at) {
+__host__ __device__ __forceinline__ int tile_at(const PlanParams& p, int start, int n, int cost, int at) {
     if (at <= start) return 0;
-    const int64_t j = (at - start - p.cost_item + cost - 1) / cost;
-    return j < 1 ? 1 : j > n ? n : (int)j;
+    const int j = (at - start - p.cost_item + cost - 1) / cost;
+    return j < 1 ? 1 : j > n ? n : j;
+}
+// Item number k of an entry: kv head, key block, item of row tiles; its key tiles, cost a tile and start (from the entry's).
+struct Item {
+    int32_t kvh, kb, it, t0, n, cost, start;
+};
+__host__ __device__ __forceinline__ Item plan_item(const PlanParams& p, const Entry& x, int k) {
+    Item m;
+    m.it = k % x.items;
+    m.kb = k / x.items % x.blocks;
+    m.kvh = k / x.items / x.blocks;
+    m.t0 = block_lo(x, m.kb);
+    m.n = block_lo(x, m.kb + 1) - m.t0;
+    m.cost = item_cost_tile(p, x, m.it);
+    const int full = p.tiles_per_item == 1 ? p.cost_one : p.cost_two;      // of every row tile item but a single last one
+    const int row = (x.items - 1) * full + item_cost_tile(p, x, x.items - 1);
+    m.start = m.kvh * (x.cost / p.Hkv) + m.kb * x.items * p.cost_item + m.t0 * row + m.it * (p.cost_item + m.n * full);
+    return m;
+}
+__host__ __device__ __forceinline__ int item_last(const PlanParams& p, const Item& m) {      // cost at which the last key tile starts, from the item's
+    return m.n > 1 ? p.cost_item + (m.n - 1) * m.cost : 0;
+}
+// The key tiles of the item that CTA `cta` takes (start: cost of the item in the chain); false if none
+__host__ __device__ __forceinline__ bool plan_segment(const PlanParams& p, const Entry& x, const Item& m, int start, int stretch, int cta, Segment& s) {
+    const int a = tile_at(p, start, m.n, m.cost, cta * stretch), b = tile_at(p, start, m.n, m.cost, (cta + 1) * stretch);
+    if (a >= b) return false;
+    s.kvh = m.kvh;
+    s.seq = x.seq;
+    s.n_rows = x.n_rows;
+    s.row0 = m.it * p.tiles_per_item * p.row_tile;
+    s.two = p.tiles_per_item == 2 && !(x.single && m.it == x.items - 1);
+    s.lo = x.lo;
+    s.hi = x.hi;
+    const int c0 = (m.t0 + a) * p.chunks_per_tile, end = (m.t0 + b) * p.chunks_per_tile, c1 = end < x.n_chunks ? end : x.n_chunks;
+    s.chunk = x.chunk0 + c0;
+    s.n_chunks = c1 - c0;
+    s.block = x.block && c1 == x.n_chunks;
+    s.ctx_chunks = s.n_chunks - s.block;
+    return true;
 }
 
-struct PlanShared {
-    int64_t warp[16], warp2[16];
-    int32_t warp_items[16];
-    int32_t n_group_items;
-    int32_t e, item;                     // entry with the CTA's first cost, and the number of its first item
-    int64_t start;
+// What the plan says to the other kernels.
+struct GroupInfo { int32_t item0, items, blocks, single; };
+// group whose prefix items cover this sequence or -1, its first packed row there; its own items
+struct SeqInfo { int32_t group, row_off, item0, blocks; };
+struct PlanOut {
+    Segment* segs;                       // [items + CTAs]: segment of item i in CTA c has index i + c, so a CTA's segments are neighbours
+    int2* list;                          // [CTAs] first segment and number of them
+    int2* ctas;                          // [items] first and last CTA
+    GroupInfo* ginfo;                    // [n_groups]
+    SeqInfo* sinfo;                      // [S]
+    int32_t* start;                      // [n_groups + S] scratch: cost and item at which an entry starts
+    int32_t* item0;                      // [n_groups + S + 1]
+    int32_t* meta;                       // [0] number of group items
 };
 
-// All threads of the CTA (n_threads of them) call this. `infos`: entry's first item and geometry for the merge, written by CTA 0.
-struct GroupInfo { int32_t item0, items, blocks, single; };
-// group whose prefix item covers this sequence or -1, its first packed row there; its own items, numbered from the first sequence's on
-struct SeqInfo { int32_t group, row_off, item0, blocks; };
+constexpr int PLAN_THREADS = 1024, MAX_CTAS = 512, PLAN_CACHE = 2048;
 
-template <int N_THREADS>
-__device__ __forceinline__ bool plan_cta(PlanParams& p, PlanShared& sh, Walker& w, GroupInfo* ginfo, SeqInfo* sinfo) {
-    constexpr int NW = N_THREADS / 32;
-    static_assert(NW <= 16, "scratch");
+// One CTA. Passes of all threads over groups and sequences (total cost, then running costs and items), then one thread per item. What
+// takes its time is latency: lengths and groups are fetched once, into shared memory where they fit (smaller code than
+// 64-bit arithmetic or passes of their own also shows).
+__global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p, const PlanOut o, int grid) {
+    constexpr int NW = PLAN_THREADS / 32;
+    __shared__ int32_t s_cost[NW], s_tiles[NW], s_items[NW];
+    __shared__ int32_t s_first[MAX_CTAS], s_n[MAX_CTAS];
+    __shared__ int32_t s_len[PLAN_CACHE], s_prefix[PLAN_CACHE], s_start[PLAN_CACHE + 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const bool teller = blockIdx.x == 0;
+    ptx::pdl_trigger();
+    for (int c = tid; c < grid; c += PLAN_THREADS) {
+        s_first[c] = 0x7fffffff;
+        s_n[c] = 0;
+    }
+    if (p.S <= PLAN_CACHE) {
+        for (int b = tid; b < p.S; b += PLAN_THREADS) s_len[b] = p.ctx_len[b];
+        p.ctx_len = s_len;
+    }
+    if (p.n_groups <= PLAN_CACHE && p.n_groups > 0) {
+        for (int g = tid; g <= p.n_groups; g += PLAN_THREADS) {
+            s_start[g] = p.group_start[g];
+            if (g < p.n_groups) s_prefix[g] = p.prefix_len[g];
+        }
+        p.group_start = s_start;
+        p.prefix_len = s_prefix;
+    }
+    __syncthreads();
     int bad = 0;
-    for (int g = tid; g <= p.n_groups && p.n_groups > 0; g += N_THREADS) {
+    for (int g = tid; g <= p.n_groups && p.n_groups > 0; g += PLAN_THREADS) {
         const int a = p.group_start[g];
         bad |= a < 0 || a > p.S || (g > 0 && p.group_start[g - 1] > a);
     }
     bad = __syncthreads_or(bad);
     const bool ok = !bad && p.n_groups > 0;
-    if (bad && teller && tid == 0 && p.status) atomicOr(p.status, DFLASH_DEV_BAD_GROUP);
-    const int n = p.n_groups + p.S, per = (n + N_THREADS - 1) / N_THREADS;
+    if (bad && tid == 0 && p.status) atomicOr(p.status, DFLASH_DEV_BAD_GROUP);
+    const int n = p.n_groups + p.S, per = (n + PLAN_THREADS - 1) / PLAN_THREADS;
     const int e0 = min(n, tid * per), e1 = min(n, e0 + per);
-    // total cost with whole prefixes gives the share of a CTA, which gives the key blocks
-    int64_t c = 0, tiles = 0;
-    for (int e = e0; e < e1; ++e) {
-        const Entry x = plan_entry(p, e, ok, 0, teller);
-        c += x.cost;
-        tiles += (int64_t)p.Hkv * x.items * x.n_tiles;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        c += __shfl_xor_sync(0xffffffffu, c, o);
-        tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
-    }
-    if (lane == 0) { sh.warp[warp] = c; sh.warp2[warp] = tiles; }
-    __syncthreads();
-    int64_t raw = 0;
-    tiles = 0;
-    for (int k = 0; k < NW; ++k) { raw += sh.warp[k]; tiles += sh.warp2[k]; }
-    if (plan_cost(p, tiles, raw, gridDim.x) == 0) raw = tiles * p.cost_two;      // both tile costs are close: only key blocks depend on it
-    const int64_t share = (raw + gridDim.x - 1) / gridDim.x;
-    // running costs and items
-    int64_t mine = 0;
-    int items = 0;
-    for (int e = e0; e < e1; ++e) {
-        const Entry x = plan_entry(p, e, ok, share, false);
-        mine += x.cost;
-        items += entry_items(p, x);
-    }
-    int64_t run = mine;
-    int run_items = items;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, run, o);
-        const int z = __shfl_up_sync(0xffffffffu, run_items, o);
-        if (lane >= o) { run += y; run_items += z; }
-    }
-    __syncthreads();
-    if (lane == 31) { sh.warp[warp] = run; sh.warp_items[warp] = run_items; }
-    __syncthreads();
-    run -= mine;
-    run_items -= items;
-    int64_t total = 0;
-    for (int k = 0; k < NW; ++k) {
-        if (k < warp) { run += sh.warp[k]; run_items += sh.warp_items[k]; }
-        total += sh.warp[k];
-    }
-    const int n_cta = plan_ctas(p, total, gridDim.x);
-    const int64_t lo = plan_lo(total, blockIdx.x, n_cta), hi = plan_lo(total, blockIdx.x + 1, n_cta);
-    for (int e = e0; e < e1; ++e) {
-        const Entry x = plan_entry(p, e, ok, share, false);
-        if (x.cost > 0 && run <= lo && lo < run + x.cost) { sh.e = e; sh.item = run_items; sh.start = run; }
-        if (e == p.n_groups) sh.n_group_items = run_items;
-        if (teller) {
-            if (e < p.n_groups) {
-                ginfo[e] = GroupInfo{run_items, x.items, x.blocks, x.single};
-            } else {
-                const int b = e - p.n_groups, g = ok ? plan_group(p, b) : -1;
-                const int shared = plan_shared(p, g, x.hi);
-                sinfo[b] = SeqInfo{shared > 0 ? g : -1, shared > 0 ? (b - p.group_start[g]) * p.R * p.G : 0, run_items /* of all */, x.blocks};
+    // pass 0: total cost with whole prefixes, which gives the share of a CTA and so the key blocks; pass 1: with these, where
+    // each thread's entries start; pass 2: write it down
+    int share = 0, run = 0, run_items = 0, total = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        int cost = 0, tiles = 0, items = 0;
+#pragma unroll 1
+        for (int e = e0; e < e1; ++e) {
+            const Entry x = plan_entry(p, e, ok, share, pass == 0);
+            if (pass == 2) {
+                o.start[e] = run + cost;
+                o.item0[e] = run_items + items;
+                if (e < p.n_groups) {
+                    o.ginfo[e] = GroupInfo{run_items + items, x.items, x.blocks, x.single};
+                } else {
+                    const int b = e - p.n_groups, g = ok ? plan_group(p, b) : -1, shared = plan_shared(p, g, x.hi);
+                    o.sinfo[b] = SeqInfo{shared > 0 ? g : -1, shared > 0 ? (b - p.group_start[g]) * p.R * p.G : 0, run_items + items, x.blocks};
+                    if (b == 0) o.meta[0] = run_items + items;
+                }
             }
+            cost += x.cost;
+            tiles += p.Hkv * x.items * x.n_tiles;
+            items += entry_items(p, x);
+            if (pass == 2 && e == n - 1) o.item0[n] = run_items + items;
         }
-        run += x.cost;
-        run_items += entry_items(p, x);
+        if (pass == 2) break;
+        int c = cost, i = items;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, c, d), z = __shfl_up_sync(0xffffffffu, i, d);
+            if (lane >= d) { c += y; i += z; }
+        }
+        tiles = __reduce_add_sync(0xffffffffu, tiles);
+        __syncthreads();
+        if (lane == 31) { s_cost[warp] = c; s_items[warp] = i; s_tiles[warp] = tiles; }
+        __syncthreads();
+        run = c - cost;
+        run_items = i - items;
+        const int wc = s_cost[lane], wi = s_items[lane];        // one warp's sums per lane
+        run += __reduce_add_sync(0xffffffffu, lane < warp ? wc : 0);
+        run_items += __reduce_add_sync(0xffffffffu, lane < warp ? wi : 0);
+        total = __reduce_add_sync(0xffffffffu, wc);
+        if (pass == 0) {
+            tiles = __reduce_add_sync(0xffffffffu, s_tiles[lane]);
+            if (plan_few(p, tiles, grid)) {
+                p.cost_item = 0;
+                total = tiles * p.cost_two;
+            }
+            share = (total + grid - 1) / grid;
+        }
+    }
+    static_assert(NW == 32, "one lane per warp");
+    const int stretch = plan_stretch(p, total, grid);
+    __syncthreads();                     // the CTA's own global writes are visible to its threads
+    const int n_items = o.item0[n], n_group_items = o.item0[p.n_groups];
+#pragma unroll 1
+    for (int i = tid; i < n_items; i += PLAN_THREADS) {
+        int lo = 0, hi = n;              // last entry that starts at item i or before (entries without items share a start)
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (o.item0[mid] <= i) lo = mid;
+            else hi = mid;
+        }
+        const Entry x = plan_entry(p, lo, ok, share, false);
+        const Item m = plan_item(p, x, i - o.item0[lo]);
+        const int start = o.start[lo] + m.start, c0 = start / stretch, c1 = (start + item_last(p, m)) / stretch;
+        o.ctas[i] = make_int2(c0, c1);
+#pragma unroll 1
+        for (int c = c0; c <= c1; ++c) {
+            Segment s{};
+            if (!plan_segment(p, x, m, start, stretch, c, s)) continue;
+            s.prefix = lo < p.n_groups;
+            s.slot = i + c - (s.prefix ? 0 : n_group_items);
+            o.segs[i + c] = s;
+            atomicMin(&s_first[c], i + c);
+            atomicAdd(&s_n[c], 1);
+        }
     }
     __syncthreads();
-    w.groups_ok = ok;
-    w.share = share;
-    w.lo = lo;
-    w.hi = hi;
-    return lo < hi;
-}
-
-// Positions the walker at the first item that has a key tile at cost w.lo or later.
-__host__ __device__ __forceinline__ void walk_begin(const PlanParams& p, const PlanShared& sh, Walker& w) {
-    w.e = sh.e;
-    w.x = plan_entry(p, w.e, w.groups_ok, w.share, false);
-    const Entry& x = w.x;
-    int64_t off = w.lo - sh.start;
-    const int64_t per_head = x.cost / p.Hkv;
-    w.kvh = (int)(off / per_head);
-    off -= w.kvh * per_head;
-    w.start = sh.start + w.kvh * per_head;
-    w.kb = 0;
-    int64_t two = 0;
-    int n = 0;
-    const int full = x.items - x.single;           // items with cost_two (or, with one tile an item, none)
-    for (;; ++w.kb) {
-        n = block_lo(x, w.kb + 1) - block_lo(x, w.kb);
-        const int64_t c2 = (int64_t)p.cost_item + (int64_t)n * p.cost_two, c1 = (int64_t)p.cost_item + (int64_t)n * p.cost_one;
-        const int64_t cost = p.tiles_per_item == 1 ? x.items * c1 : full * c2 + x.single * c1;
-        if (off < cost || w.kb == x.blocks - 1) { two = p.tiles_per_item == 1 ? c1 : c2; break; }
-        off -= cost;
-        w.start += cost;
-    }
-    w.it = off / two < x.items - 1 ? (int)(off / two) : x.items - 1;
-    w.start += w.it * two;
-    w.n_group_items = sh.n_group_items;
-    w.done = false;
-    w.item = sh.item + (w.kvh * x.blocks + w.kb) * x.items + w.it;
-}
-__host__ __device__ __forceinline__ void walk_on(const PlanParams& p, Walker& w) {       // to the next item
-    const Entry& x = w.x;
-    const int n = block_lo(x, w.kb + 1) - block_lo(x, w.kb);
-    w.start += (int64_t)p.cost_item + (int64_t)n * item_cost_tile(p, x, w.it);
-    ++w.item;
-    w.done = false;
-    if (++w.it < x.items) return;
-    w.it = 0;
-    if (++w.kb < x.blocks) return;
-    w.kb = 0;
-    if (++w.kvh < p.Hkv) return;
-    w.kvh = 0;
-    if (w.start >= w.hi) return;
-    do {
-        if (++w.e >= p.n_groups + p.S) return;
-        w.x = plan_entry(p, w.e, w.groups_ok, w.share, false);
-    } while (w.x.cost == 0);
-}
-// Next segment of this CTA, or false. The step past an item is left to the next call, so that what the segment loads can be
-// requested before the lengths of another sequence are.
-__host__ __device__ __forceinline__ bool walk_next(const PlanParams& p, Walker& w, Segment& s) {
-    for (;;) {
-        if (w.done) walk_on(p, w);
-        if (w.e >= p.n_groups + p.S || w.start >= w.hi) return false;
-        w.done = true;
-        const Entry& x = w.x;
-        const int t0 = block_lo(x, w.kb), n = block_lo(x, w.kb + 1) - t0;
-        const int cost = item_cost_tile(p, x, w.it);
-        const int a = tile_at(p, w.start, n, cost, w.lo), b = tile_at(p, w.start, n, cost, w.hi);
-        if (a >= b) continue;
-        s.kvh = w.kvh;
-        s.seq = x.seq;
-        s.n_rows = x.n_rows;
-        s.row0 = w.it * p.tiles_per_item * p.row_tile;
-        s.two = p.tiles_per_item == 2 && !(x.single && w.it == x.items - 1);
-        s.lo = x.lo;
-        s.hi = x.hi;
-        const int c0 = (t0 + a) * p.chunks_per_tile, c1 = (t0 + b) * p.chunks_per_tile < x.n_chunks ? (t0 + b) * p.chunks_per_tile : x.n_chunks;
-        s.chunk = x.chunk0 + c0;
-        s.n_chunks = c1 - c0;
-        s.block = x.block && c1 == x.n_chunks;
-        s.ctx_chunks = s.n_chunks - s.block;
-        s.prefix = w.e < p.n_groups;
-        s.item = w.item - (s.prefix ? 0 : w.n_group_items);
-        s.first = a == 0;
-        s.last = b == n;
-        return true;
-    }
+    for (int c = tid; c < grid; c += PLAN_THREADS) o.list[c] = make_int2(s_first[c], s_n[c]);
 }
 
 }  // namespace
