@@ -49,13 +49,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 
 // ---- tensor-core kernel -----------------------------------------------------------------------------------------
-constexpr int N_THREADS = 384;           // warps 0-3, 4-7: softmax; 8, 11: copies; 9, 10: products of one softmax warpgroup each
-// A softmax thread holds a row of 128 scores. The block is launched with 168 registers a thread (65536 / 384); the third
-// warpgroup gives up 80 of its own: 2 * 208 + 88 = 3 * 168.
-constexpr int REGS_SOFTMAX = 208, REGS_OTHER = 88;
+constexpr int N_THREADS = 640;           // warps 0-15: softmax; 16, 19: copies; 17, 18: products of one query tile each
+// The block is launched with 96 registers a thread; the last four warps give up 32 of theirs: 512 * 104 + 128 * 64 = 640 * 96.
+constexpr int REGS_SOFTMAX = 104, REGS_OTHER = 64;
 constexpr int KT = 128;                  // keys per tile
 constexpr uint32_t TMEM_COLS = 512;      // S0 | S1 | O0 | O1, 128 columns each
-constexpr int NI = 16;                   // ring of tile masks: more tiles than the K/V ring can hold (checked below)
+constexpr int NI = 12;                   // ring of tile masks: more tiles than the K and V rings can hold (checked below)
 
 struct TileInfo {
     unsigned long long mask[2];          // keys of each chunk that exist
@@ -79,13 +78,14 @@ struct Shape {
     static constexpr uint32_t FULL_K = Q_EMPTY + 8, FULL_V = FULL_K + 8 * NK;          // [NK], [NV]
     static constexpr uint32_t EMPTY_K = FULL_V + 8 * NV, EMPTY_V = EMPTY_K + 8 * NK;   // [NK], [NV]
     static constexpr uint32_t DRAIN = EMPTY_V + 8 * NV;       // [2] all products of an MMA thread that gives up
-    static constexpr uint32_t S_FULL = DRAIN + 16;            // [2] S_t written (and all earlier products done)
-    static constexpr uint32_t P_HALF = S_FULL + 16;           // [2] first 64 keys of P_t written, O_t rescaled, missing V rows zeroed
-    static constexpr uint32_t P_FULL = P_HALF + 16;           // [2] all of P_t written
+    static constexpr uint32_t TURN = DRAIN + 16;              // [2] the other MMA thread has issued its products
+    static constexpr uint32_t S_FULL = TURN + 16;             // [2] S_t written (and all earlier products done)
+    static constexpr uint32_t P_FULL = S_FULL + 16;           // [2] P_t written, O_t rescaled, missing V rows zeroed
     static constexpr uint32_t O_FULL = P_FULL + 16;           // [2] the segment's last product into O_t done
     static constexpr uint32_t INFO = O_FULL + 16;             // [NI] TileInfo
     static constexpr uint32_t CUR = INFO + NI * sizeof(TileInfo);       // [2] the segment whose queries are in shared memory, and the one before
-    static constexpr uint32_t TMEM_SLOT = CUR + 2 * sizeof(Segment);
+    static constexpr uint32_t XCH = CUR + 2 * sizeof(Segment);          // [2][128] words that the two threads of a row exchange
+    static constexpr uint32_t TMEM_SLOT = XCH + 1024;
     static constexpr uint32_t ABORT = TMEM_SLOT + 4;
     static constexpr int SMEM = 1024 + ABORT + 4;
     static_assert(SMEM <= 227 * 1024, "shared memory of one CTA");
@@ -120,11 +120,12 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrie
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "n"(1000000) : "memory");
     return ok != 0;
 }
-// Bounded wait; false if the limit ran out or another role gave up. The loop stays a loop: unrolled at some thirty places it
+// Bounded wait; false if the limit ran out or another role gave up. The hint lets the hardware hold the thread for up to 1 ms a try: warps that
+// poll take issue slots and memory-pipe slots from those that work. The loop stays a loop: unrolled at some thirty places it
 // was most of the kernel's code, which then missed the instruction cache.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t abort_at, long long limit = SPIN_LIMIT) {
     if (bar_try(bar, parity)) return true;
@@ -143,6 +144,15 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_
     __syncwarp();
     return ok != 0;
 }
+// One lane of a converged warp, chosen such that the compiler knows it to be one; and a value that it shall know to be the same in all
+// lanes. Products issued so (whole warp in step, operands in uniform registers) keep their rate beside sixteen busy warps, at 64 clocks
+// each; issued by `lane == 0` they took 71.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.b32 %0, 1, 0, P;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -249,7 +259,7 @@ __device__ __forceinline__ float2 poly_exp2(float2 x) {
     return mul2(y, s);
 }
 
-// ---- copies: warp 8 K tiles, queries and tile masks; warp 11 V tiles ----
+// ---- copies: warp 16 K tiles, queries and tile masks; warp 19 V tiles ----
 // A copy instruction costs its warp about 0.1 us and a tile of two 64-token pages takes four, hence two warps. The lanes
 // look 32 boxes (64 keys, or a page if that is less) up at a time, so that a tile costs two shuffles besides its copies.
 template <int HD>
@@ -257,7 +267,7 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
     using Sh = Shape<HD>;
     const uint32_t sb = role_base();
     const int lane = threadIdx.x & 31;
-    const int vs = threadIdx.x >> 5 == 11;               // V tiles (one copy of the code for both warps: it stays in the instruction cache)
+    const int vs = threadIdx.x >> 5 == 19;               // V tiles (one copy of the code for both warps: it stays in the instruction cache)
     const CUtensorMap* tmBlock = vs ? &tmVb : &tmKb;
     const uint32_t ring = sb + (vs ? Sh::RING_V : Sh::RING_K), full_at = sb + (vs ? Sh::FULL_V : Sh::FULL_K), empty_at = sb + (vs ? Sh::EMPTY_V : Sh::EMPTY_K);
     const int n_stages = vs ? Sh::NV : Sh::NK;
@@ -384,84 +394,91 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
     }
 }
 
-// ---- products: one thread for each softmax warpgroup (a wait on a barrier takes 0.1 us and more beside two busy softmax warps, even if it has
-// nothing to wait for; one thread for both warpgroups was what bound the kernel) ----
+// ---- products: a thread for each query tile ----
+// Products queue up only a few deep behind the issuing thread, and a wait on a barrier takes it 0.1 us even if there is nothing to wait for: one
+// thread for both tiles left the tensor core idle between its groups of products (3370 clocks a key tile with hardly any to do). The
+// threads take turns, so that the products of one tile run while the other tile is at its softmax, and not both tiles' at once.
 template <int HD>
 __device__ __forceinline__ void mma_role(const Params& p, int t) {
     using Sh = Shape<HD>;
-    const uint32_t sb = role_base(), tmem = lds(sb + Sh::TMEM_SLOT);
+    const uint32_t sb = role_base(), tmem = uniform(lds(sb + Sh::TMEM_SLOT));
+    const bool lead = elect_one();
     const uint32_t q_desc = desc_lo(sb), k_desc = desc_lo(sb + Sh::RING_K), v_desc = desc_lo_mn(sb + Sh::RING_V, KT * 128);
     uint32_t tile0 = 0;                                  // key tiles of the segments before
-    uint32_t p_phase = 0;                                // parity of the next waits for P_t
+    uint32_t p_phase = 0, turn = t ^ 1;                  // parities of the next waits; thread 0 begins
     bool ok = true;
 #pragma unroll 1
     for (int k = 0;; ++k) {
         if (!bar_wait(sb + Sh::Q_FULL, k & 1, sb + Sh::ABORT)) { ok = false; break; }
         const uint32_t cur = sb + Sh::CUR + (k & 1) * (uint32_t)sizeof(Segment);
-        const int two = lds(cur + offsetof(Segment, two)), n_chunks = lds(cur + offsetof(Segment, n_chunks)), n = (n_chunks + 1) >> 1;
+        const int two = uniform(lds(cur + offsetof(Segment, two))), n_chunks = uniform(lds(cur + offsetof(Segment, n_chunks))), n = (n_chunks + 1) >> 1;
         if (n == 0) break;
         // Both threads say when they are done with a stage; with one query tile its only user does so twice.
         auto release = [&](uint32_t bar) {
             commit(bar);
             if (!two) commit(bar);
         };
-        // descriptors differ in their address field alone (14 bits of 16-byte units, far from its end)
-        auto scores = [&](int j) {                // S_t = Q K_j^T
-            const uint32_t st = (tile0 + j) % Sh::NK, kd = k_desc + st * (Sh::STAGE >> 4);
-            if (!bar_wait(sb + Sh::FULL_K + 8 * st, (tile0 + j) / Sh::NK & 1, sb + Sh::ABORT)) return false;
-            tc_fence_after();
-            const uint32_t qd = q_desc + (two ? t * (Sh::Q_BYTES >> 4) : 0), d = tmem + t * 128;
-            const uint32_t idesc = instr_desc_bf16(128, 64 * min(2, n_chunks - 2 * j));
-#pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk)
-                mma_ss(d, qd + (kk >> 2) * (128 * 128 >> 4) + (kk & 3) * 2, kd + (kk >> 2) * (KT * 128 >> 4) + (kk & 3) * 2, idesc, kk > 0 ? 1u : 0u);
-            commit(sb + Sh::S_FULL + 8 * t);
-            release(sb + Sh::EMPTY_K + 8 * st);
-            return true;
-        };
-        auto values = [&](int j, bool fresh) {    // O_t (+)= P_t V_j, the first 64 keys as soon as their part of P_t is there
-            const uint32_t st = (tile0 + j) % Sh::NV, vd = v_desc + st * (Sh::STAGE >> 4);
-            constexpr uint32_t idesc = instr_desc_bf16(128, HD) | (1u << 16);     // B is MN-major
-            const uint32_t d = tmem + 256 + t * 128, a = tmem + t * 128, ph = p_phase;
-            p_phase ^= 1;
-            if (!bar_wait(sb + Sh::FULL_V + 8 * st, (tile0 + j) / Sh::NV & 1, sb + Sh::ABORT) || !bar_wait(sb + Sh::P_HALF + 8 * t, ph, sb + Sh::ABORT)) return false;
-            tc_fence_after();
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) mma_ts(d, a + kk * 8, vd + kk * (2048 >> 4), idesc, (!fresh || kk > 0) ? 1u : 0u);
-            if (!bar_wait(sb + Sh::P_FULL + 8 * t, ph, sb + Sh::ABORT)) return false;
-            tc_fence_after();
-            if (n_chunks - 2 * j > 1) {
-#pragma unroll
-                for (int kk = 4; kk < 8; ++kk) mma_ts(d, a + kk * 8, vd + kk * (2048 >> 4), idesc, 1u);
-            }
-            release(sb + Sh::EMPTY_V + 8 * st);
-            return true;
-        };
-        const int first = two ? 0 : t, step = two ? 1 : 2;      // this thread's key tiles; scores run one ahead of values
-        if (first >= n) commit(sb + Sh::Q_EMPTY);
+        const int first = two ? 0 : t, step = two ? 1 : 2;       // this thread's key tiles; scores run one ahead of values
+        const int last = two ? n : n + (n & 1) + t;              // both threads take the same number of turns
+        if (first >= n && lead) commit(sb + Sh::Q_EMPTY);
 #pragma unroll 1
-        for (int j = first; j < n + step; j += step) {
-            if (j > first) {
-                if (!(ok = values(j - step, j - step == first))) break;
-                if (j >= n) commit(sb + Sh::O_FULL + 8 * t);
+        for (int j = first; j <= last; j += step) {
+            const int v = j - step;
+            const bool do_v = v >= first && v < n, do_s = j < n;
+            const uint32_t sv = (tile0 + v) % Sh::NV, sk = (tile0 + j) % Sh::NK;
+            if (do_v) {
+                ok = bar_wait(sb + Sh::FULL_V + 8 * sv, (tile0 + v) / Sh::NV & 1, sb + Sh::ABORT) && bar_wait(sb + Sh::P_FULL + 8 * t, p_phase, sb + Sh::ABORT);
+                p_phase ^= 1;
             }
-            if (j < n) {
-                if (!(ok = scores(j))) break;
-                if (j + step >= n) commit(sb + Sh::Q_EMPTY);
+            if (do_s && ok) ok = bar_wait(sb + Sh::FULL_K + 8 * sk, (tile0 + j) / Sh::NK & 1, sb + Sh::ABORT);
+            ok = ok && bar_wait(sb + Sh::TURN + 8 * t, turn, sb + Sh::ABORT);
+            if (!ok) break;
+            turn ^= 1;
+            tc_fence_after();
+            if (lead) {
+                if (do_v) {                              // O_t (+)= P_t V_v; the first product of a segment starts its accumulator
+                    constexpr uint32_t idesc = instr_desc_bf16(128, HD) | (1u << 16);     // B is MN-major
+                    const uint32_t vd = v_desc + sv * (Sh::STAGE >> 4), d = tmem + 256 + t * 128, a = tmem + t * 128, more = v > first;
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) mma_ts(d, a + kk * 8, vd + kk * (2048 >> 4), idesc, kk > 0 ? 1u : more);
+                    if (n_chunks - 2 * v > 1) {
+#pragma unroll
+                        for (int kk = 4; kk < 8; ++kk) mma_ts(d, a + kk * 8, vd + kk * (2048 >> 4), idesc, 1u);
+                    }
+                    release(sb + Sh::EMPTY_V + 8 * sv);
+                    if (v + step >= n) commit(sb + Sh::O_FULL + 8 * t);
+                }
+                // the other thread needs about 200 clocks to see its turn, and finds these products still running
+                bar_arrive(sb + Sh::TURN + 8 * (t ^ 1));
+                if (do_s) {                              // S_t = Q K_j^T; descriptors differ in their address field alone
+                    const uint32_t kd = k_desc + sk * (Sh::STAGE >> 4), qd = q_desc + (two ? t * (Sh::Q_BYTES >> 4) : 0), d = tmem + t * 128;
+                    const uint32_t idesc = instr_desc_bf16(128, 64 * min(2, n_chunks - 2 * j));
+#pragma unroll
+                    for (int kk = 0; kk < HD / 16; ++kk) {       // 16 elements of the row are 32 bytes; 64 elements on, the other column half begins
+                        const uint32_t o = (kk >> 2) * (KT * 128 >> 4) + (kk & 3) * 2;
+                        mma_ss(d, qd + o, kd + o, idesc, kk > 0);
+                    }
+                    commit(sb + Sh::S_FULL + 8 * t);
+                    release(sb + Sh::EMPTY_K + 8 * sk);
+                    if (j + step >= n) commit(sb + Sh::Q_EMPTY);
+                }
             }
+            __syncwarp();
         }
         if (!ok) break;
         tile0 += n;
     }
     if (!ok) {
         sts(sb + Sh::ABORT, 1);
-        if (p.status) atomicOr(p.status, DFLASH_DEV_TIMEOUT);
-        commit(sb + Sh::DRAIN + 8 * t);                  // TMEM is given back below: no product may still be running
+        if (p.status && lead) atomicOr(p.status, DFLASH_DEV_TIMEOUT);
+        if (lead) commit(sb + Sh::DRAIN + 8 * t);        // TMEM is given back below: no product may still be running
         bar_wait(sb + Sh::DRAIN + 8 * t, 0, 0, DRAIN_LIMIT);
     }
 }
 
-// ---- softmax: thread = query row ----
+// ---- softmax: two threads a query row, of 64 keys each ----
+// Four warps a scheduler hide one another's latencies; with one thread a row (208 registers, two warps a scheduler) a tile's softmax took 2000 to 2900
+// clocks against the 1024 of its products.
 // P of 32 keys (16 columns), its part of the row sum. FAST: every fourth pair takes the polynomial.
 template <bool FAST>
 __device__ __forceinline__ void softmax_32(const float* s, float scale, float m, float2* sum, uint32_t* pk) {
@@ -479,114 +496,117 @@ __device__ __forceinline__ void softmax_32(const float* s, float scale, float m,
         pk[c] = pack_bf16(x.x, x.y);                     // P in bf16: as coarse as the operands V and K
     }
 }
+// Barriers over the 256 threads of one query tile. They are not bounded waits, so all eight warps have to come by: a bounded wait that ran out in
+// one of them ends the others too at the next tile_any.
+__device__ __forceinline__ void tile_bar(int t) { asm volatile("bar.sync %0, 256;" ::"r"(t + 1) : "memory"); }
+__device__ __forceinline__ bool tile_any(int t, bool v) {
+    uint32_t r;
+    __syncwarp();
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %2, 0;\n\tbar.red.or.pred p, %1, 256, q;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r) : "r"(t + 1), "r"((uint32_t)v) : "memory");
+    return r != 0;
+}
 
 template <int HD>
 __device__ __forceinline__ void softmax_role(const Params& p) {
     using Sh = Shape<HD>;
     const uint32_t sb = role_base();
-    const int t = (threadIdx.x >> 7) & 1, ew = (threadIdx.x >> 5) & 3, row = threadIdx.x & 127, lane = threadIdx.x & 31;
-    const uint32_t tS = lds(sb + Sh::TMEM_SLOT) + t * 128 + ((uint32_t)(ew * 32) << 16), tO = tS + 256;
+    const int t = threadIdx.x >> 8, h = (threadIdx.x >> 7) & 1, ew = (threadIdx.x >> 5) & 3, row = threadIdx.x & 127, lane = threadIdx.x & 31;
+    const uint32_t tS = lds(sb + Sh::TMEM_SLOT) + t * 128 + ((uint32_t)(ew * 32) << 16), tO = tS + 256 + h * (HD / 2);
+    const uint32_t xch = sb + Sh::XCH + t * 512;
     uint32_t tile0 = 0;                                  // key tiles of the segments before
     uint32_t s_phase = 0, o_phase = 0;
     bool ok = true;
 #pragma unroll 1
     for (int k = 0;; ++k) {
-        if (!bar_wait(sb + Sh::Q_FULL, k & 1, sb + Sh::ABORT)) { ok = false; break; }
+        ok = bar_wait(sb + Sh::Q_FULL, k & 1, sb + Sh::ABORT);
+        if (tile_any(t, !ok)) { ok = false; break; }
         const uint32_t cur = sb + Sh::CUR + (k & 1) * (uint32_t)sizeof(Segment);     // stays until this warp, one segment on, arrives on Q_EMPTY
         const int two = lds(cur + offsetof(Segment, two)), n_chunks = lds(cur + offsetof(Segment, n_chunks)), n = (n_chunks + 1) >> 1;
         if (n == 0) break;
         __syncwarp();
         if (lane == 0) bar_arrive(sb + Sh::Q_EMPTY);
         auto first_row = [&] { return lds(cur + offsetof(Segment, row0)) + (two ? t * p.plan.row_tile : 0); };
-        const bool busy = ew * 32 < min(p.plan.row_tile, lds(cur + offsetof(Segment, n_rows)) - first_row());       // this warp has rows
-        float m_run = -CUDART_INF_F, l_run = 0.f;
+        float m_run = -CUDART_INF_F, l_run = 0.f;        // l_run: of this thread's keys
         const int step = two ? 1 : 2, first = two ? 0 : t;
 #pragma unroll 1
         for (int j = first; j < n; j += step) {
-            if (!bar_wait(sb + Sh::S_FULL + 8 * t, s_phase, sb + Sh::ABORT)) { ok = false; break; }
+            ok = bar_wait(sb + Sh::S_FULL + 8 * t, s_phase, sb + Sh::ABORT);
             s_phase ^= 1;
             tc_fence_after();
             const uint32_t ti = sb + Sh::INFO + ((tile0 + j) % NI) * (uint32_t)sizeof(TileInfo);
             const bool all = lds(ti + offsetof(TileInfo, full));
-            if (!all) {
+            float s[64];
+            tmem_ld32_nowait(tS + h * 64, s);
+            tmem_ld32_nowait(tS + h * 64 + 32, s + 32);
+            if (!all && h == 0) {
                 // V rows that do not exist must not poison P V: 0 x whatever the page holds there
                 const uint32_t st = (tile0 + j) % Sh::NV;
-                if (!bar_wait(sb + Sh::FULL_V + 8 * st, (tile0 + j) / Sh::NV & 1, sb + Sh::ABORT)) { ok = false; break; }
+                ok = bar_wait(sb + Sh::FULL_V + 8 * st, (tile0 + j) / Sh::NV & 1, sb + Sh::ABORT) && ok;
                 if (!(lds64(ti + 8 * (row >> 6)) >> (row & 63) & 1)) {
                     const uint32_t v = sb + Sh::RING_V + st * Sh::STAGE + row * 128;
 #pragma unroll
-                    for (int h = 0; h < Sh::HALVES; ++h)
+                    for (int x = 0; x < Sh::HALVES; ++x)
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) zero16(v + h * (KT * 128) + c * 16);
+                        for (int c = 0; c < 8; ++c) zero16(v + x * (KT * 128) + c * 16);
                 }
                 fence_proxy_async();
             }
-            float s[128];
-            float m_use = 0.f, alpha = 1.f;
-            float2 sum[2] = {};
-            if (busy) {
-                tmem_ld32_nowait(tS, s);
-                tmem_ld32_nowait(tS + 32, s + 32);
-                tmem_ld32_nowait(tS + 64, s + 64);
-                tmem_ld32_nowait(tS + 96, s + 96);
-                tmem_ld_wait();
-                if (!all) {
-                    unsigned long long m0 = lds64(ti), m1 = lds64(ti + 8);
-                    const int cc = lds(ti + offsetof(TileInfo, causal_chunk)), r = (first_row() + row) / p.plan.G;      // block row, in a sequence's item
-                    const unsigned long long seen = r >= 63 ? ~0ull : (2ull << r) - 1;
-                    if (cc == 0) m0 &= seen;
-                    if (cc == 1) m1 &= seen;
-                    const uint32_t w4[4] = {(uint32_t)m0, (uint32_t)(m0 >> 32), (uint32_t)m1, (uint32_t)(m1 >> 32)};
+            tmem_ld_wait();
+            if (!all) {
+                unsigned long long m = lds64(ti + 8 * h);
+                const int r = (first_row() + row) / p.plan.G;       // block row, in a sequence's item
+                if (lds(ti + offsetof(TileInfo, causal_chunk)) == h) m &= r >= 63 ? ~0ull : (2ull << r) - 1;
+                const uint32_t w[2] = {(uint32_t)m, (uint32_t)(m >> 32)};
 #pragma unroll
-                    for (int g = 0; g < 4; ++g)
+                for (int c = 0; c < 64; ++c)
+                    if (!(w[c >> 5] >> (c & 31) & 1)) s[c] = -CUDART_INF_F;
+            }
+            float mx4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-                        for (int c = 0; c < 32; ++c)
-                            if (!(w4[g] >> c & 1)) s[g * 32 + c] = -CUDART_INF_F;
-                }
-                float mx4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-#pragma unroll
-                for (int c = 0; c < 128; c += 2) mx4[(c >> 1) & 3] = max3(mx4[(c >> 1) & 3], s[c], s[c + 1]);
-                const float mx = max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * p.scale_log2;      // scale > 0
-                const bool raise = mx > m_run + GAP || (m_run == -CUDART_INF_F && mx > -CUDART_INF_F);
-                const float m_new = raise ? mx : m_run;
-                alpha = (raise && m_run > -CUDART_INF_F) ? fast_exp2(m_run - m_new) : 1.f;
-                m_use = m_new > -CUDART_INF_F ? m_new : 0.f;
-                m_run = m_new;
-                // every earlier product into O_t is done (S_t was issued behind it)
-                if (j > first && __any_sync(0xffffffffu, alpha != 1.f)) {
+            for (int c = 0; c < 64; c += 2) mx4[(c >> 1) & 3] = max3(mx4[(c >> 1) & 3], s[c], s[c + 1]);
+            // the row's maximum, in bf16: it serves as a reference only. The barrier also says that all of S_t is in registers:
+            // P_t takes the place of its first half.
+            const uint32_t mine = pack_bf16(max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * p.scale_log2, 0.f) & 0xffffu;      // scale > 0
+            asm volatile("st.shared.b16 [%0], %1;" ::"r"(xch + h * 256 + row * 2), "h"((unsigned short)mine) : "memory");
+            if (tile_any(t, !ok)) { ok = false; break; }
+            unsigned short other;
+            asm volatile("ld.shared.b16 %0, [%1];" : "=h"(other) : "r"(xch + (h ^ 1) * 256 + row * 2) : "memory");
+            const float mx = fmaxf(__uint_as_float(mine << 16), __uint_as_float((uint32_t)other << 16));
+            const bool raise = mx > m_run + GAP || (m_run == -CUDART_INF_F && mx > -CUDART_INF_F);
+            const float m_new = raise ? mx : m_run;
+            const float alpha = (raise && m_run > -CUDART_INF_F) ? fast_exp2(m_run - m_new) : 1.f;
+            const float m_use = m_new > -CUDART_INF_F ? m_new : 0.f;
+            m_run = m_new;
+            // every earlier product into O_t is done (S_t was issued behind it)
+            if (j > first && __any_sync(0xffffffffu, alpha != 1.f)) {
 #pragma unroll 1
-                    for (int c = 0; c < HD; c += 16) {
-                        float o[16];
-                        tmem_ld16(tO + c, o);
+                for (int c = 0; c < HD / 2; c += 16) {
+                    float o[16];
+                    tmem_ld16(tO + c, o);
 #pragma unroll
-                        for (int d = 0; d < 16; ++d) o[d] *= alpha;
-                        tmem_st16(tO + c, reinterpret_cast<const uint32_t*>(o));
-                    }
+                    for (int d = 0; d < 16; ++d) o[d] *= alpha;
+                    tmem_st16(tO + c, reinterpret_cast<const uint32_t*>(o));
                 }
+            }
+            float2 sum[2] = {};
+            if (all) {
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     uint32_t pk[16];
-                    if (all) softmax_32<true>(s + 32 * g, p.scale_log2, m_use, sum, pk);
-                    else softmax_32<false>(s + 32 * g, p.scale_log2, m_use, sum, pk);
-                    tmem_st16(tS + g * 16, pk);
+                    softmax_32<true>(s + 32 * g, p.scale_log2, m_use, sum, pk);
+                    tmem_st16(tS + h * 32 + g * 16, pk);
                 }
-                tmem_st_wait();
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(sb + Sh::P_HALF + 8 * t);
-            if (busy) {
+            } else {
 #pragma unroll
-                for (int g = 2; g < 4; ++g) {
+                for (int g = 0; g < 2; ++g) {
                     uint32_t pk[16];
-                    if (all) softmax_32<true>(s + 32 * g, p.scale_log2, m_use, sum, pk);
-                    else softmax_32<false>(s + 32 * g, p.scale_log2, m_use, sum, pk);
-                    tmem_st16(tS + g * 16, pk);
+                    softmax_32<false>(s + 32 * g, p.scale_log2, m_use, sum, pk);
+                    tmem_st16(tS + h * 32 + g * 16, pk);
                 }
-                tmem_st_wait();
-                sum[0] = add2(sum[0], sum[1]);
-                l_run = l_run * alpha + (sum[0].x + sum[0].y);
             }
+            sum[0] = add2(sum[0], sum[1]);
+            l_run = l_run * alpha + (sum[0].x + sum[0].y);
+            tmem_st_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(sb + Sh::P_FULL + 8 * t);
@@ -595,29 +615,30 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
         // ---- the segment's partial result ----
         const bool any = n > first;
         if (any) {
-            if (!bar_wait(sb + Sh::O_FULL + 8 * t, o_phase, sb + Sh::ABORT)) { ok = false; break; }
+            ok = bar_wait(sb + Sh::O_FULL + 8 * t, o_phase, sb + Sh::ABORT);
             o_phase ^= 1;
             tc_fence_after();
         }
-        if (busy) {
-            const int rows_here = min(p.plan.row_tile, lds(cur + offsetof(Segment, n_rows)) - first_row());
-            const int64_t at = slot_row(p, lds(cur + offsetof(Segment, prefix)) != 0, lds(cur + offsetof(Segment, slot)), t, row);
-            if (row < rows_here) p.ml[at] = make_float2(m_run, l_run);
-            if (any) {
+        const bool mine = row < min(p.plan.row_tile, lds(cur + offsetof(Segment, n_rows)) - first_row());       // the row exists
+        const int64_t at = slot_row(p, lds(cur + offsetof(Segment, prefix)) != 0, lds(cur + offsetof(Segment, slot)), t, row);
+        if (h == 1) sts(xch + 4 * row, __float_as_int(l_run));
+        if (tile_any(t, !ok)) { ok = false; break; }
+        if (h == 0 && mine) p.ml[at] = make_float2(m_run, l_run + __int_as_float(lds(xch + 4 * row)));
+        tile_bar(t);
+        if (any && __any_sync(0xffffffffu, mine)) {
 #pragma unroll
-                for (int c4 = 0; c4 < HD / 32; ++c4) {
-                    float o[32];
-                    tmem_ld32_nowait(tO + c4 * 32, o);
-                    tmem_ld_wait();
-                    if (row < rows_here) {
+            for (int c = 0; c < HD / 2; c += 32) {
+                float o[32];
+                tmem_ld32_nowait(tO + c, o);
+                tmem_ld_wait();
+                if (mine) {
 #pragma unroll
-                        for (int d = 0; d < 32; d += 4)
-                            *reinterpret_cast<float4*>(p.part + part_offset(at, HD, c4 * 8 + d / 4)) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
-                    }
+                    for (int d = 0; d < 32; d += 4)
+                        *reinterpret_cast<float4*>(p.part + part_offset(at, HD, h * (HD / 8) + (c + d) / 4)) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
                 }
             }
         }
-        tc_fence_before();                               // O_t is read: the next segment's first P_HALF lets it be overwritten
+        tc_fence_before();                               // O_t is read: the next segment's first P_FULL lets it be overwritten
         tile0 += n;
     }
     if (threadIdx.x == 0) trace_max(p.trace, 2);
@@ -633,28 +654,30 @@ prefix_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                       const __grid_constant__ CUtensorMap tmVb, const __grid_constant__ Params p) {
     using Sh = Shape<HD>;
     const uint32_t sb = role_base();
-    const int warp = threadIdx.x >> 5;
+    const int warp = uniform(threadIdx.x >> 5);
     if (threadIdx.x == 0) {
         trace_min(p.trace, 0);
         bar_init(sb + Sh::Q_FULL, 1);
-        bar_init(sb + Sh::Q_EMPTY, 10);                  // a commit of each MMA warp and one arrival of each softmax warp
+        bar_init(sb + Sh::Q_EMPTY, 18);                  // a commit of each MMA thread and one arrival of each softmax warp
 #pragma unroll 1
         for (int s = 0; s < Sh::NK + Sh::NV; ++s) {
             bar_init(sb + Sh::FULL_K + 8 * s, 1);
             bar_init(sb + Sh::EMPTY_K + 8 * s, 2);
         }
-        for (int t = 0; t < 2; ++t) bar_init(sb + Sh::DRAIN + 8 * t, 1);
+        for (int t = 0; t < 2; ++t) {
+            bar_init(sb + Sh::DRAIN + 8 * t, 1);
+            bar_init(sb + Sh::TURN + 8 * t, 1);
+        }
         for (int t = 0; t < 2; ++t) {
             bar_init(sb + Sh::S_FULL + 8 * t, 1);
-            bar_init(sb + Sh::P_HALF + 8 * t, 4);
-            bar_init(sb + Sh::P_FULL + 8 * t, 4);
+            bar_init(sb + Sh::P_FULL + 8 * t, 8);
             bar_init(sb + Sh::O_FULL + 8 * t, 1);
         }
         sts(sb + Sh::ABORT, 0);
         fence_barrier_init();
         fence_proxy_async();
     }
-    if (warp == 9) {
+    if (warp == 17) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sb + Sh::TMEM_SLOT), "r"(TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -666,10 +689,10 @@ prefix_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     if (threadIdx.x == 0) trace_min(p.trace, 1);
     if (__ldcg(&p.po.list[blockIdx.x].y) == 0) {
         // nothing to do: on to the end
-    } else if (warp >= 8) {
+    } else if (warp >= 16) {
         reg_dealloc<REGS_OTHER>();
-        if (warp == 8 || warp == 11) copy_role<HD>(tmQ, tmPool, tmKb, tmVb, p);
-        else if ((threadIdx.x & 31) == 0) mma_role<HD>(p, warp - 9);
+        if (warp == 16 || warp == 19) copy_role<HD>(tmQ, tmPool, tmKb, tmVb, p);
+        else mma_role<HD>(p, uniform(warp - 17));
         __syncwarp();
     } else {
         reg_alloc<REGS_SOFTMAX>();
@@ -677,7 +700,7 @@ prefix_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     }
     tc_fence_before();
     __syncthreads();
-    if (threadIdx.x >> 5 == 9) {
+    if (threadIdx.x >> 5 == 17) {
         tc_fence_after();
         tmem_dealloc(lds(role_base() + Sh::TMEM_SLOT), TMEM_COLS);
     }
