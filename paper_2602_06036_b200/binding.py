@@ -248,15 +248,6 @@ def _ptr(t: Optional[torch.Tensor]):
     return C.c_void_p(t.data_ptr())
 
 
-def _ints(t: Optional[torch.Tensor], shape=None):
-    """Pointer of an int32 device tensor (of the given shape)."""
-    if t is None:
-        return None
-    assert t.dtype == torch.int32, "int32 tensor expected"
-    assert shape is None or tuple(t.shape) == tuple(shape), f"shape {tuple(shape)} expected, got {tuple(t.shape)}"
-    return _ptr(t)
-
-
 def _stream(stream) -> C.c_void_p:
     s = stream if stream is not None else torch.cuda.current_stream()
     return C.c_void_p(s.cuda_stream)
@@ -283,6 +274,7 @@ class DFlash:
         self._keep = {}
         self._ws = None
         self._scratches = {}
+        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
 
     def close(self):
@@ -511,97 +503,109 @@ class DFlash:
         _check(self.lib.dflash_block_attention_bwd(self.h, C.byref(a), _stream(stream)))
 
     # ---- a batch over a shared cache --------------------------------------------------------
-    def _scratch(self, name, need, stream):
-        """Workspace of the calls below: grown on demand, on the stream that asks for it. A smaller one stays alive, because
-        a captured graph may still write to it."""
-        if need < 0:
-            raise DFlashError(int(need))
-        kept = self._scratches.setdefault(name, [])
-        if not kept or kept[-1].numel() < need:
-            with torch.cuda.stream(stream):
-                kept.append(torch.empty(max(int(need), 256), dtype=torch.uint8, device=self.device))
-        return kept[-1]
-
-    def _on(self, stream):
-        return stream if stream is not None else torch.cuda.current_stream(self.device)
+    # (The argument checks of these calls are kept to a few attribute reads a tensor: a decode step makes several of the calls, and
+    # their kernels take no longer than the host does for one.)
+    def _dev(self, t, dtype, *shape):
+        """Address of a contiguous tensor of this handle's device, of the given type and shape; None for None."""
+        if t is None:
+            return None
+        assert t.dtype is dtype, f"{dtype} tensor expected, got {t.dtype}"
+        assert t.get_device() == self._index and t.is_contiguous(), f"contiguous tensor on {self.device} expected"
+        assert t.shape == shape, f"shape {shape} expected, got {tuple(t.shape)}"
+        return t.data_ptr()
 
     def _pool(self, kv_pool):
         c = self.cfg
-        assert kv_pool.dtype == c.torch_dtype, "pool of the handle's dtype expected"
-        assert tuple(kv_pool.shape) == (c.n_layers, kv_pool.shape[1], 2, c.n_kv_heads, c.page_size, c.head_dim), "pool layout of the handle expected"
-        return _ptr(kv_pool)
+        return self._dev(kv_pool, c.torch_dtype, c.n_layers, kv_pool.shape[1], 2, c.n_kv_heads, c.page_size, c.head_dim)
+
+    def _scratch(self, name, query, key, stream):
+        """Workspace of the calls below (address and size), for the sizes in `key`: grown on demand, on the stream that asks for it. A smaller
+        one stays alive, because a captured graph may still write to it."""
+        kept = self._scratches.get(name)
+        if kept is None:
+            kept = self._scratches[name] = {"need": {}, "held": []}
+        need = kept["need"].get(key)
+        if need is None:
+            need = int(query(*key))
+            if need < 0:
+                raise DFlashError(need)
+            kept["need"][key] = need
+        held = kept["held"]
+        if not held or held[-1].numel() < need:
+            with torch.cuda.device(self.device), torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+                held.append(torch.empty(max(need, 256), dtype=torch.uint8, device=self.device))
+        return held[-1].data_ptr(), held[-1].numel()
+
+    def _call(self, fn, args, stream):
+        """The library launches on the current device, which has to be the handle's."""
+        raw = (stream if stream is not None else torch.cuda.current_stream(self._index)).cuda_stream
+        if torch.cuda.current_device() == self._index:
+            rc = fn(self.h, C.byref(args), raw)
+        else:
+            with torch.cuda.device(self._index):
+                rc = fn(self.h, C.byref(args), raw)
+        if rc != 0:
+            raise DFlashError(rc)
+
+    def _prefix_ws(self, batch, rows, groups):
+        return self.lib.dflash_prefix_attention_workspace_bytes(self.h, batch, rows, groups)
 
     def dflash_prefix_attention(self, mode, q, k_blk, v_blk, group_start, prefix_len, ctx_len, max_ctx_len, page_table, kv_pool, layer,
                                 out, stream=None, lse_out=None):
         """dflash_block_attention of a batch in which sequences group_start[g] .. group_start[g+1]-1 share their first
         prefix_len[g] positions (read from the page-table row of the first of them, once for all). group_start int32 [n+1] and
         prefix_len int32 [n], or both None: nothing is shared."""
-        c = self.cfg
+        c, dt, i32 = self.cfg, self.cfg.torch_dtype, torch.int32
         S, R = q.shape[0], q.shape[1]
-        for t, heads in ((q, c.n_q_heads), (k_blk, c.n_kv_heads), (v_blk, c.n_kv_heads), (out, c.n_q_heads)):
-            assert t.dtype == c.torch_dtype and tuple(t.shape) == (S, R, heads, c.head_dim), "[batch, rows, heads, head_dim] of the handle's dtype expected"
-        assert lse_out is None or (lse_out.dtype == torch.float32 and tuple(lse_out.shape) == (S, R, c.n_q_heads)), "lse_out [batch, rows, Hq] fp32 expected"
+        hq, hkv, hd = c.n_q_heads, c.n_kv_heads, c.head_dim
         n = 0 if prefix_len is None else prefix_len.shape[0]
-        st = self._on(stream)
-        with torch.cuda.device(self.device):
-            ws = self._scratch("prefix_attention", self.lib.dflash_prefix_attention_workspace_bytes(self.h, S, R, n), st)
-            a = PrefixAttnArgs(mode, _ptr(q), _ptr(k_blk), _ptr(v_blk), S, R, n, _ints(group_start, (n + 1,)) if n else None,
-                               _ints(prefix_len, (n,)) if n else None, _ints(ctx_len, (S,)), int(max_ctx_len),
-                               _ints(page_table, (S, page_table.shape[1])), page_table.shape[1], self._pool(kv_pool), kv_pool.shape[1], layer,
-                               _ptr(out), _ptr(lse_out), _ptr(ws), ws.numel(), _ptr(self.status))
-            _check(self.lib.dflash_prefix_attention(self.h, C.byref(a), _stream(st)))
+        width = page_table.shape[1]
+        ws, ws_bytes = self._scratch("prefix_attention", self._prefix_ws, (S, R, n), stream)
+        a = PrefixAttnArgs(mode, self._dev(q, dt, S, R, hq, hd), self._dev(k_blk, dt, S, R, hkv, hd), self._dev(v_blk, dt, S, R, hkv, hd), S, R, n,
+                           self._dev(group_start, i32, n + 1) if n else None, self._dev(prefix_len, i32, n) if n else None, self._dev(ctx_len, i32, S),
+                           int(max_ctx_len), self._dev(page_table, i32, S, width), width, self._pool(kv_pool), kv_pool.shape[1], layer,
+                           self._dev(out, dt, S, R, hq, hd), self._dev(lse_out, torch.float32, S, R, hq), ws, ws_bytes, self.status.data_ptr())
+        self._call(self.lib.dflash_prefix_attention, a, stream)
 
     def dflash_pages_copy(self, src, dst, kv_pool, n_slots=None, count=None, stream=None):
         """Page src[i] -> dst[i] in every layer (its first n_slots[i] slots); entries with a negative source do nothing,
         nor do those from count[0] on."""
-        n = src.shape[0]
-        with torch.cuda.device(self.device):
-            a = PagesCopyArgs(n, _ints(count, (1,)), _ints(src, (n,)), _ints(dst, (n,)), _ints(n_slots, (n,)), self._pool(kv_pool), kv_pool.shape[1],
-                              _ptr(self.status))
-            _check(self.lib.dflash_pages_copy(self.h, C.byref(a), _stream(self._on(stream))))
+        n, i32 = src.shape[0], torch.int32
+        a = PagesCopyArgs(n, self._dev(count, i32, 1), self._dev(src, i32, n), self._dev(dst, i32, n), self._dev(n_slots, i32, n), self._pool(kv_pool),
+                          kv_pool.shape[1], self.status.data_ptr())
+        self._call(self.lib.dflash_pages_copy, a, stream)
 
-    def _pages_ws(self, n, page_table, ref_count, stream):
-        return self._scratch("pages", self.lib.dflash_pages_workspace_bytes(n, page_table.shape[1], ref_count.shape[0]), stream)
+    def _pages_list(self, fn, st, lists, page_table, ref_count, kv_pool, copies, stream):
+        n, i32 = lists[0].shape[0], torch.int32
+        rows, width = page_table.shape
+        pages = kv_pool.shape[1]
+        cs, cd, cn = copies if copies is not None else (None, None, None)
+        ws, ws_bytes = self._scratch("pages", self.lib.dflash_pages_workspace_bytes, (n, width, pages), stream)
+        a = st(n, *[self._dev(t, i32, n) for t in lists], self._dev(page_table, i32, rows, width), rows, width, self._dev(ref_count, i32, pages),
+               self._pool(kv_pool), pages, self._dev(cs, i32, n), self._dev(cd, i32, n), self._dev(cn, i32, n), ws, ws_bytes, self.status.data_ptr())
+        self._call(fn, a, stream)
 
     def dflash_pages_fork(self, parent, child, fork_len, page_table, ref_count, kv_pool, copies=None, stream=None):
         """Row child[i] takes over the first fork_len[i] positions of row parent[i]: whole pages shared, a last partial one
         copied. copies = (src, dst, n_slots), int32 [n] each, receives the page copies made."""
-        n = parent.shape[0]
-        rows, width = page_table.shape
-        st = self._on(stream)
-        cs, cd, cn = copies if copies is not None else (None, None, None)
-        with torch.cuda.device(self.device):
-            ws = self._pages_ws(n, page_table, ref_count, st)
-            a = PagesForkArgs(n, _ints(parent, (n,)), _ints(child, (n,)), _ints(fork_len, (n,)), _ints(page_table), rows, width,
-                              _ints(ref_count, (kv_pool.shape[1],)), self._pool(kv_pool), kv_pool.shape[1], _ints(cs, (n,)), _ints(cd, (n,)),
-                              _ints(cn, (n,)), _ptr(ws), ws.numel(), _ptr(self.status))
-            _check(self.lib.dflash_pages_fork(self.h, C.byref(a), _stream(st)))
+        self._pages_list(self.lib.dflash_pages_fork, PagesForkArgs, (parent, child, fork_len), page_table, ref_count, kv_pool, copies, stream)
 
     def dflash_pages_resize(self, rows, keep_len, capacity, page_table, ref_count, kv_pool, copies=None, stream=None):
         """Row rows[i] gets pages for capacity[i] positions (0 releases it), its own ones from position keep_len[i] on."""
-        n = rows.shape[0]
-        n_rows, width = page_table.shape
-        st = self._on(stream)
-        cs, cd, cn = copies if copies is not None else (None, None, None)
-        with torch.cuda.device(self.device):
-            ws = self._pages_ws(n, page_table, ref_count, st)
-            a = PagesResizeArgs(n, _ints(rows, (n,)), _ints(keep_len, (n,)), _ints(capacity, (n,)), _ints(page_table), n_rows, width,
-                                _ints(ref_count, (kv_pool.shape[1],)), self._pool(kv_pool), kv_pool.shape[1], _ints(cs, (n,)), _ints(cd, (n,)),
-                                _ints(cn, (n,)), _ptr(ws), ws.numel(), _ptr(self.status))
-            _check(self.lib.dflash_pages_resize(self.h, C.byref(a), _stream(st)))
+        self._pages_list(self.lib.dflash_pages_resize, PagesResizeArgs, (rows, keep_len, capacity), page_table, ref_count, kv_pool, copies, stream)
 
     def dflash_pages_compact(self, page_table, ref_count, kv_pool, n_live=None, copies=None, stream=None):
         """Moves the pages in use to the front of the pool. n_live int32 [1] receives their number; copies = (src, dst, count),
         int32 [n_pool_pages // 2], the same, and [1], the moves made."""
-        n_rows, width = page_table.shape
+        i32 = torch.int32
+        rows, width = page_table.shape
         pages = kv_pool.shape[1]
-        st = self._on(stream)
         cs, cd, cn = copies if copies is not None else (None, None, None)
-        with torch.cuda.device(self.device):
-            ws = self._pages_ws(0, page_table, ref_count, st)
-            a = PagesCompactArgs(_ints(page_table), n_rows, width, _ints(ref_count, (pages,)), self._pool(kv_pool), pages, _ints(n_live, (1,)),
-                                 _ints(cs, (pages // 2,)), _ints(cd, (pages // 2,)), _ints(cn, (1,)), _ptr(ws), ws.numel(), _ptr(self.status))
-            _check(self.lib.dflash_pages_compact(self.h, C.byref(a), _stream(st)))
+        ws, ws_bytes = self._scratch("pages", self.lib.dflash_pages_workspace_bytes, (0, width, pages), stream)
+        a = PagesCompactArgs(self._dev(page_table, i32, rows, width), rows, width, self._dev(ref_count, i32, pages), self._pool(kv_pool), pages,
+                             self._dev(n_live, i32, 1), self._dev(cs, i32, pages // 2), self._dev(cd, i32, pages // 2), self._dev(cn, i32, 1), ws, ws_bytes,
+                             self.status.data_ptr())
+        self._call(self.lib.dflash_pages_compact, a, stream)
 
     def dflash_lmhead_argmax(self, hidden, apply_norm, ids, top1=None, margin=None, logits_out=None, stream=None):
         M = hidden.shape[0]

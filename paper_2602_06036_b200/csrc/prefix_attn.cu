@@ -183,25 +183,23 @@ __global__ void __launch_bounds__(SIMT_THREADS) prefix_attn_simt_kernel(const __
 }
 
 // ---- merge ----------------------------------------------------------------------------------------------------------
-// Eight lanes a row, four neighbouring packed rows of a (sequence, kv head) a warp. The parts of a row are added in a fixed order: the
-// prefix's key blocks, then the sequence's own keys, each by rising CTA. PB parts at a time are requested together, results and statistics alike: the
-// kernel waits for L2, not for bytes.
+// Four neighbouring packed rows of a (sequence, kv head) a CTA. Its four warps take every fourth part of these rows (eight lanes a row) and are added up
+// at the end, so that the order is fixed; a warp requests PB parts together, results and statistics alike: the kernel waits for L2, not for bytes.
 constexpr int PB = 4;
 
 template <typename T, int HD>
 __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant__ Params p) {
+    __shared__ float4 s_acc[4][4][HD / 4];
+    __shared__ float2 s_ml[4][4];
     unsigned long long* trace = p.trace ? p.trace + 4 : nullptr;
     if (threadIdx.x == 0) trace_min(trace, 0);
     const int RG = p.plan.R * p.plan.G, per_head = (RG + 3) / 4;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31, sub8 = lane >> 2;          // columns 4 sub8 + 32 k
-    const int64_t bh = unit / per_head;
-    const int pr = (int)(unit % per_head) * 4 + (lane & 3);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub8 = lane >> 2;          // columns 4 sub8 + 32 k
+    const int bh = blockIdx.x / per_head, b = bh / p.plan.Hkv, kvh = bh % p.plan.Hkv;
+    const int pr = min((int)(blockIdx.x % per_head) * 4 + (lane & 3), RG - 1);              // rows behind the last one repeat it
+    const int tpi = p.plan.tiles_per_item, tr = p.plan.row_tile;
     pdl_wait();
     if (threadIdx.x == 0) trace_min(trace, 1);
-    if (bh >= (int64_t)p.plan.S * p.plan.Hkv || pr >= RG) return;
-    const int b = (int)(bh / p.plan.Hkv), kvh = (int)(bh % p.plan.Hkv);
-    const int tpi = p.plan.tiles_per_item, tr = p.plan.row_tile;
     const SeqInfo si = p.po.sinfo[b];
     const int n_group_items = __ldcg(p.po.meta);
     GroupInfo gi{};
@@ -211,6 +209,7 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
     float4 acc[HD / 32];
 #pragma unroll
     for (int k = 0; k < HD / 32; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    int skip = warp;                                 // parts until this warp's next one
     for (int own = si.group >= 0 ? 0 : 1; own < 2; ++own) {
         const int at = own ? pr : si.row_off + pr, tile = at / tr, it = tile / tpi, row = at % tr;
         const int row_tiles = (RG + tr - 1) / tr, blocks = own ? si.blocks : gi.blocks;
@@ -221,13 +220,15 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
             const int item = (own ? si.item0 : gi.item0) + (kvh * blocks + kb) * items + it;
             const int2 ctas = __ldcg(p.po.ctas + item);
             const int slot0 = item + ctas.x - (own ? n_group_items : 0), n = (ctas.y - ctas.x + 1) * subs;
-            for (int k0 = 0; k0 < n; k0 += PB) {
+            int k0 = skip;
+            for (; k0 < n; k0 += 4 * PB) {
                 float2 ml[PB];
                 float4 o[PB][HD / 32];
 #pragma unroll
                 for (int k = 0; k < PB; ++k) {
-                    if (k0 + k < n) {
-                        const int64_t r = slot_row(p, !own, slot0 + (subs == 2 ? (k0 + k) >> 1 : k0 + k), subs == 2 ? (k0 + k) & 1 : sub0, row);
+                    const int part = k0 + 4 * k;
+                    if (part < n) {
+                        const int64_t r = slot_row(p, !own, slot0 + (subs == 2 ? part >> 1 : part), subs == 2 ? part & 1 : sub0, row);
                         ml[k] = __ldcg(p.ml + r);
 #pragma unroll
                         for (int x = 0; x < HD / 32; ++x) o[k][x] = __ldcg(reinterpret_cast<const float4*>(p.part + part_offset(r, HD, x * 8 + sub8)));
@@ -259,20 +260,41 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
                     }
                 }
             }
+            // parts of this warp in the next item: those at `skip`, `skip` + 4, ... of the parts behind this item's n
+            const int passed = n - skip;
+            skip = passed <= 0 ? -passed : (4 - passed % 4) % 4;
         }
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;   // a row that saw no key gives zeros
-    const int64_t row = (int64_t)b * p.plan.R + pr / p.plan.G;
-    const int head = kvh * p.plan.G + pr % p.plan.G;
-    if (p.lse && sub8 == 0) p.lse[row * p.Hq + head] = L == 0.f ? -CUDART_INF_F : ((M > -CUDART_INF_F ? M : 0.f) + log2f(L)) * 0.6931471805599453f;
-    T* dst = (T*)p.out + (row * p.Hq + head) * HD;
+    // the four warps' sums, by warp
 #pragma unroll
-    for (int x = 0; x < HD / 32; ++x) {
-        const float4 v = make_float4(acc[x].x * inv, acc[x].y * inv, acc[x].z * inv, acc[x].w * inv);
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4*>(dst + x * 32 + sub8 * 4) = v;
-        } else {
-            *reinterpret_cast<uint2*>(dst + x * 32 + sub8 * 4) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    for (int x = 0; x < HD / 32; ++x) s_acc[warp][lane & 3][x * 8 + sub8] = acc[x];
+    if (sub8 == 0) s_ml[warp][lane & 3] = make_float2(M, L);
+    __syncthreads();
+    const int row = threadIdx.x >> 5, prow = (int)(blockIdx.x % per_head) * 4 + row;          // now a warp a row
+    if (prow < RG) {
+        float top = -CUDART_INF_F, sum = 0.f, w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, s_ml[k][row].x);
+        const float ref = top > -CUDART_INF_F ? top : 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            w[k] = exp2f(s_ml[k][row].x - ref);
+            sum = fmaf(s_ml[k][row].y, w[k], sum);
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;       // a row that saw no key gives zeros
+        const int64_t r = (int64_t)b * p.plan.R + prow / p.plan.G;
+        const int head = kvh * p.plan.G + prow % p.plan.G;
+        if (p.lse && lane == 0) p.lse[r * p.Hq + head] = sum == 0.f ? -CUDART_INF_F : (ref + log2f(sum)) * 0.6931471805599453f;
+        if (lane < HD / 4) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float4 x = s_acc[k][row][lane];
+                v.x = fmaf(x.x, w[k], v.x); v.y = fmaf(x.y, w[k], v.y); v.z = fmaf(x.z, w[k], v.z); v.w = fmaf(x.w, w[k], v.w);
+            }
+            T* dst = (T*)p.out + (r * p.Hq + head) * HD + lane * 4;
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(dst) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+            else *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
         }
     }
     if (threadIdx.x == 0) trace_max(trace, 3);
@@ -330,7 +352,10 @@ PlanParams plan_params(const dflash_config& c, const Sizes& z, int S, int R, int
     PlanParams q{};
     q.S = S; q.R = R; q.G = c.n_q_heads / c.n_kv_heads; q.Hkv = c.n_kv_heads; q.n_groups = n_groups; q.max_ctx_len = max_ctx_len;
     q.row_tile = z.row_tile; q.tiles_per_item = z.tiles_per_item; q.chunks_per_tile = z.chunks_per_tile;
-    q.cost_item = 3; q.cost_one = 4; q.cost_two = 4;
+    // Tensor-core kernel, in units of 500 clocks: a key tile takes 2650 with one query tile (its bytes at the HBM rate) and 4150 with two (its products),
+    // the change to another item 4500. CUDA cores: a chunk takes about as long as it takes to begin an item.
+    const bool tc = use_tc(c);
+    q.cost_item = tc ? 9 : 3; q.cost_one = tc ? 5 : 4; q.cost_two = tc ? 8 : 4;
     return q;
 }
 // whether the costs of any lengths up to max_ctx_len stay below 2^31 with room for the sums that plan_kernel forms
@@ -338,7 +363,7 @@ bool plan_fits(const dflash_config& c, const Sizes& z, int64_t S, int64_t R, int
     const int64_t G = c.n_q_heads / c.n_kv_heads, per_item = (int64_t)z.row_tile * z.tiles_per_item;
     const int64_t tiles = max_ctx_len / (CHUNK_KEYS * z.chunks_per_tile) + 3;
     const int64_t items = S * ((R * G + per_item - 1) / per_item) + (S * R * G / per_item + std::min(n_groups, S));
-    return items <= (1 << 24) && c.n_kv_heads * items * tiles * 8 < (1ll << 30);
+    return items <= (1 << 24) && c.n_kv_heads * items * tiles * 17 < (1ll << 30);
 }
 
 template <int HD>
@@ -490,7 +515,7 @@ int launch_prefix_attention(const Launch& L, const dflash_prefix_attn_args& a) {
     if (rc != DFLASH_OK) return rc;
     ++g_launches;
     const int64_t units = (int64_t)a.batch * p.plan.Hkv * ((a.rows * p.plan.G + 3) / 4);
-    const dim3 grid((unsigned)((units + 3) / 4)), block(128);
+    const dim3 grid((unsigned)units), block(128);
     cudaError_t e;
     if (c.dtype == DFLASH_F32) e = wide ? launch_pdl(prefix_merge_kernel<float, 128>, grid, block, 0, L.st, p) : launch_pdl(prefix_merge_kernel<float, 64>, grid, block, 0, L.st, p);
     else e = wide ? launch_pdl(prefix_merge_kernel<__nv_bfloat16, 128>, grid, block, 0, L.st, p) : launch_pdl(prefix_merge_kernel<__nv_bfloat16, 64>, grid, block, 0, L.st, p);

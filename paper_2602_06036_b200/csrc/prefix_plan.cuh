@@ -190,7 +190,7 @@ struct PlanOut {
     int32_t* meta;                       // [0] number of group items
 };
 
-constexpr int PLAN_THREADS = 1024, MAX_CTAS = 512, PLAN_CACHE = 2048;
+constexpr int PLAN_THREADS = 1024, MAX_CTAS = 512, PLAN_CACHE = 1024;
 
 // One CTA. Passes of all threads over groups and sequences (total cost, then running costs and items), then one thread per item. What
 // takes its time is latency: lengths and groups are fetched once, into shared memory where they fit (smaller code than
@@ -200,6 +200,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
     __shared__ int32_t s_cost[NW], s_tiles[NW], s_items[NW];
     __shared__ int32_t s_first[MAX_CTAS], s_n[MAX_CTAS];
     __shared__ int32_t s_len[PLAN_CACHE], s_prefix[PLAN_CACHE], s_start[PLAN_CACHE + 1];
+    __shared__ int32_t s_at[2 * PLAN_CACHE], s_item0[2 * PLAN_CACHE + 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     ptx::pdl_trigger();
     for (int c = tid; c < grid; c += PLAN_THREADS) {
@@ -229,6 +230,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
     if (bad && tid == 0 && p.status) atomicOr(p.status, DFLASH_DEV_BAD_GROUP);
     const int n = p.n_groups + p.S, per = (n + PLAN_THREADS - 1) / PLAN_THREADS;
     const int e0 = min(n, tid * per), e1 = min(n, e0 + per);
+    int32_t *at = n <= 2 * PLAN_CACHE ? s_at : o.start, *item0 = n <= 2 * PLAN_CACHE ? s_item0 : o.item0;
     // pass 0: total cost with whole prefixes, which gives the share of a CTA and so the key blocks; pass 1: with these, where
     // each thread's entries start; pass 2: write it down
     int share = 0, run = 0, run_items = 0, total = 0;
@@ -239,8 +241,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
         for (int e = e0; e < e1; ++e) {
             const Entry x = plan_entry(p, e, ok, share, pass == 0);
             if (pass == 2) {
-                o.start[e] = run + cost;
-                o.item0[e] = run_items + items;
+                at[e] = run + cost;
+                item0[e] = run_items + items;
                 if (e < p.n_groups) {
                     o.ginfo[e] = GroupInfo{run_items + items, x.items, x.blocks, x.single};
                 } else {
@@ -252,7 +254,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
             cost += x.cost;
             tiles += p.Hkv * x.items * x.n_tiles;
             items += entry_items(p, x);
-            if (pass == 2 && e == n - 1) o.item0[n] = run_items + items;
+            if (pass == 2 && e == n - 1) item0[n] = run_items + items;
         }
         if (pass == 2) break;
         int c = cost, i = items;
@@ -283,18 +285,18 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
     static_assert(NW == 32, "one lane per warp");
     const int stretch = plan_stretch(p, total, grid);
     __syncthreads();                     // the CTA's own global writes are visible to its threads
-    const int n_items = o.item0[n], n_group_items = o.item0[p.n_groups];
+    const int n_items = item0[n], n_group_items = item0[p.n_groups];
 #pragma unroll 1
     for (int i = tid; i < n_items; i += PLAN_THREADS) {
         int lo = 0, hi = n;              // last entry that starts at item i or before (entries without items share a start)
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (o.item0[mid] <= i) lo = mid;
+            if (item0[mid] <= i) lo = mid;
             else hi = mid;
         }
         const Entry x = plan_entry(p, lo, ok, share, false);
-        const Item m = plan_item(p, x, i - o.item0[lo]);
-        const int start = o.start[lo] + m.start, c0 = start / stretch, c1 = (start + item_last(p, m)) / stretch;
+        const Item m = plan_item(p, x, i - item0[lo]);
+        const int start = at[lo] + m.start, c0 = start / stretch, c1 = (start + item_last(p, m)) / stretch;
         o.ctas[i] = make_int2(c0, c1);
 #pragma unroll 1
         for (int c = c0; c <= c1; ++c) {
