@@ -11,7 +11,9 @@ namespace {
 
 using namespace ptx;
 
-constexpr float GAP = 8.f;               // log2 units by which a tile has to top the running maximum to raise it
+// log2 units by which a tile has to top the running maximum to raise it: P and the sums may grow to 2^16 times what they would be otherwise, which
+// costs no precision, and leaves fp32 2^96 for the values
+constexpr float GAP = 16.f;
 
 struct Params {
     PlanParams plan;
@@ -426,12 +428,14 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
             const int v = j - step;
             const bool do_v = v >= first && v < n, do_s = j < n;
             const uint32_t sv = (tile0 + v) % Sh::NV, sk = (tile0 + j) % Sh::NK;
-            if (do_v) {
-                ok = bar_wait(sb + Sh::FULL_V + 8 * sv, (tile0 + v) / Sh::NV & 1, sb + Sh::ABORT) && bar_wait(sb + Sh::P_FULL + 8 * t, p_phase, sb + Sh::ABORT);
-                p_phase ^= 1;
-            }
+            // the wait for P last: what comes after it adds to every tile's time
+            if (do_v) ok = bar_wait(sb + Sh::FULL_V + 8 * sv, (tile0 + v) / Sh::NV & 1, sb + Sh::ABORT);
             if (do_s && ok) ok = bar_wait(sb + Sh::FULL_K + 8 * sk, (tile0 + j) / Sh::NK & 1, sb + Sh::ABORT);
             ok = ok && bar_wait(sb + Sh::TURN + 8 * t, turn, sb + Sh::ABORT);
+            if (do_v && ok) {
+                ok = bar_wait(sb + Sh::P_FULL + 8 * t, p_phase, sb + Sh::ABORT);
+                p_phase ^= 1;
+            }
             if (!ok) break;
             turn ^= 1;
             tc_fence_after();
@@ -479,12 +483,13 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
 // ---- softmax: two threads a query row, of 64 keys each ----
 // Four warps a scheduler hide one another's latencies; with one thread a row (208 registers, two warps a scheduler) a tile's softmax took 2000 to 2900
 // clocks against the 1024 of its products.
-// P of 32 keys (16 columns), its part of the row sum. FAST: every fourth pair takes the polynomial.
+// P of 32 keys (16 columns), its part of the row sum. FAST: every fourth pair takes the polynomial, and the largest score is looked for.
 template <bool FAST>
-__device__ __forceinline__ void softmax_32(const float* s, float scale, float m, float2* sum, uint32_t* pk) {
+__device__ __forceinline__ void softmax_32(const float* s, float scale, float m, float2* sum, float& top, uint32_t* pk) {
     const float2 scale2 = make_float2(scale, scale), neg2 = make_float2(-m, -m);
 #pragma unroll
     for (int c = 0; c < 16; ++c) {
+        if (FAST) top = max3(top, s[2 * c], s[2 * c + 1]);
         float2 x = fma2(make_float2(s[2 * c], s[2 * c + 1]), scale2, neg2);
         if (FAST && (c & 3) == 3) {
             x = poly_exp2(x);
@@ -526,6 +531,7 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
         __syncwarp();
         if (lane == 0) bar_arrive(sb + Sh::Q_EMPTY);
         auto first_row = [&] { return lds(cur + offsetof(Segment, row0)) + (two ? t * p.plan.row_tile : 0); };
+        const bool mine = row < min(p.plan.row_tile, lds(cur + offsetof(Segment, n_rows)) - first_row());       // the row exists
         float m_run = -CUDART_INF_F, l_run = 0.f;        // l_run: of this thread's keys
         const int step = two ? 1 : 2, first = two ? 0 : t;
 #pragma unroll 1
@@ -536,6 +542,34 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
             const uint32_t ti = sb + Sh::INFO + ((tile0 + j) % NI) * (uint32_t)sizeof(TileInfo);
             const bool all = lds(ti + offsetof(TileInfo, full));
             float s[64];
+            if (all && j > first) {
+                // The usual case: all keys exist, and the running maximum still serves as the reference. P is worked out with it while the tile's own
+                // maximum is, and nothing is exchanged but whether some row would have its maximum raised (then the tile is done over below).
+                tmem_ld32_nowait(tS + h * 64, s);
+                tmem_ld32_nowait(tS + h * 64 + 32, s + 32);
+                tmem_ld_wait();
+                float top = -CUDART_INF_F;
+                float2 sum[2] = {};
+                uint32_t pk[32];
+                const float m_ref = m_run > -CUDART_INF_F ? m_run : 0.f;
+#pragma unroll
+                for (int g = 0; g < 2; ++g) softmax_32<true>(s + 32 * g, p.scale_log2, m_ref, sum, top, pk + 16 * g);
+                top *= p.scale_log2;                     // scale > 0
+                // The barrier also says that all of S_t is in registers: P_t takes the place of its first half. Rows that do not exist have no
+                // say: they hold whatever was in shared memory, and the two ways round differently.
+                const bool raise = mine && (top > m_run + GAP || (m_run == -CUDART_INF_F && top > -CUDART_INF_F));
+                if (!tile_any(t, !ok || raise)) {
+                    tmem_st16(tS + h * 32, pk);
+                    tmem_st16(tS + h * 32 + 16, pk + 16);
+                    sum[0] = add2(sum[0], sum[1]);
+                    l_run += sum[0].x + sum[0].y;
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(sb + Sh::P_FULL + 8 * t);
+                    continue;
+                }
+            }
             tmem_ld32_nowait(tS + h * 64, s);
             tmem_ld32_nowait(tS + h * 64 + 32, s + 32);
             if (!all && h == 0) {
@@ -589,20 +623,12 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
                 }
             }
             float2 sum[2] = {};
-            if (all) {
+            float unused = 0.f;
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    uint32_t pk[16];
-                    softmax_32<true>(s + 32 * g, p.scale_log2, m_use, sum, pk);
-                    tmem_st16(tS + h * 32 + g * 16, pk);
-                }
-            } else {
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    uint32_t pk[16];
-                    softmax_32<false>(s + 32 * g, p.scale_log2, m_use, sum, pk);
-                    tmem_st16(tS + h * 32 + g * 16, pk);
-                }
+            for (int g = 0; g < 2; ++g) {
+                uint32_t pk[16];
+                softmax_32<false>(s + 32 * g, p.scale_log2, m_use, sum, unused, pk);
+                tmem_st16(tS + h * 32 + g * 16, pk);
             }
             sum[0] = add2(sum[0], sum[1]);
             l_run = l_run * alpha + (sum[0].x + sum[0].y);
@@ -619,7 +645,6 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
             o_phase ^= 1;
             tc_fence_after();
         }
-        const bool mine = row < min(p.plan.row_tile, lds(cur + offsetof(Segment, n_rows)) - first_row());       // the row exists
         const int64_t at = slot_row(p, lds(cur + offsetof(Segment, prefix)) != 0, lds(cur + offsetof(Segment, slot)), t, row);
         if (h == 1) sts(xch + 4 * row, __float_as_int(l_run));
         if (tile_any(t, !ok)) { ok = false; break; }
