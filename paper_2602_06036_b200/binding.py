@@ -253,6 +253,12 @@ def _stream(stream) -> C.c_void_p:
     return C.c_void_p(s.cuda_stream)
 
 
+def _current_stream(index: int) -> int:
+    """cudaStream_t of a device's current stream; without the Stream object around it, where torch offers that (1 us less)."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+
+
 def launch_count() -> int:
     return int(load().dflash_launch_count())
 
@@ -523,22 +529,23 @@ class DFlash:
         one stays alive, because a captured graph may still write to it."""
         kept = self._scratches.get(name)
         if kept is None:
-            kept = self._scratches[name] = {"need": {}, "held": []}
+            kept = self._scratches[name] = {"need": {}, "held": [], "at": None, "size": -1}
         need = kept["need"].get(key)
         if need is None:
             need = int(query(*key))
             if need < 0:
                 raise DFlashError(need)
             kept["need"][key] = need
-        held = kept["held"]
-        if not held or held[-1].numel() < need:
+        if kept["size"] < need:
             with torch.cuda.device(self.device), torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
-                held.append(torch.empty(max(need, 256), dtype=torch.uint8, device=self.device))
-        return held[-1].data_ptr(), held[-1].numel()
+                t = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+            kept["held"].append(t)
+            kept["at"], kept["size"] = t.data_ptr(), t.numel()
+        return kept["at"], kept["size"]
 
     def _call(self, fn, args, stream):
         """The library launches on the current device, which has to be the handle's."""
-        raw = (stream if stream is not None else torch.cuda.current_stream(self._index)).cuda_stream
+        raw = stream.cuda_stream if stream is not None else _current_stream(self._index)
         if torch.cuda.current_device() == self._index:
             rc = fn(self.h, C.byref(args), raw)
         else:

@@ -350,6 +350,7 @@ PrefixWs carve_prefix(void* base, const Sizes& z, const dflash_config& c, int64_
     w.po.ctas = (int2*)a.take(items * sizeof(int2));
     w.po.ginfo = (GroupInfo*)a.take(std::max<int64_t>(n_groups, 1) * sizeof(GroupInfo));
     w.po.sinfo = (SeqInfo*)a.take(S * sizeof(SeqInfo));
+    w.po.entries = (Entry*)a.take(n > PLAN_CACHE ? n * sizeof(Entry) : 0);
     w.po.start = (int32_t*)a.take(n * 4);
     w.po.item0 = (int32_t*)a.take((n + 1) * 4);
     w.po.meta = (int32_t*)a.take(4);
@@ -445,7 +446,8 @@ int prefix_plan_check(const dflash_config& c, int sm_count, int S, int R, int n_
     const int n = n_groups + S;
     int total = 0, all_tiles = 0;
     for (int e = 0; e < n; ++e) {
-        const Entry x = plan_entry(p, e, n_groups > 0, 0, false);
+        Entry x = plan_entry(p, e, n_groups > 0, false);
+        entry_cost(p, x);
         total += x.cost;
         all_tiles += p.Hkv * x.items * x.n_tiles;
     }
@@ -454,10 +456,16 @@ int prefix_plan_check(const dflash_config& c, int sm_count, int S, int R, int n_
         total = all_tiles * p.cost_two;
     }
     const int share = (total + z.n_cta - 1) / z.n_cta;
+    auto entry = [&](int e) {
+        Entry x = plan_entry(p, e, n_groups > 0, false);
+        entry_blocks(p, x, share);
+        entry_cost(p, x);
+        return x;
+    };
     int64_t items = 0, group_items = 0, tiles = 0, segments = 0;
     total = 0;
     for (int e = 0; e < n; ++e) {
-        const Entry x = plan_entry(p, e, n_groups > 0, share, false);
+        const Entry x = entry(e);
         if (e == n_groups) group_items = items;
         total += x.cost;
         items += entry_items(p, x);
@@ -467,7 +475,7 @@ int prefix_plan_check(const dflash_config& c, int sm_count, int S, int R, int n_
     int at = 0, cta = 0, spent = 0, most = 0, least = INT32_MAX;      // the chain is followed item by item: CTAs take turns without a gap
     int64_t i = 0;
     for (int e = 0; rc == 0 && e < n; ++e) {
-        const Entry x = plan_entry(p, e, n_groups > 0, share, false);
+        const Entry x = entry(e);
         const int entry_at = at, count = entry_items(p, x);
         for (int k = 0; rc == 0 && k < count; ++k, ++i) {
             const Item m = plan_item(p, x, k);
@@ -522,7 +530,8 @@ int launch_prefix_attention(const Launch& L, const dflash_prefix_attn_args& a) {
     p.status = L.status; p.trace = L.trace;
     if (z.n_cta > MAX_CTAS || !plan_fits(c, z, a.batch, a.rows, a.n_groups, a.max_ctx_len)) return DFLASH_ERR_UNSUPPORTED;
     // plain stream order: the plan reads lengths that the caller's previous call may have written
-    if (launch_ordered(prefix_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, L.st, p.plan, w.po, z.n_cta) != cudaSuccess) return DFLASH_ERR_CUDA;
+    const cudaError_t e = launch_ordered(prefix_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, L.st, p.plan, w.po, z.n_cta);
+    if (e != cudaSuccess) return DFLASH_ERR_CUDA;
     ++g_launches;
     const bool wide = c.head_dim == 128;
     int rc;

@@ -706,6 +706,10 @@ prefix_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sb + Sh::TMEM_SLOT), "r"(TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    if (threadIdx.x >= 18 * 32 && threadIdx.x < 18 * 32 + 4) {           // the descriptors of the copies, while the plan is being made
+        const CUtensorMap* m = threadIdx.x == 18 * 32 ? &tmQ : threadIdx.x == 18 * 32 + 1 ? &tmPool : threadIdx.x == 18 * 32 + 2 ? &tmKb : &tmVb;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
+    }
     pdl_trigger();
     tc_fence_before();
     __syncthreads();

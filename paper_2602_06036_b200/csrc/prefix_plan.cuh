@@ -74,9 +74,8 @@ __host__ __device__ __forceinline__ int plan_stretch(const PlanParams& p, int to
     return share > gap ? share : gap;
 }
 
-// `share`: costs a CTA takes (0: not known yet, key blocks are left at 1). Long prefixes are cut into blocks of about one CTA's
-// share, ordered before the row tiles: CTAs that run side by side then read the same keys, which come out of L2.
-__host__ __device__ __forceinline__ Entry plan_entry(const PlanParams& p, int e, bool groups_ok, int32_t share, bool tell) {
+// Entry e with whole prefixes, its cost left open.
+__host__ __device__ __forceinline__ Entry plan_entry(const PlanParams& p, int e, bool groups_ok, bool tell) {
     Entry x{};
     x.blocks = 1;
     if (e < p.n_groups) {
@@ -100,13 +99,19 @@ __host__ __device__ __forceinline__ Entry plan_entry(const PlanParams& p, int e,
     const int row_tiles = (x.n_rows + p.row_tile - 1) / p.row_tile;
     x.items = (row_tiles + p.tiles_per_item - 1) / p.tiles_per_item;
     x.single = row_tiles % p.tiles_per_item != 0 || p.tiles_per_item == 1;
-    const int one = p.tiles_per_item == 1 ? x.items * p.cost_one : (x.items - x.single) * p.cost_two + x.single * p.cost_one;
-    if (share > 0 && x.items > 1) {
-        const int blocks = (x.n_tiles * p.cost_two + share / 2) / share;
-        x.blocks = blocks < 1 ? 1 : blocks > x.n_tiles ? x.n_tiles : blocks;
-    }
-    x.cost = p.Hkv * (x.items * x.blocks * p.cost_item + x.n_tiles * one);
     return x;
+}
+// `share`: cost that a CTA takes. Long prefixes are cut into key blocks of about that much, ordered before the row tiles: CTAs that run side by
+// side then read the same keys, which come out of L2.
+__host__ __device__ __forceinline__ void entry_blocks(const PlanParams& p, Entry& x, int32_t share) {
+    if (x.n_tiles == 0 || x.items < 2) return;
+    const int blocks = (x.n_tiles * p.cost_two + share / 2) / share;
+    x.blocks = blocks < 1 ? 1 : blocks > x.n_tiles ? x.n_tiles : blocks;
+}
+__host__ __device__ __forceinline__ void entry_cost(const PlanParams& p, Entry& x) {
+    if (x.n_tiles == 0) return;
+    const int one = p.tiles_per_item == 1 ? x.items * p.cost_one : (x.items - x.single) * p.cost_two + x.single * p.cost_one;
+    x.cost = p.Hkv * (x.items * x.blocks * p.cost_item + x.n_tiles * one);
 }
 __host__ __device__ __forceinline__ int entry_items(const PlanParams& p, const Entry& x) { return x.n_tiles ? p.Hkv * x.items * x.blocks : 0; }
 
@@ -185,22 +190,23 @@ struct PlanOut {
     int2* ctas;                          // [items] first and last CTA
     GroupInfo* ginfo;                    // [n_groups]
     SeqInfo* sinfo;                      // [S]
-    int32_t* start;                      // [n_groups + S] scratch: cost and item at which an entry starts
+    Entry* entries;                      // [n_groups + S] scratch, used where shared memory is too small: entries, and the cost and item at
+    int32_t* start;                      // [n_groups + S]      which each starts
     int32_t* item0;                      // [n_groups + S + 1]
     int32_t* meta;                       // [0] number of group items
 };
 
-constexpr int PLAN_THREADS = 1024, MAX_CTAS = 512, PLAN_CACHE = 1024;
+constexpr int PLAN_THREADS = 512, MAX_CTAS = 512, PLAN_CACHE = 512;
 
-// One CTA. Passes of all threads over groups and sequences (total cost, then running costs and items), then one thread per item. What
-// takes its time is latency: lengths and groups are fetched once, into shared memory where they fit (smaller code than
-// 64-bit arithmetic or passes of their own also shows).
+// One CTA. Passes of all threads over groups and sequences (entries and their total cost; then key blocks, running costs and items), then one thread per
+// item. What takes its time is latency: lengths and groups are fetched once, and everything in between stays in shared memory where it fits.
 __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p, const PlanOut o, int grid) {
     constexpr int NW = PLAN_THREADS / 32;
     __shared__ int32_t s_cost[NW], s_tiles[NW], s_items[NW];
     __shared__ int32_t s_first[MAX_CTAS], s_n[MAX_CTAS];
     __shared__ int32_t s_len[PLAN_CACHE], s_prefix[PLAN_CACHE], s_start[PLAN_CACHE + 1];
-    __shared__ int32_t s_at[2 * PLAN_CACHE], s_item0[2 * PLAN_CACHE + 1];
+    __shared__ Entry s_entry[PLAN_CACHE];
+    __shared__ int32_t s_at[PLAN_CACHE], s_item0[PLAN_CACHE + 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     ptx::pdl_trigger();
     for (int c = tid; c < grid; c += PLAN_THREADS) {
@@ -229,63 +235,75 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
     const bool ok = !bad && p.n_groups > 0;
     if (bad && tid == 0 && p.status) atomicOr(p.status, DFLASH_DEV_BAD_GROUP);
     const int n = p.n_groups + p.S, per = (n + PLAN_THREADS - 1) / PLAN_THREADS;
-    const int e0 = min(n, tid * per), e1 = min(n, e0 + per);
-    int32_t *at = n <= 2 * PLAN_CACHE ? s_at : o.start, *item0 = n <= 2 * PLAN_CACHE ? s_item0 : o.item0;
-    // pass 0: total cost with whole prefixes, which gives the share of a CTA and so the key blocks; pass 1: with these, where
-    // each thread's entries start; pass 2: write it down
-    int share = 0, run = 0, run_items = 0, total = 0;
+    const int e0 = min(n, tid * per), e1 = min(n, e0 + per);         // this thread's entries
+    const bool small = n <= PLAN_CACHE;
+    Entry* ent = small ? s_entry : o.entries;
+    int32_t *at = small ? s_at : o.start, *item0 = small ? s_item0 : o.item0;
+    int cost = 0, tiles = 0, items = 0;
 #pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-        int cost = 0, tiles = 0, items = 0;
-#pragma unroll 1
-        for (int e = e0; e < e1; ++e) {
-            const Entry x = plan_entry(p, e, ok, share, pass == 0);
-            if (pass == 2) {
-                at[e] = run + cost;
-                item0[e] = run_items + items;
-                if (e < p.n_groups) {
-                    o.ginfo[e] = GroupInfo{run_items + items, x.items, x.blocks, x.single};
-                } else {
-                    const int b = e - p.n_groups, g = ok ? plan_group(p, b) : -1, shared = plan_shared(p, g, x.hi);
-                    o.sinfo[b] = SeqInfo{shared > 0 ? g : -1, shared > 0 ? (b - p.group_start[g]) * p.R * p.G : 0, run_items + items, x.blocks};
-                    if (b == 0) o.meta[0] = run_items + items;
-                }
-            }
-            cost += x.cost;
-            tiles += p.Hkv * x.items * x.n_tiles;
-            items += entry_items(p, x);
-            if (pass == 2 && e == n - 1) item0[n] = run_items + items;
-        }
-        if (pass == 2) break;
-        int c = cost, i = items;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, c, d), z = __shfl_up_sync(0xffffffffu, i, d);
-            if (lane >= d) { c += y; i += z; }
-        }
-        tiles = __reduce_add_sync(0xffffffffu, tiles);
-        __syncthreads();
-        if (lane == 31) { s_cost[warp] = c; s_items[warp] = i; s_tiles[warp] = tiles; }
-        __syncthreads();
-        run = c - cost;
-        run_items = i - items;
-        const int wc = s_cost[lane], wi = s_items[lane];        // one warp's sums per lane
-        run += __reduce_add_sync(0xffffffffu, lane < warp ? wc : 0);
-        run_items += __reduce_add_sync(0xffffffffu, lane < warp ? wi : 0);
-        total = __reduce_add_sync(0xffffffffu, wc);
-        if (pass == 0) {
-            tiles = __reduce_add_sync(0xffffffffu, s_tiles[lane]);
-            if (plan_few(p, tiles, grid)) {
-                p.cost_item = 0;
-                total = tiles * p.cost_two;
-            }
-            share = (total + grid - 1) / grid;
-        }
+    for (int e = e0; e < e1; ++e) {
+        Entry x = plan_entry(p, e, ok, true);
+        entry_cost(p, x);
+        cost += x.cost;
+        tiles += p.Hkv * x.items * x.n_tiles;
+        ent[e] = x;
     }
-    static_assert(NW == 32, "one lane per warp");
+    cost = __reduce_add_sync(0xffffffffu, cost);
+    tiles = __reduce_add_sync(0xffffffffu, tiles);
+    if (lane == 0) { s_cost[warp] = cost; s_tiles[warp] = tiles; }
+    __syncthreads();
+    int total = __reduce_add_sync(0xffffffffu, lane < NW ? s_cost[lane] : 0);
+    tiles = __reduce_add_sync(0xffffffffu, lane < NW ? s_tiles[lane] : 0);
+    if (plan_few(p, tiles, grid)) {
+        p.cost_item = 0;
+        total = tiles * p.cost_two;
+    }
+    const int share = (total + grid - 1) / grid;
+    cost = 0;
+#pragma unroll 1
+    for (int e = e0; e < e1; ++e) {
+        Entry x = ent[e];
+        entry_blocks(p, x, share);
+        entry_cost(p, x);
+        ent[e].blocks = x.blocks;
+        ent[e].cost = x.cost;
+        cost += x.cost;
+        items += entry_items(p, x);
+    }
+    int run = cost, run_items = items;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, run, d), z = __shfl_up_sync(0xffffffffu, run_items, d);
+        if (lane >= d) { run += y; run_items += z; }
+    }
+    __syncthreads();
+    if (lane == 31) { s_cost[warp] = run; s_items[warp] = run_items; }
+    __syncthreads();
+    const int wc = lane < NW ? s_cost[lane] : 0, wi = lane < NW ? s_items[lane] : 0;        // one warp's sums per lane
+    run += __reduce_add_sync(0xffffffffu, lane < warp ? wc : 0) - cost;
+    run_items += __reduce_add_sync(0xffffffffu, lane < warp ? wi : 0) - items;
+    total = __reduce_add_sync(0xffffffffu, wc);
+    const int n_items = __reduce_add_sync(0xffffffffu, wi);
+#pragma unroll 1
+    for (int e = e0; e < e1; ++e) {
+        const Entry x = ent[e];
+        at[e] = run;
+        item0[e] = run_items;
+        if (e < p.n_groups) {
+            o.ginfo[e] = GroupInfo{run_items, x.items, x.blocks, x.single};
+        } else {
+            // the prefix is somebody else's part where the sequence's own keys begin behind it
+            const int g = x.lo > 0 ? plan_group(p, x.seq) : -1;
+            o.sinfo[x.seq] = SeqInfo{g, g >= 0 ? (x.seq - p.group_start[g]) * p.R * p.G : 0, run_items, x.blocks};
+            if (e == p.n_groups) o.meta[0] = run_items;
+        }
+        run += x.cost;
+        run_items += entry_items(p, x);
+    }
+    if (tid == 0) item0[n] = n_items;
     const int stretch = plan_stretch(p, total, grid);
-    __syncthreads();                     // the CTA's own global writes are visible to its threads
-    const int n_items = item0[n], n_group_items = item0[p.n_groups];
+    __syncthreads();
+    const int n_group_items = item0[p.n_groups];
 #pragma unroll 1
     for (int i = tid; i < n_items; i += PLAN_THREADS) {
         int lo = 0, hi = n;              // last entry that starts at item i or before (entries without items share a start)
@@ -294,7 +312,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
             if (item0[mid] <= i) lo = mid;
             else hi = mid;
         }
-        const Entry x = plan_entry(p, lo, ok, share, false);
+        const Entry& x = ent[lo];
         const Item m = plan_item(p, x, i - item0[lo]);
         const int start = at[lo] + m.start, c0 = start / stretch, c1 = (start + item_last(p, m)) / stretch;
         o.ctas[i] = make_int2(c0, c1);
