@@ -186,10 +186,9 @@ __global__ void __launch_bounds__(SIMT_THREADS) prefix_attn_simt_kernel(const __
 // Four neighbouring packed rows of a (sequence, kv head) by W warps (eight lanes a row), each of which takes every W-th part of these rows; their sums are
 // added up at the end, so that the order is fixed. A warp requests PB parts together, results and statistics alike: the kernel waits for L2, not
 // for bytes. W = 4 where there are few rows (decoding: 8.3 -> 5.4 us), W = 1 where there are enough for all SMs (17408 rows: 18 us against 38 with four).
-constexpr int PB = 4;
-
 template <typename T, int HD, int W>
 __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant__ Params p) {
+    constexpr int PB = W == 1 ? 2 : 4;
     __shared__ float4 s_acc[W == 1 ? 1 : 4][4][HD / 4];
     __shared__ float2 s_ml[4][4];
     unsigned long long* trace = p.trace ? p.trace + 4 : nullptr;
@@ -202,70 +201,90 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
     const int tpi = p.plan.tiles_per_item, tr = p.plan.row_tile;
     pdl_wait();
     if (threadIdx.x == 0) trace_min(trace, 1);
-    const SeqInfo si = p.po.sinfo[b];
-    const int n_group_items = __ldcg(p.po.meta);
-    GroupInfo gi{};
-    if (si.group >= 0) gi = p.po.ginfo[si.group];
+    const int4* sp = reinterpret_cast<const int4*>(p.po.sinfo + b);
+    const int4 s0 = __ldcg(sp), s1 = __ldcg(sp + 1);
+    const SeqInfo si{s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+    const int gat = si.row_off + pr, gtile = gat / tr, otile = pr / tr, own_tiles = (RG + tr - 1) / tr, own_items = (own_tiles + tpi - 1) / tpi;
+    const bool g_one = si.group_single && gtile / tpi == si.group_items - 1, o_one = own_tiles % tpi != 0 && otile / tpi == own_items - 1;   // one query tile
 
     float M = -CUDART_INF_F, L = 0.f;
     float4 acc[HD / 32];
 #pragma unroll
     for (int k = 0; k < HD / 32; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    // The row's items: key blocks of the group, then its own. Its eight lanes look eight of them up at a time, and then go through
+    // all the parts of these.
+    const int n_items = si.group_blocks + si.blocks;
     int skip = W == 1 ? 0 : warp;                    // parts until this warp's next one
-    for (int own = si.group >= 0 ? 0 : 1; own < 2; ++own) {
-        const int at = own ? pr : si.row_off + pr, tile = at / tr, it = tile / tpi, row = at % tr;
-        const int row_tiles = (RG + tr - 1) / tr, blocks = own ? si.blocks : gi.blocks;
-        const int items = own ? (row_tiles + tpi - 1) / tpi : gi.items;
-        const bool one = (own ? row_tiles % tpi != 0 : gi.single) && it == items - 1;      // the item has one query tile
-        const int subs = tpi == 2 && one ? 2 : 1, sub0 = one ? 0 : tile % tpi;
-        for (int kb = 0; kb < blocks; ++kb) {
-            const int item = (own ? si.item0 : gi.item0) + (kvh * blocks + kb) * items + it;
+    const int most = __reduce_max_sync(0xffffffffu, n_items);
+    for (int e0 = 0; e0 < most; e0 += 8) {
+        const int e = e0 + sub8, kb = e - si.group_blocks;
+        int slot = 0, n = 0;                         // of item e: slot of its first part, parts
+        if (e < n_items) {
+            const bool own = kb >= 0;
+            const int item = own ? si.item0 + (kvh * si.blocks + kb) * own_items + otile / tpi
+                                 : si.group_item0 + (kvh * si.group_blocks + e) * si.group_items + gtile / tpi;
             const int2 ctas = __ldcg(p.po.ctas + item);
-            const int slot0 = item + ctas.x - (own ? n_group_items : 0), n = (ctas.y - ctas.x + 1) * subs;
-            int k0 = skip;
-            for (; k0 < n; k0 += W * PB) {
-                float2 ml[PB];
-                float4 o[PB][HD / 32];
+            slot = item + ctas.x - (own ? si.n_group_items : 0);
+            n = (ctas.y - ctas.x + 1) * (tpi == 2 && (own ? o_one : g_one) ? 2 : 1);
+        }
+        int end = n;                                 // parts up to this item's end
 #pragma unroll
-                for (int k = 0; k < PB; ++k) {
-                    const int part = k0 + W * k;
-                    if (part < n) {
-                        const int64_t r = slot_row(p, !own, slot0 + (subs == 2 ? part >> 1 : part), subs == 2 ? part & 1 : sub0, row);
-                        ml[k] = __ldcg(p.ml + r);
+        for (int d = 4; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, end, d);
+            if (lane >= d) end += y;
+        }
+        const int total = __shfl_sync(0xffffffffu, end, 28 + (lane & 3));
+        const int rounds = __reduce_max_sync(0xffffffffu, total), ends = min(7, most - e0 - 1);
+        for (int k0 = 0; k0 < rounds; k0 += W * PB) {      // the same for all lanes, which exchange values in it; rows differ in `skip` and `total`
+            float2 ml[PB];
+            float4 o[PB][HD / 32];
 #pragma unroll
-                        for (int x = 0; x < HD / 32; ++x) o[k][x] = __ldcg(reinterpret_cast<const float4*>(p.part + part_offset(r, HD, x * 8 + sub8)));
-                    } else {
-                        ml[k] = make_float2(-CUDART_INF_F, 0.f);
-                    }
+            for (int k = 0; k < PB; ++k) {
+                const int part = skip + k0 + W * k;
+                int x = 0, first = 0;                // the item that holds it, and that item's first part
+#pragma unroll 1
+                for (int i = 0; i < ends; ++i) {
+                    const int y = __shfl_sync(0xffffffffu, end, 4 * i + (lane & 3));
+                    if (part >= y) { x = i + 1; first = y; }
                 }
-                float top = M;
+                const int sl = __shfl_sync(0xffffffffu, slot, 4 * x + (lane & 3));
+                const bool own = e0 + x >= si.group_blocks, two_subs = tpi == 2 && (own ? o_one : g_one);
+                ml[k] = make_float2(-CUDART_INF_F, 0.f);
+                if (part < total) {
+                    const int q = part - first, tile = own ? otile : gtile;
+                    const int64_t r = slot_row(p, !own, sl + (two_subs ? q >> 1 : q), two_subs ? q & 1 : tile % tpi, (own ? pr : gat) - tile * tr);
+                    ml[k] = __ldcg(p.ml + r);
 #pragma unroll
-                for (int k = 0; k < PB; ++k)
-                    if (ml[k].y != 0.f) top = fmaxf(top, ml[k].x);
-                const float ref = top > -CUDART_INF_F ? top : 0.f;
-                const float keep = M > -CUDART_INF_F ? exp2f(M - ref) : 0.f;
-                M = top;
-                L *= keep;
-#pragma unroll
-                for (int x = 0; x < HD / 32; ++x) { acc[x].x *= keep; acc[x].y *= keep; acc[x].z *= keep; acc[x].w *= keep; }
-#pragma unroll
-                for (int k = 0; k < PB; ++k) {
-                    if (ml[k].y == 0.f) continue;        // no key in that part: what lies there was never written
-                    const float wgt = exp2f(ml[k].x - ref);
-                    L = fmaf(ml[k].y, wgt, L);
-#pragma unroll
-                    for (int x = 0; x < HD / 32; ++x) {
-                        acc[x].x = fmaf(o[k][x].x, wgt, acc[x].x);
-                        acc[x].y = fmaf(o[k][x].y, wgt, acc[x].y);
-                        acc[x].z = fmaf(o[k][x].z, wgt, acc[x].z);
-                        acc[x].w = fmaf(o[k][x].w, wgt, acc[x].w);
-                    }
+                    for (int c = 0; c < HD / 32; ++c) o[k][c] = __ldcg(reinterpret_cast<const float4*>(p.part + part_offset(r, HD, c * 8 + sub8)));
                 }
             }
-            // parts of this warp in the next item: those at `skip`, `skip` + W, ... of the parts behind this item's n
-            const int passed = n - skip;
-            skip = passed <= 0 ? -passed : (W - passed % W) % W;
+            float top = M;
+#pragma unroll
+            for (int k = 0; k < PB; ++k)
+                if (ml[k].y != 0.f) top = fmaxf(top, ml[k].x);
+            const float ref = top > -CUDART_INF_F ? top : 0.f;
+            const float keep = M > -CUDART_INF_F ? exp2f(M - ref) : 0.f;
+            M = top;
+            L *= keep;
+#pragma unroll
+            for (int x = 0; x < HD / 32; ++x) { acc[x].x *= keep; acc[x].y *= keep; acc[x].z *= keep; acc[x].w *= keep; }
+#pragma unroll
+            for (int k = 0; k < PB; ++k) {
+                if (ml[k].y == 0.f) continue;        // no key in that part: what lies there was never written
+                const float wgt = exp2f(ml[k].x - ref);
+                L = fmaf(ml[k].y, wgt, L);
+#pragma unroll
+                for (int x = 0; x < HD / 32; ++x) {
+                    acc[x].x = fmaf(o[k][x].x, wgt, acc[x].x);
+                    acc[x].y = fmaf(o[k][x].y, wgt, acc[x].y);
+                    acc[x].z = fmaf(o[k][x].z, wgt, acc[x].z);
+                    acc[x].w = fmaf(o[k][x].w, wgt, acc[x].w);
+                }
+            }
         }
+        // parts of this warp among the next eight items: those at `skip`, `skip` + W, ... of them
+        const int passed = total - skip;
+        skip = passed <= 0 ? -passed : (W - passed % W) % W;
     }
     auto store = [&](int r4, int c, float4 v, float m, float sum) {      // four columns of row row0 + r4
         const int prow = row0 + r4;
@@ -348,12 +367,10 @@ PrefixWs carve_prefix(void* base, const Sizes& z, const dflash_config& c, int64_
     w.po.segs = (Segment*)a.take((items + z.n_cta) * sizeof(Segment));
     w.po.list = (int2*)a.take(z.n_cta * sizeof(int2));
     w.po.ctas = (int2*)a.take(items * sizeof(int2));
-    w.po.ginfo = (GroupInfo*)a.take(std::max<int64_t>(n_groups, 1) * sizeof(GroupInfo));
     w.po.sinfo = (SeqInfo*)a.take(S * sizeof(SeqInfo));
     w.po.entries = (Entry*)a.take(n > PLAN_CACHE ? n * sizeof(Entry) : 0);
     w.po.start = (int32_t*)a.take(n * 4);
     w.po.item0 = (int32_t*)a.take((n + 1) * 4);
-    w.po.meta = (int32_t*)a.take(4);
     w.bytes = a.off;
     return w;
 }

@@ -181,19 +181,20 @@ __host__ __device__ __forceinline__ bool plan_segment(const PlanParams& p, const
 }
 
 // What the plan says to the other kernels.
-struct GroupInfo { int32_t item0, items, blocks, single; };
-// group whose prefix items cover this sequence or -1, its first packed row there; its own items
-struct SeqInfo { int32_t group, row_off, item0, blocks; };
+// Of a sequence, for the merge: the items of its group (none: blocks = 0), its first packed row there, and its own items.
+struct SeqInfo {
+    int32_t group_item0, group_items, group_blocks, group_single;
+    int32_t row_off, item0, blocks, n_group_items;     // n_group_items: of the call
+};
+static_assert(sizeof(SeqInfo) == 32, "two 16-byte loads");
 struct PlanOut {
     Segment* segs;                       // [items + CTAs]: segment of item i in CTA c has index i + c, so a CTA's segments are neighbours
     int2* list;                          // [CTAs] first segment and number of them
     int2* ctas;                          // [items] first and last CTA
-    GroupInfo* ginfo;                    // [n_groups]
     SeqInfo* sinfo;                      // [S]
     Entry* entries;                      // [n_groups + S] scratch, used where shared memory is too small: entries, and the cost and item at
     int32_t* start;                      // [n_groups + S]      which each starts
     int32_t* item0;                      // [n_groups + S + 1]
-    int32_t* meta;                       // [0] number of group items
 };
 
 constexpr int PLAN_THREADS = 512, MAX_CTAS = 512, PLAN_CACHE = 512;
@@ -289,14 +290,6 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
         const Entry x = ent[e];
         at[e] = run;
         item0[e] = run_items;
-        if (e < p.n_groups) {
-            o.ginfo[e] = GroupInfo{run_items, x.items, x.blocks, x.single};
-        } else {
-            // the prefix is somebody else's part where the sequence's own keys begin behind it
-            const int g = x.lo > 0 ? plan_group(p, x.seq) : -1;
-            o.sinfo[x.seq] = SeqInfo{g, g >= 0 ? (x.seq - p.group_start[g]) * p.R * p.G : 0, run_items, x.blocks};
-            if (e == p.n_groups) o.meta[0] = run_items;
-        }
         run += x.cost;
         run_items += entry_items(p, x);
     }
@@ -304,6 +297,16 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
     const int stretch = plan_stretch(p, total, grid);
     __syncthreads();
     const int n_group_items = item0[p.n_groups];
+#pragma unroll 1
+    for (int b = tid; b < p.S; b += PLAN_THREADS) {
+        const Entry& x = ent[p.n_groups + b];
+        SeqInfo q{0, 0, 0, 0, 0, item0[p.n_groups + b], x.blocks, n_group_items};
+        if (x.lo > 0) {                  // the keys below x.lo are the group's items
+            const int g = plan_group(p, b);
+            q = SeqInfo{item0[g], ent[g].items, ent[g].blocks, ent[g].single, (b - p.group_start[g]) * p.R * p.G, q.item0, q.blocks, n_group_items};
+        }
+        o.sinfo[b] = q;
+    }
 #pragma unroll 1
     for (int i = tid; i < n_items; i += PLAN_THREADS) {
         int lo = 0, hi = n;              // last entry that starts at item i or before (entries without items share a start)

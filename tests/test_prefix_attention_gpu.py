@@ -187,6 +187,19 @@ def test_long_prefix_and_many_sequences_again_and_again_bit_for_bit(shape, rows)
     x.check(out, lse, True, seqs=(0, 7, S - 1))
 
 
+@pytest.mark.parametrize("hq,hkv,rows,S,prefix,own", [(5, 1, 7, 9, 20000, 40), (7, 1, 3, 50, 12345, 700), (10, 2, 31, 5, 9001, 3), (3, 3, 32, 11, 6000, 0)])
+def test_many_key_blocks_and_rows_that_straddle_query_tiles(hq, hkv, rows, S, prefix, own):
+    # a prefix cut into dozens of blocks; neighbouring rows belong to different items, with different numbers of parts
+    cfg = config(hq=hq, hkv=hkv, layers=1)
+    lib = binding.DFlash(cfg)
+    x = Batch(cfg, rows, [0, S], [prefix], [prefix + own * b // S for b in range(S)], seed=S, layer=0)
+    for mode in ("full", "causal"):
+        out, lse = x.run(lib, MODES[mode])
+        torch.cuda.synchronize()
+        assert int(lib.status.item()) == 0
+        x.check(out, lse, mode == "causal", seqs=(0, S // 2, S - 1))
+
+
 @pytest.mark.parametrize("seed", range(16))
 def test_random_batches(seed):
     r = random.Random(seed)
