@@ -3,16 +3,8 @@
 // over k = the cached positions of sequence b and the block's own rows. A softmax over a union of key sets is put together
 // from its parts: with (m_i, l_i, o_i) of part i, M = max m_i,  out = sum e^(m_i - M) o_i / sum e^(m_i - M) l_i. So the rows of
 // all sequences of a group go against the prefix as ONE matrix product, each sequence's rows go against its own keys,
-// and a second launch merges the parts of every row in a fixed order (prefix_plan.cuh cuts up the work).
-//
-// Tensor-core kernel (bf16): one persistent CTA per SM with a TMA warp, an MMA warp and two softmax warpgroups. An item with two
-// query tiles (128 rows each) gives one to each warpgroup, which read every K/V tile of 128 keys together; an item
-// with one tile has the warpgroups take alternate key tiles. So while one warpgroup is at its exponentials the tensor core works for the other.
-//   S_t = Q_t K^T   tcgen05.mma, operands in shared memory, 128 x 128 fp32 in TMEM
-//   softmax         one thread per row; the running maximum is only raised when a tile tops it by more than 2^8 (the row of O_t in
-//                   TMEM is then rescaled in place); P goes back into the TMEM columns of S as bf16
-//   O_t += P_t V    tcgen05.mma with P from TMEM, V as an MN-major operand straight from the page layout
-// K and V tiles go through one ring of 32 KB stages that runs on across items. Every wait is bounded.
+// and a last launch merges the parts of every row in a fixed order. A small first launch cuts up the work (prefix_plan.cuh).
+// The tensor-core kernel for bf16 is in prefix_attn_tc.cuh; here are the CUDA-core kernel, the merge and the launches.
 #include "prefix_attn.cuh"
 
 #include "prefix_attn_tc.cuh"
@@ -26,10 +18,14 @@ namespace {
 using namespace ptx;
 
 // ---- CUDA-core kernel: fp32, and bf16 with pages of less than 8 tokens ----------------------------------------------
-// 64 packed rows against chunks of 64 keys; 256 threads, each 4 x 4 scores and 4 x hd/16 outputs.
+// 64 packed rows against chunks of 64 keys; 256 threads, each 4 x 4 scores and 4 x hd/16 outputs. One call of few rows is bound by the latency of
+// its loads: with a chunk's K and V all under way at once, 16 bytes a load, 3 sequences x 5 rows behind 40 fp32 positions take 19 us in a graph (25 with 4-byte loads).
 constexpr int SIMT_THREADS = 256, SIMT_ROWS = 64;
-__device__ __forceinline__ float to_f(float v) { return v; }
-__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+}
 template <int HD>
 constexpr int simt_smem() { return (SIMT_ROWS * (HD + 4) * 2 + CHUNK_KEYS * HD + SIMT_ROWS * (CHUNK_KEYS + 4) + 2 * SIMT_ROWS) * 4; }
 
@@ -52,11 +48,11 @@ __global__ void __launch_bounds__(SIMT_THREADS) prefix_attn_simt_kernel(const __
         const Segment s = p.po.segs[list.x + k];
         __syncthreads();
         const int rows = min(SIMT_ROWS, s.n_rows - s.row0);
-        for (int i = threadIdx.x; i < SIMT_ROWS * HD; i += SIMT_THREADS) {
-            const int row = i / HD, d = i % HD, pr = s.row0 + row;
-            float v = 0.f;
-            if (row < rows) v = to_f(Q[(((int64_t)s.seq * R + pr / G) * p.Hq + s.kvh * G + pr % G) * HD + d]);
-            sQ[row * (HD + 4) + d] = v;
+        for (int i = threadIdx.x; i < SIMT_ROWS * HD / 4; i += SIMT_THREADS) {
+            const int row = i / (HD / 4), d = i % (HD / 4) * 4, pr = s.row0 + row;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (row < rows) v = load4(Q + (((int64_t)s.seq * R + pr / G) * p.Hq + s.kvh * G + pr % G) * HD + d);
+            *reinterpret_cast<float4*>(sQ + row * (HD + 4) + d) = v;
         }
         float o[4][HD / 16], m[4], l[4];
 #pragma unroll
@@ -70,32 +66,47 @@ __global__ void __launch_bounds__(SIMT_THREADS) prefix_attn_simt_kernel(const __
             const bool block = c >= s.ctx_chunks;
             const int key0 = (s.chunk + c) * CHUNK_KEYS;
             __syncthreads();                         // the previous chunk is used up
-            // a key that does not exist loads as zeros and is masked below
+            // a key that does not exist loads as zeros and is masked below; 16 threads a key, each of which looks four keys up and then has all their loads under way
             unsigned long long exist = 0;
-            for (int k = 0; k < CHUNK_KEYS; k += 16) {   // 16 threads a key: each row of 16 threads looks its keys up
-                const int key = k + ty;
-                const T *kp = nullptr, *vp = nullptr;
+            const T *kp[4], *vp[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int key = 16 * k + ty;
+                kp[k] = vp[k] = nullptr;
                 if (block) {
                     if (key < R) {
-                        kp = KB + (((int64_t)s.seq * R + key) * Hkv + s.kvh) * HD;
-                        vp = VB + (((int64_t)s.seq * R + key) * Hkv + s.kvh) * HD;
+                        kp[k] = KB + (((int64_t)s.seq * R + key) * Hkv + s.kvh) * HD;
+                        vp[k] = VB + (((int64_t)s.seq * R + key) * Hkv + s.kvh) * HD;
                     }
                 } else if (key0 + key >= s.lo && key0 + key < s.hi) {
                     const int pos = key0 + key, j = pos / p.page_size;
                     const int page = j < p.max_pages ? __ldg(p.page_table + (int64_t)s.seq * p.max_pages + j) : -1;
                     if (page >= 0 && page < p.n_pages) {
-                        kp = pool + ((((int64_t)p.layer * p.n_pages + page) * 2 * Hkv + s.kvh) * p.page_size + pos % p.page_size) * HD;
-                        vp = kp + (int64_t)Hkv * p.page_size * HD;
+                        kp[k] = pool + ((((int64_t)p.layer * p.n_pages + page) * 2 * Hkv + s.kvh) * p.page_size + pos % p.page_size) * HD;
+                        vp[k] = kp[k] + (int64_t)Hkv * p.page_size * HD;
                     } else if (tx == 0 && p.status) {
                         atomicOr(p.status, DFLASH_DEV_BAD_PAGE);
                     }
                 }
-                for (int d = tx; d < HD; d += 16) {
-                    sK[key * (HD + 4) + d] = kp ? to_f(kp[d]) : 0.f;
-                    sV[key * HD + d] = vp ? to_f(vp[d]) : 0.f;
-                }
-                if (kp) exist |= 1ull << key;
+                if (kp[k]) exist |= 1ull << key;
             }
+            float4 kv[4][2][HD / 64];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int x = 0; x < HD / 64; ++x) {
+                    const int d = 64 * x + 4 * tx;
+                    kv[k][0][x] = kp[k] ? load4(kp[k] + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    kv[k][1][x] = kp[k] ? load4(vp[k] + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int x = 0; x < HD / 64; ++x) {
+                    const int key = 16 * k + ty, d = 64 * x + 4 * tx;
+                    *reinterpret_cast<float4*>(sK + key * (HD + 4) + d) = kv[k][0][x];
+                    *reinterpret_cast<float4*>(sV + key * HD + d) = kv[k][1][x];
+                }
             // which keys exist, for everybody: each thread knows 4 of them
             uint32_t lo = (uint32_t)exist, hi = (uint32_t)(exist >> 32);
             lo = __reduce_or_sync(0xffffffffu, lo);
@@ -378,10 +389,12 @@ PlanParams plan_params(const dflash_config& c, const Sizes& z, int S, int R, int
     PlanParams q{};
     q.S = S; q.R = R; q.G = c.n_q_heads / c.n_kv_heads; q.Hkv = c.n_kv_heads; q.n_groups = n_groups; q.max_ctx_len = max_ctx_len;
     q.row_tile = z.row_tile; q.tiles_per_item = z.tiles_per_item; q.chunks_per_tile = z.chunks_per_tile;
-    // Tensor-core kernel, in units of 500 clocks: a key tile takes 2650 with one query tile (its bytes at the HBM rate) and 4150 with two (its products),
-    // the change to another item 4500. CUDA cores: a chunk takes about as long as it takes to begin an item.
+    // Tensor-core kernel, in units of 500 clocks: a key tile takes 2650 with one query tile (its bytes at the HBM rate) and 3560 with two (its products),
+    // the change to another item about 4500. (One query tile for as much as two, 8 : 5 : 9, left CTAs waiting: 32 sequences x 17 rows behind
+    // 32768 positions 311 us, now 282; an item for 15 is better for many whole contexts, 114 us against 125, and worse for decoding.)
+    // CUDA cores: a chunk takes about as long as it takes to begin an item.
     const bool tc = use_tc(c);
-    q.cost_item = tc ? 9 : 3; q.cost_one = tc ? 5 : 4; q.cost_two = tc ? 8 : 4;
+    q.cost_item = tc ? 10 : 3; q.cost_one = tc ? 5 : 4; q.cost_two = tc ? 7 : 4;
     return q;
 }
 // whether the costs of any lengths up to max_ctx_len stay below 2^31 with room for the sums that plan_kernel forms

@@ -211,12 +211,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 d;
-    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Low words: K-major operand (leading offset unused); V tile as MN-major operand, [key][64 elements] halves `half_bytes` apart.
@@ -240,25 +234,6 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d_tmem),
         "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(DESC_HI)
         : "memory");
-}
-
-// 2^x for two values of at most 127 without the special-function unit, which at 4 results a clock and SM sub-partition would take as long
-// for a tile's exponentials as the tensor core takes for its products: x = n + f with |f| <= 1/2 by adding and subtracting 1.5 * 2^23, 2^f by a
-// polynomial fitted on Chebyshev nodes (relative error 2.1e-7, as good as ex2.approx), times 2^n put together from its bits.
-// Values below -126 count as -126, NaN stays NaN.
-__device__ __forceinline__ float2 poly_exp2(float2 x) {
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
-    const float2 big = make_float2(12582912.f, 12582912.f);
-    const float2 t = add2(x, big), n = add2(t, make_float2(-12582912.f, -12582912.f));
-    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
-    float2 y = fma2(f, make_float2(0.0013276468962f, 0.0013276468962f), make_float2(0.0096755409613f, 0.0096755409613f));
-    y = fma2(y, f, make_float2(0.0555071346462f, 0.0555071346462f));
-    y = fma2(y, f, make_float2(0.2402212023735f, 0.2402212023735f));
-    y = fma2(y, f, make_float2(0.6931469440460f, 0.6931469440460f));
-    y = fma2(y, f, make_float2(1.0000001192093f, 1.0000001192093f));
-    const float2 s = make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3f800000), __int_as_float((__float_as_int(t.y) << 23) + 0x3f800000));
-    return mul2(y, s);
 }
 
 // ---- copies: warp 16 K tiles, queries and tile masks; warp 19 V tiles ----
@@ -398,8 +373,8 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
 
 // ---- products: a thread for each query tile ----
 // Products queue up only a few deep behind the issuing thread, and a wait on a barrier takes it 0.1 us even if there is nothing to wait for: one
-// thread for both tiles left the tensor core idle between its groups of products (3370 clocks a key tile with hardly any to do). The
-// threads take turns, so that the products of one tile run while the other tile is at its softmax, and not both tiles' at once.
+// thread for both tiles left the tensor core idle between its groups of products (3370 clocks a key tile with hardly any to do). Two
+// query tiles take turns, so that the products of one run while the other is at its softmax, and not both tiles' at once.
 template <int HD>
 __device__ __forceinline__ void mma_role(const Params& p, int t) {
     using Sh = Shape<HD>;
@@ -421,7 +396,7 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
             if (!two) commit(bar);
         };
         const int first = two ? 0 : t, step = two ? 1 : 2;       // this thread's key tiles; scores run one ahead of values
-        const int last = two ? n : n + (n & 1) + t;              // both threads take the same number of turns
+        const int last = two ? n : n + 1;
         if (first >= n && lead) commit(sb + Sh::Q_EMPTY);
 #pragma unroll 1
         for (int j = first; j <= last; j += step) {
@@ -431,13 +406,15 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
             // the wait for P last: what comes after it adds to every tile's time
             if (do_v) ok = bar_wait(sb + Sh::FULL_V + 8 * sv, (tile0 + v) / Sh::NV & 1, sb + Sh::ABORT);
             if (do_s && ok) ok = bar_wait(sb + Sh::FULL_K + 8 * sk, (tile0 + j) / Sh::NK & 1, sb + Sh::ABORT);
-            ok = ok && bar_wait(sb + Sh::TURN + 8 * t, turn, sb + Sh::ABORT);
+            if (two && ok) {
+                ok = bar_wait(sb + Sh::TURN + 8 * t, turn, sb + Sh::ABORT);
+                turn ^= 1;
+            }
             if (do_v && ok) {
                 ok = bar_wait(sb + Sh::P_FULL + 8 * t, p_phase, sb + Sh::ABORT);
                 p_phase ^= 1;
             }
             if (!ok) break;
-            turn ^= 1;
             tc_fence_after();
             if (lead) {
                 if (do_v) {                              // O_t (+)= P_t V_v; the first product of a segment starts its accumulator
@@ -453,7 +430,7 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
                     if (v + step >= n) commit(sb + Sh::O_FULL + 8 * t);
                 }
                 // the other thread needs about 200 clocks to see its turn, and finds these products still running
-                bar_arrive(sb + Sh::TURN + 8 * (t ^ 1));
+                if (two) bar_arrive(sb + Sh::TURN + 8 * (t ^ 1));
                 if (do_s) {                              // S_t = Q K_j^T; descriptors differ in their address field alone
                     const uint32_t kd = k_desc + sk * (Sh::STAGE >> 4), qd = q_desc + (two ? t * (Sh::Q_BYTES >> 4) : 0), d = tmem + t * 128;
                     const uint32_t idesc = instr_desc_bf16(128, 64 * min(2, n_chunks - 2 * j));
@@ -483,20 +460,17 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
 // ---- softmax: two threads a query row, of 64 keys each ----
 // Four warps a scheduler hide one another's latencies; with one thread a row (208 registers, two warps a scheduler) a tile's softmax took 2000 to 2900
 // clocks against the 1024 of its products.
-// P of 32 keys (16 columns), its part of the row sum. FAST: every fourth pair takes the polynomial, and the largest score is looked for.
-template <bool FAST>
+// P of 32 keys (16 columns), its part of the row sum, and (LOOK) the largest score. (A polynomial on the FMA pipes for a quarter of the exponentials, to
+// relieve the special-function unit, made no difference to 17 rows of 32 sequences and cost 10 % for half of them.)
+template <bool LOOK>
 __device__ __forceinline__ void softmax_32(const float* s, float scale, float m, float2* sum, float& top, uint32_t* pk) {
     const float2 scale2 = make_float2(scale, scale), neg2 = make_float2(-m, -m);
 #pragma unroll
     for (int c = 0; c < 16; ++c) {
-        if (FAST) top = max3(top, s[2 * c], s[2 * c + 1]);
+        if (LOOK) top = max3(top, s[2 * c], s[2 * c + 1]);
         float2 x = fma2(make_float2(s[2 * c], s[2 * c + 1]), scale2, neg2);
-        if (FAST && (c & 3) == 3) {
-            x = poly_exp2(x);
-        } else {
-            x.x = fast_exp2(x.x);
-            x.y = fast_exp2(x.y);
-        }
+        x.x = fast_exp2(x.x);
+        x.y = fast_exp2(x.y);
         sum[c & 1] = add2(sum[c & 1], x);
         pk[c] = pack_bf16(x.x, x.y);                     // P in bf16: as coarse as the operands V and K
     }
