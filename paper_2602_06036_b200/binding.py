@@ -280,6 +280,7 @@ class DFlash:
         self._keep = {}
         self._ws = None
         self._scratches = {}
+        self._needs = {}
         self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
 
@@ -525,23 +526,28 @@ class DFlash:
         return self._dev(kv_pool, c.torch_dtype, c.n_layers, kv_pool.shape[1], 2, c.n_kv_heads, c.page_size, c.head_dim)
 
     def _scratch(self, name, query, key, stream):
-        """Workspace of the calls below (address and size), for the sizes in `key`: grown on demand, on the stream that asks for it. A smaller
-        one stays alive, because a captured graph may still write to it."""
-        kept = self._scratches.get(name)
-        if kept is None:
-            kept = self._scratches[name] = {"need": {}, "held": [], "at": None, "size": -1}
-        need = kept["need"].get(key)
+        """Workspace of the calls below for the sizes in `key`: (tensor, address, bytes). Every stream has its own, grown on demand, so that calls
+        on two streams may overlap. A captured call takes a fresh one from its graph's memory, where it stays the graph's: graphs share
+        none with each other or with calls outside."""
+        need = self._needs.get((name, key))
         if need is None:
             need = int(query(*key))
             if need < 0:
                 raise DFlashError(need)
-            kept["need"][key] = need
-        if kept["size"] < need:
-            with torch.cuda.device(self.device), torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
-                t = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
-            kept["held"].append(t)
-            kept["at"], kept["size"] = t.data_ptr(), t.numel()
-        return kept["at"], kept["size"]
+            need = self._needs[name, key] = max(need, 256)
+        if stream is None and torch.cuda.current_device() == self._index:
+            captured, raw = torch.cuda.is_current_stream_capturing(), _current_stream(self._index)
+        else:
+            with torch.cuda.device(self._index), torch.cuda.stream(stream):
+                captured, raw = torch.cuda.is_current_stream_capturing(), _current_stream(self._index)
+        kept = None if captured else self._scratches.get((name, raw))
+        if kept is None or kept[2] < need:
+            with torch.cuda.device(self._index), torch.cuda.stream(stream):
+                t = torch.empty(need, dtype=torch.uint8, device=self.device)
+            kept = (t, t.data_ptr(), need)
+            if not captured:
+                self._scratches[name, raw] = kept
+        return kept
 
     def _call(self, fn, args, stream):
         """The library launches on the current device, which has to be the handle's."""
@@ -567,7 +573,7 @@ class DFlash:
         hq, hkv, hd = c.n_q_heads, c.n_kv_heads, c.head_dim
         n = 0 if prefix_len is None else prefix_len.shape[0]
         width = page_table.shape[1]
-        ws, ws_bytes = self._scratch("prefix_attention", self._prefix_ws, (S, R, n), stream)
+        held, ws, ws_bytes = self._scratch("prefix_attention", self._prefix_ws, (S, R, n), stream)
         a = PrefixAttnArgs(mode, self._dev(q, dt, S, R, hq, hd), self._dev(k_blk, dt, S, R, hkv, hd), self._dev(v_blk, dt, S, R, hkv, hd), S, R, n,
                            self._dev(group_start, i32, n + 1) if n else None, self._dev(prefix_len, i32, n) if n else None, self._dev(ctx_len, i32, S),
                            int(max_ctx_len), self._dev(page_table, i32, S, width), width, self._pool(kv_pool), kv_pool.shape[1], layer,
@@ -587,7 +593,7 @@ class DFlash:
         rows, width = page_table.shape
         pages = kv_pool.shape[1]
         cs, cd, cn = copies if copies is not None else (None, None, None)
-        ws, ws_bytes = self._scratch("pages", self.lib.dflash_pages_workspace_bytes, (n, width, pages), stream)
+        held, ws, ws_bytes = self._scratch("pages", self.lib.dflash_pages_workspace_bytes, (n, width, pages), stream)
         a = st(n, *[self._dev(t, i32, n) for t in lists], self._dev(page_table, i32, rows, width), rows, width, self._dev(ref_count, i32, pages),
                self._pool(kv_pool), pages, self._dev(cs, i32, n), self._dev(cd, i32, n), self._dev(cn, i32, n), ws, ws_bytes, self.status.data_ptr())
         self._call(fn, a, stream)
@@ -608,7 +614,7 @@ class DFlash:
         rows, width = page_table.shape
         pages = kv_pool.shape[1]
         cs, cd, cn = copies if copies is not None else (None, None, None)
-        ws, ws_bytes = self._scratch("pages", self.lib.dflash_pages_workspace_bytes, (0, width, pages), stream)
+        held, ws, ws_bytes = self._scratch("pages", self.lib.dflash_pages_workspace_bytes, (0, width, pages), stream)
         a = PagesCompactArgs(self._dev(page_table, i32, rows, width), rows, width, self._dev(ref_count, i32, pages), self._pool(kv_pool), pages,
                              self._dev(n_live, i32, 1), self._dev(cs, i32, pages // 2), self._dev(cd, i32, pages // 2), self._dev(cn, i32, 1), ws, ws_bytes,
                              self.status.data_ptr())

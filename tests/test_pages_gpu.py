@@ -289,6 +289,37 @@ def test_serving_round_captured_into_a_graph():
         assert torch.equal(outs2[0], outs[0]) and torch.equal(outs2[1], outs[1])
 
 
+def test_calls_on_two_streams_overlap():
+    """Two tables over two pools, worked on from two streams with one handle: each stream has its own workspace."""
+    cfg = config(hq=4, hkv=2, hd=64, page=16)
+    lib = binding.DFlash(cfg)
+    kinds = [([100, 0, 0, 0, 37], [0, 4], [1, 2], [90, 37]), ([64, 50, 0, 0], [1, 0, 1], [2, 3, 2], [33, 64, 5])]
+    states, alone, streams = [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+
+    def work(s, parent, child, keep, rows, room, stream):
+        lib.dflash_pages_fork(parent, child, keep, s.d_table, s.d_ref, s.d_pool, stream=stream)
+        lib.dflash_pages_resize(rows, keep, room, s.d_table, s.d_ref, s.d_pool, stream=stream)
+        lib.dflash_pages_compact(s.d_table, s.d_ref, s.d_pool, stream=stream)
+
+    for k, (lens, parent, child, keep) in enumerate(kinds):
+        lists = (i32(parent), i32(child), i32(keep), i32(child), i32([n + 20 for n in keep]))
+        one, two = (State(cfg, 60, len(lens), 9, lens, seed=40 + k) for _ in range(2))
+        work(one, *lists, None)
+        torch.cuda.synchronize()
+        first = int(lib.status.item())
+        lib.status.zero_()
+        states.append((two, lists, first))
+        alone.append(one)
+    torch.cuda.synchronize()
+    for (two, lists, _), stream in zip(states, streams):
+        work(two, *lists, stream)
+    torch.cuda.synchronize()
+    assert int(lib.status.item()) == states[0][2] | states[1][2]
+    for one, (two, _, _) in zip(alone, states):
+        assert torch.equal(one.d_table, two.d_table) and torch.equal(one.d_ref, two.d_ref)
+        np.testing.assert_array_equal(bits_of(one.d_pool), bits_of(two.d_pool))
+
+
 def test_refusals():
     cfg = config(hq=8, hkv=2)
     lib = binding.DFlash(cfg)

@@ -435,3 +435,42 @@ def test_refusals_leave_the_output_alone():
             lib.dflash_prefix_attention(0, a["q"], a["k"], a["v"], a["starts"], a["prefix"], a["lens"], 200, a["table"], a["pool"], 0, out)
     torch.cuda.synchronize()
     assert bool((out == 7.0).all())
+
+
+def test_calls_on_two_streams_and_graphs_of_two_streams_overlap():
+    """Eager calls on two streams have a workspace each, as have captured calls: they may run at once, in any order."""
+    cfg = config(hq=8, hkv=2)
+    lib = binding.DFlash(cfg)
+    batches = [Batch(cfg, 16, [0, 6], [1500], [1600 + 10 * i for i in range(6)], seed=31), Batch(cfg, 7, [1, 5], [700], [900, 1400, 800, 701, 2500], seed=32)]
+    data = [b.cuda() for b in batches]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    want = [b.run(lib, 1, d) for b, d in zip(batches, data)]
+    outs = [(torch.zeros_like(o), torch.zeros_like(l)) for o, l in want]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, d, o, s in zip(batches, data, outs, streams):
+            b.run(lib, 1, d, *o, stream=s)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert torch.equal(o[0], w[0]) and torch.equal(o[1], w[1])
+    graphs = []
+    for b, d, o in zip(batches, data, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(10):
+                b.run(lib, 1, d, *o)
+        graphs.append(g)
+    for o in outs:
+        o[0].zero_()
+        o[1].zero_()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        batches[0].run(lib, 1, data[0], *[torch.empty_like(t) for t in outs[0]])
+    torch.cuda.synchronize()
+    assert int(lib.status.item()) == 0
+    for b, o, w in zip(batches, outs, want):
+        assert torch.equal(o[0], w[0]) and torch.equal(o[1], w[1])
+        b.check(*o, True)
