@@ -405,13 +405,15 @@ int32_t dflash_block_attention_bwd(dflash_handle* h, const dflash_attn_bwd_args*
  * All K/V of a prefix are read once per group (and kv head); the rows of all its sequences are the rows of ONE
  * product with them.
  * Any rows 1..32, any Hq/Hkv up to 128. bf16 with 8- to 256-token pages runs on the tensor cores (head_dim 64 and
- * 128); fp32 and smaller pages take a CUDA-core kernel. Two launches (the second merges the partial results of the key ranges in a
- * fixed order: bit-reproducible). Lengths and groups are device data: a captured call may be replayed with others, as
- * long as max_ctx_len bounds every ctx_len and prefix_len (longer ones are clamped and set DFLASH_DEV_CTX_OVERFLOW).
+ * 128); fp32 and smaller pages take a CUDA-core kernel. Three launches: how the work is cut up, the attention, and the partial results
+ * of the key ranges merged in a fixed order (bit-reproducible). Lengths and groups are device data: a captured call may be
+ * replayed with others, as long as max_ctx_len bounds every ctx_len and prefix_len (longer ones are clamped and set
+ * DFLASH_DEV_CTX_OVERFLOW).
  * group_start must not fall and must lie in 0..batch, else DFLASH_DEV_BAD_GROUP is set and every sequence reads its
  * own row. A page index outside the pool sets DFLASH_DEV_BAD_PAGE and its keys are left out.
- * Errors: DFLASH_ERR_INVALID_ARG, DFLASH_ERR_UNSUPPORTED (more than 65535 sequences or groups, Hq/Hkv > 128),
- * DFLASH_ERR_WORKSPACE. Calls must not overlap in time if they share a workspace. */
+ * q, k_blk, v_blk, out and kv_pool lie on 16-byte boundaries.
+ * Errors: DFLASH_ERR_INVALID_ARG, DFLASH_ERR_UNSUPPORTED (more than 65535 sequences or groups, Hq/Hkv > 128, batch and max_ctx_len
+ * so large that their products no longer fit 32-bit costs: about 6e7 key tiles), DFLASH_ERR_WORKSPACE. Calls must not overlap in time if they share a workspace. */
 typedef struct {
     int32_t        mode;         /* DFLASH_ATTN_FULL | DFLASH_ATTN_CAUSAL                     */
     const void*    q;            /* [device] [batch, rows, Hq, hd], position-encoded          */

@@ -1,6 +1,6 @@
 // How the work of the shared-prefix attention is cut up: one chain of key tiles over all (rows, kv head) items, of which
 // every CTA takes an equal stretch by cost. A small kernel writes each CTA's segments down (the arithmetic inlined into the
-// attention kernel itself made its code 231 KB long and its instruction cache miss all the time: 567 us for what now takes a third).
+// attention kernel itself made its code 231 KB long and its instruction cache miss all the time: 32 sequences x 17 rows behind 32768 positions took 567 us, now 276).
 //
 // Entries: the groups (rows of all their sequences against the prefix), then the sequences (their rows against what is
 // their own: cached keys behind the prefix, and the block). The query rows of an entry and kv head are "packed":
