@@ -75,23 +75,32 @@ struct Shape {
     // the other warp's and still open, and the wait for a phase's parity would let it pass. A K tile is used up a softmax earlier than its V tile.
     static constexpr int NK = HD == 128 ? 2 : 5, NV = HD == 128 ? 3 : 5;
     static constexpr uint32_t RING_K = 2 * Q_BYTES, RING_V = RING_K + NK * STAGE;
-    static constexpr uint32_t Q_FULL = RING_V + NV * STAGE;   // queries and the segment they belong to are there
-    static constexpr uint32_t Q_EMPTY = Q_FULL + 8;           // queries used up, segment read by every softmax warp
-    static constexpr uint32_t FULL_K = Q_EMPTY + 8, FULL_V = FULL_K + 8 * NK;          // [NK], [NV]
-    static constexpr uint32_t EMPTY_K = FULL_V + 8 * NV, EMPTY_V = EMPTY_K + 8 * NK;   // [NK], [NV]
+    // Queries are loaded a segment ahead: one query tile goes to the half of the queries' 2 tiles that the segment before does not use. (Loaded only
+    // when the segment before had done its products, they held every change of item up: 148 sequences x 128 keys 61 us.)
+    static constexpr uint32_t Q_FULL = RING_V + NV * STAGE;   // [2] by the segment's parity: its queries and its words in CUR are there
+    static constexpr uint32_t Q_EMPTY = Q_FULL + 16;          // [2] queries used up, all earlier segments done with by every softmax warp
+    // A wait for a phase's parity cannot tell a phase from the one before the last. Key tiles that are shared out between the MMA threads leave each
+    // of them without news of the other's: it may wait for tile x while tile x - NV, the other's, has not landed. So the barriers of landed tiles are a longer ring:
+    // tile x - NF has always landed by then. (For K: the thread's tile before x is at least x - 3, that one's stage was free once tile x - 3 - NK was
+    // used. For V: with the scores of x, those of all tiles up to x - NK are there; the other thread, at most two segments behind, has used all its tiles
+    // but the last of these, which is at least x - NK - 2.)
+    static constexpr int NF = 8;
+    static constexpr uint32_t FULL_K = Q_EMPTY + 16, FULL_V = FULL_K + 8 * NF;          // [NF] by tile
+    static constexpr uint32_t EMPTY_K = FULL_V + 8 * NF, EMPTY_V = EMPTY_K + 8 * NK;   // [NK], [NV] by stage
     static constexpr uint32_t DRAIN = EMPTY_V + 8 * NV;       // [2] all products of an MMA thread that gives up
     static constexpr uint32_t TURN = DRAIN + 16;              // [2] the other MMA thread has issued its products
     static constexpr uint32_t S_FULL = TURN + 16;             // [2] S_t written (and all earlier products done)
     static constexpr uint32_t P_FULL = S_FULL + 16;           // [2] P_t written, O_t rescaled, missing V rows zeroed
     static constexpr uint32_t O_FULL = P_FULL + 16;           // [2] the segment's last product into O_t done
     static constexpr uint32_t INFO = O_FULL + 16;             // [NI] TileInfo
-    static constexpr uint32_t CUR = INFO + NI * sizeof(TileInfo);       // [2] the segment whose queries are in shared memory, and the one before
-    static constexpr uint32_t XCH = CUR + 2 * sizeof(Segment);          // [2][128] words that the two threads of a row exchange
+    static constexpr uint32_t CUR = INFO + NI * sizeof(TileInfo);       // [4] the segments whose queries are in shared memory, and the one before
+    static constexpr uint32_t XCH = CUR + 4 * sizeof(Segment);          // [2][128] words that the two threads of a row exchange
     static constexpr uint32_t TMEM_SLOT = XCH + 1024;
     static constexpr uint32_t ABORT = TMEM_SLOT + 4;
     static constexpr int SMEM = 1024 + ABORT + 4;
     static_assert(SMEM <= 227 * 1024, "shared memory of one CTA");
     static_assert(NI >= NK + NV + 2, "a tile's mask outlives its K and V stages");
+    static_assert(NF >= NK + 3 && NF >= NV && (NF & (NF - 1)) == 0, "tile x - NF has landed when tile x is waited for");
 };
 
 // ---- 32-bit shared-memory addresses ----
@@ -254,15 +263,26 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
     const int shift = 31 - __clz(p.box), per_tile = KT >> shift, page_shift = 31 - __clz(p.page_size);
     const int2 list = __ldcg(p.po.list + blockIdx.x);
     auto fetch = [&](int k) { return k < list.y && lane < (int)sizeof(Segment) / 4 ? __ldcg(reinterpret_cast<const int*>(p.po.segs + list.x + k) + lane) : 0; };
-    int next = fetch(0);                                 // a word of the next segment per lane
-    int tile0 = 0, n_seg = 0;                            // key tiles of the segments before
+    // physical page of box `box` of a segment (of its cached keys, boxes that hold none aside), or -1
+    auto page_of = [&](int seq, int key0, int lo, int hi, int n_boxes, int box) {
+        const int key = key0 + (box << shift), pg = key >> page_shift;
+        return box < n_boxes && key < hi && key + p.box > lo && pg < p.max_pages ? __ldg(p.page_table + (int64_t)seq * p.max_pages + pg) : -1;
+    };
+#define WORD(words, field) __shfl_sync(0xffffffffu, words, offsetof(Segment, field) / 4)
+    auto first_pages = [&](int words) {                  // of a segment's first 32 boxes
+        return page_of(WORD(words, seq), WORD(words, chunk) * CHUNK_KEYS, WORD(words, lo), WORD(words, hi), WORD(words, ctx_chunks) * CHUNK_KEYS >> shift, lane);
+    };
+    // A word per lane of the next segment and of the one behind it; the next one's first pages: looked up a segment ahead
+    int next = fetch(0), after = fetch(1), next_page = first_pages(next), two_before = 0;
+    int issued = 0, n_seg = 0;                           // key tiles and segments so far
     bool ok = true;
 #pragma unroll 1
     while (n_seg < list.y) {
-        const int cur = next;
-        next = fetch(n_seg + 1);
-        auto seg = [&](int word) { return __shfl_sync(0xffffffffu, cur, word); };
-#define SEG(field) seg(offsetof(Segment, field) / 4)
+        const int cur = next, first_page = next_page;
+        next = after;
+        after = fetch(n_seg + 2);
+        next_page = first_pages(next);
+#define SEG(field) WORD(cur, field)
         const int n_chunks = SEG(n_chunks), n = (n_chunks + 1) >> 1;
         const int ctx_chunks = SEG(ctx_chunks), two = SEG(two), seq = SEG(seq), kvh = SEG(kvh), key0 = SEG(chunk) * CHUNK_KEYS, key_lo = SEG(lo), key_hi = SEG(hi), row0 = SEG(row0);
         const uint64_t pol = SEG(prefix) ? keep : once;
@@ -272,10 +292,9 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
             const int box0 = j * per_tile, n_box = min(per_tile, (ctx_chunks * CHUNK_KEYS >> shift) - box0);     // boxes of cached keys
             if (n_box > 0 && box0 >= win + 32) {
                 win = box0;
-                const int key = key0 + ((box0 + lane) << shift), pg = key >> page_shift;
-                const bool in = key < key_hi && key + p.box > key_lo && box0 + lane < (ctx_chunks * CHUNK_KEYS >> shift);
-                int page = -1;
-                if (in && pg < p.max_pages) page = __ldg(p.page_table + (int64_t)seq * p.max_pages + pg);
+                const int key = key0 + ((box0 + lane) << shift), boxes = ctx_chunks * CHUNK_KEYS >> shift;
+                const bool in = key < key_hi && key + p.box > key_lo && box0 + lane < boxes;
+                const int page = j == 0 ? first_page : page_of(seq, key0, key_lo, key_hi, boxes, box0 + lane);
                 const bool good = page >= 0 && page < p.n_pages;
                 if (in && !good && !vs && p.status) atomicOr(p.status, DFLASH_DEV_BAD_PAGE);
                 row = good ? (int)(((((int64_t)p.layer * p.n_pages + page) * 2 + vs) * p.plan.Hkv + kvh) * p.page_size) + (key & (p.page_size - 1)) : -1;
@@ -286,7 +305,7 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
             const int bc = ctx_chunks - 2 * j;           // and which of its two that is
             const uint32_t sel = n_box > 0 ? (uint32_t)((1ull << n_box) - 1) << (box0 - win) : 0u;
             if (!vs && lane == 0) {
-                const uint32_t ti = sb + Sh::INFO + ((tile0 + j) % NI) * (uint32_t)sizeof(TileInfo);
+                const uint32_t ti = sb + Sh::INFO + (issued % NI) * (uint32_t)sizeof(TileInfo);
                 const bool full = n_box == per_tile && (whole & sel) == sel;
                 if (!full) {
                     unsigned long long m0 = 0, m1 = 0;
@@ -309,7 +328,8 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
                 sts(ti + offsetof(TileInfo, full), full);
             }
             if (!warp_wait(empty_at + 8 * st, phase, sb + Sh::ABORT)) return false;
-            const uint32_t dst = ring + st * Sh::STAGE, bar = full_at + 8 * st;
+            const uint32_t dst = ring + st * Sh::STAGE, bar = full_at + 8 * (issued & (Sh::NF - 1));
+            ++issued;
             if (lane == 0) bar_expect(bar, (uint32_t)(__popc(there & sel) * p.box + (block ? 32 : 0)) * (HD * 2));
 #pragma unroll 1
             for (int x = 0; x < n_box; ++x) {
@@ -326,39 +346,43 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
             if (++st == n_stages) { st = 0; phase ^= 1; }
             return true;
         };
-        // K tiles that do not need a stage the previous segment's last product still reads go ahead of the queries
+        // K tiles that do not need a stage the previous segment's last product still reads go ahead of the queries, if those have to wait for the
+        // end of the previous segment
         int j = 0;
         if (!vs) {
+            const int wait_for = two | two_before ? n_seg - 1 : n_seg - 2;       // the segment that uses the same half or halves
+            two_before = two;
+            if (wait_for == n_seg - 1) {
 #pragma unroll 1
-            for (; j < min(n, 2) && ok; ++j) ok = issue(j);
-            if (!ok) break;
-            if (n_seg > 0 && !warp_wait(sb + Sh::Q_EMPTY, (n_seg - 1) & 1, sb + Sh::ABORT)) { ok = false; break; }
-            if (lane < (int)sizeof(Segment) / 4) sts(sb + Sh::CUR + (n_seg & 1) * (uint32_t)sizeof(Segment) + 4 * lane, cur);
+                for (; j < min(n, 2) && ok; ++j) ok = issue(j);
+                if (!ok) break;
+            }
+            if (wait_for >= 0 && !warp_wait(sb + Sh::Q_EMPTY + 8 * (wait_for & 1), (wait_for >> 1) & 1, sb + Sh::ABORT)) { ok = false; break; }
+            if (lane < (int)sizeof(Segment) / 4) sts(sb + Sh::CUR + (n_seg & 3) * (uint32_t)sizeof(Segment) + 4 * lane, cur);
             __syncwarp();
             if (lane == 0) {
                 const int q_row = seq * p.plan.R + row0 / p.plan.G;        // a tile begins with a whole (sequence, row)
-                const uint32_t bytes = (uint32_t)p.plan.row_tile * HD * 2;
-                bar_expect(sb + Sh::Q_FULL, two ? 2 * bytes : bytes);
+                const uint32_t bytes = (uint32_t)p.plan.row_tile * HD * 2, bar = sb + Sh::Q_FULL + 8 * (n_seg & 1), to = sb + (two ? 0 : (n_seg & 1) * Sh::Q_BYTES);
+                bar_expect(bar, two ? 2 * bytes : bytes);
 #pragma unroll 1
                 for (int t = 0; t <= two; ++t)
 #pragma unroll
                     for (int h = 0; h < Sh::HALVES; ++h)
-                        load_4d(sb + t * Sh::Q_BYTES + h * (128 * 128), &tmQ, h * 64, 0, kvh, q_row + t * p.rows_per_tile, sb + Sh::Q_FULL, keep);
+                        load_4d(to + t * Sh::Q_BYTES + h * (128 * 128), &tmQ, h * 64, 0, kvh, q_row + t * p.rows_per_tile, bar, keep);
             }
             __syncwarp();
         }
 #undef SEG
+#undef WORD
         ++n_seg;
 #pragma unroll 1
         for (; j < n && ok; ++j) ok = issue(j);
-        if (!ok) break;
-        tile0 += n;
     }
     if (ok && !vs && lane == 0) {                        // an empty segment ends the other roles
-        if (n_seg > 0 && !bar_wait(sb + Sh::Q_EMPTY, (n_seg - 1) & 1, sb + Sh::ABORT)) ok = false;
+        if (n_seg > 1 && !bar_wait(sb + Sh::Q_EMPTY + 8 * (n_seg & 1), (n_seg >> 1) - 1 & 1, sb + Sh::ABORT)) ok = false;
         if (ok) {
-            sts(sb + Sh::CUR + (n_seg & 1) * (uint32_t)sizeof(Segment) + offsetof(Segment, n_chunks), 0);
-            bar_arrive(sb + Sh::Q_FULL);
+            sts(sb + Sh::CUR + (n_seg & 3) * (uint32_t)sizeof(Segment) + offsetof(Segment, n_chunks), 0);
+            bar_arrive(sb + Sh::Q_FULL + 8 * (n_seg & 1));
         }
     }
     if (lane == 0 && !ok) {
@@ -366,8 +390,9 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
         if (p.status) atomicOr(p.status, DFLASH_DEV_TIMEOUT);
         // copies in flight have to land before the CTA's shared memory is given up
 #pragma unroll 1
-        for (int k = 0; k < n_stages; ++k) bar_wait(full_at + 8 * k, (k < st ? phase : phase ^ 1) ^ 1, 0, DRAIN_LIMIT);      // the last copies into each stage
-        if (!vs && n_seg > 0) bar_wait(sb + Sh::Q_FULL, (n_seg - 1) & 1, 0, DRAIN_LIMIT);
+        for (int x = max(0, issued - n_stages); x < issued; ++x) bar_wait(full_at + 8 * (x & (Sh::NF - 1)), x / Sh::NF & 1, 0, DRAIN_LIMIT);      // the last copies into each stage
+#pragma unroll 1
+        for (int k = max(0, n_seg - 2); k < n_seg && !vs; ++k) bar_wait(sb + Sh::Q_FULL + 8 * (k & 1), (k >> 1) & 1, 0, DRAIN_LIMIT);
     }
 }
 
@@ -386,8 +411,8 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
     bool ok = true;
 #pragma unroll 1
     for (int k = 0;; ++k) {
-        if (!bar_wait(sb + Sh::Q_FULL, k & 1, sb + Sh::ABORT)) { ok = false; break; }
-        const uint32_t cur = sb + Sh::CUR + (k & 1) * (uint32_t)sizeof(Segment);
+        if (!bar_wait(sb + Sh::Q_FULL + 8 * (k & 1), (k >> 1) & 1, sb + Sh::ABORT)) { ok = false; break; }
+        const uint32_t cur = sb + Sh::CUR + (k & 3) * (uint32_t)sizeof(Segment), q_empty = sb + Sh::Q_EMPTY + 8 * (k & 1);
         const int two = uniform(lds(cur + offsetof(Segment, two))), n_chunks = uniform(lds(cur + offsetof(Segment, n_chunks))), n = (n_chunks + 1) >> 1;
         if (n == 0) break;
         // Both threads say when they are done with a stage; with one query tile its only user does so twice.
@@ -397,15 +422,15 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
         };
         const int first = two ? 0 : t, step = two ? 1 : 2;       // this thread's key tiles; scores run one ahead of values
         const int last = two ? n : n + 1;
-        if (first >= n && lead) commit(sb + Sh::Q_EMPTY);
+        if (first >= n && lead) commit(q_empty);
 #pragma unroll 1
         for (int j = first; j <= last; j += step) {
             const int v = j - step;
             const bool do_v = v >= first && v < n, do_s = j < n;
             const uint32_t sv = (tile0 + v) % Sh::NV, sk = (tile0 + j) % Sh::NK;
             // the wait for P last: what comes after it adds to every tile's time
-            if (do_v) ok = bar_wait(sb + Sh::FULL_V + 8 * sv, (tile0 + v) / Sh::NV & 1, sb + Sh::ABORT);
-            if (do_s && ok) ok = bar_wait(sb + Sh::FULL_K + 8 * sk, (tile0 + j) / Sh::NK & 1, sb + Sh::ABORT);
+            if (do_v) ok = bar_wait(sb + Sh::FULL_V + 8 * ((tile0 + v) % Sh::NF), (tile0 + v) / Sh::NF & 1, sb + Sh::ABORT);
+            if (do_s && ok) ok = bar_wait(sb + Sh::FULL_K + 8 * ((tile0 + j) % Sh::NF), (tile0 + j) / Sh::NF & 1, sb + Sh::ABORT);
             if (two && ok) {
                 ok = bar_wait(sb + Sh::TURN + 8 * t, turn, sb + Sh::ABORT);
                 turn ^= 1;
@@ -432,7 +457,7 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
                 // the other thread needs about 200 clocks to see its turn, and finds these products still running
                 if (two) bar_arrive(sb + Sh::TURN + 8 * (t ^ 1));
                 if (do_s) {                              // S_t = Q K_j^T; descriptors differ in their address field alone
-                    const uint32_t kd = k_desc + sk * (Sh::STAGE >> 4), qd = q_desc + (two ? t * (Sh::Q_BYTES >> 4) : 0), d = tmem + t * 128;
+                    const uint32_t kd = k_desc + sk * (Sh::STAGE >> 4), qd = q_desc + (two ? t : k & 1) * (Sh::Q_BYTES >> 4), d = tmem + t * 128;
                     const uint32_t idesc = instr_desc_bf16(128, 64 * min(2, n_chunks - 2 * j));
 #pragma unroll
                     for (int kk = 0; kk < HD / 16; ++kk) {       // 16 elements of the row are 32 bytes; 64 elements on, the other column half begins
@@ -441,7 +466,7 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
                     }
                     commit(sb + Sh::S_FULL + 8 * t);
                     release(sb + Sh::EMPTY_K + 8 * sk);
-                    if (j + step >= n) commit(sb + Sh::Q_EMPTY);
+                    if (j + step >= n) commit(q_empty);
                 }
             }
             __syncwarp();
@@ -497,13 +522,13 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
     bool ok = true;
 #pragma unroll 1
     for (int k = 0;; ++k) {
-        ok = bar_wait(sb + Sh::Q_FULL, k & 1, sb + Sh::ABORT);
+        ok = bar_wait(sb + Sh::Q_FULL + 8 * (k & 1), (k >> 1) & 1, sb + Sh::ABORT);
         if (tile_any(t, !ok)) { ok = false; break; }
-        const uint32_t cur = sb + Sh::CUR + (k & 1) * (uint32_t)sizeof(Segment);     // stays until this warp, one segment on, arrives on Q_EMPTY
+        const uint32_t cur = sb + Sh::CUR + (k & 3) * (uint32_t)sizeof(Segment);     // stays until this warp, one segment on, arrives on Q_EMPTY
         const int two = lds(cur + offsetof(Segment, two)), n_chunks = lds(cur + offsetof(Segment, n_chunks)), n = (n_chunks + 1) >> 1;
         if (n == 0) break;
         __syncwarp();
-        if (lane == 0) bar_arrive(sb + Sh::Q_EMPTY);
+        if (lane == 0) bar_arrive(sb + Sh::Q_EMPTY + 8 * (k & 1));
         auto first_row = [&] { return lds(cur + offsetof(Segment, row0)) + (two ? t * p.plan.row_tile : 0); };
         const bool mine = row < min(p.plan.row_tile, lds(cur + offsetof(Segment, n_rows)) - first_row());       // the row exists
         float m_run = -CUDART_INF_F, l_run = 0.f;        // l_run: of this thread's keys
@@ -549,13 +574,13 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
             if (!all && h == 0) {
                 // V rows that do not exist must not poison P V: 0 x whatever the page holds there
                 const uint32_t st = (tile0 + j) % Sh::NV;
-                ok = bar_wait(sb + Sh::FULL_V + 8 * st, (tile0 + j) / Sh::NV & 1, sb + Sh::ABORT) && ok;
+                ok = bar_wait(sb + Sh::FULL_V + 8 * ((tile0 + j) % Sh::NF), (tile0 + j) / Sh::NF & 1, sb + Sh::ABORT) && ok;
                 if (!(lds64(ti + 8 * (row >> 6)) >> (row & 63) & 1)) {
                     const uint32_t v = sb + Sh::RING_V + st * Sh::STAGE + row * 128;
 #pragma unroll
                     for (int x = 0; x < Sh::HALVES; ++x)
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) zero16(v + x * (KT * 128) + c * 16);
+                        for (int c = 0; c < 8; ++c) zero16(v + x * (KT * 128) + ((c ^ row) & 7) * 16);       // neighbouring rows in different banks
                 }
                 fence_proxy_async();
             }
@@ -656,13 +681,14 @@ prefix_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     const int warp = uniform(threadIdx.x >> 5);
     if (threadIdx.x == 0) {
         trace_min(p.trace, 0);
-        bar_init(sb + Sh::Q_FULL, 1);
-        bar_init(sb + Sh::Q_EMPTY, 18);                  // a commit of each MMA thread and one arrival of each softmax warp
-#pragma unroll 1
-        for (int s = 0; s < Sh::NK + Sh::NV; ++s) {
-            bar_init(sb + Sh::FULL_K + 8 * s, 1);
-            bar_init(sb + Sh::EMPTY_K + 8 * s, 2);
+        for (int k = 0; k < 2; ++k) {
+            bar_init(sb + Sh::Q_FULL + 8 * k, 1);
+            bar_init(sb + Sh::Q_EMPTY + 8 * k, 18);      // a commit of each MMA thread and one arrival of each softmax warp
         }
+#pragma unroll 1
+        for (int s = 0; s < 2 * Sh::NF; ++s) bar_init(sb + Sh::FULL_K + 8 * s, 1);
+#pragma unroll 1
+        for (int s = 0; s < Sh::NK + Sh::NV; ++s) bar_init(sb + Sh::EMPTY_K + 8 * s, 2);
         for (int t = 0; t < 2; ++t) {
             bar_init(sb + Sh::DRAIN + 8 * t, 1);
             bar_init(sb + Sh::TURN + 8 * t, 1);
