@@ -533,8 +533,36 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
         const bool mine = row < min(p.plan.row_tile, lds(cur + offsetof(Segment, n_rows)) - first_row());       // the row exists
         float m_run = -CUDART_INF_F, l_run = 0.f;        // l_run: of this thread's keys
         const int step = two ? 1 : 2, first = two ? 0 : t;
+        auto zero_missing = [&](int j, uint32_t ti) {    // V rows that do not exist must not poison P V: 0 x whatever the page holds there
+            const uint32_t x = tile0 + j, v = sb + Sh::RING_V + x % Sh::NV * Sh::STAGE + row * 128;
+            const bool landed = bar_wait(sb + Sh::FULL_V + 8 * (x % Sh::NF), x / Sh::NF & 1, sb + Sh::ABORT);
+            if (!(lds64(ti + 8 * (row >> 6)) >> (row & 63) & 1)) {
+#pragma unroll
+                for (int i = 0; i < Sh::HALVES; ++i)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) zero16(v + i * (KT * 128) + ((c ^ row) & 7) * 16);       // neighbouring rows in different banks
+            }
+            fence_proxy_async();
+            return landed;
+        };
+        // A warp without rows that exist has no P to work out (no row of O depends on another row's P, and these rows are not stored): it only comes by
+        // the barriers and sees to its V rows. Decoding has 4 rows of 128: with all warps at work 32 sequences behind 8192 positions took 44 us.
+        const bool work = __any_sync(0xffffffffu, mine);
 #pragma unroll 1
-        for (int j = first; j < n; j += step) {
+        for (int j = first; j < n && !work; j += step) {
+            ok = bar_wait(sb + Sh::S_FULL + 8 * t, s_phase, sb + Sh::ABORT);
+            s_phase ^= 1;
+            const uint32_t ti = sb + Sh::INFO + ((tile0 + j) % NI) * (uint32_t)sizeof(TileInfo);
+            const bool all = lds(ti + offsetof(TileInfo, full));
+            if (!(all && j > first) || tile_any(t, !ok)) {
+                if (!all && h == 0) ok = zero_missing(j, ti) && ok;
+                if (tile_any(t, !ok)) { ok = false; break; }
+            }
+            __syncwarp();
+            if (lane == 0) bar_arrive(sb + Sh::P_FULL + 8 * t);
+        }
+#pragma unroll 1
+        for (int j = first; j < n && work; j += step) {
             ok = bar_wait(sb + Sh::S_FULL + 8 * t, s_phase, sb + Sh::ABORT);
             s_phase ^= 1;
             tc_fence_after();
@@ -571,19 +599,7 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
             }
             tmem_ld32_nowait(tS + h * 64, s);
             tmem_ld32_nowait(tS + h * 64 + 32, s + 32);
-            if (!all && h == 0) {
-                // V rows that do not exist must not poison P V: 0 x whatever the page holds there
-                const uint32_t st = (tile0 + j) % Sh::NV;
-                ok = bar_wait(sb + Sh::FULL_V + 8 * ((tile0 + j) % Sh::NF), (tile0 + j) / Sh::NF & 1, sb + Sh::ABORT) && ok;
-                if (!(lds64(ti + 8 * (row >> 6)) >> (row & 63) & 1)) {
-                    const uint32_t v = sb + Sh::RING_V + st * Sh::STAGE + row * 128;
-#pragma unroll
-                    for (int x = 0; x < Sh::HALVES; ++x)
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) zero16(v + x * (KT * 128) + ((c ^ row) & 7) * 16);       // neighbouring rows in different banks
-                }
-                fence_proxy_async();
-            }
+            if (!all && h == 0) ok = zero_missing(j, ti) && ok;
             tmem_ld_wait();
             if (!all) {
                 unsigned long long m = lds64(ti + 8 * h);
