@@ -474,3 +474,22 @@ def test_calls_on_two_streams_and_graphs_of_two_streams_overlap():
     for b, o, w in zip(batches, outs, want):
         assert torch.equal(o[0], w[0]) and torch.equal(o[1], w[1])
         b.check(*o, True)
+
+
+@pytest.mark.parametrize("S,groups,dtype", [(600, 300, "bf16"), (400, 200, "bf16"), (530, 0, "bf16"), (700, 650, "bf16"), (1100, 3, "fp32")])
+def test_more_sequences_and_groups_than_the_plan_keeps_in_shared_memory(S, groups, dtype):
+    cfg = config(hq=4, hkv=2, hd=64, page=16, dtype=dtype, layers=1)
+    lib = binding.DFlash(cfg)
+    r = random.Random(S)
+    starts = sorted(r.randint(0, S) for _ in range(groups + 1))
+    prefix = [r.choice([0, 5, 16, 40, 70]) for _ in range(groups)]
+    lens = []
+    for b in range(S):
+        g = next((g for g in range(groups) if starts[g] <= b < starts[g + 1]), -1)
+        lens.append((prefix[g] if g >= 0 and r.random() < 0.9 else 0) + r.choice([0, 1, 15, 60, 90]))
+    lens[S // 2] += 3000
+    x = Batch(cfg, 3, starts, prefix, lens, seed=S, layer=0)
+    out, lse = x.run(lib, MODES["causal"])
+    torch.cuda.synchronize()
+    assert int(lib.status.item()) == 0
+    x.check(out, lse, True, seqs=[0, 1, S // 2 - 1, S // 2, S - 1] + [r.randrange(S) for _ in range(25)])
