@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) prefix_attn_simt_kernel(const __
 // for bytes. W = 4 where there are few rows (decoding: 8.3 -> 5.4 us), W = 1 where there are enough for all SMs (17408 rows: 18 us against 38 with four).
 template <typename T, int HD, int W>
 __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant__ Params p) {
-    constexpr int PB = W == 1 ? 2 : 4;
+    constexpr int PB = 4;
     __shared__ float4 s_acc[W == 1 ? 1 : 4][4][HD / 4];
     __shared__ float2 s_ml[4][4];
     unsigned long long* trace = p.trace ? p.trace + 4 : nullptr;
@@ -245,19 +245,16 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
             if (lane >= d) end += y;
         }
         const int total = __shfl_sync(0xffffffffu, end, 28 + (lane & 3));
-        const int rounds = __reduce_max_sync(0xffffffffu, total), ends = min(7, most - e0 - 1);
+        const int rounds = __reduce_max_sync(0xffffffffu, total);
         for (int k0 = 0; k0 < rounds; k0 += W * PB) {      // the same for all lanes, which exchange values in it; rows differ in `skip` and `total`
             float2 ml[PB];
             float4 o[PB][HD / 32];
 #pragma unroll
             for (int k = 0; k < PB; ++k) {
                 const int part = skip + k0 + W * k;
-                int x = 0, first = 0;                // the item that holds it, and that item's first part
-#pragma unroll 1
-                for (int i = 0; i < ends; ++i) {
-                    const int y = __shfl_sync(0xffffffffu, end, 4 * i + (lane & 3));
-                    if (part >= y) { x = i + 1; first = y; }
-                }
+                // the item that holds it: as many of the row's items end before it; and that item's first part
+                const int x = min(__popc(__ballot_sync(0xffffffffu, part >= end) & 0x11111111u << (lane & 3)), 7);
+                const int before = __shfl_sync(0xffffffffu, end, 4 * max(x - 1, 0) + (lane & 3)), first = x > 0 ? before : 0;
                 const int sl = __shfl_sync(0xffffffffu, slot, 4 * x + (lane & 3));
                 const bool own = e0 + x >= si.group_blocks, two_subs = tpi == 2 && (own ? o_one : g_one);
                 ml[k] = make_float2(-CUDART_INF_F, 0.f);
