@@ -388,7 +388,7 @@ PlanParams plan_params(const dflash_config& c, const Sizes& z, int S, int R, int
     q.row_tile = z.row_tile; q.tiles_per_item = z.tiles_per_item; q.chunks_per_tile = z.chunks_per_tile;
     // Tensor-core kernel, in units of 500 clocks: a key tile takes 2650 with one query tile (its bytes at the HBM rate) and 3560 with two (its products),
     // the change to another item about 4500. (One query tile for as much as two, 8 : 5 : 9, left CTAs waiting: 32 sequences x 17 rows behind
-    // 32768 positions 311 us, now 282; an item for 15 is better for many whole contexts, 114 us against 125, and worse for decoding.)
+    // 32768 positions 311 us, then 282; an item for 12 is better for many whole contexts, 112 us against 116, and no better or worse elsewhere.)
     // CUDA cores: a chunk takes about as long as it takes to begin an item.
     const bool tc = use_tc(c);
     q.cost_item = tc ? 10 : 3; q.cost_one = tc ? 5 : 4; q.cost_two = tc ? 7 : 4;
