@@ -455,7 +455,7 @@ int64_t dflash_prefix_attention_workspace_bytes(const dflash_handle* h, int32_t 
  * (DFLASH_DEV_BAD_PAGE); more positions than a row has entries for (DFLASH_DEV_CTX_OVERFLOW).
  * kv_pool is the pool of the handle's shape (all layers are copied). Where a second pool is kept under the same
  * table (a drafter's beside its target's), hand the page copies that a call reports to dflash_pages_copy with the
- * other handle. Lists hold at most 65535 entries (DFLASH_ERR_UNSUPPORTED). Two launches each (copy: one).
+ * other handle. Lists hold at most 65535 entries, pools and table rows 2^30 pages (DFLASH_ERR_UNSUPPORTED). Two launches each (copy: one).
  * Workspace: dflash_pages_workspace_bytes(n, max_pages, n_pool_pages), 256-byte aligned; calls must not overlap in time. */
 typedef struct {
     int32_t        n;            /* list entries                                              */
@@ -535,7 +535,7 @@ typedef struct {
 } dflash_pages_compact_args;
 /* Moves the pages in use to the front of the pool: with n of them, the i-th free page below n takes the contents, the
  * count and the table entries of the i-th used page at or behind n. Afterwards pages 0..n-1 are in use, the others free. A table
- * entry at or behind n whose page is not in use is left as it is and sets DFLASH_DEV_BAD_PAGE. */
+ * entry whose page is not in use is left as it is and sets DFLASH_DEV_BAD_PAGE. */
 int32_t dflash_pages_compact(dflash_handle* h, const dflash_pages_compact_args* a /*[host]*/, void* stream);
 int64_t dflash_pages_workspace_bytes(int32_t max_n, int32_t max_pages, int32_t n_pool_pages);
 

@@ -720,9 +720,10 @@ int32_t dflash_prefix_plan_check(const dflash_handle* h, int32_t batch, int32_t 
 }
 
 // ---- pages ----
+constexpr int32_t MAX_POOL_PAGES = 1 << 30;          // the kernels count pages and table entries of a row in 32 bits
 int64_t dflash_pages_workspace_bytes(int32_t max_n, int32_t max_pages, int32_t n_pool_pages) {
     if (max_n < 0 || max_pages < 1 || n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
-    if (max_n > 65535) return DFLASH_ERR_UNSUPPORTED;
+    if (max_n > 65535 || max_pages > MAX_POOL_PAGES || n_pool_pages > MAX_POOL_PAGES) return DFLASH_ERR_UNSUPPORTED;
     return pages_workspace_bytes(max_n, max_pages, n_pool_pages);
 }
 static int check_pages_ws(void* ws, int64_t bytes, int n, int max_pages, int n_pages) {
@@ -731,7 +732,7 @@ static int check_pages_ws(void* ws, int64_t bytes, int n, int max_pages, int n_p
 
 int32_t dflash_pages_copy(dflash_handle* h, const dflash_pages_copy_args* a, void* stream) {
     if (!h || !a || a->n < 0 || a->n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
-    if (a->n > 65535) return DFLASH_ERR_UNSUPPORTED;
+    if (a->n > 65535 || a->n_pool_pages > MAX_POOL_PAGES) return DFLASH_ERR_UNSUPPORTED;
     if (a->n == 0) return DFLASH_OK;
     if (!a->src || !a->dst || !a->kv_pool || !aligned16(a->kv_pool)) return DFLASH_ERR_INVALID_ARG;
     Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
@@ -741,7 +742,7 @@ int32_t dflash_pages_copy(dflash_handle* h, const dflash_pages_copy_args* a, voi
 
 int32_t dflash_pages_fork(dflash_handle* h, const dflash_pages_fork_args* a, void* stream) {
     if (!h || !a || a->n < 0 || a->n_rows < 1 || a->max_pages < 1 || a->n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
-    if (a->n > 65535) return DFLASH_ERR_UNSUPPORTED;
+    if (a->n > 65535 || a->max_pages > MAX_POOL_PAGES || a->n_pool_pages > MAX_POOL_PAGES) return DFLASH_ERR_UNSUPPORTED;
     if (a->n == 0) return DFLASH_OK;
     if (!a->parent || !a->child || !a->fork_len || !a->page_table || !a->ref_count || !a->kv_pool || !aligned16(a->kv_pool)) return DFLASH_ERR_INVALID_ARG;
     if ((a->copy_src != nullptr) != (a->copy_dst != nullptr) || (a->copy_src != nullptr) != (a->copy_slots != nullptr)) return DFLASH_ERR_INVALID_ARG;
@@ -753,7 +754,7 @@ int32_t dflash_pages_fork(dflash_handle* h, const dflash_pages_fork_args* a, voi
 
 int32_t dflash_pages_resize(dflash_handle* h, const dflash_pages_resize_args* a, void* stream) {
     if (!h || !a || a->n < 0 || a->n_rows < 1 || a->max_pages < 1 || a->n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
-    if (a->n > 65535) return DFLASH_ERR_UNSUPPORTED;
+    if (a->n > 65535 || a->max_pages > MAX_POOL_PAGES || a->n_pool_pages > MAX_POOL_PAGES) return DFLASH_ERR_UNSUPPORTED;
     if (a->n == 0) return DFLASH_OK;
     if (!a->rows || !a->keep_len || !a->capacity || !a->page_table || !a->ref_count || !a->kv_pool || !aligned16(a->kv_pool)) return DFLASH_ERR_INVALID_ARG;
     if ((a->copy_src != nullptr) != (a->copy_dst != nullptr) || (a->copy_src != nullptr) != (a->copy_slots != nullptr)) return DFLASH_ERR_INVALID_ARG;
@@ -765,6 +766,7 @@ int32_t dflash_pages_resize(dflash_handle* h, const dflash_pages_resize_args* a,
 
 int32_t dflash_pages_compact(dflash_handle* h, const dflash_pages_compact_args* a, void* stream) {
     if (!h || !a || a->n_rows < 1 || a->max_pages < 1 || a->n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
+    if (a->max_pages > MAX_POOL_PAGES || a->n_pool_pages > MAX_POOL_PAGES) return DFLASH_ERR_UNSUPPORTED;
     if (!a->page_table || !a->ref_count || !a->kv_pool || !aligned16(a->kv_pool)) return DFLASH_ERR_INVALID_ARG;
     if ((a->copy_src != nullptr) != (a->copy_dst != nullptr) || (a->copy_src != nullptr) != (a->n_copies != nullptr)) return DFLASH_ERR_INVALID_ARG;
     DFLASH_TRY(check_pages_ws(a->workspace, a->workspace_bytes, 0, a->max_pages, a->n_pool_pages));

@@ -382,14 +382,14 @@ struct CompactArgs {
     int32_t *table, *ref;
     int32_t *n_live, *copy_src, *copy_dst, *n_copies;
     int32_t *hole, *mover;               // [n_pages / 2] pairs: page mover[k] goes to page hole[k]
-    int32_t* rank;                       // [n_pages] of a page behind the border: its k, or -1
+    int32_t* rank;                       // [n_pages] of a page behind the border: its k; of one that is not in use: NOT_LIVE
     int32_t* pairs;                      // [1]
     int32_t move_ctas;
     int32_t* status;
 };
 
 // Every CTA counts the whole pool itself (the counts come out of L2) and lists the holes and movers of its own stretch.
-constexpr int NT_COMPACT = 1024;
+constexpr int NT_COMPACT = 1024, NOT_LIVE = (int)0x80000000;
 __global__ void __launch_bounds__(NT_COMPACT) pages_compact_plan_kernel(const CompactArgs a) {
     __shared__ int32_t sh[33];
     ptx::pdl_trigger();
@@ -418,12 +418,9 @@ __global__ void __launch_bounds__(NT_COMPACT) pages_compact_plan_kernel(const Co
         const int p = p0 + k;
         if (p < n) {
             const bool live = mask >> k & 1;
-            if (p < border) {
-                if (!live) a.hole[p - live_before] = p;
-            } else {
-                a.rank[p] = live ? live_before - front : -1;
-                if (live) a.mover[live_before - front] = p;
-            }
+            a.rank[p] = live ? live_before - front : NOT_LIVE;
+            if (p < border && !live) a.hole[p - live_before] = p;
+            if (p >= border && live) a.mover[live_before - front] = p;
             live_before += live;
         }
     }
@@ -460,10 +457,10 @@ __global__ void __launch_bounds__(NT) pages_compact_apply_kernel(const CompactAr
     }
     for (int64_t j = at; j < (int64_t)a.n_rows * a.max_pages; j += step) {
         const int e = a.table[j];
-        if (e < border) continue;
-        const int k = e < a.g.n_pages ? a.rank[e] : -1;
-        if (k >= 0) a.table[j] = a.hole[k];
-        else flag(a.status, DFLASH_DEV_BAD_PAGE);
+        if (e < 0) continue;
+        const int k = e < a.g.n_pages ? a.rank[e] : NOT_LIVE;
+        if (k == NOT_LIVE) flag(a.status, DFLASH_DEV_BAD_PAGE);          // it would name another sequence's page, once a mover has come there
+        else if (e >= border) a.table[j] = a.hole[k];
     }
 }
 

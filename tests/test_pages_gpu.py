@@ -215,6 +215,24 @@ def test_compact(pages):
             assert list(zip(copies[0].tolist(), copies[1].tolist())) == moves + [(-1, -1)] * (pages // 2 - len(moves))
 
 
+def test_compact_flags_entries_whose_page_is_not_in_use():
+    # pages 0 2 5 in use, border 3: page 1 is the hole that 5 moves to, and an entry that names it would come by 5's contents
+    cfg = config(hq=2, hkv=2, hd=64, page=1, layers=1, dtype="fp32")
+    lib = binding.DFlash(cfg)
+    s = State(cfg, 6, 3, 4, [0, 0, 0])
+    s.table[0, :3] = [0, 2, 5]
+    s.table[1, :4] = [1, 4, -5, 2]
+    s.table[2, :2] = [6, 2 ** 31 - 1]
+    s.ref[:] = [1, 0, 2, 0, -3, 1]
+    s.d_table.copy_(torch.from_numpy(s.table))
+    s.d_ref.copy_(torch.from_numpy(s.ref))
+    lib.dflash_pages_compact(s.d_table, s.d_ref, s.d_pool)
+    s.table[0, 2] = 1
+    s.ref[:] = [1, 1, 2, 0, -3, 0]
+    s.pool[:, 1] = s.pool[:, 5]
+    s.same(lib, binding.DEV_BAD_PAGE)
+
+
 def test_a_second_pool_follows_the_reported_copies():
     cfg, other = config(hq=8, hkv=2, layers=2), config(hq=4, hkv=4, hd=64, layers=3)
     lib, lib2 = binding.DFlash(cfg), binding.DFlash(other)

@@ -106,3 +106,22 @@ def test_pages(lib, h):
             a = make()
             a.n = 0
             assert fn(h, C.byref(a), None) == 0
+
+
+def test_pools_too_large_to_count_are_refused(lib, h):
+    most = 1 << 30
+    assert lib.dflash_pages_workspace_bytes(1, 1, most) > 0
+    for n, width, pages in ((1, 1, most + 1), (1, most + 1, 8), (1, 1, 2 ** 31 - 1), (0, 2 ** 31 - 1, 2 ** 31 - 1)):
+        assert lib.dflash_pages_workspace_bytes(n, width, pages) == -2
+    P = 1 << 20                                          # never followed
+    for pages, width in ((most + 1, 4), (2 ** 31 - 1, 4), (8, most + 1)):
+        if pages > most:
+            a = binding.PagesCopyArgs(n=1, src=P, dst=P, kv_pool=P, n_pool_pages=pages)
+            assert lib.dflash_pages_copy(h, C.byref(a), None) == -2
+        table = dict(page_table=P, n_rows=2, max_pages=width, ref_count=P, kv_pool=P, n_pool_pages=pages, workspace=P, workspace_bytes=1 << 62)
+        a = binding.PagesForkArgs(n=1, parent=P, child=P, fork_len=P, **table)
+        assert lib.dflash_pages_fork(h, C.byref(a), None) == -2
+        a = binding.PagesResizeArgs(n=1, rows=P, keep_len=P, capacity=P, **table)
+        assert lib.dflash_pages_resize(h, C.byref(a), None) == -2
+        a = binding.PagesCompactArgs(**table)
+        assert lib.dflash_pages_compact(h, C.byref(a), None) == -2
