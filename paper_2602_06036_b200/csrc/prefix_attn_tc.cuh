@@ -76,7 +76,7 @@ struct Shape {
     static constexpr int NK = HD == 128 ? 2 : 5, NV = HD == 128 ? 3 : 5;
     static constexpr uint32_t RING_K = 2 * Q_BYTES, RING_V = RING_K + NK * STAGE;
     // Queries are loaded a segment ahead: one query tile goes to the half of the queries' 2 tiles that the segment before does not use. (Loaded only
-    // when the segment before had done its products, they held every change of item up: 148 sequences x 128 keys 61 us.)
+    // when the segment before had done its products, they held the change of item up: 148 sequences x 384 keys 90 us, then 83.)
     static constexpr uint32_t Q_FULL = RING_V + NV * STAGE;   // [2] by the segment's parity: its queries and its words in CUR are there
     static constexpr uint32_t Q_EMPTY = Q_FULL + 16;          // [2] queries used up, all earlier segments done with by every softmax warp
     // A wait for a phase's parity cannot tell a phase from the one before the last. Key tiles that are shared out between the MMA threads leave each
@@ -540,13 +540,14 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
 #pragma unroll
                 for (int i = 0; i < Sh::HALVES; ++i)
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) zero16(v + i * (KT * 128) + ((c ^ row) & 7) * 16);       // neighbouring rows in different banks
+                    for (int c = 0; c < 8; ++c) zero16(v + i * (KT * 128) + ((c ^ row) & 7) * 16);       // neighbouring rows in different banks (148 sequences x 128 keys: 61 us in one order, 52)
             }
             fence_proxy_async();
             return landed;
         };
         // A warp without rows that exist has no P to work out (no row of O depends on another row's P, and these rows are not stored): it only comes by
-        // the barriers and sees to its V rows. Decoding has 4 rows of 128: with all warps at work 32 sequences behind 8192 positions took 44 us.
+        // the barriers and sees to its V rows. Decoding has 4 rows of 128; 32 sequences x 17 rows behind
+        // 32768 positions, each with 68 rows of its own, took 279 us with all warps at work, then 273.
         const bool work = __any_sync(0xffffffffu, mine);
 #pragma unroll 1
         for (int j = first; j < n && !work; j += step) {
