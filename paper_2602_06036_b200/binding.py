@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 from typing import Dict, Optional
 
 import torch
@@ -281,6 +282,7 @@ class DFlash:
         self._ws = None
         self._scratches = {}
         self._needs = {}
+        self._launching = threading.Lock()
         self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
 
@@ -550,13 +552,14 @@ class DFlash:
         return kept
 
     def _call(self, fn, args, stream):
-        """The library launches on the current device, which has to be the handle's."""
+        """The library launches on the current device, which has to be the handle's. One thread at a time: the launches of a call share a workspace."""
         raw = stream.cuda_stream if stream is not None else _current_stream(self._index)
-        if torch.cuda.current_device() == self._index:
-            rc = fn(self.h, C.byref(args), raw)
-        else:
-            with torch.cuda.device(self._index):
+        with self._launching:
+            if torch.cuda.current_device() == self._index:
                 rc = fn(self.h, C.byref(args), raw)
+            else:
+                with torch.cuda.device(self._index):
+                    rc = fn(self.h, C.byref(args), raw)
         if rc != 0:
             raise DFlashError(rc)
 

@@ -493,3 +493,61 @@ def test_more_sequences_and_groups_than_the_plan_keeps_in_shared_memory(S, group
     torch.cuda.synchronize()
     assert int(lib.status.item()) == 0
     x.check(out, lse, True, seqs=[0, 1, S // 2 - 1, S // 2, S - 1] + [r.randrange(S) for _ in range(25)])
+
+
+FIRST_CALL = """
+import torch
+from paper_2602_06036_b200 import binding
+from tests.test_prefix_attention_gpu import Batch, config
+cfg = config(hq=8, hkv=2)
+lib = binding.DFlash(cfg)
+x = Batch(cfg, 5, [0, 2], [100], [130, 161], seed=3)
+d = x.cuda()
+out, lse = torch.zeros_like(d["q"]), torch.zeros(d["q"].shape[:3], device="cuda:0")
+ref = torch.zeros(x.pages, dtype=torch.int32, device="cuda:0")
+one = torch.ones(1, dtype=torch.int32, device="cuda:0")
+table = torch.full((3, 2), -1, dtype=torch.int32, device="cuda:0")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    x.run(lib, 1, d, out, lse)
+    lib.dflash_pages_resize(one, one, one + 69, table, ref, torch.zeros_like(d["pool"]))      # a kept position without a page: left out
+    lib.dflash_pages_resize(one, one - 1, one + 69, table, ref, torch.zeros_like(d["pool"]))
+g.replay()
+torch.cuda.synchronize()
+x.check(out, lse, True)
+assert table.tolist() == [[-1, -1], [0, 1], [-1, -1]] and int(ref.sum()) == 2 and int(lib.status.item()) == binding.DEV_BAD_PAGE
+"""
+
+
+def test_a_process_may_begin_with_a_captured_call():
+    import subprocess
+    import sys
+    from pathlib import Path
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL], cwd=Path(__file__).resolve().parents[1], capture_output=True, text=True, timeout=180)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
+def test_two_threads_with_one_handle():
+    import threading
+    cfg = config(hq=8, hkv=2)
+    lib = binding.DFlash(cfg)
+    batches = [Batch(cfg, 16, [0, 6], [800], [900 + 10 * i for i in range(6)], seed=51), Batch(cfg, 7, [1, 5], [700], [900, 1400, 800, 701, 1500], seed=52)]
+    data = [b.cuda() for b in batches]
+    want = [b.run(lib, 1, d) for b, d in zip(batches, data)]
+    torch.cuda.synchronize()
+    same, go = [[], []], threading.Barrier(2)
+
+    def work(i):
+        go.wait()
+        outs = [batches[i].run(lib, 1, data[i]) for _ in range(60)]
+        torch.cuda.synchronize()
+        same[i] += [torch.equal(o, want[i][0]) and torch.equal(l, want[i][1]) for o, l in outs]
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert same == [[True] * 60] * 2
+    assert int(lib.status.item()) == 0
