@@ -12,7 +12,8 @@ namespace {
 using namespace ptx;
 
 // log2 units by which a tile has to top the running maximum to raise it: P and the sums may grow to 2^16 times what they would be otherwise, which
-// costs no precision, and leaves fp32 2^96 for the values
+// costs no precision, and leaves fp32 2^96 for the values. The maximum is an fp32 number: rounded to bf16 it is off by 128 from scores of 2^15
+// on, and the largest exponential is infinite or 0.
 constexpr float GAP = 16.f;
 
 struct Params {
@@ -94,7 +95,7 @@ struct Shape {
     static constexpr uint32_t O_FULL = P_FULL + 16;           // [2] the segment's last product into O_t done
     static constexpr uint32_t INFO = O_FULL + 16;             // [NI] TileInfo
     static constexpr uint32_t CUR = INFO + NI * sizeof(TileInfo);       // [4] the segments whose queries are in shared memory, and the one before
-    static constexpr uint32_t XCH = CUR + 4 * sizeof(Segment);          // [2][128] words that the two threads of a row exchange
+    static constexpr uint32_t XCH = CUR + 4 * sizeof(Segment);          // [2][128] sums that one thread of a row hands to the other
     static constexpr uint32_t TMEM_SLOT = XCH + 1024;
     static constexpr uint32_t ABORT = TMEM_SLOT + 4;
     static constexpr int SMEM = 1024 + ABORT + 4;
@@ -190,6 +191,14 @@ __device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, float* v) {
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr)
         : "memory");
+}
+__device__ __forceinline__ float tmem_ld1(uint32_t taddr) {
+    uint32_t v;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(v) : "r"(taddr) : "memory");
+    return __uint_as_float(v);
+}
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, float v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(taddr), "r"(__float_as_uint(v)) : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
@@ -614,14 +623,15 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
             float mx4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
             for (int c = 0; c < 64; c += 2) mx4[(c >> 1) & 3] = max3(mx4[(c >> 1) & 3], s[c], s[c + 1]);
-            // the row's maximum, in bf16: it serves as a reference only. The barrier also says that all of S_t is in registers:
-            // P_t takes the place of its first half.
-            const uint32_t mine = pack_bf16(max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * p.scale_log2, 0.f) & 0xffffu;      // scale > 0
-            asm volatile("st.shared.b16 [%0], %1;" ::"r"(xch + h * 256 + row * 2), "h"((unsigned short)mine) : "memory");
+            // The row's maximum. Its two threads tell each other by way of S_t itself, which both have in registers when they have come by the barrier
+            // (shared memory has no room for 512 words more): columns 63 and 64, each thread's own until then. P_t takes the place of columns
+            // 0 to 63; the one that holds column 63 is written by the thread that has read it.
+            const float top_here = max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * p.scale_log2;      // scale > 0
+            tmem_st1(tS + 63 + h, top_here);
+            tc_fence_before();
             if (tile_any(t, !ok)) { ok = false; break; }
-            unsigned short other;
-            asm volatile("ld.shared.b16 %0, [%1];" : "=h"(other) : "r"(xch + (h ^ 1) * 256 + row * 2) : "memory");
-            const float mx = fmaxf(__uint_as_float(mine << 16), __uint_as_float((uint32_t)other << 16));
+            tc_fence_after();
+            const float mx = fmaxf(top_here, tmem_ld1(tS + 64 - h));
             const bool raise = mx > m_run + GAP || (m_run == -CUDART_INF_F && mx > -CUDART_INF_F);
             const float m_new = raise ? mx : m_run;
             const float alpha = (raise && m_run > -CUDART_INF_F) ? fast_exp2(m_run - m_new) : 1.f;
