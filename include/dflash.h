@@ -401,7 +401,8 @@ int32_t dflash_block_attention_bwd(dflash_handle* h, const dflash_attn_bwd_args*
  * block rows (all of them, or those <= r in mode CAUSAL). Sequences group_start[g] .. group_start[g+1]-1 form group g and
  * share their first prefix_len[g] positions: these are read from the page-table row of the group's FIRST sequence, the
  * rest of a sequence from its own row (the own row's entries below the prefix are not looked at, nor does the prefix have to
- * end on a page border). A sequence with ctx_len[b] < prefix_len[g], and one outside every group, reads its own row only.
+ * end on a page border). A sequence with ctx_len[b] < prefix_len[g], and one outside every group, reads its own row only. Where any sequence of
+ * a group reads its prefix, the first one's row has to hold that prefix's pages, even if the first is shorter itself; a prefix that none reads is not looked at.
  * All K/V of a prefix are read once per group (and kv head); the rows of all its sequences are the rows of ONE
  * product with them.
  * Any rows 1..32, any Hq/Hkv up to 128. bf16 with 8- to 256-token pages runs on the tensor cores (head_dim 64 and

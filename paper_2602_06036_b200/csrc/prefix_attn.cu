@@ -11,6 +11,8 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <memory>
+#include <new>
 
 namespace dflash {
 namespace {
@@ -472,8 +474,11 @@ int prefix_plan_check(const dflash_config& c, int sm_count, int S, int R, int n_
     p.group_start = group_start; p.prefix_len = prefix_len; p.ctx_len = ctx_len;
     const int n = n_groups + S;
     int total = 0, all_tiles = 0;
+    const std::unique_ptr<char[]> read(new (std::nothrow) char[n]());       // of a group: any of its sequences reads the prefix
+    if (!read) return DFLASH_ERR_CUDA;
     for (int e = 0; e < n; ++e) {
         Entry x = plan_entry(p, e, n_groups > 0, false);
+        if (x.lo > 0) read[x.group] = 1;
         entry_cost(p, x);
         total += x.cost;
         all_tiles += p.Hkv * x.items * x.n_tiles;
@@ -485,14 +490,16 @@ int prefix_plan_check(const dflash_config& c, int sm_count, int S, int R, int n_
     const int share = (total + z.n_cta - 1) / z.n_cta;
     auto entry = [&](int e) {
         Entry x = plan_entry(p, e, n_groups > 0, false);
+        if (e < n_groups && !read[e]) entry_unread(x);
         entry_blocks(p, x, share);
         entry_cost(p, x);
         return x;
     };
     int64_t items = 0, group_items = 0, tiles = 0, segments = 0;
-    total = 0;
+    total = all_tiles = 0;
     for (int e = 0; e < n; ++e) {
         const Entry x = entry(e);
+        all_tiles += p.Hkv * x.items * x.n_tiles;
         if (e == n_groups) group_items = items;
         total += x.cost;
         items += entry_items(p, x);

@@ -28,6 +28,7 @@ struct PlanParams {
 
 struct Entry {
     int32_t seq, n_rows;                 // first sequence; packed rows per kv head
+    int32_t group;                       // of a sequence, or -1
     int32_t lo, hi, block;               // cached keys [lo, hi); block rows are keys too
     int32_t chunk0, n_chunks, n_tiles;   // chunks of 64 keys from chunk0 * 64 on, the block's chunk last
     int32_t items, blocks;               // items of row tiles per kv head and key block; key blocks
@@ -88,7 +89,8 @@ __host__ __device__ __forceinline__ Entry plan_entry(const PlanParams& p, int e,
         x.seq = e - p.n_groups;
         x.n_rows = p.R * p.G;
         x.hi = plan_len(p, p.ctx_len[x.seq], tell);
-        x.lo = groups_ok ? plan_shared(p, plan_group(p, x.seq), x.hi) : 0;
+        x.group = groups_ok ? plan_group(p, x.seq) : -1;
+        x.lo = plan_shared(p, x.group, x.hi);
         x.block = 1;
     }
     x.chunk0 = x.lo / CHUNK_KEYS;
@@ -101,6 +103,9 @@ __host__ __device__ __forceinline__ Entry plan_entry(const PlanParams& p, int e,
     x.single = row_tiles % p.tiles_per_item != 0 || p.tiles_per_item == 1;
     return x;
 }
+// A prefix that none of its group's sequences reads is no work, and its pages need not exist. Which these are is known when all entries are: they
+// count in the shares that key blocks are measured by, and not in what is handed out.
+__host__ __device__ __forceinline__ void entry_unread(Entry& x) { x.n_rows = x.n_chunks = x.n_tiles = x.items = x.cost = 0; }
 // `share`: cost that a CTA takes. Long prefixes are cut into key blocks of about that much, ordered before the row tiles: CTAs that run side by
 // side then read the same keys, which come out of L2.
 __host__ __device__ __forceinline__ void entry_blocks(const PlanParams& p, Entry& x, int32_t share) {
@@ -199,8 +204,8 @@ struct PlanOut {
 
 constexpr int PLAN_THREADS = 512, MAX_CTAS = 512, PLAN_CACHE = 512;
 
-// One CTA. Passes of all threads over groups and sequences (entries and their total cost; then key blocks, running costs and items), then one thread per
-// item. What takes its time is latency: lengths and groups are fetched once, and everything in between stays in shared memory where it fits.
+// One CTA. Passes of all threads over groups and sequences (entries and their total cost, and which prefixes are read at all; then key blocks,
+// running costs and items), then one thread per item. What takes its time is latency: lengths and groups are fetched once, and everything in between stays in shared memory where it fits.
 __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p, const PlanOut o, int grid) {
     constexpr int NW = PLAN_THREADS / 32;
     __shared__ int32_t s_cost[NW], s_tiles[NW], s_items[NW];
@@ -226,6 +231,11 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
         p.group_start = s_start;
         p.prefix_len = s_prefix;
     }
+    const int n = p.n_groups + p.S, per = (n + PLAN_THREADS - 1) / PLAN_THREADS;
+    const bool small = n <= PLAN_CACHE;
+    Entry* ent = small ? s_entry : o.entries;
+    int32_t *at = small ? s_at : o.start, *item0 = small ? s_item0 : o.item0;
+    for (int g = tid; g < p.n_groups; g += PLAN_THREADS) at[g] = 0;          // until the running costs are known: whether a group's prefix is read
     __syncthreads();
     int bad = 0;
     for (int g = tid; g <= p.n_groups && p.n_groups > 0; g += PLAN_THREADS) {
@@ -235,15 +245,12 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
     bad = __syncthreads_or(bad);
     const bool ok = !bad && p.n_groups > 0;
     if (bad && tid == 0 && p.status) atomicOr(p.status, DFLASH_DEV_BAD_GROUP);
-    const int n = p.n_groups + p.S, per = (n + PLAN_THREADS - 1) / PLAN_THREADS;
     const int e0 = min(n, tid * per), e1 = min(n, e0 + per);         // this thread's entries
-    const bool small = n <= PLAN_CACHE;
-    Entry* ent = small ? s_entry : o.entries;
-    int32_t *at = small ? s_at : o.start, *item0 = small ? s_item0 : o.item0;
     int cost = 0, tiles = 0, items = 0;
 #pragma unroll 1
     for (int e = e0; e < e1; ++e) {
         Entry x = plan_entry(p, e, ok, true);
+        if (x.lo > 0) at[x.group] = 1;
         entry_cost(p, x);
         cost += x.cost;
         tiles += p.Hkv * x.items * x.n_tiles;
@@ -264,6 +271,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
 #pragma unroll 1
     for (int e = e0; e < e1; ++e) {
         Entry x = ent[e];
+        if (e < p.n_groups && !at[e]) {
+            entry_unread(x);
+            ent[e] = x;
+        }
         entry_blocks(p, x, share);
         entry_cost(p, x);
         ent[e].blocks = x.blocks;
@@ -302,7 +313,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) prefix_plan_kernel(PlanParams p,
         const Entry& x = ent[p.n_groups + b];
         SeqInfo q{0, 0, 0, 0, 0, item0[p.n_groups + b], x.blocks, n_group_items};
         if (x.lo > 0) {                  // the keys below x.lo are the group's items
-            const int g = plan_group(p, b);
+            const int g = x.group;
             q = SeqInfo{item0[g], ent[g].items, ent[g].blocks, ent[g].single, (b - p.group_start[g]) * p.R * p.G, q.item0, q.blocks, n_group_items};
         }
         o.sinfo[b] = q;
