@@ -208,11 +208,24 @@ __global__ void __launch_bounds__(NT) pages_fork_plan_kernel(const ForkArgs a) {
     }
 }
 
-__device__ __forceinline__ int need_before(const Plan* plan, int i, int32_t* sh) {
-    int v = 0;
-    for (int k = threadIdx.x; k < i; k += (int)blockDim.x) v += plan[k].need;
-    return block_sum(v, sh);
+// Pages that the requests before i take, for every thread of a CTA of NT. In 64 bits: 65535 requests may ask for 2^30 pages each, and a sum that
+// wrapped to a negative number would pass for one that fits. The warps add up 24-bit words (below 2^29) and what lies above them.
+__device__ __forceinline__ int64_t need_before(const Plan* plan, int i, int32_t* sh) {
+    int64_t v = 0;
+    for (int k = threadIdx.x; k < i; k += NT) v += plan[k].need;
+    const int low = __reduce_add_sync(0xffffffffu, (int)(v & 0xffffff)), high = __reduce_add_sync(0xffffffffu, (int)(v >> 24));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) {
+        sh[threadIdx.x >> 5] = low;
+        sh[NT / 32 + (threadIdx.x >> 5)] = high;
+    }
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) v += ((int64_t)sh[NT / 32 + w] << 24) + sh[w];
+    return v;
 }
+static_assert(2 * NT / 32 <= 33, "words of need_before");
 // Page copies of the planned requests: chunk c of all, CTA `cta` of `n_cta`.
 __device__ void apply_copies(const Geometry& g, const Plan* plan, int n, const Free& f, int avail, int cta, int n_cta, int32_t* sh) {
     int at = -1, dst = -1;
@@ -223,8 +236,8 @@ __device__ void apply_copies(const Geometry& g, const Plan* plan, int n, const F
             at = i;
             p = plan[i];
             if (p.src >= 0) {
-                const int base = need_before(plan, i, sh);
-                dst = base + p.need <= avail ? free_page(f, base) : -1;
+                const int64_t base = need_before(plan, i, sh);
+                dst = base + p.need <= avail ? free_page(f, (int)base) : -1;
             }
         }
         if (p.src >= 0 && dst >= 0) copy_chunk(g, p.src, dst, p.slots, (int)(c % g.chunks));
@@ -250,9 +263,9 @@ __global__ void __launch_bounds__(NT) pages_fork_apply_kernel(const ForkArgs a) 
     int fresh = -1;
     bool go = p.ok;
     if (p.need) {
-        const int base = need_before(a.plan, i, sh);
+        const int64_t base = need_before(a.plan, i, sh);
         go = base + p.need <= avail;
-        if (go) fresh = free_page(f, base);
+        if (go) fresh = free_page(f, (int)base);
         else if (threadIdx.x == 0) flag(a.status, DFLASH_DEV_POOL_FULL);
     }
     report_copy(a.copy_src, a.copy_dst, a.copy_slots, i, p.src, fresh, p.slots);
@@ -339,9 +352,10 @@ __global__ void __launch_bounds__(NT) pages_resize_apply_kernel(const ResizeArgs
     int base = 0;
     bool go = p.ok;
     if (p.need) {
-        base = need_before(a.plan, i, sh);
-        go = base + p.need <= avail;
-        if (!go && threadIdx.x == 0) flag(a.status, DFLASH_DEV_POOL_FULL);
+        const int64_t before = need_before(a.plan, i, sh);
+        go = before + p.need <= avail;
+        if (go) base = (int)before;
+        else if (threadIdx.x == 0) flag(a.status, DFLASH_DEV_POOL_FULL);
     }
     report_copy(a.copy_src, a.copy_dst, a.copy_slots, i, p.src, go && p.src >= 0 ? free_page(f, base) : -1, p.slots);
     if (!go) return;
