@@ -768,7 +768,9 @@ int32_t dflash_pages_compact(dflash_handle* h, const dflash_pages_compact_args* 
     if (!h || !a || a->n_rows < 1 || a->max_pages < 1 || a->n_pool_pages < 1) return DFLASH_ERR_INVALID_ARG;
     if (a->max_pages > MAX_POOL_PAGES || a->n_pool_pages > MAX_POOL_PAGES) return DFLASH_ERR_UNSUPPORTED;
     if (!a->page_table || !a->ref_count || !a->kv_pool || !aligned16(a->kv_pool)) return DFLASH_ERR_INVALID_ARG;
-    if ((a->copy_src != nullptr) != (a->copy_dst != nullptr) || (a->copy_src != nullptr) != (a->n_copies != nullptr)) return DFLASH_ERR_INVALID_ARG;
+    // a pool of one page has no moves to list, and an empty array may have no address
+    if (a->n_pool_pages > 1 && ((a->copy_src != nullptr) != (a->copy_dst != nullptr) || (a->copy_src != nullptr) != (a->n_copies != nullptr)))
+        return DFLASH_ERR_INVALID_ARG;
     DFLASH_TRY(check_pages_ws(a->workspace, a->workspace_bytes, 0, a->max_pages, a->n_pool_pages));
     Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
     RUN(FAM_MISC, launch_pages_compact(L, *a));

@@ -38,3 +38,15 @@ def test_requests_for_more_pages_than_32_bits_count_are_left_out(n, first):
     assert int(table.max()) == int(table.min()) == -1
     assert all(int(c.max()) <= 0 for c in copies) and int(copies[1].max()) == -1
     assert torch.equal(s.d_pool.cpu().view(torch.int32), torch.from_numpy(s.pool))
+
+
+@pytest.mark.parametrize("used", [0, 1])
+def test_compacting_a_pool_of_one_page_reports_its_moves_too(used):
+    cfg = config(hq=2, hkv=2, hd=64, page=1, layers=1, dtype="fp32")
+    lib = binding.DFlash(cfg)
+    s = State(cfg, 1, 1, 2, [used])
+    n_live, none = i32([-1]), torch.zeros(0, dtype=torch.int32, device=DEV)
+    moved = i32([-7])
+    lib.dflash_pages_compact(s.d_table, s.d_ref, s.d_pool, n_live=n_live, copies=(none, none.clone(), moved))
+    s.same(lib, 0)
+    assert int(n_live) == used and int(moved) == 0
