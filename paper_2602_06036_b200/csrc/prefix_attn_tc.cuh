@@ -417,10 +417,13 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
     const uint32_t q_desc = desc_lo(sb), k_desc = desc_lo(sb + Sh::RING_K), v_desc = desc_lo_mn(sb + Sh::RING_V, KT * 128);
     uint32_t tile0 = 0;                                  // key tiles of the segments before
     uint32_t p_phase = 0, turn = t ^ 1;                  // parities of the next waits; thread 0 begins
+    // The lanes look at the barriers one by one, so that one may give up where another finds the phase complete: they vote before any of them acts on it.
+    // (Lanes that went separate ways would stand at different barriers of the warp for good.)
     bool ok = true;
 #pragma unroll 1
     for (int k = 0;; ++k) {
-        if (!bar_wait(sb + Sh::Q_FULL + 8 * (k & 1), (k >> 1) & 1, sb + Sh::ABORT)) { ok = false; break; }
+        ok = __all_sync(0xffffffffu, bar_wait(sb + Sh::Q_FULL + 8 * (k & 1), (k >> 1) & 1, sb + Sh::ABORT));
+        if (!ok) break;
         const uint32_t cur = sb + Sh::CUR + (k & 3) * (uint32_t)sizeof(Segment), q_empty = sb + Sh::Q_EMPTY + 8 * (k & 1);
         const int two = uniform(lds(cur + offsetof(Segment, two))), n_chunks = uniform(lds(cur + offsetof(Segment, n_chunks))), n = (n_chunks + 1) >> 1;
         if (n == 0) break;
@@ -448,6 +451,7 @@ __device__ __forceinline__ void mma_role(const Params& p, int t) {
                 ok = bar_wait(sb + Sh::P_FULL + 8 * t, p_phase, sb + Sh::ABORT);
                 p_phase ^= 1;
             }
+            ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
             if (lead) {
