@@ -394,14 +394,18 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
             bar_arrive(sb + Sh::Q_FULL + 8 * (n_seg & 1));
         }
     }
-    if (lane == 0 && !ok) {
-        sts(sb + Sh::ABORT, 1);
-        if (p.status) atomicOr(p.status, DFLASH_DEV_TIMEOUT);
-        // copies in flight have to land before the CTA's shared memory is given up
+    if (lane == 0) {
+        if (!ok) {
+            sts(sb + Sh::ABORT, 1);
+            if (p.status) atomicOr(p.status, DFLASH_DEV_TIMEOUT);
+        }
+        // Copies in flight have to land before the CTA's shared memory is given up: also when all are issued, since the roles that use them may
+        // give up later on. (Where none does, they land while these are at work, which this warp has nothing to do with any more.)
 #pragma unroll 1
         for (int x = max(0, issued - n_stages); x < issued; ++x) bar_wait(full_at + 8 * (x & (Sh::NF - 1)), x / Sh::NF & 1, 0, DRAIN_LIMIT);      // the last copies into each stage
 #pragma unroll 1
-        for (int k = max(0, n_seg - 2); k < n_seg && !vs; ++k) bar_wait(sb + Sh::Q_FULL + 8 * (k & 1), (k >> 1) & 1, 0, DRAIN_LIMIT);
+        for (int k = max(0, n_seg - (ok ? 1 : 2)); k < n_seg && !vs; ++k)      // the empty segment came by the barrier of the one before the last
+            bar_wait(sb + Sh::Q_FULL + 8 * (k & 1), (k >> 1) & 1, 0, DRAIN_LIMIT);
     }
 }
 

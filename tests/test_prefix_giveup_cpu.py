@@ -64,3 +64,34 @@ def test_the_lanes_leave_together():
 
 def test_without_a_vote_they_would_not():
     assert any(play(steps, False, seed) is None for seed, steps in programs(3000))
+
+
+def end_of_block(tiles, stages, drain, seed):
+    """A copy warp issues its tiles as stages come free, the roles behind it use them up, or give up at some time. Returns how many copies are in flight
+    when the last of them has left."""
+    r = random.Random(seed)
+    give_up = r.choice([None, r.randint(0, 60)])
+    t, lands, used = 0, [], []
+    for x in range(tiles):
+        if x >= stages:
+            if used[x - stages] is None:
+                break                                             # its stage stays taken: the copy warp sees the others give up
+            t = max(t, used[x - stages])
+        t += r.randint(1, 3)
+        lands.append(t + (r.randint(10, 100) if r.random() < 0.2 else r.randint(1, 10)))
+        at = max(lands[-1], max([u for u in used if u is not None], default=0)) + r.randint(1, 5)
+        used.append(at if give_up is None or at < give_up and None not in used else None)
+    end_copy = t
+    complete = len(lands) == tiles
+    if drain or not complete:                                     # the last copy into each stage; those before have been used up
+        end_copy = max([end_copy] + lands[-stages:])
+    end_roles = give_up if None in used else max([u for u in used if u is not None])
+    end = max(end_copy, end_roles)
+    return sum(at > end for at in lands)
+
+
+def test_no_copy_is_in_flight_when_the_block_ends():
+    r = random.Random(2)
+    plans = [(r.randint(1, 20), r.choice([2, 3, 5]), seed) for seed in range(4000)]
+    assert all(end_of_block(n, k, True, seed) == 0 for n, k, seed in plans)
+    assert any(end_of_block(n, k, False, seed) for n, k, seed in plans)
