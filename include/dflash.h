@@ -398,7 +398,8 @@ int32_t dflash_block_attention_bwd(dflash_handle* h, const dflash_attn_bwd_args*
  * (The paper serves independent sequences; its block attention, App. A.3, is computed here with the keys that several
  * sequences have in common read and multiplied once for all of them.)
  * The same result as dflash_block_attention: row r of sequence b attends over the ctx_len[b] cached positions and the
- * block rows (all of them, or those <= r in mode CAUSAL). Sequences group_start[g] .. group_start[g+1]-1 form group g and
+ * block rows (all of them, or those <= r in mode CAUSAL; what later rows hold, NaN and infinities among it, has no say here, while
+ * dflash_block_attention may weight a hidden row of v_blk by 0, which makes NaN of such numbers). Sequences group_start[g] .. group_start[g+1]-1 form group g and
  * share their first prefix_len[g] positions: these are read from the page-table row of the group's FIRST sequence, the
  * rest of a sequence from its own row (the own row's entries below the prefix are not looked at, nor does the prefix have to
  * end on a page border). A sequence with ctx_len[b] < prefix_len[g], and one outside every group, reads its own row only. Where any sequence of

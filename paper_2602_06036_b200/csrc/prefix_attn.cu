@@ -13,6 +13,7 @@
 #include <cstdint>
 #include <memory>
 #include <new>
+#include <type_traits>
 
 namespace dflash {
 namespace {
@@ -164,22 +165,28 @@ __global__ void __launch_bounds__(SIMT_THREADS) prefix_attn_simt_kernel(const __
                 for (int j = 0; j < HD / 16; ++j) o[i][j] *= alpha;
             }
             __syncwarp();                            // a row's 16 threads sit in one warp
-            for (int k = 0; k < CHUNK_KEYS; ++k) {
-                float pr[4];
+            // hidden: a row of V that a row does not see has no say in it, whatever it holds (0 x infinity is NaN)
+            auto values = [&](auto hidden) {
+                for (int key = 0; key < CHUNK_KEYS; ++key) {
+                    float pr[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) pr[i] = sP[(4 * ty + i) * (CHUNK_KEYS + 4) + k];
+                    for (int i = 0; i < 4; ++i) pr[i] = sP[(4 * ty + i) * (CHUNK_KEYS + 4) + key];
 #pragma unroll
-                for (int j = 0; j < HD / 64; ++j) {
-                    const float4 v = *reinterpret_cast<const float4*>(sV + k * HD + 64 * j + 4 * tx);
+                    for (int j = 0; j < HD / 64; ++j) {
+                        const float4 v = *reinterpret_cast<const float4*>(sV + key * HD + 64 * j + 4 * tx);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        o[i][4 * j + 0] = fmaf(pr[i], v.x, o[i][4 * j + 0]);
-                        o[i][4 * j + 1] = fmaf(pr[i], v.y, o[i][4 * j + 1]);
-                        o[i][4 * j + 2] = fmaf(pr[i], v.z, o[i][4 * j + 2]);
-                        o[i][4 * j + 3] = fmaf(pr[i], v.w, o[i][4 * j + 3]);
+                        for (int i = 0; i < 4; ++i) {
+                            if (hidden && key > (s.row0 + 4 * ty + i) / G) continue;
+                            o[i][4 * j + 0] = fmaf(pr[i], v.x, o[i][4 * j + 0]);
+                            o[i][4 * j + 1] = fmaf(pr[i], v.y, o[i][4 * j + 1]);
+                            o[i][4 * j + 2] = fmaf(pr[i], v.z, o[i][4 * j + 2]);
+                            o[i][4 * j + 3] = fmaf(pr[i], v.w, o[i][4 * j + 3]);
+                        }
                     }
                 }
-            }
+            };
+            if (block && p.causal) values(std::true_type{});
+            else values(std::false_type{});
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

@@ -61,7 +61,7 @@ constexpr int NI = 12;                   // ring of tile masks: more tiles than 
 
 struct TileInfo {
     unsigned long long mask[2];          // keys of each chunk that exist
-    int32_t causal_chunk;                // chunk (0 or 1) that holds the block in causal mode, else 2
+    int32_t causal_chunk;                // chunk (0 or 1) that holds the block in causal mode, else 2 (as for a block of one row)
     int32_t full;                        // all 128 keys exist and nothing is causal
 };
 // Shared memory as offsets from a 1024-byte boundary. The roles work with 32-bit addresses that each of them forms anew
@@ -96,7 +96,8 @@ struct Shape {
     static constexpr uint32_t INFO = O_FULL + 16;             // [NI] TileInfo
     static constexpr uint32_t CUR = INFO + NI * sizeof(TileInfo);       // [4] the segments whose queries are in shared memory, and the one before
     static constexpr uint32_t XCH = CUR + 4 * sizeof(Segment);          // [2][128] sums that one thread of a row hands to the other
-    static constexpr uint32_t TMEM_SLOT = XCH + 1024;
+    static constexpr uint32_t ODD_V = XCH + 1024;             // [4] by segment: its number + 1, if a block's V is not finite everywhere (CAUSAL)
+    static constexpr uint32_t TMEM_SLOT = ODD_V + 16;
     static constexpr uint32_t ABORT = TMEM_SLOT + 4;
     static constexpr int SMEM = 1024 + ABORT + 4;
     static_assert(SMEM <= 227 * 1024, "shared memory of one CTA");
@@ -120,6 +121,14 @@ __device__ __forceinline__ unsigned long long lds64(uint32_t a) {
     unsigned long long v;
     asm volatile("ld.shared.b64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
     return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 __device__ __forceinline__ void sts(uint32_t a, int v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
 __device__ __forceinline__ void sts64(uint32_t a, unsigned long long v) { asm volatile("st.shared.b64 [%0], %1;" ::"r"(a), "l"(v) : "memory"); }
@@ -214,6 +223,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
+}
+// the bf16 numbers of a pair that are infinite or NaN, all bits of each set
+__device__ __forceinline__ uint32_t odd_bf16(uint32_t w) {
+    return (((w & 0x7f807f80u) + 0x00800080u) >> 15 & 0x00010001u) * 0xffffu;      // an exponent of ones, and one more, carries into the sign's place
 }
 // two fp32 operations an instruction
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -332,7 +345,7 @@ __device__ __forceinline__ void copy_role(const CUtensorMap& tmQ, const CUtensor
                     if (block && bc == 1) m1 = rows;
                     sts64(ti, m0);
                     sts64(ti + 8, m1);
-                    sts(ti + offsetof(TileInfo, causal_chunk), block && p.causal ? bc : 2);
+                    sts(ti + offsetof(TileInfo, causal_chunk), block && p.causal && p.plan.R > 1 ? bc : 2);
                 }
                 sts(ti + offsetof(TileInfo, full), full);
             }
@@ -527,6 +540,18 @@ __device__ __forceinline__ bool tile_any(int t, bool v) {
     return r != 0;
 }
 
+// Numbers of a block's V that are not finite, added to a row's numerators (this thread's half of the columns) for block rows 0 .. last. Rare, and so done
+// to the stored numbers: done before, in registers, it cost all calls up to 2 % (how the compiler then laid out the registers of the usual tiles).
+template <int HD>
+__device__ __forceinline__ void add_odd(const Params& p, float* part, int seq, int kvh, int h, int last) {
+    const uint16_t* v = static_cast<const uint16_t*>(p.v_blk) + ((int64_t)seq * p.plan.R * p.plan.Hkv + kvh) * HD + h * (HD / 2);
+#pragma unroll 1
+    for (int key = 0; key <= last; ++key, v += p.plan.Hkv * HD) {
+#pragma unroll 1
+        for (int d = 0; d < HD / 2; ++d)
+            if ((v[d] & 0x7f80) == 0x7f80) part[(d >> 2) * 32 + (d & 3)] += __uint_as_float((uint32_t)v[d] << 16);
+    }
+}
 template <int HD>
 __device__ __forceinline__ void softmax_role(const Params& p) {
     using Sh = Shape<HD>;
@@ -550,14 +575,36 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
         const bool mine = row < min(p.plan.row_tile, lds(cur + offsetof(Segment, n_rows)) - first_row());       // the row exists
         float m_run = -CUDART_INF_F, l_run = 0.f;        // l_run: of this thread's keys
         const int step = two ? 1 : 2, first = two ? 0 : t;
-        auto zero_missing = [&](int j, uint32_t ti) {    // V rows that do not exist must not poison P V: 0 x whatever the page holds there
-            const uint32_t x = tile0 + j, v = sb + Sh::RING_V + x % Sh::NV * Sh::STAGE + row * 128;
+        // What a tile of V holds in places where P is 0 must not reach the rows: 0 x infinity or NaN is NaN. Threads h = 0 zero the rows that do not exist;
+        // threads h = 1, in mode CAUSAL, see to the block's rows, each of which is hidden from some: numbers that are not finite (the padding of a block,
+        // say) are taken out of the tile, and added at the end to the rows that see them. Four threads look at a row of V. (No time that shows: 32 whole
+        // contexts of 8000 positions and 17 rows take 114 us in either mode.)
+        auto mend_v = [&](int j, uint32_t ti) {
+            const int chunk = lds(ti + offsetof(TileInfo, causal_chunk));
+            if (h == 1 && chunk > 1) return true;
+            const uint32_t x = tile0 + j, v = sb + Sh::RING_V + x % Sh::NV * Sh::STAGE;
             const bool landed = bar_wait(sb + Sh::FULL_V + 8 * (x % Sh::NF), x / Sh::NF & 1, sb + Sh::ABORT);
-            if (!(lds64(ti + 8 * (row >> 6)) >> (row & 63) & 1)) {
+            if (h == 0) {
+                if (!(lds64(ti + 8 * (row >> 6)) >> (row & 63) & 1)) {
 #pragma unroll
-                for (int i = 0; i < Sh::HALVES; ++i)
+                    for (int i = 0; i < Sh::HALVES; ++i)
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) zero16(v + i * (KT * 128) + ((c ^ row) & 7) * 16);       // neighbouring rows in different banks (148 sequences x 128 keys: 61 us in one order, 52)
+                        for (int c = 0; c < 8; ++c) zero16(v + row * 128 + i * (KT * 128) + ((c ^ row) & 7) * 16);       // neighbouring rows in different banks (148 sequences x 128 keys: 61 us in one order, 52)
+                }
+            } else if ((row & 31) < p.plan.R) {
+                constexpr int VECS = HD / 32;            // 16-byte vectors a thread
+                const int key = row & 31;
+#pragma unroll 2
+                for (int c = (row >> 5) * VECS; c < ((row >> 5) + 1) * VECS; ++c) {
+                    const uint32_t at = v + (chunk * 64 + key) * 128 + (c >> 3) * (KT * 128) + ((c ^ key) & 7) * 16;
+                    uint4 w = lds128(at);
+                    const uint4 odd = make_uint4(odd_bf16(w.x), odd_bf16(w.y), odd_bf16(w.z), odd_bf16(w.w));
+                    if ((odd.x | odd.y | odd.z | odd.w) == 0) continue;
+                    sts(sb + Sh::ODD_V + 4 * (k & 3), k + 1);
+                    __threadfence_block();               // threads of the other query tile that find it taken out know of it
+                    w = make_uint4(w.x & ~odd.x, w.y & ~odd.y, w.z & ~odd.z, w.w & ~odd.w);
+                    sts128(at, w);
+                }
             }
             fence_proxy_async();
             return landed;
@@ -573,7 +620,7 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
             const uint32_t ti = sb + Sh::INFO + ((tile0 + j) % NI) * (uint32_t)sizeof(TileInfo);
             const bool all = lds(ti + offsetof(TileInfo, full));
             if (!(all && j > first) || tile_any(t, !ok)) {
-                if (!all && h == 0) ok = zero_missing(j, ti) && ok;
+                if (!all) ok = mend_v(j, ti) && ok;
                 if (tile_any(t, !ok)) { ok = false; break; }
             }
             __syncwarp();
@@ -617,7 +664,7 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
             }
             tmem_ld32_nowait(tS + h * 64, s);
             tmem_ld32_nowait(tS + h * 64 + 32, s + 32);
-            if (!all && h == 0) ok = zero_missing(j, ti) && ok;
+            if (!all) ok = mend_v(j, ti) && ok;
             tmem_ld_wait();
             if (!all) {
                 unsigned long long m = lds64(ti + 8 * h);
@@ -696,6 +743,9 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
                         *reinterpret_cast<float4*>(p.part + part_offset(at, HD, h * (HD / 8) + (c + d) / 4)) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
                 }
             }
+            if (lds(sb + Sh::ODD_V + 4 * (k & 3)) == k + 1 && (two || (n - 1 & 1) == t) && mine)      // the block is in the last key tile
+                add_odd<HD>(p, p.part + part_offset(at, HD, h * (HD / 8)), lds(cur + offsetof(Segment, seq)), lds(cur + offsetof(Segment, kvh)), h,
+                            min((first_row() + row) / p.plan.G, p.plan.R - 1));
         }
         tc_fence_before();                               // O_t is read: the next segment's first P_FULL lets it be overwritten
         tile0 += n;
@@ -734,6 +784,7 @@ prefix_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             bar_init(sb + Sh::O_FULL + 8 * t, 1);
         }
         sts(sb + Sh::ABORT, 0);
+        for (int k = 0; k < 4; ++k) sts(sb + Sh::ODD_V + 4 * k, 0);
         fence_barrier_init();
         fence_proxy_async();
     }
