@@ -684,6 +684,7 @@ int32_t dflash_block_attention(dflash_handle* h, const dflash_attn_args* a, void
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+constexpr int32_t MAX_CTX_LEN = INT32_MAX - 512;      // positions up to the end of a key tile are counted in 32 bits
 int64_t dflash_prefix_attention_workspace_bytes(const dflash_handle* h, int32_t max_batch, int32_t max_rows, int32_t max_groups) {
     if (!h || max_batch < 0 || max_rows < 0 || max_rows > 32 || max_groups < 0) return DFLASH_ERR_INVALID_ARG;
     if (max_batch > 65535 || max_groups > 65535 || !prefix_attn_supported(h->cfg)) return DFLASH_ERR_UNSUPPORTED;
@@ -696,7 +697,7 @@ int32_t dflash_prefix_attention(dflash_handle* h, const dflash_prefix_attn_args*
         a->layer >= h->cfg.n_layers || a->max_ctx_len < 0)
         return DFLASH_ERR_INVALID_ARG;
     if (a->mode != DFLASH_ATTN_FULL && a->mode != DFLASH_ATTN_CAUSAL) return DFLASH_ERR_INVALID_ARG;
-    if (a->batch > 65535 || a->n_groups > 65535 || a->max_ctx_len > INT32_MAX - 512 || !prefix_attn_supported(h->cfg)) return DFLASH_ERR_UNSUPPORTED;
+    if (a->batch > 65535 || a->n_groups > 65535 || a->max_ctx_len > MAX_CTX_LEN || !prefix_attn_supported(h->cfg)) return DFLASH_ERR_UNSUPPORTED;
     if (a->batch == 0 || a->rows == 0) return DFLASH_OK;
     if (!a->q || !a->k_blk || !a->v_blk || !a->ctx_len || !a->page_table || !a->kv_pool || !a->out || (a->n_groups > 0 && (!a->group_start || !a->prefix_len)))
         return DFLASH_ERR_INVALID_ARG;
@@ -714,6 +715,7 @@ int32_t dflash_prefix_plan_check(const dflash_handle* h, int32_t batch, int32_t 
     if (!h || batch < 1 || batch > 65535 || rows < 1 || rows > 32 || n_groups < 0 || n_groups > 65535 || max_ctx_len < 0 || !ctx_len ||
         (n_groups > 0 && (!group_start || !prefix_len)))
         return DFLASH_ERR_INVALID_ARG;
+    if (max_ctx_len > MAX_CTX_LEN || !prefix_attn_supported(h->cfg)) return DFLASH_ERR_UNSUPPORTED;
     for (int g = 0; g <= n_groups && n_groups > 0; ++g)
         if (group_start[g] < 0 || group_start[g] > batch || (g > 0 && group_start[g - 1] > group_start[g])) return DFLASH_ERR_INVALID_ARG;
     return prefix_plan_check(h->cfg, h->sm_count, batch, rows, n_groups, group_start, prefix_len, ctx_len, max_ctx_len, info);

@@ -33,3 +33,21 @@ def test_every_tile_is_taken_once_where_most_prefixes_are_not_read(lib, shape):
         read = any(0 < prefix[g] <= lens[b] for g in range(n) for b in range(starts[g], starts[g + 1]))
         assert (info[1] > 0) == read
     lib.dflash_destroy(h)
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 128, 64, "bf16"), (2, 2, 64, 256, "bf16"), (4, 1, 128, 8, "bf16")])
+def test_the_longest_contexts(lib, shape):
+    h = _handle(lib, *shape)
+    longest = 2 ** 31 - 1 - 512
+    for starts, prefix, lens in (([0], [], [longest]), ([0, 1], [longest - 70], [longest]), ([0, 1], [longest], [longest])):
+        rc, info = _check(lib, h, 1, starts, prefix, lens, longest)
+        assert rc == 0 and info[2] >= longest // 128, (rc, info)
+    for bound in (longest + 1, 2 ** 31 - 1):
+        assert _check(lib, h, 1, [0], [], [bound], bound)[0] == -2
+    lib.dflash_destroy(h)
+
+
+def test_more_heads_a_group_than_the_call_takes_are_refused_by_the_check_too(lib):
+    h = _handle(lib, 129, 1, 64, 64, "fp32")
+    assert _check(lib, h, 1, [0], [], [5], 100)[0] == -2
+    lib.dflash_destroy(h)
