@@ -35,7 +35,7 @@ def test_every_tile_is_taken_once_where_most_prefixes_are_not_read(lib, shape):
     lib.dflash_destroy(h)
 
 
-@pytest.mark.parametrize("shape", [(1, 1, 128, 64, "bf16"), (2, 2, 64, 256, "bf16"), (4, 1, 128, 8, "bf16")])
+@pytest.mark.parametrize("shape", [(1, 1, 128, 64, "bf16"), (1, 1, 128, 256, "bf16"), (4, 1, 128, 8, "bf16")])
 def test_the_longest_contexts(lib, shape):
     h = _handle(lib, *shape)
     longest = 2 ** 31 - 1 - 512
