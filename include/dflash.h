@@ -406,6 +406,13 @@ int32_t dflash_block_attention_bwd(dflash_handle* h, const dflash_attn_bwd_args*
  * a group reads its prefix, the first one's row has to hold that prefix's pages, even if the first is shorter itself; a prefix that none reads is not looked at.
  * All K/V of a prefix are read once per group (and kv head); the rows of all its sequences are the rows of ONE
  * product with them.
+ * Which of the two to call. Where dflash_block_attention runs on tensor cores (bf16, head_dim 128, 64-token pages, Hq/Hkv a divisor of 128, rows * Hq/Hkv
+ * <= 128) it is one launch and takes 10 us where this call takes 18. This call is the faster one from about 64 thousand positions of prefix on, counted once
+ * for every sequence that shares it, with 16 rows a sequence, and from about 16 thousand with one row. (32/8 heads, one layer, this call against the other: 32
+ * sequences x 16 rows behind 1024 positions 56 and 39 us, behind 4096 80 and 94, behind 16384 156 and 381; 32 x 1 row behind 1024 positions 30 and 37.)
+ * Without shared prefixes it is ahead by up to a quarter for 16 sequences and more of 2048 to 8192 positions (192 and 233 us for 32 of 8192; behind for 32 of
+ * 2048, 70 and 60), and behind for fewer and shorter ones. Of all other shapes dflash_block_attention runs on CUDA cores, and this call is the faster
+ * one at any size (8 sequences x 16 rows of 2048 positions: 22 to 40 us against 1000 to 5300).
  * Any rows 1..32, any Hq/Hkv up to 128. bf16 with 8- to 256-token pages runs on the tensor cores (head_dim 64 and
  * 128); fp32 and smaller pages take a CUDA-core kernel. Three launches: how the work is cut up, the attention, and the partial results
  * of the key ranges merged in a fixed order (bit-reproducible). Lengths and groups are device data: a captured call may be
@@ -414,6 +421,8 @@ int32_t dflash_block_attention_bwd(dflash_handle* h, const dflash_attn_bwd_args*
  * group_start must not fall and must lie in 0..batch, else DFLASH_DEV_BAD_GROUP is set and every sequence reads its
  * own row. A page index outside the pool sets DFLASH_DEV_BAD_PAGE and its keys are left out.
  * q, k_blk, v_blk, out and kv_pool lie on 16-byte boundaries.
+ * Workspace: fp32 partial results of two query tiles for every item and CTA, whether an item is cut up or not. 121 MB for 32 sequences x 17 rows in one
+ * group, 52 MB in none; 1 GB for 1024 x 17, 3.7 GB for 4096 x 17 (32/8 heads of 128).
  * Errors: DFLASH_ERR_INVALID_ARG, DFLASH_ERR_UNSUPPORTED (more than 65535 sequences or groups, Hq/Hkv > 128, batch and max_ctx_len
  * so large that their products no longer fit 32-bit costs: about 6e7 key tiles), DFLASH_ERR_WORKSPACE. Calls must not overlap in time if they share a workspace. */
 typedef struct {
@@ -457,7 +466,8 @@ int64_t dflash_prefix_attention_workspace_bytes(const dflash_handle* h, int32_t 
  * (DFLASH_DEV_BAD_PAGE); more positions than a row has entries for (DFLASH_DEV_CTX_OVERFLOW).
  * kv_pool is the pool of the handle's shape (all layers are copied). Where a second pool is kept under the same
  * table (a drafter's beside its target's), hand the page copies that a call reports to dflash_pages_copy with the
- * other handle. Lists hold at most 65535 entries, pools and table rows 2^30 pages (DFLASH_ERR_UNSUPPORTED). Two launches each (copy: one).
+ * other handle. Time goes up with the square of very long lists and pools, since an entry is compared with the others of its list, and every 4096
+ * pages are compacted by a look at all counts: 16384 entries 0.15 to 0.25 ms, 65535 copies 9 ms and resizes 0.7 ms (4 KB pages), a pool of 16 million pages 25 ms. Lists hold at most 65535 entries, pools and table rows 2^30 pages (DFLASH_ERR_UNSUPPORTED). Two launches each (copy: one).
  * Workspace: dflash_pages_workspace_bytes(n, max_pages, n_pool_pages), 256-byte aligned; calls must not overlap in time. */
 typedef struct {
     int32_t        n;            /* list entries                                              */
@@ -471,7 +481,7 @@ typedef struct {
 } dflash_pages_copy_args;
 /* Copies the first n_slots[i] slots of page src[i] onto those of page dst[i]: every layer, K and V, every head. A page
  * may be the source of several entries. An entry is left out, and DFLASH_DEV_BAD_PAGE set, if a page index lies
- * outside the pool, if its destination is that of an earlier entry, or if its destination is the source of an entry (a
+ * outside the pool, if its destination is that of an earlier entry (also one with nothing to do), or if its destination is the source of an entry (a
  * copy of a page onto itself among them): what is copied never depends on the order. */
 int32_t dflash_pages_copy(dflash_handle* h, const dflash_pages_copy_args* a /*[host]*/, void* stream);
 

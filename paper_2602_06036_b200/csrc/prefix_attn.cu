@@ -205,7 +205,8 @@ __global__ void __launch_bounds__(SIMT_THREADS) prefix_attn_simt_kernel(const __
 // ---- merge ----------------------------------------------------------------------------------------------------------
 // Four neighbouring packed rows of a (sequence, kv head) by W warps (eight lanes a row), each of which takes every W-th part of these rows; their sums are
 // added up at the end, so that the order is fixed. A warp requests PB parts together, results and statistics alike: the kernel waits for L2, not
-// for bytes. W = 4 where there are few rows (decoding: 8.3 -> 5.4 us), W = 1 where there are enough for all SMs (17408 rows: 18 us against 38 with four).
+// for bytes. W = 4 where there are few rows (decoding: 8.3 -> 5.4 us), W = 1 where there are enough for all SMs, which is said of 8 units (of four rows) an SM.
+// Whole calls behind 4096 positions, W = 4 and W = 1: 1024 units 39.6 us and 42.8, 1280 (on W = 1's side) 46.6 and 50.3, 1536 47.4 and 46.5, 2048 54.8 and 50.7, 4096 85.7 and 75.4.
 template <typename T, int HD, int W>
 __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant__ Params p) {
     constexpr int PB = 4;
