@@ -629,6 +629,7 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
 #pragma unroll 1
         for (int j = first; j < n && work; j += step) {
             ok = bar_wait(sb + Sh::S_FULL + 8 * t, s_phase, sb + Sh::ABORT);
+            __syncwarp();                                // the lanes wait one by one, and loads and stores of TMEM are made by the whole warp in step
             s_phase ^= 1;
             tc_fence_after();
             const uint32_t ti = sb + Sh::INFO + ((tile0 + j) % NI) * (uint32_t)sizeof(TileInfo);
@@ -665,6 +666,7 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
             tmem_ld32_nowait(tS + h * 64, s);
             tmem_ld32_nowait(tS + h * 64 + 32, s + 32);
             if (!all) ok = mend_v(j, ti) && ok;
+            __syncwarp();
             tmem_ld_wait();
             if (!all) {
                 unsigned long long m = lds64(ti + 8 * h);
@@ -723,6 +725,7 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
         const bool any = n > first;
         if (any) {
             ok = bar_wait(sb + Sh::O_FULL + 8 * t, o_phase, sb + Sh::ABORT);
+            __syncwarp();
             o_phase ^= 1;
             tc_fence_after();
         }
@@ -735,6 +738,7 @@ __device__ __forceinline__ void softmax_role(const Params& p) {
 #pragma unroll
             for (int c = 0; c < HD / 2; c += 32) {
                 float o[32];
+                __syncwarp();
                 tmem_ld32_nowait(tO + c, o);
                 tmem_ld_wait();
                 if (mine) {
