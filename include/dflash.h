@@ -53,6 +53,7 @@ extern "C" {
 #define DFLASH_DEV_BAD_ROW          16   /* page-table row that a page operation cannot take: request left out */
 #define DFLASH_DEV_POOL_FULL        32   /* not enough free pages: request left out             */
 #define DFLASH_DEV_BAD_GROUP        64   /* group bounds not rising or outside the batch: prefixes read unshared */
+#define DFLASH_DEV_NOT_FINITE      128   /* norm of the gradients infinite or NaN: step left out */
 
 #define DFLASH_F32   0
 #define DFLASH_BF16  1
@@ -599,6 +600,112 @@ typedef struct {
     int32_t*       dev_status;         /* [device] may be NULL                                          */
 } dflash_block_loss_args;
 int32_t dflash_block_loss(dflash_handle* h, const dflash_block_loss_args* a /*[host]*/, void* stream);
+
+/* ---- log probabilities of given tokens, with entropy and top alternatives ----
+ * (No counterpart in the paper: what a serving answer reports about its tokens, and, with the gradient below, the losses that take a
+ * teacher's distribution or a reward in place of block_loss's hard targets.) For each row of logits z, with M = max z and S = sum exp((z - M) / T):
+ *   logprob[i] = (z[tokens[i]] - M) / T - ln S          stats = (M, ln S)  (log-sum-exp of z / T = M / T + ln S)
+ *   entropy    = ln S - (1/S) sum exp((z - M) / T) (z - M) / T
+ *   top_ids    = the n_top tokens of the largest logits in falling order (equal ones: lowest index first), top_logprob theirs.
+ * -inf (a token that a mask forbids) has probability 0 and is no alternative: where a row has fewer than n_top others, the last top_ids
+ * are -1 and their top_logprob -inf. A row of -inf only: stats (-inf, 0), entropy 0, every logprob -inf. A row that holds NaN or +inf:
+ * NaN in all numbers but M; NaN is never an alternative. A negative token stands for none (logprob 0), and so does one >= vocab, which
+ * sets DFLASH_DEV_BAD_TOKEN. Temperature scales the distribution, not the order of the alternatives.
+ * One launch and one pass over the logits, no scratch memory: calls may overlap. Sums in fp32; against exact arithmetic the log probabilities are off by
+ * about 1e-6 (plus 2^-24 of their size). Rows may start anywhere (an odd vocabulary or stride costs nothing).
+ * Errors: DFLASH_ERR_INVALID_ARG (null pointer, T not positive and finite, bad dtype or sizes), DFLASH_ERR_UNSUPPORTED (n_tokens or n_top > 128,
+ * vocab > 2^30, more than 2^28 rows). */
+typedef struct {
+    const void*    logits;        /* [device] [n_rows, vocab]                                   */
+    int32_t        logits_dtype;  /* DFLASH_F32 | DFLASH_BF16                                   */
+    int64_t        row_stride;    /* elements (0 = vocab)                                       */
+    int32_t        n_rows, vocab;
+    float          temperature;   /* > 0                                                        */
+    int32_t        n_tokens;      /* given tokens of a row, 0..128                              */
+    const int32_t* tokens;        /* [device] [n_rows, n_tokens]; the same token may stand in a row more than once */
+    float*         logprob;       /* [device] out [n_rows, n_tokens]                            */
+    float*         stats;         /* [device] out [n_rows, 2]; may be NULL                      */
+    float*         entropy;       /* [device] out [n_rows], nats; may be NULL                   */
+    int32_t        n_top;         /* alternatives of a row, 0..128                              */
+    int32_t*       top_ids;       /* [device] out [n_rows, n_top]                               */
+    float*         top_logprob;   /* [device] out [n_rows, n_top]                               */
+    int32_t*       dev_status;    /* [device] may be NULL                                       */
+} dflash_token_logprobs_args;
+int32_t dflash_token_logprobs(dflash_handle* h, const dflash_token_logprobs_args* a /*[host]*/, void* stream);
+
+/* Gradient of the above with respect to the logits, given those of a loss with respect to logprob (g_i) and entropy (gH), p = softmax(z / T):
+ *   dlogits[v] = (1/T) [ sum of g_i over the i with tokens[i] = v  -  p_v (G + gH (ln p_v + entropy)) ],   G = sum of the g_i of tokens inside the vocabulary.
+ * The gradient through top_logprob is had by giving top_ids as tokens. Equal tokens' gradients add up in the order of the list. A row whose
+ * incoming gradients are all 0 gets zeros, whatever its logits hold (they are not read), and so does a row of -inf only.
+ * stats (and entropy, where d_entropy is given) are those of the forward call with the same logits and temperature. dlogits may be
+ * the logits' own buffer if dtype and stride agree (otherwise the two must not overlap). One launch; reads the logits once and writes the gradient once.
+ * Errors as above; DFLASH_ERR_UNSUPPORTED also for more than 2^31 pieces of 8192 entries. */
+typedef struct {
+    const void*    logits;             /* [device] [n_rows, vocab]                              */
+    int32_t        logits_dtype;       /* DFLASH_F32 | DFLASH_BF16                              */
+    int64_t        row_stride;         /* elements (0 = vocab)                                  */
+    int32_t        n_rows, vocab;
+    float          temperature;        /* > 0                                                   */
+    int32_t        n_tokens;           /* 0..128                                                */
+    const int32_t* tokens;             /* [device] [n_rows, n_tokens]                           */
+    const float*   stats;              /* [device] [n_rows, 2]                                  */
+    const float*   entropy;            /* [device] [n_rows]; needed with d_entropy              */
+    const float*   d_logprob;          /* [device] [n_rows, n_tokens]                           */
+    const float*   d_entropy;          /* [device] [n_rows]; may be NULL                        */
+    void*          dlogits;            /* [device] out [n_rows, vocab]                          */
+    int32_t        dlogits_dtype;      /* DFLASH_F32 | DFLASH_BF16                              */
+    int64_t        dlogits_row_stride; /* elements (0 = vocab)                                  */
+    int32_t*       dev_status;         /* [device] may be NULL                                  */
+} dflash_token_logprobs_bwd_args;
+int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_bwd_args* a /*[host]*/, void* stream);
+
+/* ---- training side: one AdamW step over many tensors (App. A.1: AdamW, gradients clipped by their norm) ----
+ * For every entry of every tensor, with norm = the 2-norm of all grad * grad_scale of the call and t = the step's number, from 1:
+ *   g = grad * grad_scale * min(1, max_grad_norm / (norm + 1e-6))            (max_grad_norm <= 0: no clipping)
+ *   m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
+ *   w = w - lr_t weight_decay w - lr_t (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),     lr_t = lr * lr_scale
+ * Arithmetic is fp32, the norm is added up in double in a fixed order. The weights w are `param` (fp32; or bf16, to which
+ * every step is rounded to nearest, so that steps below 2^-9 of a weight are lost), or an fp32 `master` copy, which `param` (bf16) then receives rounded.
+ * States: state_bits 32: exp_avg and exp_avg_sq hold m and v in fp32. state_bits 8: they hold e4m3 codes of m and of sqrt(v), with one
+ * fp32 scale for each 128 entries (value = code * scale, scale = largest magnitude / 448, rounded to nearest; 0 where that magnitude is below 2^-117). The step itself uses m and v before
+ * that rounding. Zeroed buffers are states of 0 in either form.
+ * Where the norm is computed (max_grad_norm > 0, or grad_norm given) and is not finite (a gradient is NaN, infinite or above 1e19), the whole step is left out: nothing but
+ * grad_norm is written and DFLASH_DEV_NOT_FINITE is set. Without it such a gradient makes NaN of its own entry (states of 8 bits: of its
+ * block's 128 states).
+ * Launches: one per 320 tensors, twice with the norm. Captured calls may be replayed: lr_dev and step_dev are then read at each replay. No two tensors
+ * of a call may overlap; calls must not overlap in time if they share tensors or a workspace.
+ * Errors: DFLASH_ERR_INVALID_ARG (null pointer, address that is no multiple of the element's size, n < 0, bad dtype or state_bits, a master copy beside an fp32 param,
+ * step < 1, betas outside [0, 1), eps or grad_scale not positive), DFLASH_ERR_WORKSPACE (only where the norm is computed). */
+typedef struct {
+    void*       param;             /* [device] in/out [n] (out only with `master`)              */
+    const void* grad;              /* [device] [n]                                              */
+    float*      master;            /* [device] in/out [n]; NULL: `param` itself is stepped      */
+    void*       exp_avg;           /* [device] in/out [n] fp32 or e4m3                          */
+    void*       exp_avg_sq;        /* [device] in/out [n]                                       */
+    float*      exp_avg_scale;     /* [device] in/out [(n + 127) / 128]; state_bits 8 only      */
+    float*      exp_avg_sq_scale;  /* [device] in/out [(n + 127) / 128]; state_bits 8 only      */
+    int64_t     n;
+    int32_t     param_dtype;       /* DFLASH_F32 | DFLASH_BF16                                  */
+    int32_t     grad_dtype;        /* DFLASH_F32 | DFLASH_BF16                                  */
+    int32_t     state_bits;        /* 32 | 8                                                    */
+    float       weight_decay, lr_scale;
+} dflash_adamw_tensor;
+typedef struct {
+    const dflash_adamw_tensor* tensors;   /* [host] [n_tensors]                                 */
+    int32_t        n_tensors;
+    int32_t        step;                  /* t >= 1 (ignored with step_dev)                     */
+    const int32_t* step_dev;              /* [device] [1] t, below 1 = 1; may be NULL           */
+    double         lr;                    /* (ignored with lr_dev)                              */
+    const float*   lr_dev;                /* [device] [1]; may be NULL                          */
+    double         beta1, beta2, eps, grad_scale;
+    double         max_grad_norm;         /* <= 0: no clipping                                  */
+    float*         grad_norm;             /* [device] out [1] the norm before clipping; may be NULL */
+    void*          workspace;             /* [device] >= dflash_adamw_workspace_bytes(h, n_tensors), 256-byte aligned; may be NULL without the norm */
+    int64_t        workspace_bytes;
+    int32_t*       dev_status;            /* [device] may be NULL                               */
+} dflash_adamw_args;
+int32_t dflash_adamw_step(dflash_handle* h, const dflash_adamw_args* a /*[host]*/, void* stream);
+int64_t dflash_adamw_workspace_bytes(const dflash_handle* h, int32_t n_tensors);
 
 /* ---- per-kernel-family timing (host-side CUDA events; off by default) ----
  * While enabled, every launch the library issues is bracketed by an event pair on the caller's

@@ -495,6 +495,106 @@ def block_loss(logits, targets, gamma, want_grad=True):
 # --------------------------------------------------------------------------------------------
 # toy causal target model (only for the losslessness check of the speculative cycle)
 # --------------------------------------------------------------------------------------------
+# ---------------------------------------------------------------------------------------------
+# log probabilities of given tokens, entropy, alternatives and their gradient
+# ---------------------------------------------------------------------------------------------
+def token_logprobs(logits, tokens, T=1.0, n_top=0):
+    """logits [n, V], tokens [n, k] (negative or >= V: none). A dict of logprob [n, k], stats [n, 2], entropy [n], top_ids and
+    top_logprob [n, n_top], and lp [n, V], the log probabilities of all tokens."""
+    z = np.asarray(logits, dtype=np.float64)
+    tokens = np.asarray(tokens)
+    n, V = z.shape
+    lp = np.empty((n, V))
+    out = dict(logprob=np.zeros(tokens.shape), stats=np.zeros((n, 2)), entropy=np.zeros(n), lp=lp,
+               top_ids=np.full((n, n_top), -1), top_logprob=np.full((n, n_top), -np.inf))
+    for r in range(n):
+        bad = np.isnan(z[r]).any() or np.isposinf(z[r]).any()
+        seen = z[r][~np.isnan(z[r])]
+        M = seen.max() if len(seen) else -np.inf
+        if bad:
+            lp[r] = np.nan
+            out["stats"][r] = M, np.nan
+            out["entropy"][r] = np.nan
+        elif M == -np.inf:
+            lp[r] = -np.inf
+            out["stats"][r] = M, 0.0
+        else:
+            y = (z[r] - M) / T
+            log_sum = np.log(np.exp(y).sum())
+            lp[r] = y - log_sum
+            out["stats"][r] = M, log_sum
+            p = np.exp(lp[r])
+            out["entropy"][r] = -(p[p > 0] * lp[r][p > 0]).sum()
+        for i, t in enumerate(tokens[r]):
+            if 0 <= t < V:
+                out["logprob"][r, i] = lp[r, t]
+        can = np.flatnonzero(z[r] > -np.inf)                  # NaN and -inf are no alternatives
+        order = can[np.argsort(-z[r][can], kind="stable")][:n_top]
+        out["top_ids"][r, :len(order)] = order
+        out["top_logprob"][r, :len(order)] = lp[r, order]
+    return out
+
+
+def token_logprobs_backward(logits, tokens, d_logprob, d_entropy=None, T=1.0):
+    """Gradient [n, V] of sum(d_logprob * logprob) + sum(d_entropy * entropy) with respect to the logits."""
+    z = np.asarray(logits, dtype=np.float64)
+    tokens = np.asarray(tokens)
+    n, V = z.shape
+    f = token_logprobs(z, tokens, T)
+    d = np.zeros((n, V))
+    for r in range(n):
+        valid = (tokens[r] >= 0) & (tokens[r] < V)
+        g = np.where(valid, np.asarray(d_logprob[r], dtype=np.float64), 0.0)
+        gh = 0.0 if d_entropy is None else float(d_entropy[r])
+        if (np.all(g == 0.0) and gh == 0.0) or f["stats"][r, 0] == -np.inf and f["stats"][r, 1] == 0.0:
+            continue
+        lp = f["lp"][r]
+        p = np.exp(lp)
+        d[r] = -p * g.sum()
+        if gh != 0.0:
+            d[r] -= gh * np.where(p > 0, p * (np.where(p > 0, lp, 0.0) + f["entropy"][r]), p)
+        np.add.at(d[r], tokens[r][valid], g[valid])
+        d[r] /= T
+    return d
+
+
+# ---------------------------------------------------------------------------------------------
+# AdamW step, clipped by the norm of all gradients
+# ---------------------------------------------------------------------------------------------
+def e4m3(x):
+    """x rounded to the nearest number of 4 significant bits from 2^-6 up and of steps of 2^-9 below, ties to even, at most 448."""
+    a = np.minimum(np.abs(x), 448.0)
+    step = 2.0 ** (np.floor(np.log2(np.maximum(a, 2.0 ** -6))) - 3)
+    return np.sign(x) * np.minimum(np.round(a / step) * step, 448.0)
+
+
+def state_codes(x, root):
+    """An 8-bit state of the values x: (code values, scale of each 128). `root`: no value that is not 0 gets the code 0."""
+    n = len(x)
+    scale = np.zeros(-(-n // 128))
+    codes = np.zeros(n)
+    for b in range(len(scale)):
+        part = slice(128 * b, min(n, 128 * b + 128))
+        scale[b] = np.abs(x[part]).max() / 448.0
+        if scale[b] > 0:
+            c = x[part] / scale[b]
+            codes[part] = e4m3(np.where(c > 0, np.maximum(c, 2.0 ** -9), c) if root else c)
+    return codes, scale
+
+
+def adamw_norm(grads, grad_scale=1.0):
+    return float(np.sqrt(sum((np.asarray(g, dtype=np.float64) ** 2).sum() for g in grads)) * grad_scale)
+
+
+def adamw_step(w, g, m, v, t, lr, beta1, beta2, eps, weight_decay, factor=1.0):
+    """One tensor, in 64 bits; factor: grad_scale times what clipping leaves. Returns (w, m, v)."""
+    w, g, m, v = (np.asarray(x, dtype=np.float64) for x in (w, g, m, v))
+    g = g * factor
+    m = beta1 * m + (1 - beta1) * g
+    v = beta2 * v + (1 - beta2) * g * g
+    return w - lr * weight_decay * w - lr * (m / (1 - beta1 ** t)) / (np.sqrt(v / (1 - beta2 ** t)) + eps), m, v
+
+
 def toy_target_forward(tokens, tw, tcfg, tap_layers):
     """Plain causal transformer over the whole token list. Returns (logits [T, V], feats
     [T, k*D] = hidden states after the tapped layers, concatenated along features)."""

@@ -22,7 +22,7 @@ F32, BF16 = 0, 1
 ATTN_FULL, ATTN_CAUSAL = 0, 1
 VERIFY_LOGITS, VERIFY_IDS = 0, 1
 DEV_BAD_TOKEN, DEV_BAD_PAGE, DEV_CTX_OVERFLOW, DEV_TIMEOUT = 1, 2, 4, 8
-DEV_BAD_ROW, DEV_POOL_FULL, DEV_BAD_GROUP = 16, 32, 64
+DEV_BAD_ROW, DEV_POOL_FULL, DEV_BAD_GROUP, DEV_NOT_FINITE = 16, 32, 64, 128
 
 EXPORTS = (
     "dflash_create", "dflash_destroy", "dflash_set_weights", "dflash_workspace_bytes",
@@ -33,7 +33,8 @@ EXPORTS = (
     "dflash_sample_workspace_bytes", "dflash_target_verify", "dflash_block_loss", "dflash_attention_plan",
     "dflash_block_attention_bwd", "dflash_gemm_plan_check", "dflash_prefix_attention",
     "dflash_prefix_attention_workspace_bytes", "dflash_prefix_plan_check", "dflash_pages_copy", "dflash_pages_fork",
-    "dflash_pages_resize", "dflash_pages_compact", "dflash_pages_workspace_bytes",
+    "dflash_pages_resize", "dflash_pages_compact", "dflash_pages_workspace_bytes", "dflash_token_logprobs",
+    "dflash_token_logprobs_bwd", "dflash_adamw_step", "dflash_adamw_workspace_bytes",
 )
 N_FAMILIES = 15
 
@@ -167,6 +168,32 @@ class PagesCompactArgs(C.Structure):
                 ("dev_status", C.c_void_p)]
 
 
+class TokenLogprobsArgs(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("logits_dtype", C.c_int32), ("row_stride", C.c_int64), ("n_rows", C.c_int32), ("vocab", C.c_int32),
+                ("temperature", C.c_float), ("n_tokens", C.c_int32), ("tokens", C.c_void_p), ("logprob", C.c_void_p), ("stats", C.c_void_p),
+                ("entropy", C.c_void_p), ("n_top", C.c_int32), ("top_ids", C.c_void_p), ("top_logprob", C.c_void_p), ("dev_status", C.c_void_p)]
+
+
+class TokenLogprobsBwdArgs(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("logits_dtype", C.c_int32), ("row_stride", C.c_int64), ("n_rows", C.c_int32), ("vocab", C.c_int32),
+                ("temperature", C.c_float), ("n_tokens", C.c_int32), ("tokens", C.c_void_p), ("stats", C.c_void_p), ("entropy", C.c_void_p),
+                ("d_logprob", C.c_void_p), ("d_entropy", C.c_void_p), ("dlogits", C.c_void_p), ("dlogits_dtype", C.c_int32),
+                ("dlogits_row_stride", C.c_int64), ("dev_status", C.c_void_p)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("master", C.c_void_p), ("exp_avg", C.c_void_p), ("exp_avg_sq", C.c_void_p),
+                ("exp_avg_scale", C.c_void_p), ("exp_avg_sq_scale", C.c_void_p), ("n", C.c_int64), ("param_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("state_bits", C.c_int32), ("weight_decay", C.c_float), ("lr_scale", C.c_float)]
+
+
+class AdamwArgs(C.Structure):
+    _fields_ = [("tensors", C.POINTER(AdamwTensor)), ("n_tensors", C.c_int32), ("step", C.c_int32), ("step_dev", C.c_void_p), ("lr", C.c_double),
+                ("lr_dev", C.c_void_p), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("grad_scale", C.c_double),
+                ("max_grad_norm", C.c_double), ("grad_norm", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
+                ("dev_status", C.c_void_p)]
+
+
 class LmHeadArgs(C.Structure):
     _fields_ = [("hidden", C.c_void_p), ("hidden_is_f32", C.c_int32), ("n_rows", C.c_int32),
                 ("apply_norm", C.c_int32), ("ids", C.c_void_p), ("top1", C.c_void_p), ("margin", C.c_void_p),
@@ -196,7 +223,8 @@ def load():
                      ("dflash_verify_accept_sample", VerifySampleArgs), ("dflash_target_verify", TargetArgs),
                      ("dflash_block_loss", BlockLossArgs), ("dflash_block_attention_bwd", AttnBwdArgs),
                      ("dflash_prefix_attention", PrefixAttnArgs), ("dflash_pages_copy", PagesCopyArgs), ("dflash_pages_fork", PagesForkArgs),
-                     ("dflash_pages_resize", PagesResizeArgs), ("dflash_pages_compact", PagesCompactArgs)):
+                     ("dflash_pages_resize", PagesResizeArgs), ("dflash_pages_compact", PagesCompactArgs),
+                     ("dflash_token_logprobs", TokenLogprobsArgs), ("dflash_token_logprobs_bwd", TokenLogprobsBwdArgs), ("dflash_adamw_step", AdamwArgs)):
         fn = getattr(lib, name)
         fn.argtypes = [C.c_void_p, C.POINTER(st), C.c_void_p]
         fn.restype = C.c_int32
@@ -210,6 +238,8 @@ def load():
     lib.dflash_prefix_attention_workspace_bytes.restype = C.c_int64
     lib.dflash_pages_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
     lib.dflash_pages_workspace_bytes.restype = C.c_int64
+    lib.dflash_adamw_workspace_bytes.argtypes = [C.c_void_p, C.c_int32]
+    lib.dflash_adamw_workspace_bytes.restype = C.c_int64
     i32p = C.POINTER(C.c_int32)
     lib.dflash_prefix_plan_check.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, i32p, i32p, i32p, C.c_int32, C.POINTER(C.c_int64)]
     lib.dflash_prefix_plan_check.restype = C.c_int32
@@ -262,6 +292,46 @@ def _current_stream(index: int) -> int:
 
 def launch_count() -> int:
     return int(load().dflash_launch_count())
+
+
+class AdamwPlan:
+    """The tensors of an optimiser step as the library takes them (see DFlash.adamw_plan). Keeps them alive; their addresses are those of the plan."""
+
+    def __init__(self, entries, index: int):
+        self.tensors = [dict(e) for e in entries]
+        self.n = len(self.tensors)
+        self.table = (AdamwTensor * max(self.n, 1))()
+        written = []
+        for i, e in enumerate(self.tensors):
+            unknown = set(e) - {"param", "grad", "exp_avg", "exp_avg_sq", "master", "exp_avg_scale", "exp_avg_sq_scale", "weight_decay", "lr_scale"}
+            assert not unknown, f"tensor {i}: unknown {sorted(unknown)}"
+            param, n = e["param"], e["param"].numel()
+            bits = 32 if e["exp_avg"].dtype is torch.float32 else 8
+            state = (torch.float32,) if bits == 32 else (torch.float8_e4m3fn, torch.uint8)
+            weights = (torch.float32, torch.bfloat16)
+
+            def address(name, types, size, needed=True):
+                t = e.get(name)
+                if t is None:
+                    assert not needed, f"tensor {i}: {name} missing"
+                    return None
+                assert t.dtype in types, f"tensor {i}: {name} has type {t.dtype}, expected {types}"
+                assert t.get_device() == index and t.is_contiguous(), f"tensor {i}: {name} has to be contiguous and on device {index}"
+                assert t.numel() == size, f"tensor {i}: {name} has {t.numel()} entries, expected {size}"
+                if name != "grad" and size:
+                    written.append((t.data_ptr(), t.data_ptr() + size * t.element_size(), i, name))
+                return t.data_ptr()
+
+            assert e.get("master") is None or param.dtype is torch.bfloat16, f"tensor {i}: a master copy goes with a bf16 param"
+            scales = -(-n // 128)
+            self.table[i] = AdamwTensor(
+                address("param", weights, n), address("grad", weights, n), address("master", (torch.float32,), n, False), address("exp_avg", state, n),
+                address("exp_avg_sq", state, n), *((address(k, (torch.float32,), scales) if bits == 8 else None) for k in ("exp_avg_scale", "exp_avg_sq_scale")),
+                n, F32 if param.dtype is torch.float32 else BF16, F32 if e["grad"].dtype is torch.float32 else BF16, bits,
+                float(e.get("weight_decay", 0.0)), float(e.get("lr_scale", 1.0)))
+        written.sort()
+        for a, b in zip(written, written[1:]):
+            assert a[1] <= b[0], f"{a[3]} of tensor {a[2]} and {b[3]} of tensor {b[2]} overlap"
 
 
 class DFlash:
@@ -622,6 +692,62 @@ class DFlash:
                              self._dev(n_live, i32, 1), self._dev(cs, i32, pages // 2), self._dev(cd, i32, pages // 2), self._dev(cn, i32, 1), ws, ws_bytes,
                              self.status.data_ptr())
         self._call(self.lib.dflash_pages_compact, a, stream)
+
+    # ---- scoring, distilling, stepping --------------------------------------------------------
+    def _logit_rows(self, t, n=None, vocab=None):
+        """Address, type and row stride of logits [n, vocab] whose rows may lie apart."""
+        assert t.dim() == 2 and t.dtype in (torch.float32, torch.bfloat16), "fp32 or bf16 logits [rows, vocab] expected"
+        assert t.get_device() == self._index, f"tensor on {self.device} expected"
+        rows, v = t.shape
+        assert (n is None or rows == n) and (vocab is None or v == vocab), f"shape {(n, vocab)} expected, got {tuple(t.shape)}"
+        assert (v <= 1 or t.stride(1) == 1) and (rows <= 1 or t.stride(0) >= v), "rows of neighbouring entries that do not overlap expected"
+        return t.data_ptr(), F32 if t.dtype is torch.float32 else BF16, t.stride(0) if rows > 1 else v
+
+    def dflash_token_logprobs(self, logits, tokens, logprob, temperature=1.0, stats=None, entropy=None, top_ids=None, top_logprob=None, stream=None):
+        """logprob [n, k] of tokens int32 [n, k] (negative: none) under softmax(logits [n, V] / T). stats [n, 2] receives (M, ln sum exp((z - M) / T)),
+        entropy [n] nats, top_ids / top_logprob [n, m] the m most likely tokens. tokens and logprob may both be None."""
+        n, v = logits.shape
+        k = 0 if tokens is None else tokens.shape[1]
+        m = 0 if top_ids is None else top_ids.shape[1]
+        z, dt, ld = self._logit_rows(logits)
+        f32 = torch.float32
+        a = TokenLogprobsArgs(z, dt, ld, n, v, float(temperature), k, self._dev(tokens, torch.int32, n, k), self._dev(logprob, f32, n, k),
+                              self._dev(stats, f32, n, 2), self._dev(entropy, f32, n), m, self._dev(top_ids, torch.int32, n, m),
+                              self._dev(top_logprob, f32, n, m), self.status.data_ptr())
+        self._call(self.lib.dflash_token_logprobs, a, stream)
+
+    def dflash_token_logprobs_bwd(self, logits, tokens, stats, d_logprob, dlogits, temperature=1.0, entropy=None, d_entropy=None, stream=None):
+        """dlogits [n, V] from the gradients d_logprob [n, k] and d_entropy [n] (or None) of dflash_token_logprobs; stats and entropy are its outputs.
+        dlogits may be logits."""
+        n, v = logits.shape
+        k = 0 if tokens is None else tokens.shape[1]
+        z, dt, ld = self._logit_rows(logits)
+        dz, ddt, dld = self._logit_rows(dlogits, n, v)
+        f32 = torch.float32
+        a = TokenLogprobsBwdArgs(z, dt, ld, n, v, float(temperature), k, self._dev(tokens, torch.int32, n, k), self._dev(stats, f32, n, 2),
+                                 self._dev(entropy, f32, n), self._dev(d_logprob, f32, n, k), self._dev(d_entropy, f32, n), dz, ddt, dld,
+                                 self.status.data_ptr())
+        self._call(self.lib.dflash_token_logprobs_bwd, a, stream)
+
+    def adamw_plan(self, entries) -> AdamwPlan:
+        """entries: one dict a tensor with param (fp32 or bf16), grad (fp32 or bf16), exp_avg and exp_avg_sq (fp32; or float8_e4m3fn with fp32
+        exp_avg_scale and exp_avg_sq_scale, one for 128 entries), and where wanted master (fp32, beside a bf16 param), weight_decay (0), lr_scale (1). All contiguous."""
+        return AdamwPlan(entries, self._index)
+
+    def _adamw_ws(self, n):
+        return self.lib.dflash_adamw_workspace_bytes(self.h, n)
+
+    def dflash_adamw_step(self, plan: AdamwPlan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, max_grad_norm=0.0, grad_norm=None, stream=None):
+        """One AdamW step of all tensors of the plan. step (from 1) and lr: numbers, or int32 / fp32 tensors of one entry on the device (for captured
+        calls). max_grad_norm > 0 clips by the norm of all gradients; grad_norm fp32 [1] receives it."""
+        on_device = lambda x: isinstance(x, torch.Tensor)  # noqa: E731
+        ws, ws_bytes = None, 0
+        if max_grad_norm > 0 or grad_norm is not None:
+            held, ws, ws_bytes = self._scratch("adamw", self._adamw_ws, (plan.n,), stream)
+        a = AdamwArgs(plan.table, plan.n, 0 if on_device(step) else int(step), self._dev(step, torch.int32, 1) if on_device(step) else None,
+                      0.0 if on_device(lr) else float(lr), self._dev(lr, torch.float32, 1) if on_device(lr) else None, float(beta1), float(beta2), float(eps),
+                      float(grad_scale), float(max_grad_norm), self._dev(grad_norm, torch.float32, 1), ws, ws_bytes, self.status.data_ptr())
+        self._call(self.lib.dflash_adamw_step, a, stream)
 
     def dflash_lmhead_argmax(self, hidden, apply_norm, ids, top1=None, margin=None, logits_out=None, stream=None):
         M = hidden.shape[0]

@@ -1,0 +1,376 @@
+// AdamW over many tensors at once, with clipping by the norm of all gradients and states of 32 or 8 bits:
+//   g' = grad * grad_scale * min(1, max_norm / (norm + 1e-6)),   m = b1 m + (1 - b1) g',   v = b2 v + (1 - b2) g'^2,
+//   w = w - lr wd w - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps).
+// The tensors are described in the launch's parameters (no table in device memory to keep), as many as fit one launch. A launch cuts them into
+// chunks of CHUNK entries and every CTA takes chunks in turn. Bound by HBM: 2 to 4 bytes of gradient, 4 to 10 of weights and 16 (or 4.1) of states an entry.
+// Norm: a launch in front adds the squares up, a partial sum a CTA; each CTA of the step adds the partial sums up itself, in their order, which
+// costs less than a third launch and gives all of them, and every run, the same number.
+// 8-bit states: e4m3 codes of m and of sqrt(v), with one fp32 scale (the largest magnitude / 448) for 128 entries. A float code keeps its 4
+// significant bits over a factor of 2^15 below the largest of its 128 (half a step: 2^-4 of the value), where an 8-bit linear code loses all entries
+// below 1/254 of it; sqrt(v) spans half as many powers of two as v. The update of a step uses m and v before their rounding. A root that is not
+// 0 is never rounded to 0, which would make its next step m / eps.
+#include "adamw.cuh"
+#include "ptx_sm100.cuh"
+
+#include <cuda_fp8.h>
+#include <math_constants.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+namespace dflash {
+namespace {
+
+constexpr int THREADS = 256, WARPS = THREADS / 32, PER_LANE = 4;
+constexpr int BLOCK = 32 * PER_LANE;                    // entries of a warp's turn, and of an 8-bit state that share a scale
+constexpr int UNROLL = 2;                               // blocks of a warp under way
+constexpr int CHUNK = WARPS * UNROLL * BLOCK;           // 2048
+constexpr int CTAS_PER_SM = 4, NORM_CTAS_PER_SM = 4;
+constexpr int MAX_TENSORS = 320;                        // descriptors of a launch: 28 KB of its 32 KB of parameters
+
+enum Weights { W_F32 = 0, W_BF16 = 1, W_MASTER = 2 };      // fp32, bf16, bf16 with a master copy in fp32
+
+struct Tensor {
+    void* param;
+    const void* grad;
+    float* master;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int64_t n;
+    float lr_wd, step_size;                             // lr * weight_decay; lr / (1 - b1^t), or both without lr and t where those live on the device
+    int32_t kind;                                       // Weights * 4 + (gradients bf16) * 2 + (states of 8 bits)
+    int32_t aligned;                                    // every pointer allows its widest access
+};
+struct Table {
+    Tensor t[MAX_TENSORS];
+    int64_t first[MAX_TENSORS + 1];                     // chunks in front of each tensor
+    int32_t n;
+};
+struct StepParams {
+    const double* partial;                              // [n_partial] sums of squared gradients, or nullptr: no norm
+    int32_t n_partial;
+    float* norm_out;
+    const float* lr;                                    // nullptr: in the table
+    const int32_t* step;
+    double ln_b1, ln_b2;
+    float b1, b2, one_b1, one_b2, eps, rsqrt_bc2, grad_scale, max_norm;
+    int32_t* status;
+};
+
+__device__ __forceinline__ int tensor_of(const Table& tab, int64_t chunk) {
+    int a = 0, b = tab.n;                               // first[a] <= chunk < first[b]
+    while (b - a > 1) {
+        const int mid = (a + b) / 2;
+        if (tab.first[mid] <= chunk) a = mid;
+        else b = mid;
+    }
+    return a;
+}
+
+// ---- 4 neighbouring entries: at `i` of a tensor of n, zeros behind its end -------------------------------------------
+__device__ __forceinline__ void load4(const float* p, int64_t i, int64_t n, bool vec, float (&f)[4]) {
+    if (vec && i + 4 <= n) {
+        const float4 v = __ldcs(reinterpret_cast<const float4*>(p + i));
+        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = i + e < n ? p[i + e] : 0.f;
+    }
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, int64_t i, int64_t n, bool vec, float (&f)[4]) {
+    if (vec && i + 4 <= n) {
+        const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p + i));
+        f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
+        f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = i + e < n ? __bfloat162float(p[i + e]) : 0.f;
+    }
+}
+__device__ __forceinline__ void store4(float* p, int64_t i, int64_t n, bool vec, const float (&f)[4]) {
+    if (vec && i + 4 <= n) {
+        __stcs(reinterpret_cast<float4*>(p + i), make_float4(f[0], f[1], f[2], f[3]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i + e < n) p[i + e] = f[e];
+    }
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, int64_t i, int64_t n, bool vec, const float (&f)[4]) {
+    if (vec && i + 4 <= n) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+        __stcs(reinterpret_cast<uint2*>(p + i), make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b)));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i + e < n) p[i + e] = __float2bfloat16_rn(f[e]);
+    }
+}
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t i, int64_t n, bool vec) {
+    if (vec && i + 4 <= n) return __ldcs(reinterpret_cast<const uint32_t*>(p + i));
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (i + e < n) w |= (uint32_t)p[i + e] << (8 * e);
+    return w;
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int64_t n, bool vec, uint32_t w) {
+    if (vec && i + 4 <= n) {
+        __stcs(reinterpret_cast<uint32_t*>(p + i), w);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i + e < n) p[i + e] = (uint8_t)(w >> (8 * e));
+    }
+}
+__device__ __forceinline__ void decode(uint32_t w, float scale, float (&f)[4]) {
+    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffffu), __NV_E4M3);
+    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+    const float2 x = __half22float2(__half2(a)), y = __half22float2(__half2(b));
+    f[0] = x.x * scale; f[1] = x.y * scale; f[2] = y.x * scale; f[3] = y.y * scale;
+}
+__device__ __forceinline__ uint32_t encode(const float (&f)[4]) {
+    const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
+    return a | b << 16;
+}
+// The scale of a block whose largest magnitude is `top` (all lanes), and what its entries are multiplied by. A block that holds NaN or an
+// infinity gets the scale NaN, one below 2^-117 the scale 0 (its own would no longer be a normal number).
+__device__ __forceinline__ float scale_of(float top, float& inv) {
+    const float scale = top < 6.0185e-36f ? 0.f : top / 448.f;
+    inv = scale > 0.f ? 1.f / scale : 0.f;
+    return top < CUDART_INF_F ? scale : CUDART_NAN_F;
+}
+__device__ __forceinline__ float block_top(const float (&f)[4]) {                     // NaN if any is NaN
+    float t = 0.f, bad = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        t = fmaxf(t, fabsf(f[e]));
+        bad = fmaf(f[e], 0.f, bad);                                                    // NaN for NaN and infinities
+    }
+    // magnitudes order like their bits, NaN above all
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, bad == 0.f ? __float_as_uint(t) : 0x7fffffffu));
+}
+
+template <int KIND>
+__device__ __forceinline__ void step_chunk(const Tensor& t, int64_t at, const StepParams& p, float gs, float lr_wd, float step_size, float rsqrt_bc2) {
+    constexpr int W = KIND >> 2;
+    constexpr bool G16 = KIND & 2, S8 = KIND & 1, MASTER = W == W_MASTER, P16 = W != W_F32;
+    using G = std::conditional_t<G16, __nv_bfloat16, float>;
+    using P = std::conditional_t<P16, __nv_bfloat16, float>;
+    const bool vec = t.aligned;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float g[UNROLL][4], w[UNROLL][4], m[UNROLL][4], v[UNROLL][4];
+    uint32_t cm[UNROLL], cv[UNROLL];
+    float sm[UNROLL], sv[UNROLL];
+    auto place = [&](int u) { return at + (int64_t)(u * WARPS + warp) * BLOCK + lane * PER_LANE; };
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const int64_t i = place(u), b = i / BLOCK;
+        load4(reinterpret_cast<const G*>(t.grad), i, t.n, vec, g[u]);
+        if constexpr (MASTER) load4(t.master, i, t.n, vec, w[u]);
+        else load4(reinterpret_cast<const P*>(t.param), i, t.n, vec, w[u]);
+        if constexpr (S8) {
+            cm[u] = load_codes(reinterpret_cast<const uint8_t*>(t.m), i, t.n, vec);
+            cv[u] = load_codes(reinterpret_cast<const uint8_t*>(t.v), i, t.n, vec);
+            sm[u] = b * BLOCK < t.n ? t.m_scale[b] : 0.f;
+            sv[u] = b * BLOCK < t.n ? t.v_scale[b] : 0.f;
+        } else {
+            load4(reinterpret_cast<const float*>(t.m), i, t.n, vec, m[u]);
+            load4(reinterpret_cast<const float*>(t.v), i, t.n, vec, v[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const int64_t i = place(u), b = i / BLOCK;
+        if constexpr (S8) {
+            decode(cm[u], sm[u], m[u]);
+            decode(cv[u], sv[u], v[u]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] *= v[u][e];
+        }
+        float root[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = g[u][e] * gs;
+            m[u][e] = fmaf(p.b1, m[u][e], p.one_b1 * x);
+            v[u][e] = fmaf(p.b2, v[u][e], p.one_b2 * x * x);
+            root[e] = sqrtf(v[u][e]);
+            const float d = step_size * m[u][e] / fmaf(root[e], rsqrt_bc2, p.eps);
+            w[u][e] = fmaf(-lr_wd, w[u][e], w[u][e]) - d;
+        }
+        if constexpr (MASTER) store4(t.master, i, t.n, vec, w[u]);
+        // (the weights that the model reads: their rounding to bf16 is not fed back where there is a master copy)
+        store4(reinterpret_cast<P*>(t.param), i, t.n, vec, w[u]);
+        if constexpr (S8) {
+            float inv;
+            const float s1 = scale_of(block_top(m[u]), inv);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m[u][e] *= inv;
+            store_codes(reinterpret_cast<uint8_t*>(t.m), i, t.n, vec, encode(m[u]));
+            const float s2 = scale_of(block_top(root), inv);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) root[e] = root[e] > 0.f && inv > 0.f ? fmaxf(root[e] * inv, 0.001953125f) : 0.f;      // 2^-9: the smallest code
+            store_codes(reinterpret_cast<uint8_t*>(t.v), i, t.n, vec, encode(root));
+            if (lane == 0 && b * BLOCK < t.n) {
+                t.m_scale[b] = s1;
+                t.v_scale[b] = s2;
+            }
+        } else {
+            store4(reinterpret_cast<float*>(t.m), i, t.n, vec, m[u]);
+            store4(reinterpret_cast<float*>(t.v), i, t.n, vec, v[u]);
+        }
+    }
+}
+
+// sum over the CTA in a fixed order; every thread gets it
+__device__ __forceinline__ double cta_sum(double x, double* sh) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
+    __syncthreads();
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < WARPS; ++k) s += sh[k];
+    return s;
+}
+
+__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) adamw_kernel(const __grid_constant__ Table tab, const StepParams p) {
+    __shared__ double sh[WARPS];
+    __shared__ float s_bc[2];
+    ptx::pdl_trigger();
+    ptx::pdl_wait();
+    float gs = p.grad_scale;
+    if (p.partial) {
+        double x = 0.0;
+        for (int i = threadIdx.x; i < p.n_partial; i += THREADS) x += p.partial[i];
+        const float norm = (float)(sqrt(cta_sum(x, sh)) * fabs((double)p.grad_scale));
+        const bool fine = norm < CUDART_INF_F;
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            if (p.norm_out) *p.norm_out = norm;
+            if (!fine && p.status) atomicOr(p.status, DFLASH_DEV_NOT_FINITE);
+        }
+        if (!fine) return;                              // every CTA alike: the step is left out
+        if (p.max_norm > 0.f) gs *= fminf(1.f, p.max_norm / (norm + 1e-6f));
+    }
+    float lr = 1.f, rsqrt_bc2 = p.rsqrt_bc2;
+    if (p.lr || p.step) {                               // what of the bias correction and the rate lives on the device
+        if (threadIdx.x == 0) {
+            const double t = p.step ? (double)max(*p.step, 1) : 1.0;
+            s_bc[0] = (p.lr ? *p.lr : 1.f) * (p.step ? (float)(-1.0 / expm1(t * p.ln_b1)) : 1.f);
+            s_bc[1] = p.step ? (float)rsqrt(-expm1(t * p.ln_b2)) : p.rsqrt_bc2;
+        }
+        __syncthreads();
+        lr = s_bc[0];
+        rsqrt_bc2 = s_bc[1];
+    }
+    const float wd_lr = p.lr ? *p.lr : 1.f;
+    int64_t chunks = tab.first[tab.n];
+    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+        const int k = tensor_of(tab, c);
+        const Tensor& t = tab.t[k];
+        const int64_t at = (c - tab.first[k]) * CHUNK;
+        const float lr_wd = t.lr_wd * wd_lr, step_size = t.step_size * lr;
+        switch (t.kind) {
+#define DFLASH_ADAMW_CASE(K) case K: step_chunk<K>(t, at, p, gs, lr_wd, step_size, rsqrt_bc2); break;
+            DFLASH_ADAMW_CASE(0) DFLASH_ADAMW_CASE(1) DFLASH_ADAMW_CASE(2) DFLASH_ADAMW_CASE(3)
+            DFLASH_ADAMW_CASE(4) DFLASH_ADAMW_CASE(5) DFLASH_ADAMW_CASE(6) DFLASH_ADAMW_CASE(7)
+            DFLASH_ADAMW_CASE(8) DFLASH_ADAMW_CASE(9) DFLASH_ADAMW_CASE(10) DFLASH_ADAMW_CASE(11)
+#undef DFLASH_ADAMW_CASE
+        }
+    }
+}
+
+// partial[blockIdx.x] = sum of the squares of the gradients in this CTA's chunks
+__global__ void __launch_bounds__(THREADS, NORM_CTAS_PER_SM) adamw_norm_kernel(const __grid_constant__ Table tab, double* __restrict__ partial) {
+    __shared__ double sh[WARPS];
+    ptx::pdl_trigger();
+    ptx::pdl_wait();
+    double sum = 0.0;
+    const int64_t chunks = tab.first[tab.n];
+    constexpr int TURN = THREADS * PER_LANE;
+    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+        const int k = tensor_of(tab, c);
+        const Tensor& t = tab.t[k];
+        const int64_t at = (c - tab.first[k]) * CHUNK + threadIdx.x * PER_LANE;
+        float s = 0.f;
+        float g[CHUNK / TURN][4];
+#pragma unroll
+        for (int u = 0; u < CHUNK / TURN; ++u) {
+            if (t.kind & 2) load4(reinterpret_cast<const __nv_bfloat16*>(t.grad), at + u * TURN, t.n, t.aligned, g[u]);
+            else load4(reinterpret_cast<const float*>(t.grad), at + u * TURN, t.n, t.aligned, g[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < CHUNK / TURN; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = fmaf(g[u][e], g[u][e], s);
+        sum += (double)s;
+    }
+    sum = cta_sum(sum, sh);
+    if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+}
+
+bool on(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+}  // namespace
+
+int64_t adamw_workspace_bytes(int sm_count, int n_tensors) {
+    const int64_t launches = std::max(1, (n_tensors + MAX_TENSORS - 1) / MAX_TENSORS);
+    return align_up(launches * sm_count * NORM_CTAS_PER_SM * (int64_t)sizeof(double), 256);
+}
+
+int launch_adamw(const Launch& L, const dflash_adamw_args& a) {
+    const int launches = std::max(1, (a.n_tensors + MAX_TENSORS - 1) / MAX_TENSORS);
+    const bool norm = a.max_grad_norm > 0.0 || a.grad_norm;
+    StepParams p{};
+    p.norm_out = a.grad_norm; p.lr = a.lr_dev; p.step = a.step_dev;
+    p.ln_b1 = a.beta1 > 0.0 ? std::log(a.beta1) : -INFINITY;
+    p.ln_b2 = a.beta2 > 0.0 ? std::log(a.beta2) : -INFINITY;
+    p.b1 = (float)a.beta1; p.b2 = (float)a.beta2; p.one_b1 = (float)(1.0 - a.beta1); p.one_b2 = (float)(1.0 - a.beta2);
+    p.eps = (float)a.eps; p.grad_scale = (float)a.grad_scale; p.max_norm = (float)a.max_grad_norm; p.status = L.status;
+    const double bc1 = a.step_dev ? 1.0 : -std::expm1(a.step * p.ln_b1), bc2 = a.step_dev ? 1.0 : -std::expm1(a.step * p.ln_b2);
+    p.rsqrt_bc2 = (float)(1.0 / std::sqrt(bc2));
+    const double lr = a.lr_dev ? 1.0 : a.lr;
+    const auto table = [&](int l, Table& tab) {
+        const int from = l * MAX_TENSORS, n = std::min(MAX_TENSORS, a.n_tensors - from);
+        int64_t chunks = 0;
+        for (int i = 0; i < n; ++i) {
+            const dflash_adamw_tensor& s = a.tensors[from + i];
+            Tensor& t = tab.t[i];
+            const bool p16 = s.param_dtype == DFLASH_BF16, g16 = s.grad_dtype == DFLASH_BF16, s8 = s.state_bits == 8;
+            t.param = s.param; t.grad = s.grad; t.master = s.master; t.m = s.exp_avg; t.v = s.exp_avg_sq;
+            t.m_scale = s.exp_avg_scale; t.v_scale = s.exp_avg_sq_scale; t.n = s.n;
+            t.lr_wd = (float)(lr * s.weight_decay * s.lr_scale);
+            t.step_size = (float)(lr * s.lr_scale / bc1);
+            t.kind = (s.master ? W_MASTER : p16 ? W_BF16 : W_F32) * 4 + g16 * 2 + s8;
+            t.aligned = on(s.param, p16 ? 8 : 16) && on(s.grad, g16 ? 8 : 16) && on(s.master, 16) && on(s.exp_avg, s8 ? 4 : 16) && on(s.exp_avg_sq, s8 ? 4 : 16);
+            tab.first[i] = chunks;
+            chunks += (s.n + CHUNK - 1) / CHUNK;
+        }
+        tab.first[n] = chunks;
+        tab.n = n;
+        return chunks;
+    };
+    const auto grid = [&](int64_t chunks, int per_sm) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(chunks, (int64_t)L.h->sm_count * per_sm)); };
+    Table tab;
+    if (norm) {
+        double* partial = reinterpret_cast<double*>(a.workspace);
+        p.partial = partial;
+        for (int l = 0; l < launches; ++l) {
+            const unsigned g = grid(table(l, tab), NORM_CTAS_PER_SM);
+            if (launch_pdl(adamw_norm_kernel, dim3(g), dim3(THREADS), 0, L.st, tab, partial + p.n_partial) != cudaSuccess) return DFLASH_ERR_CUDA;
+            p.n_partial += (int)g;
+            g_launches += 1;
+        }
+    }
+    for (int l = 0; l < launches; ++l) {
+        const int64_t chunks = table(l, tab);
+        if (launch_pdl(adamw_kernel, dim3(grid(chunks, CTAS_PER_SM)), dim3(THREADS), 0, L.st, tab, p) != cudaSuccess) return DFLASH_ERR_CUDA;
+        p.norm_out = nullptr;
+        g_launches += 1;
+    }
+    return DFLASH_OK;
+}
+
+}  // namespace dflash

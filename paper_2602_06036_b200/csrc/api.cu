@@ -1,11 +1,14 @@
 // C ABI of the library: argument validation, workspace carving and the launch sequence of each call.
 #include "dflash_internal.h"
+#include "adamw.cuh"
 #include "gemm_tc.cuh"
 #include "attn_tc.cuh"
+#include "logprobs.cuh"
 #include "pages.cuh"
 #include "prefix_attn.cuh"
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <new>
 
@@ -796,6 +799,76 @@ int32_t dflash_block_attention_bwd(dflash_handle* h, const dflash_attn_bwd_args*
     Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
     // ws.tmp holds rows * d_model floats: room for one float per (row, q head)
     RUN(FAM_ATTENTION, launch_attention_bwd(L, *a, ws.tmp));
+    return DFLASH_OK;
+}
+
+// ---- log probabilities ----
+static bool is_dtype(int32_t d) { return d == DFLASH_F32 || d == DFLASH_BF16; }
+static bool on_elements(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % elem_size(dtype) == 0; }
+constexpr int32_t MAX_VOCAB = 1 << 30, MAX_LOGIT_ROWS = 1 << 28;      // the kernels count entries of a row, and their CTAs, in 32 bits
+
+int32_t dflash_token_logprobs(dflash_handle* h, const dflash_token_logprobs_args* a, void* stream) {
+    if (!h || !a) return DFLASH_ERR_INVALID_ARG;
+    if (a->n_rows < 0 || a->vocab < 1 || a->n_tokens < 0 || a->n_top < 0 || !is_dtype(a->logits_dtype)) return DFLASH_ERR_INVALID_ARG;
+    if (!(a->temperature > 0.f) || !std::isfinite(a->temperature) || !std::isfinite(1.f / a->temperature)) return DFLASH_ERR_INVALID_ARG;
+    if (a->n_tokens > LP_MAX_TOKENS || a->n_top > LP_MAX_TOP || a->vocab > MAX_VOCAB || a->n_rows > MAX_LOGIT_ROWS) return DFLASH_ERR_UNSUPPORTED;
+    if (a->n_rows == 0) return DFLASH_OK;
+    if (!a->logits || !on_elements(a->logits, a->logits_dtype) || (a->row_stride && a->row_stride < a->vocab)) return DFLASH_ERR_INVALID_ARG;
+    if ((a->n_tokens > 0 && (!a->tokens || !a->logprob)) || (a->n_top > 0 && (!a->top_ids || !a->top_logprob))) return DFLASH_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(a->stats) & 7) return DFLASH_ERR_INVALID_ARG;
+    Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
+    RUN(FAM_MISC, launch_token_logprobs(L, *a));
+    return DFLASH_OK;
+}
+
+int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_bwd_args* a, void* stream) {
+    if (!h || !a) return DFLASH_ERR_INVALID_ARG;
+    if (a->n_rows < 0 || a->vocab < 1 || a->n_tokens < 0 || !is_dtype(a->logits_dtype) || !is_dtype(a->dlogits_dtype)) return DFLASH_ERR_INVALID_ARG;
+    if (!(a->temperature > 0.f) || !std::isfinite(a->temperature) || !std::isfinite(1.f / a->temperature)) return DFLASH_ERR_INVALID_ARG;
+    if (a->n_tokens > LP_MAX_TOKENS || a->vocab > MAX_VOCAB || a->n_rows > MAX_LOGIT_ROWS) return DFLASH_ERR_UNSUPPORTED;
+    if ((int64_t)a->n_rows * ((a->vocab + 8191) / 8192) > INT32_MAX) return DFLASH_ERR_UNSUPPORTED;
+    if (a->n_rows == 0) return DFLASH_OK;
+    const int64_t ld = a->row_stride ? a->row_stride : a->vocab, d_ld = a->dlogits_row_stride ? a->dlogits_row_stride : a->vocab;
+    if (!a->logits || !a->dlogits || !a->stats || (a->n_tokens > 0 && (!a->tokens || !a->d_logprob)) || (a->d_entropy && !a->entropy) || ld < a->vocab ||
+        d_ld < a->vocab || !on_elements(a->logits, a->logits_dtype) || !on_elements(a->dlogits, a->dlogits_dtype))
+        return DFLASH_ERR_INVALID_ARG;
+    if (a->logits == a->dlogits && (a->logits_dtype != a->dlogits_dtype || ld != d_ld)) return DFLASH_ERR_INVALID_ARG;
+    Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
+    RUN(FAM_MISC, launch_token_logprobs_bwd(L, *a));
+    return DFLASH_OK;
+}
+
+// ---- optimiser ----
+int64_t dflash_adamw_workspace_bytes(const dflash_handle* h, int32_t n_tensors) {
+    if (!h || n_tensors < 0) return DFLASH_ERR_INVALID_ARG;
+    return adamw_workspace_bytes(h->sm_count, n_tensors);
+}
+
+int32_t dflash_adamw_step(dflash_handle* h, const dflash_adamw_args* a, void* stream) {
+    if (!h || !a || a->n_tensors < 0 || (a->n_tensors > 0 && !a->tensors)) return DFLASH_ERR_INVALID_ARG;
+    if (!(a->beta1 >= 0.0 && a->beta1 < 1.0 && a->beta2 >= 0.0 && a->beta2 < 1.0) || !((float)a->eps > 0.f) || !std::isfinite((float)a->eps) || !((float)a->grad_scale > 0.f) ||
+        !std::isfinite((float)a->grad_scale) || std::isnan(a->max_grad_norm))
+        return DFLASH_ERR_INVALID_ARG;
+    if ((!a->step_dev && a->step < 1) || (!a->lr_dev && !std::isfinite((float)a->lr))) return DFLASH_ERR_INVALID_ARG;
+    for (int i = 0; i < a->n_tensors; ++i) {
+        const dflash_adamw_tensor& t = a->tensors[i];
+        if (t.n < 0 || !is_dtype(t.param_dtype) || !is_dtype(t.grad_dtype) || (t.state_bits != 32 && t.state_bits != 8) || !std::isfinite(t.weight_decay) ||
+            !std::isfinite(t.lr_scale) || (t.master && t.param_dtype == DFLASH_F32))
+            return DFLASH_ERR_INVALID_ARG;
+        if (t.n == 0) continue;
+        const int state = t.state_bits == 32 ? 4 : 1;
+        if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (state == 1 && (!t.exp_avg_scale || !t.exp_avg_sq_scale))) return DFLASH_ERR_INVALID_ARG;
+        if (!on_elements(t.param, t.param_dtype) || !on_elements(t.grad, t.grad_dtype) || !on_elements(t.master, DFLASH_F32) ||
+            ((reinterpret_cast<uintptr_t>(t.exp_avg) | reinterpret_cast<uintptr_t>(t.exp_avg_sq)) & (state - 1)) || !on_elements(t.exp_avg_scale, DFLASH_F32) ||
+            !on_elements(t.exp_avg_sq_scale, DFLASH_F32))
+            return DFLASH_ERR_INVALID_ARG;
+    }
+    if ((a->max_grad_norm > 0.0 || a->grad_norm) &&
+        (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 255) || adamw_workspace_bytes(h->sm_count, a->n_tensors) > a->workspace_bytes))
+        return DFLASH_ERR_WORKSPACE;
+    if (a->n_tensors == 0 && !a->grad_norm) return DFLASH_OK;
+    Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
+    RUN(FAM_MISC, launch_adamw(L, *a));
     return DFLASH_OK;
 }
 
