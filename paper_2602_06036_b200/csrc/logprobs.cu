@@ -13,41 +13,64 @@
 namespace dflash {
 namespace {
 
-constexpr int THREADS = 512, UNROLL = 4, CTAS_PER_SM = 2;      // 16-byte vectors per thread in flight; 32 KB a CTA
+constexpr int THREADS = 256, UNROLL = 4, CTAS_PER_SM = 4;      // a tile: UNROLL 16-byte vectors a thread, 16 KB a CTA
+constexpr int STAGES = 2;                                      // tiles under way
 constexpr int MAX_CLUSTER = 8;
-constexpr int RANK_MAX = 256;                                  // candidates ranked by comparing each with each
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float FAR = -1.0e4f;                                 // below this many powers of two a term is 0, and its exponent only has to stay finite
 
 // ---- a row as 16-byte vectors -----------------------------------------------------------------------------------
-// Vector j holds entries j * VE - shift + (0 .. VE-1): the vectors lie on 16-byte borders whatever the row's start. The first and
-// the last one may reach beyond the row: what they hold outside of it is not read and stands for -inf.
+// Vector j holds entries j * VE - shift + (0 .. VE-1): the vectors lie on 16-byte borders whatever the row's start. The first and the last one may
+// reach beyond the row; what they hold outside of it stands for -inf.
 template <typename T>
 struct Row {
     static constexpr int VE = 16 / (int)sizeof(T);
-    const T* z;
+    const char* base;                                          // vector 0
     int vocab, shift, n_vec;
-    __device__ __forceinline__ Row(const T* row, int v) : z(row), vocab(v) {
-        shift = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    __device__ __forceinline__ Row() {}
+    __device__ __forceinline__ Row(const T* row, int v) : vocab(v) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(row);
+        base = reinterpret_cast<const char*>(at & ~(uintptr_t)15);
+        shift = (int)((at & 15) / sizeof(T));
         n_vec = (v + shift + VE - 1) / VE;
     }
     __device__ __forceinline__ int first(int j) const { return j * VE - shift; }
-    __device__ __forceinline__ uint4 load(int j) const {
-        const int i0 = first(j);
-        if (i0 >= 0 && i0 + VE <= vocab) return __ldcs(reinterpret_cast<const uint4*>(z + i0));
-        uint32_t w[4];
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = i0 + e >= 0 && i0 + e < vocab ? __float_as_uint(z[i0 + e]) : 0xff800000u;
-        } else {
-            const uint16_t* h = reinterpret_cast<const uint16_t*>(z);
-            auto one = [&](int i) { return (uint32_t)(i >= 0 && i < vocab ? h[i] : (uint16_t)0xff80u); };
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = one(i0 + 2 * e) | one(i0 + 2 * e + 1) << 16;
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    __device__ __forceinline__ const char* address(int j) const { return base + (int64_t)j * 16; }
+    __device__ __forceinline__ uint4 load(int j) const;        // with -inf outside of the row
+    __device__ __forceinline__ bool whole(int j) const { return j * VE >= shift && (j + 1) * VE - shift <= vocab; }
 };
+template <typename T>
+__device__ __forceinline__ uint4 no_entries() {
+    const uint32_t w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    return make_uint4(w, w, w, w);
+}
+// A vector at address `at` whose entries are first, first + 1, ... of a row, with -inf outside of the row. `v`: as it lies in memory, or, where it reaches beyond
+// the buffer, nothing: its entries are read one by one.
+template <typename T>
+__device__ __noinline__ uint4 edge_of(const char* at, int first, int vocab, uint4 v, bool in_memory) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < Row<T>::VE; ++e) {
+        const int i = first + e;
+        const bool in = i >= 0 && i < vocab;
+        if constexpr (sizeof(T) == 4) {
+            if (!in) w[e] = 0xff800000u;
+            else if (!in_memory) w[e] = reinterpret_cast<const uint32_t*>(at)[e];
+        } else {
+            uint32_t h = (w[e / 2] >> (16 * (e & 1))) & 0xffffu;
+            if (!in) h = 0xff80u;
+            else if (!in_memory) h = reinterpret_cast<const uint16_t*>(at)[e];
+            w[e / 2] = e & 1 ? (w[e / 2] & 0xffffu) | h << 16 : (w[e / 2] & 0xffff0000u) | h;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 Row<T>::load(int j) const {
+    if (whole(j)) return *reinterpret_cast<const uint4*>(address(j));
+    return edge_of<T>(address(j), first(j), vocab, no_entries<T>(), false);
+}
 
 // largest entry of a vector; NaN has no say
 __device__ __forceinline__ float vec_max(const uint4& v, float) {
@@ -58,6 +81,15 @@ __device__ __forceinline__ float vec_max(const uint4& v, __nv_bfloat16) {
     const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
     return fmaxf(__low2float(m), __high2float(m));
 }
+
+// ---- copies to shared memory under way --------------------------------------------------------------------------------
+template <int OFFSET = 0>
+__device__ __forceinline__ void copy_async16(uint32_t smem, const void* gmem) {
+    asm volatile("cp.async.cg.shared.global [%0+%2], [%1+%2], 16;" ::"r"(smem), "l"(gmem), "n"(OFFSET) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }      // all but the latest N groups have landed
 
 // ---- statistics ----------------------------------------------------------------------------------------------------
 // m: maximum, s: sum of 2^((z - m) c), w: sum of 2^((z - m) c) (z - m) c
@@ -75,16 +107,123 @@ __device__ __forceinline__ Stat merged(const Stat& a, const Stat& b, float c) {
     const Stat x = raised(a, m, c), y = raised(b, m, c);
     return Stat{m, x.s + y.s, x.w + y.w};
 }
-// entries f[] into the sums; base = m, or 0 as long as m is -inf (every term is 0 then)
-template <int N>
-__device__ __forceinline__ void add_terms(Stat& t, const float (&f)[N], float base, float c) {
+// of a warp's lanes (of each LANES neighbouring ones): the maximum first, then one rescaling
+template <int LANES>
+__device__ __forceinline__ Stat lanes_merged(const Stat& a, float c) {
+    float m = a.m;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const float y = (f[e] - base) * c, x = fast_exp2(y);
-        t.s += x;
-        t.w = fmaf(x, fmaxf(y, FAR), t.w);
+    for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    Stat t = raised(a, m, c);
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+        t.s += __shfl_xor_sync(0xffffffffu, t.s, o);
+        t.w += __shfl_xor_sync(0xffffffffu, t.w, o);
     }
+    return t;
 }
+// two fp32 operations by one instruction
+__device__ __forceinline__ unsigned long long pair(float a, float b) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 halves(unsigned long long p) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// A thread's running sums of 2^y and 2^y y, those of even and odd entries apart, y = (z - m) c + rest: m is the largest entry of some tile, and it is not
+// raised before an entry lies 2^60 terms above it, so that tiles after the first hardly ever do. y = z c - r by one fused operation, with r = m c rounded and rest
+// = m c - r, which is exact; the size of m does not touch the terms. Entries below LOW, -inf among them, count as LOW: their terms are 0, and
+// y has to be finite. Where any of that does not hold (a maximum near LOW or that large that `rest` is no small number, a temperature of an extreme size), `plain`
+// terms take the differences one by one.
+constexpr float LOW = -1.2676506002282294e30f;                 // -2^100
+__device__ __forceinline__ uint4 not_below_low(const uint4& v, float) {
+    const auto one = [](uint32_t z) {
+        float r;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(z)), "f"(LOW));
+        return __float_as_uint(r);
+    };
+    return make_uint4(one(v.x), one(v.y), one(v.z), one(v.w));
+}
+__device__ __forceinline__ uint4 not_below_low(const uint4& v, __nv_bfloat16) {
+    const auto two = [](uint32_t z) {
+        uint32_t r;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(z), "r"(0xf180f180u));
+        return r;
+    };
+    return make_uint4(two(v.x), two(v.y), two(v.z), two(v.w));
+}
+struct Running {
+    float m, limit, rest, neg_r;                               // limit: from which on m is raised
+    bool plain;
+    unsigned long long s, w;
+    __device__ __forceinline__ void reset() {
+        m = limit = -CUDART_INF_F;
+        rest = neg_r = 0.f;
+        plain = true;
+        s = w = 0;
+    }
+    __device__ __forceinline__ void raise(float to, float c) {
+        const float old = m, old_rest = rest, r = to * c;
+        m = to;
+        limit = to + 60.f / c;
+        plain = !(fabsf(r) < 1048576.f && c < 1.0e8f && c > 1.0e-20f);
+        neg_r = -r;
+        rest = plain ? 0.f : fmaf(to, c, -r);
+        const float d = old == -CUDART_INF_F ? FAR : fmaxf((old - to) * c, FAR) - old_rest + rest, f = fast_exp2(d);
+        const float2 a = halves(s), b = halves(w);
+        s = pair(a.x * f, a.y * f);
+        w = pair((b.x + a.x * d) * f, (b.y + a.y * d) * f);
+    }
+    template <typename T>
+    __device__ __forceinline__ void add(const uint4& v, float c) {
+        constexpr int N = 16 / (int)sizeof(T);
+        float f[N];
+        unpack16(not_below_low(v, T()), f, T());
+        const unsigned long long cc = pair(c, c), rr = pair(neg_r, neg_r);
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+            const unsigned long long y = fma2(pair(f[e], f[e + 1]), cc, rr);
+            const float2 yy = halves(y);
+            const unsigned long long x = pair(fast_exp2(yy.x), fast_exp2(yy.y));
+            s = add2(s, x);
+            w = fma2(x, y, w);
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void add_plain(const uint4& v, float c) {
+        constexpr int N = 16 / (int)sizeof(T);
+        float f[N];
+        unpack16(v, f, T());
+        float2 a = halves(s), b = halves(w);
+        const float base = m == -CUDART_INF_F ? 0.f : m;       // every term is 0 then
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float y = (f[e] - base) * c, x = fast_exp2(y);
+            a.x += x;
+            b.x = fmaf(x, fmaxf(y, FAR), b.x);
+        }
+        s = pair(a.x, a.y);
+        w = pair(b.x, b.y);
+    }
+    // with `top`, the largest entry so far, in the place of m
+    __device__ __forceinline__ Stat total(float top, float c) const {
+        const float2 a = halves(s), b = halves(w);
+        const float f = fast_exp2(-rest), sum = a.x + a.y;
+        return raised(Stat{m, sum * f, (b.x + b.y - sum * rest) * f}, top, c);
+    }
+};
 
 // ---- candidates for the alternatives ---------------------------------------------------------------------------------
 // An entry is ordered by (value, lower index first) as one 64-bit key, so that no two are equal and the result does not depend on
@@ -97,129 +236,194 @@ __device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(
 __device__ __forceinline__ unsigned long long key_of(float z, int i) { return (unsigned long long)ordered(z) << 32 | (0xffffffffu - (uint32_t)i); }
 __device__ __forceinline__ float value_of(unsigned long long key) { return unordered((uint32_t)(key >> 32)); }
 __device__ __forceinline__ int index_of(unsigned long long key) { return (int)(0xffffffffu - (uint32_t)key); }
-constexpr unsigned long long NO_KEY = (unsigned long long)0x007fffffu << 32 | 0xffffffffu;      // not below any key of -inf, below all others
+constexpr uint32_t ORDERED_NONE = 0x007fffffu;                 // ordered(-inf)
+constexpr unsigned long long NO_KEY = (unsigned long long)ORDERED_NONE << 32 | 0xffffffffu;      // not below any key of -inf, below all others
 
-// most threads of a tile that may hold candidates; their entries fit behind a full list
-__host__ __device__ __forceinline__ int most_threads(int n_top) { return n_top + n_top / 4 + 8; }
-template <typename T>
-__host__ __device__ __forceinline__ int list_capacity(int n_top) {
-    const int a = n_top + most_threads(n_top) * UNROLL * Row<T>::VE;
-    return a > RANK_MAX ? a : RANK_MAX;
-}
+constexpr int CELLS = 8;                                       // of a thread: its part of a row in as many runs of tiles
+constexpr int CAPACITY = 512;                                  // of the list
+__host__ __device__ __forceinline__ int most_of(int n_top) { return n_top + n_top / 4 + 8; }      // entries that a bound on the n_top-th largest may leave
+static_assert(LP_MAX_TOP + LP_MAX_TOP / 4 + 8 + THREADS <= CAPACITY && LP_MAX_TOP + LP_MAX_TOP / 4 + 8 <= THREADS, "a turn's entries fit behind a list that has been cut");
 
-// The list of a CTA: keys above `floor`, of which at least n_top have been seen as soon as floor > NO_KEY. Later tiles hold larger indices, so
-// that an entry equal in value to the floor's loses to those: they are compared by value alone.
+// The search for a stretch's n_top largest entries, after the pass over it that has left the largest entry of every thread and of each of its cells. At least
+// n_top threads' largest entries bound the n_top-th largest of the stretch from below, and little else is above a bound that few of them are (`bound`).
+// What is, lies in a few cells, which are read again (from L2, mostly) by all threads together. The pass itself so needs no barrier and looks at no
+// entry twice; taking candidates out as they come by cost a barrier a tile and more than the reading of the row.
 struct Candidates {
-    unsigned long long* list;      // [capacity]
-    unsigned long long* few;       // [RANK_MAX]
-    int* count;                    // entries of list
-    int n_top, capacity;
-    unsigned long long floor;
+    unsigned long long* list;      // [CAPACITY] keys
+    unsigned long long* few;       // [most]
+    float* cells;                  // [CELLS][THREADS]
+    int* found;                    // [most * CELLS] cells to be read again: cell * THREADS + thread
+    int* count;                    // entries of list, of found
+    uint32_t* ends;                // [2][THREADS / 32]
+    int n_top, most;
+    unsigned long long floor;      // keys that are not above it are none of the n_top largest
     float floor_z;
 
     __device__ __forceinline__ void raise(unsigned long long to) {
         floor = to;
-        floor_z = value_of(to);
+        // (a bound between the two zeros, which are equal as values, stands below both)
+        floor_z = (uint32_t)(to >> 32) == 0x7fffffffu ? -1.4e-45f : value_of(to);
     }
-    // all threads: the list becomes its n_top largest keys in falling order
-    __device__ void rank() {
-        __syncthreads();
-        int n = *count;
-        const unsigned long long* from = list;
-        if (n > RANK_MAX) {        // a lower bound that leaves few enough, found by halving
-            unsigned long long lo = 0, hi = ~0ull;
-            while (true) {
-                const unsigned long long mid = lo + (hi - lo) / 2;
-                int above = 0;
-                for (int i = 0; i < n; i += THREADS) above += __syncthreads_count(i + (int)threadIdx.x < n && list[i + threadIdx.x] > mid);
-                if (above < n_top) { hi = mid; continue; }
+    // all threads, between barriers: the list loses entries that are not among its n_top largest until at most `most` are left
+    __device__ void cut() {
+        const int n = *count;
+        if (n <= most) return;
+        const unsigned long long mine = (int)threadIdx.x < n ? list[threadIdx.x] : 0;
+        const auto above = [&](unsigned long long k) {
+            int a = __syncthreads_count(mine > k);
+            for (int i = THREADS; i < n; i += THREADS) a += __syncthreads_count(i + (int)threadIdx.x < n && list[i + threadIdx.x] > k);
+            return a;
+        };
+        unsigned long long lo = floor, hi = ~0ull;             // (not all entries above the floor need be in the list)
+        for (int left = above(lo); left > most;) {             // more than `most` above lo, fewer than n_top above hi
+            const unsigned long long mid = lo + (hi - lo) / 2;
+            const int a = above(mid);
+            if (a < n_top) {
+                hi = mid;
+            } else {
                 lo = mid;
-                if (above <= RANK_MAX) break;
+                left = a;
             }
-            if (threadIdx.x == 0) *count = 0;
-            __syncthreads();
-            for (int i = threadIdx.x; i < n; i += THREADS)
-                if (list[i] > lo) few[atomicAdd(count, 1)] = list[i];
-            __syncthreads();
-            n = *count;
-            from = few;
         }
-        unsigned long long mine = 0;
-        int above = 0;
-        if ((int)threadIdx.x < n) {
-            mine = from[threadIdx.x];
-            for (int i = 0; i < n; ++i) above += from[i] > mine;
-        }
+        if (threadIdx.x == 0) *count = 0;
         __syncthreads();
-        if ((int)threadIdx.x < n && above < n_top) list[above] = mine;
-        if (threadIdx.x == 0) *count = min(n, n_top);
+        if (mine > lo) few[atomicAdd(count, 1)] = mine;
+        for (int i = THREADS + threadIdx.x; i < n; i += THREADS)
+            if (list[i] > lo) few[atomicAdd(count, 1)] = list[i];
         __syncthreads();
-        if (n >= n_top) raise(list[n_top - 1]);
-        __syncthreads();           // (the floor has been read before the next append)
+        if ((int)threadIdx.x < *count) list[threadIdx.x] = few[threadIdx.x];
+        raise(lo);
+        __syncthreads();
     }
-    // all threads, once a tile: `raw` are the thread's vectors tid + u * THREADS of the tile at vector j0, top its largest entry
+    // first vector of a cell; its vectors are THREADS apart
+    __device__ __forceinline__ static int first_of(int lo, int per_cell, int cell, int thread) { return lo + cell * per_cell * THREADS + thread; }
+    // all threads: a floor that at least n_top of the threads' largest entries lie above, and at most `most`. Found by halving: first between values, and where too many
+    // are equal, between keys. Returns whether this thread's entries may lie above it.
     template <typename T>
-    __device__ void take(const Row<T>& row, const uint4 (&raw)[UNROLL], int j0, float top) {
-        constexpr int VE = Row<T>::VE;
-        int hits = __syncthreads_count(top > floor_z);
-        if (hits == 0) return;
-        bool strict = true;        // by value alone
-        if (hits > most_threads(n_top)) {
-            // The n_top-th largest of the threads' maxima bounds the n_top-th largest entry from below, and few entries lie above it:
-            // halve until between n_top and most_threads(n_top) maxima do.
-            unsigned long long best = 0;
-            if (top > floor_z) {
-#pragma unroll
-                for (int u = UNROLL - 1; u >= 0; --u) {
-                    float f[VE];
-                    unpack16(raw[u], f, T());
-#pragma unroll
-                    for (int e = VE - 1; e >= 0; --e)
-                        if (f[e] == top) best = key_of(top, row.first(j0 + u * THREADS + (int)threadIdx.x) + e);
-                }
-            }
-            unsigned long long lo = floor, hi = ~0ull;
-            while (true) {
-                const unsigned long long mid = lo + (hi - lo) / 2;
-                hits = __syncthreads_count(best > mid);
-                if (hits < n_top) { hi = mid; continue; }
-                lo = mid;
-                if (hits <= most_threads(n_top)) break;
-            }
-            raise(lo);
-            strict = false;
-        }
-        if (*count + hits * UNROLL * VE > capacity) {      // (no thread appends before all have read the count: rank() and the barrier below)
-            const unsigned long long f = floor;
-            rank();
-            if (f >= floor) raise(f);                       // the tile's own bound, where that is the higher one
-            else strict = true;                             // the list's n_top-th, an entry of an earlier tile
+    __device__ bool bound(const Row<T>& row, int lo_j, int hi_j, int per_cell, float top) {
+        raise(NO_KEY);
+        const bool hit = top > -CUDART_INF_F;
+        int above = __syncthreads_count(hit);
+        if (above <= most) return hit;
+        const uint32_t mine = hit ? ordered(top) : 0;
+        const int warp = threadIdx.x >> 5;
+        const uint32_t top_of_warp = __reduce_max_sync(0xffffffffu, mine), least = __reduce_min_sync(0xffffffffu, mine);
+        if ((threadIdx.x & 31) == 0) {
+            ends[warp] = top_of_warp;
+            ends[THREADS / 32 + warp] = least;
         }
         __syncthreads();
-        if (top >= floor_z) {
+        const int w = threadIdx.x & (THREADS / 32 - 1);
+        uint32_t hi = __reduce_max_sync(0xffffffffu, ends[w]), lo = __reduce_min_sync(0xffffffffu, ends[THREADS / 32 + w]);
+        lo = max(lo ? lo - 1 : 0u, ORDERED_NONE);              // more than `most` above lo, none above hi
+        while (hi - lo > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            above = __syncthreads_count(mine > mid);
+            if (above < n_top) { hi = mid; continue; }
+            lo = mid;
+            if (above <= most) {
+                raise((unsigned long long)lo << 32 | 0xffffffffu);
+                return mine > lo;
+            }
+        }
+        // ties: fewer than n_top lie above the value `hi`, more than `most` at or above it. Of those at it the first place in the row decides.
+        unsigned long long best = mine > hi ? ~(unsigned long long)threadIdx.x : 0;
+        if (mine == hi) {
+            int cell = 0;
+            while (!(cells[cell * THREADS + threadIdx.x] == top)) ++cell;
+            int at = -1;
+            for (int k = 0; at < 0; ++k) {
+                const int j = first_of(lo_j, per_cell, cell, threadIdx.x) + k * THREADS;
+                float f[Row<T>::VE];
+                unpack16(row.load(j), f, T());
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                float f[VE];
-                unpack16(raw[u], f, T());
+                for (int e = Row<T>::VE - 1; e >= 0; --e)
+                    if (f[e] == top) at = row.first(j) + e;
+            }
+            best = key_of(top, at);
+        }
+        unsigned long long l = (unsigned long long)lo << 32 | 0xffffffffu, h = (unsigned long long)hi << 32 | 0xffffffffu;
+        while (true) {
+            const unsigned long long mid = l + (h - l) / 2;
+            above = __syncthreads_count(best > mid);
+            if (above < n_top) { h = mid; continue; }
+            l = mid;
+            if (above <= most) break;
+        }
+        raise(l);
+        return best > l;
+    }
+    // entries of the found cells' vectors [from, to) that are above the floor go to the list, as far as there is room: `count` may rise above CAPACITY
+    template <typename T>
+    __device__ __forceinline__ void append(const Row<T>& row, int lo_j, int hi_j, int per_cell, int from, int to) {
+        for (int i = from + (int)threadIdx.x; i < to; i += THREADS) {
+            const int c = found[i / per_cell], k = i % per_cell, j = first_of(lo_j, per_cell, c / THREADS, c % THREADS) + k * THREADS;
+            if (j < hi_j) {
+                float f[Row<T>::VE];
+                unpack16(row.load(j), f, T());
 #pragma unroll
-                for (int e = 0; e < VE; ++e) {
+                for (int e = 0; e < Row<T>::VE; ++e) {
                     if (f[e] >= floor_z) {
-                        const unsigned long long k = key_of(f[e], row.first(j0 + u * THREADS + (int)threadIdx.x) + e);
-                        if (strict ? f[e] > floor_z : k > floor) list[atomicAdd(count, 1)] = k;
+                        const unsigned long long key = key_of(f[e], row.first(j) + e);
+                        if (key > floor) {
+                            const int at = atomicAdd(count, 1);
+                            if (at < CAPACITY) list[at] = key;
+                        }
                     }
                 }
             }
         }
     }
+    // all threads, after the pass over vectors [lo_j, hi_j): the list becomes the n_top largest keys in falling order; returns how many there are. per_cell:
+    // vectors of a cell, top: the thread's largest entry
+    template <typename T>
+    __device__ int search(const Row<T>& row, int lo_j, int hi_j, int per_cell, float top) {
+        if (threadIdx.x < 2) count[threadIdx.x] = 0;
+        if (bound(row, lo_j, hi_j, per_cell, top)) {           // (begins with a barrier)
+            for (int c = 0; c < CELLS; ++c) {
+                const float z = cells[c * THREADS + threadIdx.x];
+                if (z >= floor_z && key_of(z, max(0, row.first(first_of(lo_j, per_cell, c, threadIdx.x)))) > floor) found[atomicAdd(count + 1, 1)] = c * THREADS + threadIdx.x;
+            }
+        }
+        __syncthreads();
+        const int n = count[1] * per_cell;
+        append(row, lo_j, hi_j, per_cell, 0, n);
+        __syncthreads();
+        if (*count > CAPACITY) {                               // too many at once (a row whose large entries lie in few threads): in turns with room for all
+            __syncthreads();
+            if (threadIdx.x == 0) *count = 0;
+            __syncthreads();
+            constexpr int TURN = THREADS / Row<T>::VE;         // vectors
+            for (int i = 0; i < n; i += TURN) {
+                if (*count + THREADS > CAPACITY) cut();
+                __syncthreads();
+                append(row, lo_j, hi_j, per_cell, i, min(n, i + TURN));
+                __syncthreads();
+            }
+        }
+        cut();
+        const int m = *count;
+        unsigned long long mine = 0;
+        int above = 0;
+        if ((int)threadIdx.x < m) {
+            mine = list[threadIdx.x];
+            for (int i = 0; i < m; ++i) above += list[i] > mine;
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < m && above < n_top) list[above] = mine;
+        __syncthreads();
+        return min(m, n_top);
+    }
 };
 
 struct ForwardParams {
     const void* logits;
+    const char* end;               // behind the last row
     const int32_t* tokens;
     float *logprob, *stats, *entropy, *top_logprob;
     int32_t *top_ids, *status;
     int64_t ld;
-    int32_t vocab, n_tokens, n_top, capacity;
+    int32_t n_rows, vocab, n_tokens, n_top;
     float temperature, c;          // c = log2(e) / T
 };
 
@@ -233,175 +437,275 @@ __device__ __forceinline__ void st_cluster_u64(const void* local_smem, uint32_t 
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(ptx::mapa_shared(ptx::smem_u32(local_smem), rank)), "l"(v) : "memory");
 }
 
-// A cluster of CS CTAs per row, a CTA per stretch of its vectors.
+// Shared memory behind the tiles under way, in 8-byte words: cells, list, few, what the CTAs of a cluster tell each other (twice 8 bytes each) and their keys, found
+struct Layout {
+    int cells, list, few, told, keys, found, words;
+    __host__ __device__ Layout(int n_top, int cs) {
+        const int most = n_top > 0 ? most_of(n_top) : 0;
+        cells = 0;
+        told = cells + (n_top > 0 ? CELLS * THREADS / 2 : 0);
+        list = told + 2 * cs;
+        few = list + (n_top > 0 ? CAPACITY : 0);
+        keys = few + most;
+        found = keys + cs * n_top;
+        words = found + most * CELLS / 2;
+    }
+};
+constexpr int TILE_BYTES = UNROLL * THREADS * 16;
+
+// The tiles of a CTA's rows, in order: its stretch of each
+template <typename T, int CS>
+struct Cursor {
+    Row<T> row;
+    int r, j, lo, hi;
+    __device__ __forceinline__ void to(const ForwardParams& p, int rank, int to_row) {
+        r = to_row;
+        lo = hi = 0;
+        if (r < p.n_rows) {
+            row = Row<T>(reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld, p.vocab);
+            const int per = (row.n_vec + CS - 1) / CS;
+            lo = min(rank * per, row.n_vec);
+            hi = min(row.n_vec, lo + per);
+        }
+        j = lo;
+    }
+};
+
+// A cluster of CS CTAs per row, a CTA per stretch of its vectors. One CTA a row: it goes on with another row, whose first tiles are then already under way;
+// several: the grid has a cluster for each row.
 template <typename T, int CS>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(const ForwardParams p) {
-    extern __shared__ unsigned long long dyn[];            // list [capacity], few [RANK_MAX], then from every CTA: told [CS][2], keys [CS][n_top]
+    extern __shared__ uint4 ring[];                        // [STAGES][UNROLL][THREADS]: a thread reads what it has copied itself
     __shared__ Stat sh[THREADS / 32];
-    __shared__ int count;
+    __shared__ uint32_t ends[2 * THREADS / 32];
+    __shared__ int count[2];
+    constexpr int TILE = UNROLL * THREADS;                 // vectors
+    const int tid = threadIdx.x, rank = CS > 1 ? (int)ptx::cluster_ctarank() : 0;
+    unsigned long long* words = reinterpret_cast<unsigned long long*>(ring + STAGES * TILE);
+    const Layout at(p.n_top, CS);
+    Told* told = reinterpret_cast<Told*>(words + at.told);
+    unsigned long long* keys = words + at.keys;
+    Candidates cand;
+    cand.list = words + at.list;
+    cand.few = words + at.few;
+    cand.cells = reinterpret_cast<float*>(words + at.cells);
+    cand.found = reinterpret_cast<int*>(words + at.found);
+    cand.count = count;
+    cand.ends = ends;
+    cand.n_top = p.n_top;
+    cand.most = most_of(p.n_top);
     ptx::pdl_trigger();
     ptx::pdl_wait();
     if constexpr (CS > 1) ptx::cluster_arrive();           // (waited for before the first store into another CTA)
-    const int tid = threadIdx.x, r = blockIdx.x / CS, rank = CS > 1 ? (int)ptx::cluster_ctarank() : 0;
-    const T* z = reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld;
-    const Row<T> row(z, p.vocab);
-    const int per = (row.n_vec + CS - 1) / CS, lo = min(rank * per, row.n_vec), hi = min(row.n_vec, lo + per);
-    // a given token's logit, early (every CTA holds the row's result in the end; the first one writes it)
-    const int tok = tid < p.n_tokens && rank == 0 ? p.tokens[(int64_t)r * p.n_tokens + tid] : -1;
-    float z_tok = 0.f;
-    if (tok >= p.vocab && p.status) atomicOr(p.status, DFLASH_DEV_BAD_TOKEN);
-    if (tok >= 0 && tok < p.vocab) z_tok = as_f(z[tok]);
-    Candidates cand;
-    cand.list = dyn;
-    cand.few = dyn + p.capacity;
-    cand.count = &count;
-    cand.n_top = p.n_top;
-    cand.capacity = p.capacity;
-    cand.raise(NO_KEY);
-    if (tid == 0) count = 0;
-    const uint4 none = sizeof(T) == 4 ? make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u) : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
-    Stat t{-CUDART_INF_F, 0.f, 0.f};
-    uint4 next[UNROLL];
+    const int step = gridDim.x / CS;
+    const char* begin = reinterpret_cast<const char*>(p.logits);
+    const auto in_memory = [&](const char* a) { return a >= begin && a + 16 <= p.end; };
+    Cursor<T, CS> ahead;
+    ahead.to(p, rank, blockIdx.x / CS);
+    const uint32_t slots = ptx::smem_u32(ring + tid), slots_end = slots + STAGES * TILE_BYTES;
+    uint32_t fill = slots;                                 // the next tile's place in the ring
+    const auto request = [&]() {
+        while (ahead.j >= ahead.hi && ahead.r < p.n_rows) ahead.to(p, rank, ahead.r + step);
+        if (ahead.r < p.n_rows) {
+            const char* tile = ahead.row.address(ahead.j);
+            const char* a = tile + tid * 16;
+            static_assert(UNROLL == 4, "");
+            if (ahead.j + TILE <= ahead.hi && tile >= begin && tile + TILE_BYTES <= p.end) {
+                copy_async16<0 * THREADS * 16>(fill, a);
+                copy_async16<1 * THREADS * 16>(fill, a);
+                copy_async16<2 * THREADS * 16>(fill, a);
+                copy_async16<3 * THREADS * 16>(fill, a);
+            } else {
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) next[u] = lo + u * THREADS + tid < hi ? row.load(lo + u * THREADS + tid) : none;
-    for (int j0 = lo; j0 < hi; j0 += UNROLL * THREADS) {
-        uint4 raw[UNROLL];
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            raw[u] = next[u];
-            const int j = j0 + (UNROLL + u) * THREADS + tid;
-            next[u] = j < hi ? row.load(j) : none;
-        }
-        float top = vec_max(raw[0], T());
-#pragma unroll
-        for (int u = 1; u < UNROLL; ++u) top = fmaxf(top, vec_max(raw[u], T()));
-        if (top > t.m) t = raised(t, top, p.c);
-        const float base = t.m == -CUDART_INF_F ? 0.f : t.m;
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            float f[Row<T>::VE];
-            unpack16(raw[u], f, T());
-            add_terms(t, f, base, p.c);
-        }
-        if (p.n_top > 0) cand.take(row, raw, j0, top);
-    }
-    // ---- the CTA's results: warp, CTA
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        t = merged(t, Stat{__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o), __shfl_xor_sync(0xffffffffu, t.w, o)}, p.c);
-    if ((tid & 31) == 0) sh[tid >> 5] = t;
-    if (p.n_top > 0) cand.rank();
-    else __syncthreads();
-    t = sh[tid & (THREADS / 32 - 1)];
-#pragma unroll
-    for (int o = THREADS / 64; o > 0; o >>= 1)
-        t = merged(t, Stat{__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o), __shfl_xor_sync(0xffffffffu, t.w, o)}, p.c);
-    int n_list = p.n_top > 0 ? count : 0;
-    // ---- the cluster's
-    Told* told = reinterpret_cast<Told*>(dyn + p.capacity + RANK_MAX);
-    unsigned long long* keys = dyn + p.capacity + RANK_MAX + 2 * CS;
-    if constexpr (CS > 1) {
-        ptx::cluster_wait();                               // every CTA runs
-        if (tid < CS) {
-            const Told mine{t.m, t.s, t.w, n_list};
-            const unsigned long long* w = reinterpret_cast<const unsigned long long*>(&mine);
-            st_cluster_u64(told + rank, tid, w[0]);
-            st_cluster_u64(reinterpret_cast<const char*>(told + rank) + 8, tid, w[1]);
-        }
-        for (int i = tid; i < CS * n_list; i += THREADS) st_cluster_u64(keys + rank * p.n_top + i % n_list, i / n_list, cand.list[i % n_list]);
-        __syncwarp();
-        ptx::cluster_sync_all();                           // no CTA writes into another one after this
-        t = Stat{told[0].m, told[0].s, told[0].w};
-#pragma unroll
-        for (int q = 1; q < CS; ++q) t = merged(t, Stat{told[q].m, told[q].s, told[q].w}, p.c);
-    }
-    const bool empty = t.m == -CUDART_INF_F;
-    // (a row that holds NaN has a sum of NaN; one of -inf and NaN has no maximum, but is not empty either)
-    const float log_sum = empty && t.s == 0.f ? 0.f : logf(t.s);
-    if (rank == 0) {
-        if (tid == 0) {
-            if (p.stats) *reinterpret_cast<float2*>(p.stats + 2 * (int64_t)r) = make_float2(t.m, log_sum);
-            if (p.entropy) p.entropy[r] = empty && t.s == 0.f ? 0.f : log_sum - t.w * LN2 / t.s;
-        }
-        if (tid < p.n_tokens) {
-            float lp = 0.f;
-            if (tok >= 0 && tok < p.vocab) lp = empty && t.s == 0.f ? -CUDART_INF_F : (z_tok - t.m) / p.temperature - log_sum;
-            p.logprob[(int64_t)r * p.n_tokens + tid] = lp;
-        }
-    }
-    if (p.n_top > 0) {
-        int32_t* ids = p.top_ids + (int64_t)r * p.n_top;
-        float* lps = p.top_logprob + (int64_t)r * p.n_top;
-        int total = n_list;
-        if constexpr (CS == 1) {
-            if (tid < n_list) {
-                ids[tid] = index_of(cand.list[tid]);
-                lps[tid] = (value_of(cand.list[tid]) - t.m) / p.temperature - log_sum;
+                for (int u = 0; u < UNROLL; ++u)
+                    if (ahead.j + u * THREADS + tid < ahead.hi && in_memory(a + u * THREADS * 16)) copy_async16(fill + u * THREADS * 16, a + u * THREADS * 16);
             }
-        } else {
-            // a key's place in the row: its place in the CTA's own list and the number of larger ones in each other list, one lane a list
-            total = 0;
+            ahead.j += TILE;
+        }
+        copy_commit();
+        fill += TILE_BYTES;
+        if (fill == slots_end) fill = slots;
+    };
+    for (int i = 0; i < STAGES; ++i) request();
+    const uint4* use = ring + tid;
+    for (int r = blockIdx.x / CS; r < p.n_rows; r += step) {
+        Cursor<T, CS> cur;
+        cur.to(p, rank, r);
+        const Row<T>& row = cur.row;
+        // a given token's logit (every CTA holds the row's result in the end; the first one writes it)
+        const int tok = tid < p.n_tokens && rank == 0 ? p.tokens[(int64_t)r * p.n_tokens + tid] : -1;
+        Running t;
+        t.reset();
+        float peak = -CUDART_INF_F, cell_top = -CUDART_INF_F;
+        const int tiles = (cur.hi - cur.lo + TILE - 1) / TILE, per_cell = (tiles + CELLS - 1) / CELLS * UNROLL;
+        int cell = 0, cell_end = cur.lo + per_cell * THREADS;
+        for (int j0 = cur.lo; j0 < cur.hi; j0 += TILE) {
+            copy_wait<STAGES - 1>();
+            uint4 raw[UNROLL];
+            if (j0 + TILE <= cur.hi && row.whole(j0) && row.whole(j0 + TILE - 1)) {
 #pragma unroll
-            for (int q = 0; q < CS; ++q) total += told[q].n;
-            const int q = tid % CS;
-            for (int i0 = 0; i0 < n_list; i0 += THREADS / CS) {
-                const int i = i0 + tid / CS;
-                int above = 0;
-                unsigned long long k = 0;
-                if (i < n_list) {
-                    k = cand.list[i];
-                    int b = told[q].n, a = 0;              // keys [0, a) of list q are larger, those from b on are not
-                    while (a < b) {
-                        const int mid = (a + b) / 2;
-                        if (keys[q * p.n_top + mid] > k) a = mid + 1;
-                        else b = mid;
+                for (int u = 0; u < UNROLL; ++u) raw[u] = use[u * THREADS];
+            } else {
+#pragma unroll
+                for (int u = 0; u < UNROLL; ++u) {
+                    const int j = j0 + u * THREADS + tid;
+                    raw[u] = no_entries<T>();
+                    if (j < cur.hi) {
+                        raw[u] = use[u * THREADS];
+                        if (!row.whole(j)) raw[u] = edge_of<T>(row.address(j), row.first(j), p.vocab, raw[u], in_memory(row.address(j)));
                     }
-                    above = a;
-                }
-#pragma unroll
-                for (int o = CS / 2; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
-                if (q == 0 && i < n_list && above < p.n_top) {
-                    ids[above] = index_of(k);
-                    lps[above] = (value_of(k) - t.m) / p.temperature - log_sum;
                 }
             }
+            const float top = fmaxf(fmaxf(vec_max(raw[0], T()), vec_max(raw[1], T())), fmaxf(vec_max(raw[2], T()), vec_max(raw[3], T())));
+            if (top > t.limit) t.raise(top, p.c);
+            peak = fmaxf(peak, top);
+            if (p.n_top > 0) {
+                if (j0 == cell_end) {
+                    ++cell;
+                    cell_end += per_cell * THREADS;
+                    cell_top = top;
+                } else {
+                    cell_top = fmaxf(cell_top, top);
+                }
+                cand.cells[cell * THREADS + tid] = cell_top;
+            }
+            use += TILE;
+            if (use == ring + tid + STAGES * TILE) use = ring + tid;
+            request();                                     // into the place that has just been read
+            if (!t.plain) {
+#pragma unroll
+                for (int u = 0; u < UNROLL; ++u) t.add<T>(raw[u], p.c);
+            } else {
+#pragma unroll
+                for (int u = 0; u < UNROLL; ++u) t.add_plain<T>(raw[u], p.c);
+            }
         }
-        for (int i = total + tid; rank == 0 && i < p.n_top; i += THREADS) {      // fewer entries than were asked for
-            ids[i] = -1;
-            lps[i] = -CUDART_INF_F;
+        if (p.n_top > 0)
+            for (int k = tiles == 0 ? 0 : cell + 1; k < CELLS; ++k) cand.cells[k * THREADS + tid] = -CUDART_INF_F;
+        float z_tok = 0.f;
+        if (tok >= p.vocab && p.status) atomicOr(p.status, DFLASH_DEV_BAD_TOKEN);
+        if (tok >= 0 && tok < p.vocab) z_tok = as_f(reinterpret_cast<const T*>(p.logits)[(int64_t)r * p.ld + tok]);
+        // ---- the CTA's results: warp, CTA
+        Stat x = lanes_merged<32>(t.total(peak, p.c), p.c);
+        if ((tid & 31) == 0) sh[tid >> 5] = x;
+        int n_list = 0;
+        if (p.n_top > 0) {
+            n_list = cand.search(row, cur.lo, cur.hi, per_cell, peak);
+        } else {
+            __syncthreads();
         }
+        x = lanes_merged<THREADS / 32>(sh[tid & (THREADS / 32 - 1)], p.c);
+        // ---- the cluster's
+        if constexpr (CS > 1) {
+            ptx::cluster_wait();                           // every CTA runs
+            if (tid < CS) {
+                const Told mine{x.m, x.s, x.w, n_list};
+                const unsigned long long* w = reinterpret_cast<const unsigned long long*>(&mine);
+                st_cluster_u64(told + rank, tid, w[0]);
+                st_cluster_u64(reinterpret_cast<const char*>(told + rank) + 8, tid, w[1]);
+            }
+            for (int i = tid; i < CS * n_list; i += THREADS) st_cluster_u64(keys + rank * p.n_top + i / CS, i % CS, cand.list[i / CS]);
+            __syncwarp();
+            ptx::cluster_sync_all();                       // no CTA writes into another one after this
+            x = Stat{told[0].m, told[0].s, told[0].w};
+#pragma unroll
+            for (int q = 1; q < CS; ++q) x = merged(x, Stat{told[q].m, told[q].s, told[q].w}, p.c);
+        }
+        // (a row that holds NaN has a sum of NaN; one of -inf and NaN has no maximum, but is not empty either)
+        const bool empty = x.m == -CUDART_INF_F && x.s == 0.f;
+        const float log_sum = empty ? 0.f : logf(x.s);
+        if (rank == 0) {
+            if (tid == 0) {
+                if (p.stats) *reinterpret_cast<float2*>(p.stats + 2 * (int64_t)r) = make_float2(x.m, log_sum);
+                if (p.entropy) p.entropy[r] = empty ? 0.f : log_sum - x.w * LN2 / x.s;
+            }
+            if (tid < p.n_tokens) {
+                float lp = 0.f;
+                if (tok >= 0 && tok < p.vocab) lp = empty ? -CUDART_INF_F : (z_tok - x.m) / p.temperature - log_sum;
+                p.logprob[(int64_t)r * p.n_tokens + tid] = lp;
+            }
+        }
+        if (p.n_top > 0) {
+            int32_t* ids = p.top_ids + (int64_t)r * p.n_top;
+            float* lps = p.top_logprob + (int64_t)r * p.n_top;
+            int total = n_list;
+            if constexpr (CS == 1) {
+                if (tid < n_list) {
+                    const unsigned long long k = cand.list[tid];
+                    ids[tid] = index_of(k);
+                    lps[tid] = (value_of(k) - x.m) / p.temperature - log_sum;
+                }
+            } else {
+                // a key's place in the row: its place in the CTA's own list and the number of larger ones in each other list, one lane a list
+                total = 0;
+#pragma unroll
+                for (int q = 0; q < CS; ++q) total += told[q].n;
+                const int q = tid % CS;
+                for (int i0 = 0; i0 < n_list; i0 += THREADS / CS) {
+                    const int i = i0 + tid / CS;
+                    int above = 0;
+                    unsigned long long k = 0;
+                    if (i < n_list) {
+                        k = cand.list[i];
+                        int b = told[q].n, a = 0;          // keys [0, a) of list q are larger, those from b on are not
+                        while (a < b) {
+                            const int mid = (a + b) / 2;
+                            if (keys[q * p.n_top + mid] > k) a = mid + 1;
+                            else b = mid;
+                        }
+                        above = a;
+                    }
+#pragma unroll
+                    for (int o = CS / 2; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
+                    if (q == 0 && i < n_list && above < p.n_top) {
+                        ids[above] = index_of(k);
+                        lps[above] = (value_of(k) - x.m) / p.temperature - log_sum;
+                    }
+                }
+            }
+            for (int i = total + tid; rank == 0 && i < p.n_top; i += THREADS) {      // fewer entries than were asked for
+                ids[i] = -1;
+                lps[i] = -CUDART_INF_F;
+            }
+        }
+        __syncthreads();                                   // list and sums have been read
     }
 }
 
 template <typename T, int CS>
-cudaError_t launch_forward(const ForwardParams& p, int rows, cudaStream_t st) {
-    const size_t smem = p.n_top > 0 ? (size_t)(p.capacity + RANK_MAX + CS * (2 + p.n_top)) * 8 : (size_t)(2 * CS) * 8;
+cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
+    const int words = Layout(p.n_top, CS).words * 8;
     static bool attr_set[MAX_DEVICES] = {};
     const int dev = current_device_slot();
     if (dev < 0) return cudaErrorInvalidDevice;
     if (!attr_set[dev]) {
-        const int most = (list_capacity<T>(LP_MAX_TOP) + RANK_MAX + CS * (2 + LP_MAX_TOP)) * 8;
-        const cudaError_t e = cudaFuncSetAttribute(token_logprobs_kernel<T, CS>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+        const cudaError_t e = cudaFuncSetAttribute(token_logprobs_kernel<T, CS>, cudaFuncAttributeMaxDynamicSharedMemorySize, STAGES * TILE_BYTES + Layout(LP_MAX_TOP, CS).words * 8);
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
-    if (CS == 1) return launch_pdl(token_logprobs_kernel<T, CS>, dim3(rows), dim3(THREADS), smem, st, p);
-    return launch_pdl_cluster(token_logprobs_kernel<T, CS>, dim3(rows * CS), dim3(THREADS), smem, st, CS, p);
+    const size_t smem = (size_t)STAGES * TILE_BYTES + words;
+    if (CS == 1) return launch_pdl(token_logprobs_kernel<T, CS>, dim3(std::min(p.n_rows, CTAS_PER_SM * sm_count)), dim3(THREADS), smem, st, p);
+    return launch_pdl_cluster(token_logprobs_kernel<T, CS>, dim3(p.n_rows * CS), dim3(THREADS), smem, st, CS, p);
 }
 
 template <typename T>
-cudaError_t launch_forward(ForwardParams p, int rows, int sm_count, cudaStream_t st) {
-    p.capacity = p.n_top > 0 ? list_capacity<T>(p.n_top) : 0;
-    if (p.n_top == 0) p.capacity = -RANK_MAX;              // (no list: what the CTAs tell each other comes first)
-    // CTAs per row: as many as it takes to fill the GPU, as long as each has a tile of its own
+cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
+    // CTAs per row: what takes the fewest tile times, a CTA's start and end counted as two
     const int tiles = (p.vocab + UNROLL * THREADS * Row<T>::VE - 1) / (UNROLL * THREADS * Row<T>::VE);
     int cs = 1;
-    while (cs < MAX_CLUSTER && cs < tiles && (int64_t)rows * cs < CTAS_PER_SM * sm_count) cs *= 2;
+    int64_t least = INT64_MAX;
+    for (int s = 1; s <= MAX_CLUSTER && s / 2 < tiles; s *= 2) {
+        const int64_t turns = ((int64_t)p.n_rows * s + CTAS_PER_SM * sm_count - 1) / (CTAS_PER_SM * sm_count), time = turns * ((tiles + s - 1) / s + 2);
+        if (time < least) {
+            least = time;
+            cs = s;
+        }
+    }
     switch (cs) {
-        case 1: return launch_forward<T, 1>(p, rows, st);
-        case 2: return launch_forward<T, 2>(p, rows, st);
-        case 4: return launch_forward<T, 4>(p, rows, st);
-        default: return launch_forward<T, 8>(p, rows, st);
+        case 1: return launch_forward<T, 1>(p, sm_count, st);
+        case 2: return launch_forward<T, 2>(p, sm_count, st);
+        case 4: return launch_forward<T, 4>(p, sm_count, st);
+        default: return launch_forward<T, 8>(p, sm_count, st);
     }
 }
 
@@ -552,10 +856,11 @@ int launch_token_logprobs(const Launch& L, const dflash_token_logprobs_args& a) 
     ForwardParams p{};
     p.logits = a.logits; p.tokens = a.tokens; p.logprob = a.logprob; p.stats = a.stats; p.entropy = a.entropy;
     p.top_ids = a.top_ids; p.top_logprob = a.top_logprob; p.status = L.status;
-    p.ld = a.row_stride ? a.row_stride : a.vocab; p.vocab = a.vocab; p.n_tokens = a.n_tokens; p.n_top = a.n_top;
+    p.ld = a.row_stride ? a.row_stride : a.vocab; p.n_rows = a.n_rows; p.vocab = a.vocab; p.n_tokens = a.n_tokens; p.n_top = a.n_top;
+    p.end = reinterpret_cast<const char*>(a.logits) + ((int64_t)(a.n_rows - 1) * p.ld + a.vocab) * elem_size(a.logits_dtype);
     p.temperature = a.temperature; p.c = (float)(1.4426950408889634 / (double)a.temperature);
-    const cudaError_t e = a.logits_dtype == DFLASH_BF16 ? launch_forward<__nv_bfloat16>(p, a.n_rows, L.h->sm_count, L.st)
-                                                        : launch_forward<float>(p, a.n_rows, L.h->sm_count, L.st);
+    const cudaError_t e = a.logits_dtype == DFLASH_BF16 ? launch_forward<__nv_bfloat16>(p, L.h->sm_count, L.st)
+                                                        : launch_forward<float>(p, L.h->sm_count, L.st);
     g_launches += 1;
     return e == cudaSuccess ? DFLASH_OK : DFLASH_ERR_CUDA;
 }

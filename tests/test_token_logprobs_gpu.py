@@ -4,7 +4,8 @@ Tolerances. u = 2^-24. A term exp(y), y = (z - M) / T, is off by at most 4 |y| u
 (the exponential itself, 2 ulp, and its rescaling); a thread adds at most V / 512 + 32 terms one behind the other, the merges add 16.
 So ln S is off by (V / 512 + 56 + 4 E|y|) u, with E|y| = entropy - ln S + 2 ln S at most. A log probability adds 4 u of its own two parts.
 The entropy's sum has terms exp(y) y: the same relative error of each, so E|y| times it, and u of the whole. Gradients: p = exp(y - ln S) is off by
-4 (|y| + ln S) u + 8 u, its factor by 8 u (|G| + |gH| (|ln p| + entropy)), and the result is rounded to its type."""
+4 (|y| + ln S) u + 8 u, its factor by 8 u (|G| + |gH| (|ln p| + entropy)), and the result is rounded to its type. ln p and the entropy are themselves off by
+the tolerances above whatever their size, which adds |gH| times those: a row of one entry has ln p = entropy = 0, and both come out as some u."""
 import numpy as np
 import pytest
 import torch
@@ -220,7 +221,7 @@ def check_backward(d, z, tokens, g, gh, T, out, rows=slice(None)):
     log_sum = np.nan_to_num(f["stats"][:, 1:])
     G = np.abs(np.where(valid, g64, 0)).sum(1, keepdims=True)
     H = np.zeros_like(G) if h64 is None else np.abs(h64)[:, None]
-    size = p * (G + H * (np.abs(lp) + np.nan_to_num(f["entropy"])[:, None]))
+    size = p * (G + H * (1 + np.abs(lp) + np.nan_to_num(f["entropy"])[:, None]))
     own = np.zeros_like(zz)
     for r in range(len(zz)):
         np.add.at(own[r], tokens.numpy()[r][valid[r]], np.abs(g64[r][valid[r]]))
