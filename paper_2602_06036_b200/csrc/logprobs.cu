@@ -13,7 +13,8 @@
 namespace dflash {
 namespace {
 
-constexpr int THREADS = 256, UNROLL = 4, CTAS_PER_SM = 4;      // a tile: UNROLL 16-byte vectors a thread, 16 KB a CTA
+constexpr int THREADS = 256, WARPS = THREADS / 32, UNROLL = 4, CTAS_PER_SM = 4;
+constexpr int TILE = THREADS * UNROLL, TILE_BYTES = TILE * 16;      // 16-byte vectors of a tile: UNROLL a thread
 constexpr int STAGES = 2;                                      // tiles under way
 constexpr int MAX_CLUSTER = 8;
 constexpr float LN2 = 0.6931471805599453f;
@@ -85,12 +86,11 @@ __device__ __forceinline__ float vec_max(const uint4& v, __nv_bfloat16) {
 // ---- copies to shared memory under way --------------------------------------------------------------------------------
 template <int OFFSET = 0>
 __device__ __forceinline__ void copy_async16(uint32_t smem, const void* gmem) {
-    asm volatile("cp.async.cg.shared.global [%0+%2], [%1+%2], 16;" ::"r"(smem), "l"(gmem), "n"(OFFSET) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0+%2], [%1+%2], 16;" ::"r"(smem), "l"(gmem), "n"(OFFSET) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }      // all but the latest N groups have landed
-
 // ---- statistics ----------------------------------------------------------------------------------------------------
 // m: maximum, s: sum of 2^((z - m) c), w: sum of 2^((z - m) c) (z - m) c
 struct Stat {
@@ -239,23 +239,25 @@ __device__ __forceinline__ int index_of(unsigned long long key) { return (int)(0
 constexpr uint32_t ORDERED_NONE = 0x007fffffu;                 // ordered(-inf)
 constexpr unsigned long long NO_KEY = (unsigned long long)ORDERED_NONE << 32 | 0xffffffffu;      // not below any key of -inf, below all others
 
-constexpr int CELLS = 8;                                       // of a thread: its part of a row in as many runs of tiles
-constexpr int CAPACITY = 512;                                  // of the list
 __host__ __device__ __forceinline__ int most_of(int n_top) { return n_top + n_top / 4 + 8; }      // entries that a bound on the n_top-th largest may leave
-static_assert(LP_MAX_TOP + LP_MAX_TOP / 4 + 8 + THREADS <= CAPACITY && LP_MAX_TOP + LP_MAX_TOP / 4 + 8 <= THREADS, "a turn's entries fit behind a list that has been cut");
+__host__ __device__ __forceinline__ int capacity_of(int n_top) { return most_of(n_top) + THREADS; }      // of the list: a turn's entries fit behind one that has been cut
+// Cells of a thread: its part of a row in as many runs of tiles. More of them are read again by fewer vectors (8 cells of 3 tiles at 151936 bf16 entries; 2048 rows with
+// 64 alternatives: 154 us with 8), but shared memory is taken from L1 in steps, which the copies under way need: CTAs of more than 48.5 KB leave it too little.
+__host__ __device__ __forceinline__ int cells_of(int n_top) { return n_top > 32 && n_top <= 64 ? 16 : 8; }
+static_assert(LP_MAX_TOP + LP_MAX_TOP / 4 + 8 <= THREADS && 16 * THREADS <= 65536, "");
 
 // The search for a stretch's n_top largest entries, after the pass over it that has left the largest entry of every thread and of each of its cells. At least
 // n_top threads' largest entries bound the n_top-th largest of the stretch from below, and little else is above a bound that few of them are (`bound`).
 // What is, lies in a few cells, which are read again (from L2, mostly) by all threads together. The pass itself so needs no barrier and looks at no
 // entry twice; taking candidates out as they come by cost a barrier a tile and more than the reading of the row.
 struct Candidates {
-    unsigned long long* list;      // [CAPACITY] keys
+    unsigned long long* list;      // [capacity] keys
     unsigned long long* few;       // [most]
-    float* cells;                  // [CELLS][THREADS]
-    int* found;                    // [most * CELLS] cells to be read again: cell * THREADS + thread
+    uint16_t* cells;               // [n_cells][THREADS] largest entries as bf16, rounded up
+    uint16_t* found;               // [most * n_cells] cells to be read again: cell * THREADS + thread
     int* count;                    // entries of list, of found
-    uint32_t* ends;                // [2][THREADS / 32]
-    int n_top, most;
+    uint32_t* ends;                // [2][WARPS]
+    int n_top, most, capacity, n_cells;
     unsigned long long floor;      // keys that are not above it are none of the n_top largest
     float floor_z;
 
@@ -295,8 +297,11 @@ struct Candidates {
         raise(lo);
         __syncthreads();
     }
-    // first vector of a cell; its vectors are THREADS apart
-    __device__ __forceinline__ static int first_of(int lo, int per_cell, int cell, int thread) { return lo + cell * per_cell * THREADS + thread; }
+    __device__ __forceinline__ float cell_top(int cell) const { return __uint_as_float((uint32_t)cells[cell * THREADS + threadIdx.x] << 16); }
+    // k-th vector of a cell
+    __device__ __forceinline__ static int vector_of(int lo, int per_cell, int cell, int thread, int k) {
+        return lo + (cell * per_cell + k) * THREADS + thread;
+    }
     // all threads: a floor that at least n_top of the threads' largest entries lie above, and at most `most`. Found by halving: first between values, and where too many
     // are equal, between keys. Returns whether this thread's entries may lie above it.
     template <typename T>
@@ -310,11 +315,11 @@ struct Candidates {
         const uint32_t top_of_warp = __reduce_max_sync(0xffffffffu, mine), least = __reduce_min_sync(0xffffffffu, mine);
         if ((threadIdx.x & 31) == 0) {
             ends[warp] = top_of_warp;
-            ends[THREADS / 32 + warp] = least;
+            ends[WARPS + warp] = least;
         }
         __syncthreads();
-        const int w = threadIdx.x & (THREADS / 32 - 1);
-        uint32_t hi = __reduce_max_sync(0xffffffffu, ends[w]), lo = __reduce_min_sync(0xffffffffu, ends[THREADS / 32 + w]);
+        const int w = threadIdx.x & (WARPS - 1);
+        uint32_t hi = __reduce_max_sync(0xffffffffu, ends[w]), lo = __reduce_min_sync(0xffffffffu, ends[WARPS + w]);
         lo = max(lo ? lo - 1 : 0u, ORDERED_NONE);              // more than `most` above lo, none above hi
         while (hi - lo > 1) {
             const uint32_t mid = lo + (hi - lo) / 2;
@@ -329,16 +334,18 @@ struct Candidates {
         // ties: fewer than n_top lie above the value `hi`, more than `most` at or above it. Of those at it the first place in the row decides.
         unsigned long long best = mine > hi ? ~(unsigned long long)threadIdx.x : 0;
         if (mine == hi) {
-            int cell = 0;
-            while (!(cells[cell * THREADS + threadIdx.x] == top)) ++cell;
             int at = -1;
-            for (int k = 0; at < 0; ++k) {
-                const int j = first_of(lo_j, per_cell, cell, threadIdx.x) + k * THREADS;
-                float f[Row<T>::VE];
-                unpack16(row.load(j), f, T());
+            for (int cell = 0; at < 0 && cell < n_cells; ++cell) {      // (what is rounded up may be smaller)
+                if (!(cell_top(cell) >= top)) continue;
+                for (int k = 0; at < 0 && k < per_cell; ++k) {
+                    const int j = vector_of(lo_j, per_cell, cell, threadIdx.x, k);
+                    if (j >= hi_j) break;
+                    float f[Row<T>::VE];
+                    unpack16(row.load(j), f, T());
 #pragma unroll
-                for (int e = Row<T>::VE - 1; e >= 0; --e)
-                    if (f[e] == top) at = row.first(j) + e;
+                    for (int e = Row<T>::VE - 1; e >= 0; --e)
+                        if (f[e] == top) at = row.first(j) + e;
+                }
             }
             best = key_of(top, at);
         }
@@ -353,68 +360,82 @@ struct Candidates {
         raise(l);
         return best > l;
     }
-    // entries of the found cells' vectors [from, to) that are above the floor go to the list, as far as there is room: `count` may rise above CAPACITY
+    // entries of the found cells' vectors [from, to) that are above the floor go to the list, as far as there is room: `count` may rise above capacity
     template <typename T>
     __device__ __forceinline__ void append(const Row<T>& row, int lo_j, int hi_j, int per_cell, int from, int to) {
-        for (int i = from + (int)threadIdx.x; i < to; i += THREADS) {
-            const int c = found[i / per_cell], k = i % per_cell, j = first_of(lo_j, per_cell, c / THREADS, c % THREADS) + k * THREADS;
-            if (j < hi_j) {
-                float f[Row<T>::VE];
-                unpack16(row.load(j), f, T());
+        constexpr int AT_ONCE = 2;
+        for (int i0 = from + (int)threadIdx.x; i0 < to; i0 += AT_ONCE * THREADS) {
+            uint4 v[AT_ONCE];
+            int j[AT_ONCE];
 #pragma unroll
-                for (int e = 0; e < Row<T>::VE; ++e) {
-                    if (f[e] >= floor_z) {
-                        const unsigned long long key = key_of(f[e], row.first(j) + e);
-                        if (key > floor) {
-                            const int at = atomicAdd(count, 1);
-                            if (at < CAPACITY) list[at] = key;
-                        }
+            for (int q = 0; q < AT_ONCE; ++q) {
+                const int i = i0 + q * THREADS, c = i < to ? found[i / per_cell] : 0;
+                j[q] = i < to ? vector_of(lo_j, per_cell, c / THREADS, c % THREADS, i % per_cell) : hi_j;
+                v[q] = j[q] < hi_j ? row.load(j[q]) : no_entries<T>();
+            }
+#pragma unroll
+            for (int q = 0; q < AT_ONCE; ++q) {
+                float f[Row<T>::VE];
+                unpack16(v[q], f, T());
+                uint32_t hits = 0;
+#pragma unroll
+                for (int e = 0; e < Row<T>::VE; ++e) hits |= f[e] >= floor_z ? 1u << e : 0u;
+                for (; hits; hits &= hits - 1) {
+                    const int e = __ffs(hits) - 1;
+                    float z = f[0];
+#pragma unroll
+                    for (int k = 1; k < Row<T>::VE; ++k) z = e == k ? f[k] : z;
+                    const unsigned long long key = key_of(z, row.first(j[q]) + e);
+                    if (key > floor) {
+                        const int at = atomicAdd(count, 1);
+                        if (at < capacity) list[at] = key;
                     }
                 }
             }
         }
     }
-    // all threads, after the pass over vectors [lo_j, hi_j): the list becomes the n_top largest keys in falling order; returns how many there are. per_cell:
-    // vectors of a cell, top: the thread's largest entry
+    // all threads, after the pass over vectors [lo_j, hi_j): the n_top largest keys are among the at most THREADS of the list; returns how many those are. per_cell: vectors
+    // of a cell, top: the thread's largest entry
     template <typename T>
     __device__ int search(const Row<T>& row, int lo_j, int hi_j, int per_cell, float top) {
         if (threadIdx.x < 2) count[threadIdx.x] = 0;
         if (bound(row, lo_j, hi_j, per_cell, top)) {           // (begins with a barrier)
-            for (int c = 0; c < CELLS; ++c) {
-                const float z = cells[c * THREADS + threadIdx.x];
-                if (z >= floor_z && key_of(z, max(0, row.first(first_of(lo_j, per_cell, c, threadIdx.x)))) > floor) found[atomicAdd(count + 1, 1)] = c * THREADS + threadIdx.x;
+            for (int c = 0; c < n_cells; ++c) {
+                const float z = cell_top(c);
+                if (z >= floor_z && key_of(z, max(0, row.first(vector_of(lo_j, per_cell, c, threadIdx.x, 0)))) > floor) found[atomicAdd(count + 1, 1)] = (uint16_t)(c * THREADS + threadIdx.x);
             }
         }
         __syncthreads();
         const int n = count[1] * per_cell;
         append(row, lo_j, hi_j, per_cell, 0, n);
         __syncthreads();
-        if (*count > CAPACITY) {                               // too many at once (a row whose large entries lie in few threads): in turns with room for all
+        if (*count > capacity) {                               // too many at once (a row whose large entries lie in few threads): in turns with room for all
             __syncthreads();
             if (threadIdx.x == 0) *count = 0;
             __syncthreads();
             constexpr int TURN = THREADS / Row<T>::VE;         // vectors
             for (int i = 0; i < n; i += TURN) {
-                if (*count + THREADS > CAPACITY) cut();
+                if (*count + THREADS > capacity) cut();
                 __syncthreads();
                 append(row, lo_j, hi_j, per_cell, i, min(n, i + TURN));
                 __syncthreads();
             }
         }
-        cut();
-        const int m = *count;
-        unsigned long long mine = 0;
-        int above = 0;
-        if ((int)threadIdx.x < m) {
-            mine = list[threadIdx.x];
-            for (int i = 0; i < m; ++i) above += list[i] > mine;
-        }
-        __syncthreads();
-        if ((int)threadIdx.x < m && above < n_top) list[above] = mine;
-        __syncthreads();
-        return min(m, n_top);
+        if (*count > THREADS) cut();
+        return *count;
     }
 };
+// thread i < n: the place of the i-th of n keys among them, largest first
+__device__ __forceinline__ int rank_of(const unsigned long long* list, int n, unsigned long long mine) {
+    int above = 0, i = 0;
+    for (; i + 4 <= n; i += 4) above += (list[i] > mine) + (list[i + 1] > mine) + (list[i + 2] > mine) + (list[i + 3] > mine);
+    for (; i < n; ++i) above += list[i] > mine;
+    return above;
+}
+__device__ __forceinline__ void set_cell(uint16_t* cells, int cell, float top) {
+    const uint32_t b = __float_as_uint(top);                   // (towards +inf: of a negative number the rest is cut off; NaN stays NaN in a cell that then counts as none)
+    cells[cell * THREADS + threadIdx.x] = (uint16_t)((b & 0x80000000u ? b : b + 0xffffu) >> 16);
+}
 
 struct ForwardParams {
     const void* logits;
@@ -441,17 +462,35 @@ __device__ __forceinline__ void st_cluster_u64(const void* local_smem, uint32_t 
 struct Layout {
     int cells, list, few, told, keys, found, words;
     __host__ __device__ Layout(int n_top, int cs) {
-        const int most = n_top > 0 ? most_of(n_top) : 0;
+        const int most = n_top > 0 ? most_of(n_top) : 0, n_cells = n_top > 0 ? cells_of(n_top) : 0;
         cells = 0;
-        told = cells + (n_top > 0 ? CELLS * THREADS / 2 : 0);
-        list = told + 2 * cs;
-        few = list + (n_top > 0 ? CAPACITY : 0);
+        told = cells + n_cells * THREADS / 4;
+        list = told + (cs > 1 ? 2 * cs : 0);
+        few = list + (n_top > 0 ? capacity_of(n_top) : 0);
         keys = few + most;
-        found = keys + cs * n_top;
-        words = found + most * CELLS / 2;
+        found = keys + (cs > 1 ? cs * n_top : 0);
+        words = found + most * n_cells / 4;
     }
 };
-constexpr int TILE_BYTES = UNROLL * THREADS * 16;
+
+// The search as a call of its own: its registers are not the pass's
+template <typename T>
+__device__ __noinline__ int search_stretch(const T* z, int vocab, int lo_j, int hi_j, int per_cell, float top, int n_top, int cs, unsigned long long* words, int* count,
+                                           uint32_t* ends) {
+    const Layout at(n_top, cs);
+    Candidates cand;
+    cand.list = words + at.list;
+    cand.few = words + at.few;
+    cand.cells = reinterpret_cast<uint16_t*>(words + at.cells);
+    cand.found = reinterpret_cast<uint16_t*>(words + at.found);
+    cand.count = count;
+    cand.ends = ends;
+    cand.n_top = n_top;
+    cand.most = most_of(n_top);
+    cand.capacity = capacity_of(n_top);
+    cand.n_cells = cells_of(n_top);
+    return cand.search(Row<T>(z, vocab), lo_j, hi_j, per_cell, top);
+}
 
 // The tiles of a CTA's rows, in order: its stretch of each
 template <typename T, int CS>
@@ -475,25 +514,18 @@ struct Cursor {
 // several: the grid has a cluster for each row.
 template <typename T, int CS>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(const ForwardParams p) {
-    extern __shared__ uint4 ring[];                        // [STAGES][UNROLL][THREADS]: a thread reads what it has copied itself
-    __shared__ Stat sh[THREADS / 32];
-    __shared__ uint32_t ends[2 * THREADS / 32];
+    extern __shared__ uint4 ring[];                        // [STAGES][TILE]: a thread reads what it has copied itself
+    __shared__ Stat sh[WARPS];
+    __shared__ uint32_t ends[2 * WARPS];
     __shared__ int count[2];
-    constexpr int TILE = UNROLL * THREADS;                 // vectors
-    const int tid = threadIdx.x, rank = CS > 1 ? (int)ptx::cluster_ctarank() : 0;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = CS > 1 ? (int)ptx::cluster_ctarank() : 0;
     unsigned long long* words = reinterpret_cast<unsigned long long*>(ring + STAGES * TILE);
     const Layout at(p.n_top, CS);
     Told* told = reinterpret_cast<Told*>(words + at.told);
     unsigned long long* keys = words + at.keys;
-    Candidates cand;
-    cand.list = words + at.list;
-    cand.few = words + at.few;
-    cand.cells = reinterpret_cast<float*>(words + at.cells);
-    cand.found = reinterpret_cast<int*>(words + at.found);
-    cand.count = count;
-    cand.ends = ends;
-    cand.n_top = p.n_top;
-    cand.most = most_of(p.n_top);
+    unsigned long long* list = words + at.list;
+    uint16_t* cells = reinterpret_cast<uint16_t*>(words + at.cells);
+    const int n_cells = cells_of(p.n_top);
     ptx::pdl_trigger();
     ptx::pdl_wait();
     if constexpr (CS > 1) ptx::cluster_arrive();           // (waited for before the first store into another CTA)
@@ -537,8 +569,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
         Running t;
         t.reset();
         float peak = -CUDART_INF_F, cell_top = -CUDART_INF_F;
-        const int tiles = (cur.hi - cur.lo + TILE - 1) / TILE, per_cell = (tiles + CELLS - 1) / CELLS * UNROLL;
-        int cell = 0, cell_end = cur.lo + per_cell * THREADS;
+        const int tiles = (cur.hi - cur.lo + TILE - 1) / TILE, tiles_a_cell = (tiles + n_cells - 1) / n_cells, per_cell = tiles_a_cell * UNROLL;
+        int cell = 0, cell_end = cur.lo + tiles_a_cell * TILE;
         for (int j0 = cur.lo; j0 < cur.hi; j0 += TILE) {
             copy_wait<STAGES - 1>();
             uint4 raw[UNROLL];
@@ -556,21 +588,22 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
                     }
                 }
             }
-            const float top = fmaxf(fmaxf(vec_max(raw[0], T()), vec_max(raw[1], T())), fmaxf(vec_max(raw[2], T()), vec_max(raw[3], T())));
+            float top = vec_max(raw[0], T());
+#pragma unroll
+            for (int u = 1; u < UNROLL; ++u) top = fmaxf(top, vec_max(raw[u], T()));
             if (top > t.limit) t.raise(top, p.c);
             peak = fmaxf(peak, top);
             if (p.n_top > 0) {
                 if (j0 == cell_end) {
                     ++cell;
-                    cell_end += per_cell * THREADS;
+                    cell_end += tiles_a_cell * TILE;
                     cell_top = top;
                 } else {
                     cell_top = fmaxf(cell_top, top);
                 }
-                cand.cells[cell * THREADS + tid] = cell_top;
+                set_cell(cells, cell, cell_top);
             }
-            use += TILE;
-            if (use == ring + tid + STAGES * TILE) use = ring + tid;
+            use = use + TILE == ring + tid + STAGES * TILE ? ring + tid : use + TILE;
             request();                                     // into the place that has just been read
             if (!t.plain) {
 #pragma unroll
@@ -581,20 +614,25 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
             }
         }
         if (p.n_top > 0)
-            for (int k = tiles == 0 ? 0 : cell + 1; k < CELLS; ++k) cand.cells[k * THREADS + tid] = -CUDART_INF_F;
+            for (int k = tiles == 0 ? 0 : cell + 1; k < n_cells; ++k) set_cell(cells, k, -CUDART_INF_F);
         float z_tok = 0.f;
         if (tok >= p.vocab && p.status) atomicOr(p.status, DFLASH_DEV_BAD_TOKEN);
         if (tok >= 0 && tok < p.vocab) z_tok = as_f(reinterpret_cast<const T*>(p.logits)[(int64_t)r * p.ld + tok]);
         // ---- the CTA's results: warp, CTA
         Stat x = lanes_merged<32>(t.total(peak, p.c), p.c);
-        if ((tid & 31) == 0) sh[tid >> 5] = x;
+        if (lane == 0) sh[warp] = x;
         int n_list = 0;
-        if (p.n_top > 0) {
-            n_list = cand.search(row, cur.lo, cur.hi, per_cell, peak);
-        } else {
+        if (p.n_top > 0) n_list = search_stretch(reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld, p.vocab, cur.lo, cur.hi, per_cell, peak, p.n_top, CS, words, count, ends);
+        else __syncthreads();
+        x = lanes_merged<WARPS>(sh[lane % WARPS], p.c);
+        unsigned long long key = tid < n_list ? list[tid] : 0;
+        const int place = tid < n_list ? rank_of(list, n_list, key) : p.n_top;
+        n_list = min(n_list, p.n_top);
+        if constexpr (CS > 1) {
+            __syncthreads();
+            if (place < p.n_top) list[place] = key;
             __syncthreads();
         }
-        x = lanes_merged<THREADS / 32>(sh[tid & (THREADS / 32 - 1)], p.c);
         // ---- the cluster's
         if constexpr (CS > 1) {
             ptx::cluster_wait();                           // every CTA runs
@@ -604,7 +642,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
                 st_cluster_u64(told + rank, tid, w[0]);
                 st_cluster_u64(reinterpret_cast<const char*>(told + rank) + 8, tid, w[1]);
             }
-            for (int i = tid; i < CS * n_list; i += THREADS) st_cluster_u64(keys + rank * p.n_top + i / CS, i % CS, cand.list[i / CS]);
+            for (int i = tid; i < CS * n_list; i += THREADS) st_cluster_u64(keys + rank * p.n_top + i / CS, i % CS, list[i / CS]);
             __syncwarp();
             ptx::cluster_sync_all();                       // no CTA writes into another one after this
             x = Stat{told[0].m, told[0].s, told[0].w};
@@ -630,10 +668,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
             float* lps = p.top_logprob + (int64_t)r * p.n_top;
             int total = n_list;
             if constexpr (CS == 1) {
-                if (tid < n_list) {
-                    const unsigned long long k = cand.list[tid];
-                    ids[tid] = index_of(k);
-                    lps[tid] = (value_of(k) - x.m) / p.temperature - log_sum;
+                if (place < p.n_top) {
+                    ids[place] = index_of(key);
+                    lps[place] = (value_of(key) - x.m) / p.temperature - log_sum;
                 }
             } else {
                 // a key's place in the row: its place in the CTA's own list and the number of larger ones in each other list, one lane a list
@@ -646,7 +683,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
                     int above = 0;
                     unsigned long long k = 0;
                     if (i < n_list) {
-                        k = cand.list[i];
+                        k = list[i];
                         int b = told[q].n, a = 0;          // keys [0, a) of list q are larger, those from b on are not
                         while (a < b) {
                             const int mid = (a + b) / 2;
@@ -672,30 +709,56 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
     }
 }
 
+// The rows by clusters of CS CTAs. Clusters are placed on as few SMs as hold them, while others idle; so a CTA takes a share of
+// the SM's shared memory that leaves room for `per_sm` of them and no more (32 x 151936 bf16, four CTAs a row: 9.8 us with room for four, 6.9 for one).
 template <typename T, int CS>
 cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
-    const int words = Layout(p.n_top, CS).words * 8;
+    constexpr int SM_SMEM = 228 * 1024, CTA_EXTRA = 2048;      // what an SM has, and what a CTA takes beside its dynamic part, rounded up
     static bool attr_set[MAX_DEVICES] = {};
-    const int dev = current_device_slot();
+    static int alone[MAX_DEVICES] = {};                        // clusters that fit at one CTA per SM
+    const int dev = current_device_slot(), words = Layout(p.n_top, CS).words * 8;
     if (dev < 0) return cudaErrorInvalidDevice;
+    const auto kernel = token_logprobs_kernel<T, CS>;
     if (!attr_set[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(token_logprobs_kernel<T, CS>, cudaFuncAttributeMaxDynamicSharedMemorySize, STAGES * TILE_BYTES + Layout(LP_MAX_TOP, CS).words * 8);
+        const int most = SM_SMEM - 1024 - CTA_EXTRA;
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
         if (e != cudaSuccess) return e;
+        int n = sm_count;
+        if (CS > 1) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(CS);
+            cfg.blockDim = dim3(THREADS);
+            cfg.dynamicSmemBytes = most;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = CS;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) n = std::max(1, sm_count / CS);
+        }
+        alone[dev] = n;
         attr_set[dev] = true;
     }
-    const size_t smem = (size_t)STAGES * TILE_BYTES + words;
-    if (CS == 1) return launch_pdl(token_logprobs_kernel<T, CS>, dim3(std::min(p.n_rows, CTAS_PER_SM * sm_count)), dim3(THREADS), smem, st, p);
-    return launch_pdl_cluster(token_logprobs_kernel<T, CS>, dim3(p.n_rows * CS), dim3(THREADS), smem, st, CS, p);
+    const int per_sm = std::max(1, std::min(CTAS_PER_SM, (p.n_rows + alone[dev] - 1) / alone[dev]));
+    const size_t smem = std::max<size_t>((size_t)STAGES * TILE_BYTES + words, per_sm < CTAS_PER_SM ? SM_SMEM / (per_sm + 1) : 0);
+    if (CS == 1) return launch_pdl(kernel, dim3(std::min(p.n_rows, CTAS_PER_SM * sm_count)), dim3(THREADS), smem, st, p);
+    return launch_pdl_cluster(kernel, dim3(p.n_rows * CS), dim3(THREADS), smem, st, CS, p);
 }
 
 template <typename T>
 cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
-    // CTAs per row: what takes the fewest tile times, a CTA's start and end counted as two
-    const int tiles = (p.vocab + UNROLL * THREADS * Row<T>::VE - 1) / (UNROLL * THREADS * Row<T>::VE);
+    // CTAs per row: what takes the least time by a count of tile times. CTAs that share an SM share its rate, so that what counts is how evenly a turn of
+    // CTAs fills the SMs; beside its tiles a turn takes the time of 4 tiles (9 with the search), and a cluster's meeting that of 2 to 4. (A tile time is
+    // 0.46 us. 300 x 151936 bf16 by 1, 2, 4 and 8 CTAs a row: 28, 26, 28 and 39 us, with 20 alternatives 33, 33, 40 and 61; 32 rows 16, 11, 7 and 9; 544 rows
+    // 41, 40, 45 and 66.)
+    const int tiles = (p.vocab + TILE * Row<T>::VE - 1) / (TILE * Row<T>::VE);
+    const int64_t slots = (int64_t)CTAS_PER_SM * sm_count;
     int cs = 1;
     int64_t least = INT64_MAX;
     for (int s = 1; s <= MAX_CLUSTER && s / 2 < tiles; s *= 2) {
-        const int64_t turns = ((int64_t)p.n_rows * s + CTAS_PER_SM * sm_count - 1) / (CTAS_PER_SM * sm_count), time = turns * ((tiles + s - 1) / s + 2);
+        const int64_t n = (int64_t)p.n_rows * s, full = n / slots, last = (n % slots + sm_count - 1) / sm_count, each = (tiles + s - 1) / s;
+        const int64_t time = (full * CTAS_PER_SM + last) * each + (full + (last > 0)) * (p.n_top > 0 ? 9 : 4) + (s == 1 ? 0 : s == 8 ? 4 : 2);
         if (time < least) {
             least = time;
             cs = s;
