@@ -675,7 +675,7 @@ int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_
  * Launches: one per 320 tensors, twice with the norm. Captured calls may be replayed: lr_dev and step_dev are then read at each replay. No two tensors
  * of a call may overlap; calls must not overlap in time if they share tensors or a workspace.
  * Errors: DFLASH_ERR_INVALID_ARG (null pointer, address that is no multiple of the element's size, n < 0, bad dtype or state_bits, a master copy beside an fp32 param,
- * step < 1, betas outside [0, 1), eps or grad_scale not positive), DFLASH_ERR_WORKSPACE (only where the norm is computed). */
+ * step < 1, betas outside [0, 1), eps below 2^-126, grad_scale not positive), DFLASH_ERR_WORKSPACE (only where the norm is computed). */
 typedef struct {
     void*       param;             /* [device] in/out [n] (out only with `master`)              */
     const void* grad;              /* [device] [n]                                              */

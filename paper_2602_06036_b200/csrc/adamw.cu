@@ -40,7 +40,8 @@ struct Tensor {
     int64_t n;
     float lr_wd, step_size;                             // lr * weight_decay; lr / (1 - b1^t), or both without lr and t where those live on the device
     int32_t kind;                                       // Weights * 4 + (gradients bf16) * 2 + (states of 8 bits)
-    int32_t aligned;                                    // every pointer allows its widest access
+    int32_t wide;                                       // entries in groups of four lie on borders that allow one access each,
+    int32_t lead;                                       // those that start `lead` entries in front of the first one
 };
 struct Table {
     Tensor t[MAX_TENSORS];
@@ -58,8 +59,11 @@ struct StepParams {
     int32_t* status;
 };
 
-__device__ __forceinline__ int tensor_of(const Table& tab, int64_t chunk) {
-    int a = 0, b = tab.n;                               // first[a] <= chunk < first[b]
+static_assert(sizeof(Table) + sizeof(StepParams) <= 32764, "the parameters of a launch");
+
+__device__ __forceinline__ int tensor_of(const Table& tab, int64_t chunk, int a) {
+    if (chunk < tab.first[a + 1]) return a;             // (as for the chunk before)
+    int b = tab.n;                                      // first[a] <= chunk < first[b]
     while (b - a > 1) {
         const int mid = (a + b) / 2;
         if (tab.first[mid] <= chunk) a = mid;
@@ -68,60 +72,69 @@ __device__ __forceinline__ int tensor_of(const Table& tab, int64_t chunk) {
     return a;
 }
 
-// ---- 4 neighbouring entries: at `i` of a tensor of n, zeros behind its end -------------------------------------------
-__device__ __forceinline__ void load4(const float* p, int64_t i, int64_t n, bool vec, float (&f)[4]) {
-    if (vec && i + 4 <= n) {
-        const float4 v = __ldcs(reinterpret_cast<const float4*>(p + i));
+// ---- the four entries of a lane in a block: neighbouring ones (WIDE: all of them there and on their border), or lane, lane + 32, ... (some may be outside) ----
+template <bool WIDE>
+__device__ __forceinline__ int entry(int e) { return WIDE ? (int)(threadIdx.x & 31) * 4 + e : (int)(threadIdx.x & 31) + 32 * e; }
+
+template <bool WIDE>
+__device__ __forceinline__ void load4(const float* p, int from, int to, float (&f)[4]) {
+    if constexpr (WIDE) {
+        const float4 v = __ldcs(reinterpret_cast<const float4*>(p) + (threadIdx.x & 31));
         f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = i + e < n ? p[i + e] : 0.f;
+        for (int e = 0; e < 4; ++e) f[e] = entry<false>(e) >= from && entry<false>(e) < to ? p[entry<false>(e)] : 0.f;
     }
 }
-__device__ __forceinline__ void load4(const __nv_bfloat16* p, int64_t i, int64_t n, bool vec, float (&f)[4]) {
-    if (vec && i + 4 <= n) {
-        const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p + i));
+template <bool WIDE>
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, int from, int to, float (&f)[4]) {
+    if constexpr (WIDE) {
+        const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p) + (threadIdx.x & 31));
         f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
         f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = i + e < n ? __bfloat162float(p[i + e]) : 0.f;
+        for (int e = 0; e < 4; ++e) f[e] = entry<false>(e) >= from && entry<false>(e) < to ? __bfloat162float(p[entry<false>(e)]) : 0.f;
     }
 }
-__device__ __forceinline__ void store4(float* p, int64_t i, int64_t n, bool vec, const float (&f)[4]) {
-    if (vec && i + 4 <= n) {
-        __stcs(reinterpret_cast<float4*>(p + i), make_float4(f[0], f[1], f[2], f[3]));
+template <bool WIDE>
+__device__ __forceinline__ void store4(float* p, int from, int to, const float (&f)[4]) {
+    if constexpr (WIDE) {
+        __stcs(reinterpret_cast<float4*>(p) + (threadIdx.x & 31), make_float4(f[0], f[1], f[2], f[3]));
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (i + e < n) p[i + e] = f[e];
+            if (entry<false>(e) >= from && entry<false>(e) < to) p[entry<false>(e)] = f[e];
     }
 }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, int64_t i, int64_t n, bool vec, const float (&f)[4]) {
-    if (vec && i + 4 <= n) {
+template <bool WIDE>
+__device__ __forceinline__ void store4(__nv_bfloat16* p, int from, int to, const float (&f)[4]) {
+    if constexpr (WIDE) {
         const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
-        __stcs(reinterpret_cast<uint2*>(p + i), make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b)));
+        __stcs(reinterpret_cast<uint2*>(p) + (threadIdx.x & 31), make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b)));
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (i + e < n) p[i + e] = __float2bfloat16_rn(f[e]);
+            if (entry<false>(e) >= from && entry<false>(e) < to) p[entry<false>(e)] = __float2bfloat16_rn(f[e]);
     }
 }
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t i, int64_t n, bool vec) {
-    if (vec && i + 4 <= n) return __ldcs(reinterpret_cast<const uint32_t*>(p + i));
+template <bool WIDE>
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int to) {
+    if constexpr (WIDE) return __ldcs(reinterpret_cast<const uint32_t*>(p) + (threadIdx.x & 31));
     uint32_t w = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (i + e < n) w |= (uint32_t)p[i + e] << (8 * e);
+        if (entry<false>(e) < to) w |= (uint32_t)p[entry<false>(e)] << (8 * e);
     return w;
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int64_t n, bool vec, uint32_t w) {
-    if (vec && i + 4 <= n) {
-        __stcs(reinterpret_cast<uint32_t*>(p + i), w);
+template <bool WIDE>
+__device__ __forceinline__ void store_codes(uint8_t* p, int to, uint32_t w) {
+    if constexpr (WIDE) {
+        __stcs(reinterpret_cast<uint32_t*>(p) + (threadIdx.x & 31), w);
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (i + e < n) p[i + e] = (uint8_t)(w >> (8 * e));
+            if (entry<false>(e) < to) p[entry<false>(e)] = (uint8_t)(w >> (8 * e));
     }
 }
 __device__ __forceinline__ void decode(uint32_t w, float scale, float (&f)[4]) {
@@ -142,48 +155,61 @@ __device__ __forceinline__ float scale_of(float top, float& inv) {
     inv = scale > 0.f ? 1.f / scale : 0.f;
     return top < CUDART_INF_F ? scale : CUDART_NAN_F;
 }
-__device__ __forceinline__ float block_top(const float (&f)[4]) {                     // NaN if any is NaN
-    float t = 0.f, bad = 0.f;
+// largest magnitude: magnitudes order like their bits, infinities and then NaN above all numbers
+__device__ __forceinline__ float block_top(const float (&f)[4]) {
+    uint32_t t = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        t = fmaxf(t, fabsf(f[e]));
-        bad = fmaf(f[e], 0.f, bad);                                                    // NaN for NaN and infinities
-    }
-    // magnitudes order like their bits, NaN above all
-    return __uint_as_float(__reduce_max_sync(0xffffffffu, bad == 0.f ? __float_as_uint(t) : 0x7fffffffu));
+    for (int e = 0; e < 4; ++e) t = max(t, __float_as_uint(f[e]) & 0x7fffffffu);
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, t));
+}
+// a / b for b of a normal number's size (2 ulp)
+__device__ __forceinline__ float quotient(float a, float b) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(b));
+    return a * r;
 }
 
-template <int KIND>
+// One chunk: entries at, at + 1, ... of the tensor. WIDE: all of them lie inside.
+// Products and sums of the states are rounded one by one, as the formula is written: a code that lies between two is then rounded alike by whatever else computes it so.
+template <int KIND, bool WIDE>
 __device__ __forceinline__ void step_chunk(const Tensor& t, int64_t at, const StepParams& p, float gs, float lr_wd, float step_size, float rsqrt_bc2) {
     constexpr int W = KIND >> 2;
     constexpr bool G16 = KIND & 2, S8 = KIND & 1, MASTER = W == W_MASTER, P16 = W != W_F32;
     using G = std::conditional_t<G16, __nv_bfloat16, float>;
     using P = std::conditional_t<P16, __nv_bfloat16, float>;
-    const bool vec = t.aligned;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    at += warp * UNROLL * BLOCK;
+    const G* grad = reinterpret_cast<const G*>(t.grad) + at;
+    P* param = reinterpret_cast<P*>(t.param) + at;
+    float* master = MASTER ? t.master + at : nullptr;
+    uint8_t *c1 = reinterpret_cast<uint8_t*>(t.m) + at, *c2 = reinterpret_cast<uint8_t*>(t.v) + at;
+    float *f1 = reinterpret_cast<float*>(t.m) + at, *f2 = reinterpret_cast<float*>(t.v) + at;
+    float *s1 = S8 ? t.m_scale + at / BLOCK : nullptr, *s2 = S8 ? t.v_scale + at / BLOCK : nullptr;
+    // entries of block u that lie inside: [from(u), to(u))
+    const auto from = [&](int u) { return WIDE ? 0 : (int)max(-(at + u * BLOCK), (int64_t)0); };
+    const auto to = [&](int u) { return WIDE ? BLOCK : (int)max(min(t.n - (at + u * BLOCK), (int64_t)BLOCK), (int64_t)0); };
     float g[UNROLL][4], w[UNROLL][4], m[UNROLL][4], v[UNROLL][4];
     uint32_t cm[UNROLL], cv[UNROLL];
     float sm[UNROLL], sv[UNROLL];
-    auto place = [&](int u) { return at + (int64_t)(u * WARPS + warp) * BLOCK + lane * PER_LANE; };
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-        const int64_t i = place(u), b = i / BLOCK;
-        load4(reinterpret_cast<const G*>(t.grad), i, t.n, vec, g[u]);
-        if constexpr (MASTER) load4(t.master, i, t.n, vec, w[u]);
-        else load4(reinterpret_cast<const P*>(t.param), i, t.n, vec, w[u]);
+        const int o = u * BLOCK;
+        load4<WIDE>(grad + o, from(u), to(u), g[u]);
+        if constexpr (MASTER) load4<WIDE>(master + o, from(u), to(u), w[u]);
+        else load4<WIDE>(param + o, from(u), to(u), w[u]);
         if constexpr (S8) {
-            cm[u] = load_codes(reinterpret_cast<const uint8_t*>(t.m), i, t.n, vec);
-            cv[u] = load_codes(reinterpret_cast<const uint8_t*>(t.v), i, t.n, vec);
-            sm[u] = b * BLOCK < t.n ? t.m_scale[b] : 0.f;
-            sv[u] = b * BLOCK < t.n ? t.v_scale[b] : 0.f;
+            cm[u] = load_codes<WIDE>(c1 + o, to(u));
+            cv[u] = load_codes<WIDE>(c2 + o, to(u));
+            sm[u] = to(u) > 0 ? s1[u] : 0.f;
+            sv[u] = to(u) > 0 ? s2[u] : 0.f;
         } else {
-            load4(reinterpret_cast<const float*>(t.m), i, t.n, vec, m[u]);
-            load4(reinterpret_cast<const float*>(t.v), i, t.n, vec, v[u]);
+            load4<WIDE>(f1 + o, from(u), to(u), m[u]);
+            load4<WIDE>(f2 + o, from(u), to(u), v[u]);
         }
     }
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-        const int64_t i = place(u), b = i / BLOCK;
+        const int o = u * BLOCK;
         if constexpr (S8) {
             decode(cm[u], sm[u], m[u]);
             decode(cv[u], sv[u], v[u]);
@@ -193,33 +219,33 @@ __device__ __forceinline__ void step_chunk(const Tensor& t, int64_t at, const St
         float root[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float x = g[u][e] * gs;
-            m[u][e] = fmaf(p.b1, m[u][e], p.one_b1 * x);
-            v[u][e] = fmaf(p.b2, v[u][e], p.one_b2 * x * x);
+            const float x = __fmul_rn(g[u][e], gs);
+            m[u][e] = __fadd_rn(__fmul_rn(p.b1, m[u][e]), __fmul_rn(p.one_b1, x));
+            v[u][e] = __fadd_rn(__fmul_rn(p.b2, v[u][e]), __fmul_rn(p.one_b2, __fmul_rn(x, x)));
             root[e] = sqrtf(v[u][e]);
-            const float d = step_size * m[u][e] / fmaf(root[e], rsqrt_bc2, p.eps);
-            w[u][e] = fmaf(-lr_wd, w[u][e], w[u][e]) - d;
+            w[u][e] = fmaf(-lr_wd, w[u][e], w[u][e]) - quotient(step_size * m[u][e], fmaf(root[e], rsqrt_bc2, p.eps));
         }
-        if constexpr (MASTER) store4(t.master, i, t.n, vec, w[u]);
+        if constexpr (MASTER) store4<WIDE>(master + o, from(u), to(u), w[u]);
         // (the weights that the model reads: their rounding to bf16 is not fed back where there is a master copy)
-        store4(reinterpret_cast<P*>(t.param), i, t.n, vec, w[u]);
+        store4<WIDE>(param + o, from(u), to(u), w[u]);
         if constexpr (S8) {
             float inv;
-            const float s1 = scale_of(block_top(m[u]), inv);
+            const float m_scale = scale_of(block_top(m[u]), inv);
 #pragma unroll
             for (int e = 0; e < 4; ++e) m[u][e] *= inv;
-            store_codes(reinterpret_cast<uint8_t*>(t.m), i, t.n, vec, encode(m[u]));
-            const float s2 = scale_of(block_top(root), inv);
+            store_codes<WIDE>(c1 + o, to(u), encode(m[u]));
+            const float v_scale = scale_of(block_top(root), inv);
+            const float least = inv > 0.f ? 0.001953125f : 0.f;      // 2^-9: the smallest code
 #pragma unroll
-            for (int e = 0; e < 4; ++e) root[e] = root[e] > 0.f && inv > 0.f ? fmaxf(root[e] * inv, 0.001953125f) : 0.f;      // 2^-9: the smallest code
-            store_codes(reinterpret_cast<uint8_t*>(t.v), i, t.n, vec, encode(root));
-            if (lane == 0 && b * BLOCK < t.n) {
-                t.m_scale[b] = s1;
-                t.v_scale[b] = s2;
+            for (int e = 0; e < 4; ++e) root[e] = root[e] > 0.f ? fmaxf(root[e] * inv, least) : 0.f;
+            store_codes<WIDE>(c2 + o, to(u), encode(root));
+            if (lane == 0 && to(u) > 0) {
+                s1[u] = m_scale;
+                s2[u] = v_scale;
             }
         } else {
-            store4(reinterpret_cast<float*>(t.m), i, t.n, vec, m[u]);
-            store4(reinterpret_cast<float*>(t.v), i, t.n, vec, v[u]);
+            store4<WIDE>(f1 + o, from(u), to(u), m[u]);
+            store4<WIDE>(f2 + o, from(u), to(u), v[u]);
         }
     }
 }
@@ -266,14 +292,18 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) adamw_kernel(const __gri
         rsqrt_bc2 = s_bc[1];
     }
     const float wd_lr = p.lr ? *p.lr : 1.f;
-    int64_t chunks = tab.first[tab.n];
+    const int64_t chunks = tab.first[tab.n];
+    int k = 0;
     for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int k = tensor_of(tab, c);
+        k = tensor_of(tab, c, k);
         const Tensor& t = tab.t[k];
-        const int64_t at = (c - tab.first[k]) * CHUNK;
+        const int64_t at = (c - tab.first[k]) * CHUNK - t.lead;
         const float lr_wd = t.lr_wd * wd_lr, step_size = t.step_size * lr;
-        switch (t.kind) {
-#define DFLASH_ADAMW_CASE(K) case K: step_chunk<K>(t, at, p, gs, lr_wd, step_size, rsqrt_bc2); break;
+        const bool wide = t.wide && at >= 0 && at + CHUNK <= t.n;
+        switch (t.kind * 2 + wide) {
+#define DFLASH_ADAMW_CASE(K)                                                              \
+    case 2 * K: step_chunk<K, false>(t, at, p, gs, lr_wd, step_size, rsqrt_bc2); break;   \
+    case 2 * K + 1: step_chunk<K, true>(t, at, p, gs, lr_wd, step_size, rsqrt_bc2); break;
             DFLASH_ADAMW_CASE(0) DFLASH_ADAMW_CASE(1) DFLASH_ADAMW_CASE(2) DFLASH_ADAMW_CASE(3)
             DFLASH_ADAMW_CASE(4) DFLASH_ADAMW_CASE(5) DFLASH_ADAMW_CASE(6) DFLASH_ADAMW_CASE(7)
             DFLASH_ADAMW_CASE(8) DFLASH_ADAMW_CASE(9) DFLASH_ADAMW_CASE(10) DFLASH_ADAMW_CASE(11)
@@ -289,20 +319,31 @@ __global__ void __launch_bounds__(THREADS, NORM_CTAS_PER_SM) adamw_norm_kernel(c
     ptx::pdl_wait();
     double sum = 0.0;
     const int64_t chunks = tab.first[tab.n];
-    constexpr int TURN = THREADS * PER_LANE;
+    constexpr int GROUPS = CHUNK / (WARPS * BLOCK);
+    int k = 0;
     for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int k = tensor_of(tab, c);
+        k = tensor_of(tab, c, k);
         const Tensor& t = tab.t[k];
-        const int64_t at = (c - tab.first[k]) * CHUNK + threadIdx.x * PER_LANE;
-        float s = 0.f;
-        float g[CHUNK / TURN][4];
+        const int64_t at = (c - tab.first[k]) * CHUNK - t.lead;
+        const bool wide = t.wide && at >= 0 && at + CHUNK <= t.n;
+        float g[GROUPS][4];
 #pragma unroll
-        for (int u = 0; u < CHUNK / TURN; ++u) {
-            if (t.kind & 2) load4(reinterpret_cast<const __nv_bfloat16*>(t.grad), at + u * TURN, t.n, t.aligned, g[u]);
-            else load4(reinterpret_cast<const float*>(t.grad), at + u * TURN, t.n, t.aligned, g[u]);
+        for (int u = 0; u < GROUPS; ++u) {
+            const int64_t o = at + (u * WARPS + (threadIdx.x >> 5)) * BLOCK;
+            const int from = (int)max(-o, (int64_t)0), to = (int)max(min(t.n - o, (int64_t)BLOCK), (int64_t)0);
+            if (t.kind & 2) {
+                const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(t.grad) + o;
+                if (wide) load4<true>(p, 0, BLOCK, g[u]);
+                else load4<false>(p, from, to, g[u]);
+            } else {
+                const float* p = reinterpret_cast<const float*>(t.grad) + o;
+                if (wide) load4<true>(p, 0, BLOCK, g[u]);
+                else load4<false>(p, from, to, g[u]);
+            }
         }
+        float s = 0.f;
 #pragma unroll
-        for (int u = 0; u < CHUNK / TURN; ++u)
+        for (int u = 0; u < GROUPS; ++u)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s = fmaf(g[u][e], g[u][e], s);
         sum += (double)s;
@@ -310,8 +351,6 @@ __global__ void __launch_bounds__(THREADS, NORM_CTAS_PER_SM) adamw_norm_kernel(c
     sum = cta_sum(sum, sh);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
-
-bool on(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 }  // namespace
 
@@ -344,9 +383,15 @@ int launch_adamw(const Launch& L, const dflash_adamw_args& a) {
             t.lr_wd = (float)(lr * s.weight_decay * s.lr_scale);
             t.step_size = (float)(lr * s.lr_scale / bc1);
             t.kind = (s.master ? W_MASTER : p16 ? W_BF16 : W_F32) * 4 + g16 * 2 + s8;
-            t.aligned = on(s.param, p16 ? 8 : 16) && on(s.grad, g16 ? 8 : 16) && on(s.master, 16) && on(s.exp_avg, s8 ? 4 : 16) && on(s.exp_avg_sq, s8 ? 4 : 16);
+            // entries in front of the first one to the next border, by the weights; the same has to do for the others. (The blocks of an 8-bit state start with the
+            // tensor.)
+            const int pb = p16 ? 2 : 4, gb = g16 ? 2 : 4, sb = s8 ? 1 : 4;
+            t.lead = s8 ? 0 : (int)((reinterpret_cast<uintptr_t>(s.param) / pb) & 3);
+            const auto border = [&](const void* q, int bytes) { return !q || (reinterpret_cast<uintptr_t>(q) - (uintptr_t)t.lead * bytes) % (4 * bytes) == 0; };
+            t.wide = border(s.param, pb) && border(s.grad, gb) && border(s.master, 4) && border(s.exp_avg, sb) && border(s.exp_avg_sq, sb);
+            if (!t.wide) t.lead = 0;
             tab.first[i] = chunks;
-            chunks += (s.n + CHUNK - 1) / CHUNK;
+            chunks += s.n > 0 ? (s.n + t.lead + CHUNK - 1) / CHUNK : 0;
         }
         tab.first[n] = chunks;
         tab.n = n;

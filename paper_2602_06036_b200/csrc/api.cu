@@ -846,7 +846,7 @@ int64_t dflash_adamw_workspace_bytes(const dflash_handle* h, int32_t n_tensors) 
 
 int32_t dflash_adamw_step(dflash_handle* h, const dflash_adamw_args* a, void* stream) {
     if (!h || !a || a->n_tensors < 0 || (a->n_tensors > 0 && !a->tensors)) return DFLASH_ERR_INVALID_ARG;
-    if (!(a->beta1 >= 0.0 && a->beta1 < 1.0 && a->beta2 >= 0.0 && a->beta2 < 1.0) || !((float)a->eps > 0.f) || !std::isfinite((float)a->eps) || !((float)a->grad_scale > 0.f) ||
+    if (!(a->beta1 >= 0.0 && a->beta1 < 1.0 && a->beta2 >= 0.0 && a->beta2 < 1.0) || !((float)a->eps >= 1.17549435e-38f) || !std::isfinite((float)a->eps) || !((float)a->grad_scale > 0.f) ||
         !std::isfinite((float)a->grad_scale) || std::isnan(a->max_grad_norm))
         return DFLASH_ERR_INVALID_ARG;
     if ((!a->step_dev && a->step < 1) || (!a->lr_dev && !std::isfinite((float)a->lr))) return DFLASH_ERR_INVALID_ARG;
