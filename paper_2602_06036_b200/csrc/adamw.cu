@@ -24,9 +24,10 @@ namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32, PER_LANE = 4;
 constexpr int BLOCK = 32 * PER_LANE;                    // entries of a warp's turn, and of an 8-bit state that share a scale
-constexpr int UNROLL = 2;                               // blocks of a warp under way
+constexpr int UNROLL = 4;                               // blocks of a warp under way
 constexpr int CHUNK = WARPS * UNROLL * BLOCK;           // 2048
-constexpr int CTAS_PER_SM = 4, NORM_CTAS_PER_SM = 4;
+constexpr int CTAS_PER_SM = 2, NORM_CTAS_PER_SM = 4;
+constexpr int NORM_UNROLL = 4, NORM_BYTES = NORM_UNROLL * THREADS * 16;      // of a chunk of gradients
 constexpr int MAX_TENSORS = 320;                        // descriptors of a launch: 28 KB of its 32 KB of parameters
 
 enum Weights { W_F32 = 0, W_BF16 = 1, W_MASTER = 2 };      // fp32, bf16, bf16 with a master copy in fp32
@@ -45,8 +46,8 @@ struct Tensor {
 };
 struct Table {
     Tensor t[MAX_TENSORS];
-    int64_t first[MAX_TENSORS + 1];                     // chunks in front of each tensor
-    int32_t n;
+    int64_t first[MAX_TENSORS + 1];                     // spans in front of each tensor
+    int32_t n, span;                                    // a span: so many chunks one behind the other
 };
 struct StepParams {
     const double* partial;                              // [n_partial] sums of squared gradients, or nullptr: no norm
@@ -151,16 +152,16 @@ __device__ __forceinline__ uint32_t encode(const float (&f)[4]) {
 // The scale of a block whose largest magnitude is `top` (all lanes), and what its entries are multiplied by. A block that holds NaN or an
 // infinity gets the scale NaN, one below 2^-117 the scale 0 (its own would no longer be a normal number).
 __device__ __forceinline__ float scale_of(float top, float& inv) {
-    const float scale = top < 6.0185e-36f ? 0.f : top / 448.f;
+    const float scale = top < 6.0185e-36f ? 0.f : top * (1.f / 448.f);
     inv = scale > 0.f ? 1.f / scale : 0.f;
     return top < CUDART_INF_F ? scale : CUDART_NAN_F;
 }
-// largest magnitude: magnitudes order like their bits, infinities and then NaN above all numbers
-__device__ __forceinline__ float block_top(const float (&f)[4]) {
+// largest magnitude, as its bits: magnitudes order like them, infinities and then NaN above all numbers
+__device__ __forceinline__ uint32_t block_top(const float (&f)[4]) {
     uint32_t t = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) t = max(t, __float_as_uint(f[e]) & 0x7fffffffu);
-    return __uint_as_float(__reduce_max_sync(0xffffffffu, t));
+    return __reduce_max_sync(0xffffffffu, t);
 }
 // a / b for b of a normal number's size (2 ulp)
 __device__ __forceinline__ float quotient(float a, float b) {
@@ -169,44 +170,61 @@ __device__ __forceinline__ float quotient(float a, float b) {
     return a * r;
 }
 
-// One chunk: entries at, at + 1, ... of the tensor. WIDE: all of them lie inside.
-// Products and sums of the states are rounded one by one, as the formula is written: a code that lies between two is then rounded alike by whatever else computes it so.
-template <int KIND, bool WIDE>
-__device__ __forceinline__ void step_chunk(const Tensor& t, int64_t at, const StepParams& p, float gs, float lr_wd, float step_size, float rsqrt_bc2) {
-    constexpr int W = KIND >> 2;
-    constexpr bool G16 = KIND & 2, S8 = KIND & 1, MASTER = W == W_MASTER, P16 = W != W_F32;
+// What a thread needs of a tensor, at its warp's first block of a chunk
+template <int KIND>
+struct Place {
+    static constexpr int W = KIND >> 2;
+    static constexpr bool G16 = KIND & 2, S8 = KIND & 1, MASTER = W == W_MASTER, P16 = W != W_F32;
     using G = std::conditional_t<G16, __nv_bfloat16, float>;
     using P = std::conditional_t<P16, __nv_bfloat16, float>;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    at += warp * UNROLL * BLOCK;
-    const G* grad = reinterpret_cast<const G*>(t.grad) + at;
-    P* param = reinterpret_cast<P*>(t.param) + at;
-    float* master = MASTER ? t.master + at : nullptr;
-    uint8_t *c1 = reinterpret_cast<uint8_t*>(t.m) + at, *c2 = reinterpret_cast<uint8_t*>(t.v) + at;
-    float *f1 = reinterpret_cast<float*>(t.m) + at, *f2 = reinterpret_cast<float*>(t.v) + at;
-    float *s1 = S8 ? t.m_scale + at / BLOCK : nullptr, *s2 = S8 ? t.v_scale + at / BLOCK : nullptr;
+    using S = std::conditional_t<S8, uint8_t, float>;
+    const G* grad;
+    P* param;
+    float* master;
+    S *m, *v;
+    float *m_scale, *v_scale;
+    __device__ __forceinline__ Place(const Tensor& t, int64_t at)
+        : grad(reinterpret_cast<const G*>(t.grad) + at), param(reinterpret_cast<P*>(t.param) + at), master(MASTER ? t.master + at : nullptr),
+          m(reinterpret_cast<S*>(t.m) + at), v(reinterpret_cast<S*>(t.v) + at), m_scale(S8 ? t.m_scale + at / BLOCK : nullptr), v_scale(S8 ? t.v_scale + at / BLOCK : nullptr) {}
+    __device__ __forceinline__ void next_chunk() {
+        grad += CHUNK; param += CHUNK; m += CHUNK; v += CHUNK;
+        if constexpr (MASTER) master += CHUNK;
+        if constexpr (S8) { m_scale += CHUNK / BLOCK; v_scale += CHUNK / BLOCK; }
+    }
+};
+struct Rates {
+    float gs, lr_wd, step_size, rsqrt_bc2;
+};
+
+// The warp's blocks of one chunk; at: their first entry's place in the tensor of n. WIDE: all of them lie inside.
+// Products and sums of the states are rounded one by one, as the formula is written: a code that lies between two is then rounded alike by whatever else computes it so.
+template <int KIND, bool WIDE>
+__device__ __forceinline__ void step_blocks(const Place<KIND>& q, int64_t at, int64_t n, const StepParams& p, const Rates& r) {
+    constexpr bool S8 = Place<KIND>::S8, MASTER = Place<KIND>::MASTER;
+    const int lane = threadIdx.x & 31;
     // entries of block u that lie inside: [from(u), to(u))
     const auto from = [&](int u) { return WIDE ? 0 : (int)max(-(at + u * BLOCK), (int64_t)0); };
-    const auto to = [&](int u) { return WIDE ? BLOCK : (int)max(min(t.n - (at + u * BLOCK), (int64_t)BLOCK), (int64_t)0); };
+    const auto to = [&](int u) { return WIDE ? BLOCK : (int)max(min(n - (at + u * BLOCK), (int64_t)BLOCK), (int64_t)0); };
     float g[UNROLL][4], w[UNROLL][4], m[UNROLL][4], v[UNROLL][4];
     uint32_t cm[UNROLL], cv[UNROLL];
     float sm[UNROLL], sv[UNROLL];
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
         const int o = u * BLOCK;
-        load4<WIDE>(grad + o, from(u), to(u), g[u]);
-        if constexpr (MASTER) load4<WIDE>(master + o, from(u), to(u), w[u]);
-        else load4<WIDE>(param + o, from(u), to(u), w[u]);
+        load4<WIDE>(q.grad + o, from(u), to(u), g[u]);
+        if constexpr (MASTER) load4<WIDE>(q.master + o, from(u), to(u), w[u]);
+        else load4<WIDE>(q.param + o, from(u), to(u), w[u]);
         if constexpr (S8) {
-            cm[u] = load_codes<WIDE>(c1 + o, to(u));
-            cv[u] = load_codes<WIDE>(c2 + o, to(u));
-            sm[u] = to(u) > 0 ? s1[u] : 0.f;
-            sv[u] = to(u) > 0 ? s2[u] : 0.f;
+            cm[u] = load_codes<WIDE>(q.m + o, to(u));
+            cv[u] = load_codes<WIDE>(q.v + o, to(u));
+            sm[u] = to(u) > 0 ? q.m_scale[u] : 0.f;
+            sv[u] = to(u) > 0 ? q.v_scale[u] : 0.f;
         } else {
-            load4<WIDE>(f1 + o, from(u), to(u), m[u]);
-            load4<WIDE>(f2 + o, from(u), to(u), v[u]);
+            load4<WIDE>(q.m + o, from(u), to(u), m[u]);
+            load4<WIDE>(q.v + o, from(u), to(u), v[u]);
         }
     }
+    uint32_t tops[2 * UNROLL];                          // largest magnitudes of m, and roots of v, of each block
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
         const int o = u * BLOCK;
@@ -216,37 +234,60 @@ __device__ __forceinline__ void step_chunk(const Tensor& t, int64_t at, const St
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[u][e] *= v[u][e];
         }
-        float root[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float x = __fmul_rn(g[u][e], gs);
+            const float x = __fmul_rn(g[u][e], r.gs);
             m[u][e] = __fadd_rn(__fmul_rn(p.b1, m[u][e]), __fmul_rn(p.one_b1, x));
             v[u][e] = __fadd_rn(__fmul_rn(p.b2, v[u][e]), __fmul_rn(p.one_b2, __fmul_rn(x, x)));
-            root[e] = sqrtf(v[u][e]);
-            w[u][e] = fmaf(-lr_wd, w[u][e], w[u][e]) - quotient(step_size * m[u][e], fmaf(root[e], rsqrt_bc2, p.eps));
+            const float root = sqrtf(v[u][e]);
+            w[u][e] = fmaf(-r.lr_wd, w[u][e], w[u][e]) - quotient(r.step_size * m[u][e], fmaf(root, r.rsqrt_bc2, p.eps));
+            if constexpr (S8) v[u][e] = root;
         }
-        if constexpr (MASTER) store4<WIDE>(master + o, from(u), to(u), w[u]);
+        if constexpr (MASTER) store4<WIDE>(q.master + o, from(u), to(u), w[u]);
         // (the weights that the model reads: their rounding to bf16 is not fed back where there is a master copy)
-        store4<WIDE>(param + o, from(u), to(u), w[u]);
+        store4<WIDE>(q.param + o, from(u), to(u), w[u]);
         if constexpr (S8) {
-            float inv;
-            const float m_scale = scale_of(block_top(m[u]), inv);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) m[u][e] *= inv;
-            store_codes<WIDE>(c1 + o, to(u), encode(m[u]));
-            const float v_scale = scale_of(block_top(root), inv);
-            const float least = inv > 0.f ? 0.001953125f : 0.f;      // 2^-9: the smallest code
-#pragma unroll
-            for (int e = 0; e < 4; ++e) root[e] = root[e] > 0.f ? fmaxf(root[e] * inv, least) : 0.f;
-            store_codes<WIDE>(c2 + o, to(u), encode(root));
-            if (lane == 0 && to(u) > 0) {
-                s1[u] = m_scale;
-                s2[u] = v_scale;
-            }
+            tops[2 * u] = block_top(m[u]);
+            tops[2 * u + 1] = block_top(v[u]);
         } else {
-            store4<WIDE>(f1 + o, from(u), to(u), m[u]);
-            store4<WIDE>(f2 + o, from(u), to(u), v[u]);
+            store4<WIDE>(q.m + o, from(u), to(u), m[u]);
+            store4<WIDE>(q.v + o, from(u), to(u), v[u]);
         }
+    }
+    if constexpr (S8) {
+        // a share of the lanes works out each scale, and what entries are multiplied by
+        constexpr int SHARE = 32 / (2 * UNROLL);
+        uint32_t top = tops[0];
+#pragma unroll
+        for (int k = 1; k < 2 * UNROLL; ++k) top = lane / SHARE == k ? tops[k] : top;
+        float inv;
+        const float scale = scale_of(__uint_as_float(top), inv);
+        if (lane % SHARE == 0 && to(lane / SHARE / 2) > 0) (lane / SHARE % 2 ? q.v_scale : q.m_scale)[lane / SHARE / 2] = scale;
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const float im = __shfl_sync(0xffffffffu, inv, 2 * u * SHARE), iv = __shfl_sync(0xffffffffu, inv, (2 * u + 1) * SHARE);
+            const float least = iv > 0.f ? 0.001953125f : 0.f;      // 2^-9: the smallest code
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                m[u][e] *= im;
+                v[u][e] = v[u][e] > 0.f ? fmaxf(v[u][e] * iv, least) : 0.f;
+            }
+            store_codes<WIDE>(q.m + u * BLOCK, to(u), encode(m[u]));
+            store_codes<WIDE>(q.v + u * BLOCK, to(u), encode(v[u]));
+        }
+    }
+}
+
+// `chunks` chunks from entry `at` of the tensor on
+template <int KIND>
+__device__ __forceinline__ void step_chunks(const Tensor& t, int64_t at, int chunks, const StepParams& p, const Rates& r) {
+    const int first = (threadIdx.x >> 5) * UNROLL * BLOCK;
+    const int64_t n = t.n;
+    const bool can = t.wide;
+    Place<KIND> q(t, at + first);
+    for (; chunks > 0 && at < n; --chunks, at += CHUNK, q.next_chunk()) {
+        if (can && at >= 0 && at + CHUNK <= n) step_blocks<KIND, true>(q, at + first, n, p, r);
+        else step_blocks<KIND, false>(q, at + first, n, p, r);
     }
 }
 
@@ -262,7 +303,7 @@ __device__ __forceinline__ double cta_sum(double x, double* sh) {
     return s;
 }
 
-__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) adamw_kernel(const __grid_constant__ Table tab, const StepParams p) {
+__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) adamw_kernel(const __grid_constant__ Table tab, const __grid_constant__ StepParams p) {
     __shared__ double sh[WARPS];
     __shared__ float s_bc[2];
     ptx::pdl_trigger();
@@ -297,13 +338,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) adamw_kernel(const __gri
     for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
         k = tensor_of(tab, c, k);
         const Tensor& t = tab.t[k];
-        const int64_t at = (c - tab.first[k]) * CHUNK - t.lead;
-        const float lr_wd = t.lr_wd * wd_lr, step_size = t.step_size * lr;
-        const bool wide = t.wide && at >= 0 && at + CHUNK <= t.n;
-        switch (t.kind * 2 + wide) {
-#define DFLASH_ADAMW_CASE(K)                                                              \
-    case 2 * K: step_chunk<K, false>(t, at, p, gs, lr_wd, step_size, rsqrt_bc2); break;   \
-    case 2 * K + 1: step_chunk<K, true>(t, at, p, gs, lr_wd, step_size, rsqrt_bc2); break;
+        const int64_t at = (c - tab.first[k]) * CHUNK * tab.span - t.lead;
+        const Rates r{gs, t.lr_wd * wd_lr, t.step_size * lr, rsqrt_bc2};
+        switch (t.kind) {
+#define DFLASH_ADAMW_CASE(K) case K: step_chunks<K>(t, at, tab.span, p, r); break;
             DFLASH_ADAMW_CASE(0) DFLASH_ADAMW_CASE(1) DFLASH_ADAMW_CASE(2) DFLASH_ADAMW_CASE(3)
             DFLASH_ADAMW_CASE(4) DFLASH_ADAMW_CASE(5) DFLASH_ADAMW_CASE(6) DFLASH_ADAMW_CASE(7)
             DFLASH_ADAMW_CASE(8) DFLASH_ADAMW_CASE(9) DFLASH_ADAMW_CASE(10) DFLASH_ADAMW_CASE(11)
@@ -312,40 +350,63 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) adamw_kernel(const __gri
     }
 }
 
-// partial[blockIdx.x] = sum of the squares of the gradients in this CTA's chunks
+// sum of the squares of the entries [from, to) of 16-byte vectors at p, NORM_UNROLL a thread and THREADS apart
+template <typename G, bool WIDE>
+__device__ __forceinline__ float squares(const G* p, int64_t from, int64_t to) {
+    constexpr int VE = 16 / (int)sizeof(G);
+    float s = 0.f;
+    uint4 raw[NORM_UNROLL];
+#pragma unroll
+    for (int u = 0; u < NORM_UNROLL; ++u) {
+        const int64_t i = (int64_t)(u * THREADS + threadIdx.x) * VE;
+        raw[u] = make_uint4(0, 0, 0, 0);
+        if (WIDE || (i >= from && i + VE <= to)) {
+            raw[u] = *reinterpret_cast<const uint4*>(p + i);       // (read again by the step: kept in L2 as far as it goes)
+        } else {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                if (i + e < from || i + e >= to) continue;
+                const float x = (float)p[i + e];
+                s = fmaf(x, x, s);
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < NORM_UNROLL; ++u) {
+        const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (sizeof(G) == 4) {
+                s = fmaf(__uint_as_float(w[k]), __uint_as_float(w[k]), s);
+            } else {
+                const float x = __uint_as_float(w[k] << 16), y = __uint_as_float(w[k] & 0xffff0000u);
+                s = fmaf(x, x, s);
+                s = fmaf(y, y, s);
+            }
+        }
+    }
+    return s;
+}
+
+// partial[blockIdx.x] = sum of the squares of the gradients in this CTA's chunks. In the table a chunk has NORM_BYTES, and `lead` entries lie between
+// a gradient's start and the 16-byte border in front of it. The few squares of a thread and chunk are added up in fp32, those sums in double.
 __global__ void __launch_bounds__(THREADS, NORM_CTAS_PER_SM) adamw_norm_kernel(const __grid_constant__ Table tab, double* __restrict__ partial) {
     __shared__ double sh[WARPS];
     ptx::pdl_trigger();
     ptx::pdl_wait();
     double sum = 0.0;
     const int64_t chunks = tab.first[tab.n];
-    constexpr int GROUPS = CHUNK / (WARPS * BLOCK);
     int k = 0;
     for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
         k = tensor_of(tab, c, k);
         const Tensor& t = tab.t[k];
-        const int64_t at = (c - tab.first[k]) * CHUNK - t.lead;
-        const bool wide = t.wide && at >= 0 && at + CHUNK <= t.n;
-        float g[GROUPS][4];
-#pragma unroll
-        for (int u = 0; u < GROUPS; ++u) {
-            const int64_t o = at + (u * WARPS + (threadIdx.x >> 5)) * BLOCK;
-            const int from = (int)max(-o, (int64_t)0), to = (int)max(min(t.n - o, (int64_t)BLOCK), (int64_t)0);
-            if (t.kind & 2) {
-                const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(t.grad) + o;
-                if (wide) load4<true>(p, 0, BLOCK, g[u]);
-                else load4<false>(p, from, to, g[u]);
-            } else {
-                const float* p = reinterpret_cast<const float*>(t.grad) + o;
-                if (wide) load4<true>(p, 0, BLOCK, g[u]);
-                else load4<false>(p, from, to, g[u]);
-            }
-        }
-        float s = 0.f;
-#pragma unroll
-        for (int u = 0; u < GROUPS; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s = fmaf(g[u][e], g[u][e], s);
+        const int es = t.kind & 2 ? 2 : 4, size = NORM_BYTES / es;
+        const int64_t at = (c - tab.first[k]) * size - t.lead, from = -at, to = t.n - at;
+        const bool wide = from <= 0 && to >= size;
+        const char* p = reinterpret_cast<const char*>(t.grad) + at * es;
+        float s;
+        if (t.kind & 2) s = wide ? squares<__nv_bfloat16, true>(reinterpret_cast<const __nv_bfloat16*>(p), from, to) : squares<__nv_bfloat16, false>(reinterpret_cast<const __nv_bfloat16*>(p), from, to);
+        else s = wide ? squares<float, true>(reinterpret_cast<const float*>(p), from, to) : squares<float, false>(reinterpret_cast<const float*>(p), from, to);
         sum += (double)s;
     }
     sum = cta_sum(sum, sh);
@@ -371,9 +432,12 @@ int launch_adamw(const Launch& L, const dflash_adamw_args& a) {
     const double bc1 = a.step_dev ? 1.0 : -std::expm1(a.step * p.ln_b1), bc2 = a.step_dev ? 1.0 : -std::expm1(a.step * p.ln_b2);
     p.rsqrt_bc2 = (float)(1.0 / std::sqrt(bc2));
     const double lr = a.lr_dev ? 1.0 : a.lr;
-    const auto table = [&](int l, Table& tab) {
+    const auto table = [&](int l, bool for_norm, Table& tab) {
         const int from = l * MAX_TENSORS, n = std::min(MAX_TENSORS, a.n_tensors - from);
-        int64_t chunks = 0;
+        int64_t chunks = 0, entries = 0;
+        for (int i = 0; i < n; ++i) entries += a.tensors[from + i].n;
+        // four chunks one behind the other share a look at the table and the addresses, where that leaves every CTA several turns
+        tab.span = entries >= (int64_t)64 * CHUNK * CTAS_PER_SM * L.h->sm_count ? 4 : 1;
         for (int i = 0; i < n; ++i) {
             const dflash_adamw_tensor& s = a.tensors[from + i];
             Tensor& t = tab.t[i];
@@ -390,8 +454,10 @@ int launch_adamw(const Launch& L, const dflash_adamw_args& a) {
             const auto border = [&](const void* q, int bytes) { return !q || (reinterpret_cast<uintptr_t>(q) - (uintptr_t)t.lead * bytes) % (4 * bytes) == 0; };
             t.wide = border(s.param, pb) && border(s.grad, gb) && border(s.master, 4) && border(s.exp_avg, sb) && border(s.exp_avg_sq, sb);
             if (!t.wide) t.lead = 0;
+            if (for_norm) t.lead = (int)((reinterpret_cast<uintptr_t>(s.grad) & 15) / gb);
+            const int64_t size = for_norm ? NORM_BYTES / gb : (int64_t)CHUNK * tab.span;
             tab.first[i] = chunks;
-            chunks += s.n > 0 ? (s.n + t.lead + CHUNK - 1) / CHUNK : 0;
+            chunks += s.n > 0 ? (s.n + t.lead + size - 1) / size : 0;
         }
         tab.first[n] = chunks;
         tab.n = n;
@@ -403,14 +469,14 @@ int launch_adamw(const Launch& L, const dflash_adamw_args& a) {
         double* partial = reinterpret_cast<double*>(a.workspace);
         p.partial = partial;
         for (int l = 0; l < launches; ++l) {
-            const unsigned g = grid(table(l, tab), NORM_CTAS_PER_SM);
+            const unsigned g = grid(table(l, true, tab), NORM_CTAS_PER_SM);
             if (launch_pdl(adamw_norm_kernel, dim3(g), dim3(THREADS), 0, L.st, tab, partial + p.n_partial) != cudaSuccess) return DFLASH_ERR_CUDA;
             p.n_partial += (int)g;
             g_launches += 1;
         }
     }
     for (int l = 0; l < launches; ++l) {
-        const int64_t chunks = table(l, tab);
+        const int64_t chunks = table(l, false, tab);
         if (launch_pdl(adamw_kernel, dim3(grid(chunks, CTAS_PER_SM)), dim3(THREADS), 0, L.st, tab, p) != cudaSuccess) return DFLASH_ERR_CUDA;
         p.norm_out = nullptr;
         g_launches += 1;

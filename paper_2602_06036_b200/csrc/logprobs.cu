@@ -142,8 +142,9 @@ __device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigne
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
-// A thread's running sums of 2^y and 2^y y, those of even and odd entries apart, y = (z - m) c + rest: m is the largest entry of some tile, and it is not
-// raised before an entry lies 2^60 terms above it, so that tiles after the first hardly ever do. y = z c - r by one fused operation, with r = m c rounded and rest
+// A thread's running sums of 2^y and 2^y y, those of even and odd entries apart, y = (z - m) c + rest: m is the largest entry of a warp's tile, and it is not
+// raised before an entry's term is above 2^3, so that tiles after the first seldom do. (Where m is far below the maximum, the sum of 2^y y is all but
+// taken off again in the end: terms of 2^14 cost the entropy a decimal.) A tile's terms are added up on their own first. y = z c - r by one fused operation, with r = m c rounded and rest
 // = m c - r, which is exact; the size of m does not touch the terms. Entries below LOW, -inf among them, count as LOW: their terms are 0, and
 // y has to be finite. Where any of that does not hold (a maximum near LOW or that large that `rest` is no small number, a temperature of an extreme size), `plain`
 // terms take the differences one by one.
@@ -177,7 +178,7 @@ struct Running {
     __device__ __forceinline__ void raise(float to, float c) {
         const float old = m, old_rest = rest, r = to * c;
         m = to;
-        limit = to + 60.f / c;
+        limit = to + 3.f / c;
         plain = !(fabsf(r) < 1048576.f && c < 1.0e8f && c > 1.0e-20f);
         neg_r = -r;
         rest = plain ? 0.f : fmaf(to, c, -r);
@@ -187,19 +188,25 @@ struct Running {
         w = pair((b.x + a.x * d) * f, (b.y + a.y * d) * f);
     }
     template <typename T>
-    __device__ __forceinline__ void add(const uint4& v, float c) {
+    __device__ __forceinline__ void add(const uint4 (&raw)[UNROLL], float c) {
         constexpr int N = 16 / (int)sizeof(T);
-        float f[N];
-        unpack16(not_below_low(v, T()), f, T());
         const unsigned long long cc = pair(c, c), rr = pair(neg_r, neg_r);
+        unsigned long long ts = 0, tw = 0;
 #pragma unroll
-        for (int e = 0; e < N; e += 2) {
-            const unsigned long long y = fma2(pair(f[e], f[e + 1]), cc, rr);
-            const float2 yy = halves(y);
-            const unsigned long long x = pair(fast_exp2(yy.x), fast_exp2(yy.y));
-            s = add2(s, x);
-            w = fma2(x, y, w);
+        for (int u = 0; u < UNROLL; ++u) {
+            float f[N];
+            unpack16(not_below_low(raw[u], T()), f, T());
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const unsigned long long y = fma2(pair(f[e], f[e + 1]), cc, rr);
+                const float2 yy = halves(y);
+                const unsigned long long x = pair(fast_exp2(yy.x), fast_exp2(yy.y));
+                ts = add2(ts, x);
+                tw = fma2(x, y, tw);
+            }
         }
+        s = add2(s, ts);
+        w = add2(w, tw);
     }
     template <typename T>
     __device__ __forceinline__ void add_plain(const uint4& v, float c) {
@@ -217,11 +224,11 @@ struct Running {
         s = pair(a.x, a.y);
         w = pair(b.x, b.y);
     }
-    // with `top`, the largest entry so far, in the place of m
+    // with `top`, the thread's largest entry, in the place of a smaller m
     __device__ __forceinline__ Stat total(float top, float c) const {
         const float2 a = halves(s), b = halves(w);
         const float f = fast_exp2(-rest), sum = a.x + a.y;
-        return raised(Stat{m, sum * f, (b.x + b.y - sum * rest) * f}, top, c);
+        return raised(Stat{m, sum * f, (b.x + b.y - sum * rest) * f}, fmaxf(m, top), c);
     }
 };
 
@@ -591,7 +598,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
             float top = vec_max(raw[0], T());
 #pragma unroll
             for (int u = 1; u < UNROLL; ++u) top = fmaxf(top, vec_max(raw[u], T()));
-            if (top > t.limit) t.raise(top, p.c);
+            if (__any_sync(0xffffffffu, top > t.limit)) {  // (lanes of a warp have the same m)
+                const uint32_t most = __reduce_max_sync(0xffffffffu, top > -CUDART_INF_F ? ordered(top) : ORDERED_NONE);
+                t.raise(unordered(most), p.c);
+            }
             peak = fmaxf(peak, top);
             if (p.n_top > 0) {
                 if (j0 == cell_end) {
@@ -606,8 +616,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
             use = use + TILE == ring + tid + STAGES * TILE ? ring + tid : use + TILE;
             request();                                     // into the place that has just been read
             if (!t.plain) {
-#pragma unroll
-                for (int u = 0; u < UNROLL; ++u) t.add<T>(raw[u], p.c);
+                t.add<T>(raw, p.c);
             } else {
 #pragma unroll
                 for (int u = 0; u < UNROLL; ++u) t.add_plain<T>(raw[u], p.c);
