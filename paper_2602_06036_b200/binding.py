@@ -290,6 +290,12 @@ def _current_stream(index: int) -> int:
     return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
 
 
+def _current_device() -> int:
+    """torch.cuda.current_device() without its look at whether CUDA is initialised, which a handle's tensors have seen to."""
+    get = getattr(torch._C, "_cuda_getDevice", None)
+    return get() if get is not None else torch.cuda.current_device()
+
+
 def launch_count() -> int:
     return int(load().dflash_launch_count())
 
@@ -607,7 +613,7 @@ class DFlash:
             if need < 0:
                 raise DFlashError(need)
             need = self._needs[name, key] = max(need, 256)
-        if stream is None and torch.cuda.current_device() == self._index:
+        if stream is None and _current_device() == self._index:
             captured, raw = torch.cuda.is_current_stream_capturing(), _current_stream(self._index)
         else:
             with torch.cuda.device(self._index), torch.cuda.stream(stream):
@@ -625,7 +631,7 @@ class DFlash:
         """The library launches on the current device, which has to be the handle's. One thread at a time: the launches of a call share a workspace."""
         raw = stream.cuda_stream if stream is not None else _current_stream(self._index)
         with self._launching:
-            if torch.cuda.current_device() == self._index:
+            if _current_device() == self._index:
                 rc = fn(self.h, C.byref(args), raw)
             else:
                 with torch.cuda.device(self._index):
@@ -694,14 +700,16 @@ class DFlash:
         self._call(self.lib.dflash_pages_compact, a, stream)
 
     # ---- scoring, distilling, stepping --------------------------------------------------------
-    def _logit_rows(self, t, n=None, vocab=None):
-        """Address, type and row stride of logits [n, vocab] whose rows may lie apart."""
-        assert t.dim() == 2 and t.dtype in (torch.float32, torch.bfloat16), "fp32 or bf16 logits [rows, vocab] expected"
+    def _logit_rows(self, t, shape=None):
+        """Address, type and row stride of logits [rows, vocab] whose rows may lie apart."""
+        rows, v = size = t.shape
+        apart, step = t.stride()
+        dt = t.dtype
+        assert dt is torch.bfloat16 or dt is torch.float32, "fp32 or bf16 logits [rows, vocab] expected"
         assert t.get_device() == self._index, f"tensor on {self.device} expected"
-        rows, v = t.shape
-        assert (n is None or rows == n) and (vocab is None or v == vocab), f"shape {(n, vocab)} expected, got {tuple(t.shape)}"
-        assert (v <= 1 or t.stride(1) == 1) and (rows <= 1 or t.stride(0) >= v), "rows of neighbouring entries that do not overlap expected"
-        return t.data_ptr(), F32 if t.dtype is torch.float32 else BF16, t.stride(0) if rows > 1 else v
+        assert shape is None or size == shape, f"shape {tuple(shape)} expected, got {tuple(size)}"
+        assert (step == 1 or v <= 1) and (apart >= v or rows <= 1), "rows of neighbouring entries that do not overlap expected"
+        return t.data_ptr(), F32 if dt is torch.float32 else BF16, apart if rows > 1 else v
 
     def dflash_token_logprobs(self, logits, tokens, logprob, temperature=1.0, stats=None, entropy=None, top_ids=None, top_logprob=None, stream=None):
         """logprob [n, k] of tokens int32 [n, k] (negative: none) under softmax(logits [n, V] / T). stats [n, 2] receives (M, ln sum exp((z - M) / T)),
@@ -722,7 +730,7 @@ class DFlash:
         n, v = logits.shape
         k = 0 if tokens is None else tokens.shape[1]
         z, dt, ld = self._logit_rows(logits)
-        dz, ddt, dld = self._logit_rows(dlogits, n, v)
+        dz, ddt, dld = self._logit_rows(dlogits, logits.shape)
         f32 = torch.float32
         a = TokenLogprobsBwdArgs(z, dt, ld, n, v, float(temperature), k, self._dev(tokens, torch.int32, n, k), self._dev(stats, f32, n, 2),
                                  self._dev(entropy, f32, n), self._dev(d_logprob, f32, n, k), self._dev(d_entropy, f32, n), dz, ddt, dld,

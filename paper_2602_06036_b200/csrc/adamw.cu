@@ -28,7 +28,8 @@ constexpr int UNROLL = 4;                               // blocks of a warp unde
 constexpr int CHUNK = WARPS * UNROLL * BLOCK;           // 2048
 constexpr int CTAS_PER_SM = 2, NORM_CTAS_PER_SM = 4;
 constexpr int NORM_UNROLL = 4, NORM_BYTES = NORM_UNROLL * THREADS * 16;      // of a chunk of gradients
-constexpr int MAX_TENSORS = 320;                        // descriptors of a launch: 28 KB of its 32 KB of parameters
+constexpr int MAX_TENSORS = 320;                        // descriptors of a launch: 30 KB of its 32 KB of parameters
+constexpr int FEW_TENSORS = 32;                         // a launch of that many carries 3 KB, which takes 1 us less
 
 enum Weights { W_F32 = 0, W_BF16 = 1, W_MASTER = 2 };      // fp32, bf16, bf16 with a master copy in fp32
 
@@ -44,9 +45,10 @@ struct Tensor {
     int32_t wide;                                       // entries in groups of four lie on borders that allow one access each,
     int32_t lead;                                       // those that start `lead` entries in front of the first one
 };
+template <int N>
 struct Table {
-    Tensor t[MAX_TENSORS];
-    int64_t first[MAX_TENSORS + 1];                     // spans in front of each tensor
+    Tensor t[N];
+    int64_t first[N + 1];                     // spans in front of each tensor
     int32_t n, span;                                    // a span: so many chunks one behind the other
 };
 struct StepParams {
@@ -60,9 +62,10 @@ struct StepParams {
     int32_t* status;
 };
 
-static_assert(sizeof(Table) + sizeof(StepParams) <= 32764, "the parameters of a launch");
+static_assert(sizeof(Table<MAX_TENSORS>) + sizeof(StepParams) <= 32764, "the parameters of a launch");
 
-__device__ __forceinline__ int tensor_of(const Table& tab, int64_t chunk, int a) {
+template <int N>
+__device__ __forceinline__ int tensor_of(const Table<N>& tab, int64_t chunk, int a) {
     if (chunk < tab.first[a + 1]) return a;             // (as for the chunk before)
     int b = tab.n;                                      // first[a] <= chunk < first[b]
     while (b - a > 1) {
@@ -303,7 +306,8 @@ __device__ __forceinline__ double cta_sum(double x, double* sh) {
     return s;
 }
 
-__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) adamw_kernel(const __grid_constant__ Table tab, const __grid_constant__ StepParams p) {
+template <int N>
+__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) adamw_kernel(const __grid_constant__ Table<N> tab, const __grid_constant__ StepParams p) {
     __shared__ double sh[WARPS];
     __shared__ float s_bc[2];
     ptx::pdl_trigger();
@@ -390,7 +394,8 @@ __device__ __forceinline__ float squares(const G* p, int64_t from, int64_t to) {
 
 // partial[blockIdx.x] = sum of the squares of the gradients in this CTA's chunks. In the table a chunk has NORM_BYTES, and `lead` entries lie between
 // a gradient's start and the 16-byte border in front of it. The few squares of a thread and chunk are added up in fp32, those sums in double.
-__global__ void __launch_bounds__(THREADS, NORM_CTAS_PER_SM) adamw_norm_kernel(const __grid_constant__ Table tab, double* __restrict__ partial) {
+template <int N>
+__global__ void __launch_bounds__(THREADS, NORM_CTAS_PER_SM) adamw_norm_kernel(const __grid_constant__ Table<N> tab, double* __restrict__ partial) {
     __shared__ double sh[WARPS];
     ptx::pdl_trigger();
     ptx::pdl_wait();
@@ -413,15 +418,9 @@ __global__ void __launch_bounds__(THREADS, NORM_CTAS_PER_SM) adamw_norm_kernel(c
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
-}  // namespace
-
-int64_t adamw_workspace_bytes(int sm_count, int n_tensors) {
-    const int64_t launches = std::max(1, (n_tensors + MAX_TENSORS - 1) / MAX_TENSORS);
-    return align_up(launches * sm_count * NORM_CTAS_PER_SM * (int64_t)sizeof(double), 256);
-}
-
-int launch_adamw(const Launch& L, const dflash_adamw_args& a) {
-    const int launches = std::max(1, (a.n_tensors + MAX_TENSORS - 1) / MAX_TENSORS);
+template <int N>
+int launch_tables(const Launch& L, const dflash_adamw_args& a) {
+    const int launches = std::max(1, (a.n_tensors + N - 1) / N);
     const bool norm = a.max_grad_norm > 0.0 || a.grad_norm;
     StepParams p{};
     p.norm_out = a.grad_norm; p.lr = a.lr_dev; p.step = a.step_dev;
@@ -432,8 +431,8 @@ int launch_adamw(const Launch& L, const dflash_adamw_args& a) {
     const double bc1 = a.step_dev ? 1.0 : -std::expm1(a.step * p.ln_b1), bc2 = a.step_dev ? 1.0 : -std::expm1(a.step * p.ln_b2);
     p.rsqrt_bc2 = (float)(1.0 / std::sqrt(bc2));
     const double lr = a.lr_dev ? 1.0 : a.lr;
-    const auto table = [&](int l, bool for_norm, Table& tab) {
-        const int from = l * MAX_TENSORS, n = std::min(MAX_TENSORS, a.n_tensors - from);
+    const auto table = [&](int l, bool for_norm, Table<N>& tab) {
+        const int from = l * N, n = std::min(N, a.n_tensors - from);
         int64_t chunks = 0, entries = 0;
         for (int i = 0; i < n; ++i) entries += a.tensors[from + i].n;
         // four chunks one behind the other share a look at the table and the addresses, where that leaves every CTA several turns
@@ -464,24 +463,35 @@ int launch_adamw(const Launch& L, const dflash_adamw_args& a) {
         return chunks;
     };
     const auto grid = [&](int64_t chunks, int per_sm) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(chunks, (int64_t)L.h->sm_count * per_sm)); };
-    Table tab;
+    Table<N> tab;
     if (norm) {
         double* partial = reinterpret_cast<double*>(a.workspace);
         p.partial = partial;
         for (int l = 0; l < launches; ++l) {
             const unsigned g = grid(table(l, true, tab), NORM_CTAS_PER_SM);
-            if (launch_pdl(adamw_norm_kernel, dim3(g), dim3(THREADS), 0, L.st, tab, partial + p.n_partial) != cudaSuccess) return DFLASH_ERR_CUDA;
+            if (launch_pdl(adamw_norm_kernel<N>, dim3(g), dim3(THREADS), 0, L.st, tab, partial + p.n_partial) != cudaSuccess) return DFLASH_ERR_CUDA;
             p.n_partial += (int)g;
             g_launches += 1;
         }
     }
     for (int l = 0; l < launches; ++l) {
         const int64_t chunks = table(l, false, tab);
-        if (launch_pdl(adamw_kernel, dim3(grid(chunks, CTAS_PER_SM)), dim3(THREADS), 0, L.st, tab, p) != cudaSuccess) return DFLASH_ERR_CUDA;
+        if (launch_pdl(adamw_kernel<N>, dim3(grid(chunks, CTAS_PER_SM)), dim3(THREADS), 0, L.st, tab, p) != cudaSuccess) return DFLASH_ERR_CUDA;
         p.norm_out = nullptr;
         g_launches += 1;
     }
     return DFLASH_OK;
+}
+
+}  // namespace
+
+int64_t adamw_workspace_bytes(int sm_count, int n_tensors) {
+    const int64_t launches = std::max(1, (n_tensors + MAX_TENSORS - 1) / MAX_TENSORS);
+    return align_up(launches * sm_count * NORM_CTAS_PER_SM * (int64_t)sizeof(double), 256);
+}
+
+int launch_adamw(const Launch& L, const dflash_adamw_args& a) {
+    return a.n_tensors <= FEW_TENSORS ? launch_tables<FEW_TENSORS>(L, a) : launch_tables<MAX_TENSORS>(L, a);
 }
 
 }  // namespace dflash
