@@ -9,6 +9,7 @@
 #include "softmax_rows.cuh"
 
 #include <cmath>
+#include <type_traits>
 
 namespace dflash {
 namespace {
@@ -253,6 +254,8 @@ __host__ __device__ __forceinline__ int capacity_of(int n_top) { return most_of(
 __host__ __device__ __forceinline__ int cells_of(int n_top) { return n_top > 32 && n_top <= 64 ? 16 : 8; }
 static_assert(LP_MAX_TOP + LP_MAX_TOP / 4 + 8 <= THREADS && 16 * THREADS <= 65536, "");
 
+constexpr int BIN_BITS = 6, BINS = 1 << BIN_BITS;                   // of the range of the threads' largest entries
+
 // The search for a stretch's n_top largest entries, after the pass over it that has left the largest entry of every thread and of each of its cells. At least
 // n_top threads' largest entries bound the n_top-th largest of the stretch from below, and little else is above a bound that few of them are (`bound`).
 // What is, lies in a few cells, which are read again (from L2, mostly) by all threads together. The pass itself so needs no barrier and looks at no
@@ -264,6 +267,7 @@ struct Candidates {
     uint16_t* found;               // [most * n_cells] cells to be read again: cell * THREADS + thread
     int* count;                    // entries of list, of found
     uint32_t* ends;                // [2][WARPS]
+    int* bins;                     // [BINS]
     int n_top, most, capacity, n_cells;
     unsigned long long floor;      // keys that are not above it are none of the n_top largest
     float floor_z;
@@ -315,19 +319,43 @@ struct Candidates {
     __device__ bool bound(const Row<T>& row, int lo_j, int hi_j, int per_cell, float top) {
         raise(NO_KEY);
         const bool hit = top > -CUDART_INF_F;
-        int above = __syncthreads_count(hit);
-        if (above <= most) return hit;
         const uint32_t mine = hit ? ordered(top) : 0;
-        const int warp = threadIdx.x >> 5;
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
         const uint32_t top_of_warp = __reduce_max_sync(0xffffffffu, mine), least = __reduce_min_sync(0xffffffffu, mine);
-        if ((threadIdx.x & 31) == 0) {
+        if (lane == 0) {
             ends[warp] = top_of_warp;
             ends[WARPS + warp] = least;
         }
+        if (threadIdx.x < BINS) bins[threadIdx.x] = 0;
+        int above = __syncthreads_count(hit);
+        if (above <= most) return hit;
+        uint32_t hi = __reduce_max_sync(0xffffffffu, ends[lane % WARPS]), lo = __reduce_min_sync(0xffffffffu, ends[WARPS + lane % WARPS]);
+        lo = max(lo, ORDERED_NONE + 1) - 1;                    // more than `most` above lo, none above hi
+        // counted by bins of the range, the bins' sums from the top: mostly a bin's border does
+        const int shift = max(0, 32 - __clz(hi - lo - 1) - BIN_BITS);
+        if (mine > lo) atomicAdd(bins + ((mine - lo - 1) >> shift), 1);
         __syncthreads();
-        const int w = threadIdx.x & (WARPS - 1);
-        uint32_t hi = __reduce_max_sync(0xffffffffu, ends[w]), lo = __reduce_min_sync(0xffffffffu, ends[WARPS + w]);
-        lo = max(lo ? lo - 1 : 0u, ORDERED_NONE);              // more than `most` above lo, none above hi
+        {
+            static_assert(BINS == 64, "two bins a lane");
+            const int upper = bins[BINS - 1 - 2 * lane], lower = bins[BINS - 2 - 2 * lane];
+            int sum = upper + lower;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int other = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += other;
+            }
+            const int at = __ffs(__ballot_sync(0xffffffffu, sum >= n_top)) - 1;      // (all of them are more than n_top)
+            const int to_lower = __shfl_sync(0xffffffffu, sum, at), to_upper = to_lower - __shfl_sync(0xffffffffu, lower, at);
+            const bool in_upper = to_upper >= n_top;
+            const uint32_t bin = BINS - 1 - 2 * at - !in_upper, from = lo + (bin << shift);
+            above = in_upper ? to_upper : to_lower;
+            hi = min(hi, from + (1u << shift));
+            lo = from;
+        }
+        if (above <= most) {
+            raise((unsigned long long)lo << 32 | 0xffffffffu);
+            return mine > lo;
+        }
         while (hi - lo > 1) {
             const uint32_t mid = lo + (hi - lo) / 2;
             above = __syncthreads_count(mine > mid);
@@ -432,11 +460,14 @@ struct Candidates {
         return *count;
     }
 };
-// thread i < n: the place of the i-th of n keys among them, largest first
-__device__ __forceinline__ int rank_of(const unsigned long long* list, int n, unsigned long long mine) {
-    int above = 0, i = 0;
-    for (; i + 4 <= n; i += 4) above += (list[i] > mine) + (list[i + 1] > mine) + (list[i + 2] > mine) + (list[i + 3] > mine);
-    for (; i < n; ++i) above += list[i] > mine;
+// Lanes that share a key's comparisons: as many as there are threads for
+__device__ __forceinline__ int lanes_a_key(int n) { return n <= THREADS / 8 ? 8 : n <= THREADS / 4 ? 4 : n <= THREADS / 2 ? 2 : 1; }
+// The place of key `mine` among n keys, largest first: by `lanes` neighbouring lanes, of which this is the part-th; all of them get it
+__device__ __forceinline__ int rank_of(const unsigned long long* list, int n, unsigned long long mine, int part, int lanes) {
+    int above = 0;
+#pragma unroll 4
+    for (int i = part; i < n; i += lanes) above += list[i] > mine;
+    for (int o = lanes >> 1; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
     return above;
 }
 __device__ __forceinline__ void set_cell(uint16_t* cells, int cell, float top) {
@@ -492,6 +523,7 @@ __device__ __noinline__ int search_stretch(const T* z, int vocab, int lo_j, int 
     cand.found = reinterpret_cast<uint16_t*>(words + at.found);
     cand.count = count;
     cand.ends = ends;
+    cand.bins = reinterpret_cast<int*>(ends + 2 * WARPS);
     cand.n_top = n_top;
     cand.most = most_of(n_top);
     cand.capacity = capacity_of(n_top);
@@ -523,7 +555,7 @@ template <typename T, int CS>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(const ForwardParams p) {
     extern __shared__ uint4 ring[];                        // [STAGES][TILE]: a thread reads what it has copied itself
     __shared__ Stat sh[WARPS];
-    __shared__ uint32_t ends[2 * WARPS];
+    __shared__ uint32_t ends[2 * WARPS + BINS];            // and the search's bins
     __shared__ int count[2];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = CS > 1 ? (int)ptx::cluster_ctarank() : 0;
     unsigned long long* words = reinterpret_cast<unsigned long long*>(ring + STAGES * TILE);
@@ -634,8 +666,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
         if (p.n_top > 0) n_list = search_stretch(reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld, p.vocab, cur.lo, cur.hi, per_cell, peak, p.n_top, CS, words, count, ends);
         else __syncthreads();
         x = lanes_merged<WARPS>(sh[lane % WARPS], p.c);
-        unsigned long long key = tid < n_list ? list[tid] : 0;
-        const int place = tid < n_list ? rank_of(list, n_list, key) : p.n_top;
+        const int lanes = lanes_a_key(n_list), own = tid / lanes;
+        const unsigned long long key = own < n_list ? list[own] : 0;
+        const int rank_in_list = p.n_top > 0 ? rank_of(list, n_list, key, tid % lanes, lanes) : 0;
+        const int place = own < n_list && tid % lanes == 0 ? rank_in_list : p.n_top;
         n_list = min(n_list, p.n_top);
         if constexpr (CS > 1) {
             __syncthreads();
@@ -782,7 +816,7 @@ cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st
 }
 
 // ---- gradient ----------------------------------------------------------------------------------------------------------
-constexpr int B_THREADS = 256, B_UNROLL = 4, GROUP = 8;        // groups of 8 entries a thread, 4 of them under way
+constexpr int B_THREADS = 256, GROUP = 8;                      // groups of 8 entries a thread
 
 struct BackwardParams {
     const void* logits;
@@ -795,17 +829,42 @@ struct BackwardParams {
     float inv_t, c;
 };
 
-template <typename T>
-__device__ __forceinline__ void load_group(const T* src, float (&z)[GROUP]) {
-    constexpr int VE = Row<T>::VE;
+// A group's 16-byte vectors from the border in front of it on: `off` entries lie between the two (OFF: which is not 0, and takes one vector more)
+template <typename T, bool OFF>
+struct Raw {
+    static constexpr int VE = Row<T>::VE, VECS = GROUP / VE + OFF, WORDS = 4 * VECS;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const T* src, int off) {
+        const uint4* v = reinterpret_cast<const uint4*>(src - off);
 #pragma unroll
-    for (int k = 0; k < GROUP / VE; ++k) {
-        float f[VE];
-        unpack16(__ldcs(reinterpret_cast<const uint4*>(src) + k), f, T());
-#pragma unroll
-        for (int e = 0; e < VE; ++e) z[k * VE + e] = f[e];
+        for (int k = 0; k < VECS; ++k) {
+            const uint4 x = OFF ? v[k] : __ldcs(v + k);          // (a vector that two groups share comes from L1 the second time)
+            w[4 * k] = x.x; w[4 * k + 1] = x.y; w[4 * k + 2] = x.z; w[4 * k + 3] = x.w;
+        }
     }
-}
+    __device__ __forceinline__ void entries(int off, float (&z)[GROUP]) {
+        if constexpr (OFF) {                                   // the same for all groups of a row
+            const int words = off * (int)sizeof(T) / 4;
+#pragma unroll
+            for (int bit = 2; bit > 0; bit >>= 1)
+                if (words & bit) {
+#pragma unroll
+                    for (int k = 0; k < WORDS; ++k) w[k] = k + bit < WORDS ? w[k + bit] : 0;
+                }
+            if (sizeof(T) == 2 && (off & 1)) {
+#pragma unroll
+                for (int k = 0; k + 1 < WORDS; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < GROUP / VE; ++k) {
+            float f[VE];
+            unpack16(make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]), f, T());
+#pragma unroll
+            for (int e = 0; e < VE; ++e) z[k * VE + e] = f[e];
+        }
+    }
+};
 __device__ __forceinline__ void store_group(float* dst, const float (&g)[GROUP]) {
     __stcs(reinterpret_cast<float4*>(dst), make_float4(g[0], g[1], g[2], g[3]));
     __stcs(reinterpret_cast<float4*>(dst) + 1, make_float4(g[4], g[5], g[6], g[7]));
@@ -858,46 +917,52 @@ __global__ void __launch_bounds__(B_THREADS) token_logprobs_bwd_kernel(const Bac
     for (int w = 0; w < LP_MAX_TOKENS / 32; ++w) sum += s_sum[w];
     const float top = p.stats[2 * (int64_t)r], log_sum = p.stats[2 * (int64_t)r + 1];
     const float gh = p.d_entropy ? p.d_entropy[r] : 0.f, h = p.d_entropy ? p.entropy[r] : 0.f;
-    const bool off = (!any && gh == 0.f) || (top == -CUDART_INF_F && log_sum == 0.f);      // nothing comes in, or a row of -inf
+    const bool off_row = (!any && gh == 0.f) || (top == -CUDART_INF_F && log_sum == 0.f);      // nothing comes in, or a row of -inf
     // with y = log2 p = (z - top) c - log_sum / ln 2:  dz = p (a + b y)
     const float sub = log_sum * LOG2E, a = -(sum + gh * h) * p.inv_t, b = -gh * LN2 * p.inv_t;
     auto grad = [&](float v) {
         const float y = fmaf(v - top, p.c, -sub);
         return fast_exp2(y) * fmaf(b, fmaxf(y, FAR), a);
     };
-    // ---- the piece: groups whose loads and stores both lie on 16-byte borders start at entry `first`, if there is such a place
-    constexpr int AZ = 16 / (int)sizeof(T), AO = 16 / (int)sizeof(O), AM = AZ > AO ? AZ : AO;
-    const int pz = (int)((reinterpret_cast<uintptr_t>(z + lo) & 15) / sizeof(T)), po = (int)((reinterpret_cast<uintptr_t>(dz + lo) & 15) / sizeof(O));
-    int first = 0;
-    while (first < AM && ((pz + first) % AZ != 0 || (po + first) % AO != 0)) ++first;
-    const bool vec = first < AM;
-    const int begin = vec ? min(lo + first, hi) : hi, n_group = (hi - begin) / GROUP;
-    for (int i0 = 0; i0 < n_group; i0 += B_UNROLL * B_THREADS) {
-        float v[B_UNROLL][GROUP];
-        if (!off) {
+    // ---- the piece: groups whose stores lie on 16-byte borders; their loads begin `off` entries behind one, and their vectors have to lie inside of the row
+    constexpr int AZ = 16 / (int)sizeof(T), AO = 16 / (int)sizeof(O);
+    int begin = lo + (AO - (int)((reinterpret_cast<uintptr_t>(dz + lo) & 15) / sizeof(O))) % AO;
+    const int off = (int)((reinterpret_cast<uintptr_t>(z + begin) & 15) / sizeof(T));
+    while (begin < off) begin += AO > AZ ? AO : AZ;            // (a step that leaves `off` as it is)
+    const int last = off ? min(hi, p.vocab - (AZ - off)) : hi, n_group = max(0, (last - begin) / GROUP);
+    const auto groups = [&](auto shifted) {
+        constexpr bool OFF = decltype(shifted)::value;
+        constexpr int U = OFF && sizeof(T) == 4 ? 2 : 4;       // groups of a thread under way
+        for (int i0 = 0; i0 < n_group; i0 += U * B_THREADS) {
+            Raw<T, OFF> raw[U];
+            if (!off_row) {
 #pragma unroll
-            for (int u = 0; u < B_UNROLL; ++u) {
+                for (int u = 0; u < U; ++u) {
+                    const int i = i0 + u * B_THREADS + tid;
+                    if (i < n_group) raw[u].load(z + begin + i * GROUP, off);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
                 const int i = i0 + u * B_THREADS + tid;
-                if (i < n_group) load_group(z + begin + i * GROUP, v[u]);
+                if (i < n_group) {
+                    float v[GROUP], d[GROUP];
+                    if (!off_row) raw[u].entries(off, v);
+#pragma unroll
+                    for (int e = 0; e < GROUP; ++e) d[e] = off_row ? 0.f : grad(v[e]);
+                    store_group(dz + begin + i * GROUP, d);
+                }
             }
         }
-#pragma unroll
-        for (int u = 0; u < B_UNROLL; ++u) {
-            const int i = i0 + u * B_THREADS + tid;
-            if (i < n_group) {
-                float d[GROUP];
-#pragma unroll
-                for (int e = 0; e < GROUP; ++e) d[e] = off ? 0.f : grad(v[u][e]);
-                store_group(dz + begin + i * GROUP, d);
-            }
-        }
-    }
+    };
+    if (off) groups(std::true_type());
+    else groups(std::false_type());
     const int rest = begin + n_group * GROUP;                  // entries in front of and behind the groups: all of them where there are none
-    for (int i = lo + tid; i < begin && vec; i += B_THREADS) store_entry(dz + i, off ? 0.f : grad(as_f(z[i])));
-    for (int i = (vec ? rest : lo) + tid; i < hi; i += B_THREADS) store_entry(dz + i, off ? 0.f : grad(as_f(z[i])));
+    for (int i = lo + tid; i < min(begin, hi); i += B_THREADS) store_entry(dz + i, off_row ? 0.f : grad(as_f(z[i])));
+    for (int i = rest + tid; i < hi; i += B_THREADS) store_entry(dz + i, off_row ? 0.f : grad(as_f(z[i])));
     // ---- the given tokens' own entries: the first of equal ones adds their gradients up, in the order of the list
     __syncthreads();
-    if (!off && tok >= lo && tok < hi) {
+    if (!off_row && tok >= lo && tok < hi) {
         float own = 0.f;
         bool earlier = false;
         for (int i = 0; i < p.n_tokens; ++i) {
@@ -913,7 +978,7 @@ __global__ void __launch_bounds__(B_THREADS) token_logprobs_bwd_kernel(const Bac
 template <typename T, typename O>
 cudaError_t launch_backward(BackwardParams p, int rows, int sm_count, cudaStream_t st) {
     // pieces of a row: whole tiles, few enough that a CTA's start is little beside its work, enough to fill the GPU
-    constexpr int TILE = B_THREADS * B_UNROLL * GROUP;
+    constexpr int TILE = B_THREADS * 4 * GROUP;
     const int tiles = (p.vocab + TILE - 1) / TILE;
     int per = std::min(tiles, 4);
     while (per > 1 && (int64_t)rows * ((tiles + per - 1) / per) < 8ll * sm_count) --per;
