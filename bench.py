@@ -513,6 +513,38 @@ def run_kernel_only(args, step, device):
                           "bound": "tensor", "peak_tflops": peak, "frac": tf / peak, "hbm_bytes": nbytes,
                           "us_at_tensor_peak": flops / (peak * 1e12) * 1e6, "us_at_hbm_peak": nbytes / (peaks["hbm_gbs"] * 1e9) * 1e6}))
         return
+    elif args.kernel in ("token_logprobs", "token_logprobs_bwd"):
+        # Log probabilities of one token a row with entropy and 20 alternatives, or their gradient, over --loss-blocks blocks of bf16 logits.
+        # Algorithmic bytes: logits read once (gradient: and written once).
+        n = args.loss_blocks * B
+        z = torch.empty((n, cfg.vocab), dtype=torch.bfloat16, device=device).normal_(0.0, 3.0)
+        t = torch.randint(0, cfg.vocab, (n, 1), dtype=torch.int32, device=device)
+        lp, stats, ent = (torch.empty(s, device=device) for s in ((n, 1), (n, 2), (n,)))
+        ids, top = torch.empty((n, 20), dtype=torch.int32, device=device), torch.empty((n, 20), device=device)
+        fn = lambda: step.lib.dflash_token_logprobs(z, t, lp, stats=stats, entropy=ent, top_ids=ids, top_logprob=top)
+        nbytes = z.numel() * 2
+        if args.kernel == "token_logprobs_bwd":
+            fn()
+            dz, g, gh = torch.empty_like(z), torch.full((n, 1), -1.0 / n, device=device), torch.full((n,), 0.01 / n, device=device)
+            fn = lambda: step.lib.dflash_token_logprobs_bwd(z, t, stats, g, dz, entropy=ent, d_entropy=gh)
+            nbytes = 2 * z.numel() * 2
+    elif args.kernel == "adamw":
+        # One clipped AdamW step of the drafter's layers and fusion: bf16 weights and gradients, fp32 master copies, states of --state-bits.
+        # Algorithmic bytes: everything read once and written once.
+        shapes = [cfg.d_model * cfg.feat_dim] + cfg.n_layers * [(cfg.q_dim + 2 * cfg.kv_dim) * cfg.d_model, cfg.d_model * cfg.q_dim,
+                                                                2 * cfg.d_ffn * cfg.d_model, cfg.d_model * cfg.d_ffn, cfg.d_model, cfg.d_model]
+        entries = []
+        for n in shapes:
+            w = torch.randn(n, device=device) * 0.02
+            e = {"param": w.bfloat16(), "master": w, "grad": (torch.randn(n, device=device) * 1e-3).bfloat16(), "weight_decay": 0.1}
+            state = torch.float32 if args.state_bits == 32 else torch.float8_e4m3fn
+            e.update({k: torch.zeros(n, dtype=torch.uint8 if args.state_bits == 8 else state, device=device).view(state) for k in ("exp_avg", "exp_avg_sq")})
+            if args.state_bits == 8:
+                e.update({k + "_scale": torch.zeros(-(-n // 128), device=device) for k in ("exp_avg", "exp_avg_sq")})
+            entries.append(e)
+        plan, count = step.lib.adamw_plan(entries), iter(range(1, 1 << 30))
+        fn = lambda: step.lib.dflash_adamw_step(plan, next(count), 6e-4, max_grad_norm=1.0)
+        nbytes = sum(shapes) * (12 + (16 if args.state_bits == 32 else 4)) + (16 * sum(-(-n // 128) for n in shapes) if args.state_bits == 8 else 0)
     elif args.kernel == "lmhead":
         hid = torch.randn(S * B, cfg.d_model, device=device).to(cfg.torch_dtype)
         ids = torch.zeros(S * B, dtype=torch.int32, device=device)
@@ -703,9 +735,10 @@ def main():
     ap.add_argument("--workload", default="cfg1")
     ap.add_argument("--impl", default="b200", choices=["b200", "reference"])
     ap.add_argument("--no-cpu-baseline", action="store_true")
-    ap.add_argument("--kernel", default=None, choices=["lmhead", "attention", "target_verify", "block_loss", "attention_bwd", "verify"],
+    ap.add_argument("--kernel", default=None, choices=["lmhead", "attention", "target_verify", "block_loss", "attention_bwd", "verify", "token_logprobs", "token_logprobs_bwd", "adamw"],
                     help="run one building block alone (for profiler captures) instead of the step")
     ap.add_argument("--loss-blocks", type=int, default=512, help="--kernel block_loss: blocks (of block_size rows) per call")
+    ap.add_argument("--state-bits", type=int, default=32, choices=[32, 8], help="--kernel adamw: bits of the optimiser's states")
     ap.add_argument("--trace", default=None, help="write a device-side timeline of one step to this file")
     ap.add_argument("--temperature", type=float, default=0.0,
                     help="> 0: drafts are drawn from the draft's logits and verified by speculative sampling (default: greedy)")
@@ -757,7 +790,7 @@ def main():
     # One handle (one copy of the weights) serves every workload of the run.
     max_ctx = max([max(wl.ctx_lens)] + [max(synth.workload(n).ctx_lens) for n in others])
     lib = make_lib(cfg, device, max_ctx, seed=0)
-    if args.kernel in ("verify", "lmhead", "block_loss", "attention_bwd"):      # no cached context needed
+    if args.kernel in ("verify", "lmhead", "block_loss", "attention_bwd", "token_logprobs", "token_logprobs_bwd", "adamw"):      # no cached context needed
         run_kernel_only(args, _LibOnly(wl, lib, device), device)
         return
     step = Step(wl, device, seed=0, temperature=args.temperature, fuse_ctx=not args.separate_ctx, lib=lib)

@@ -2,9 +2,12 @@
 // With y = (z - M) / T, M the row's maximum and S = sum exp(y):
 //   logprob(v) = y_v - ln S,   entropy = ln S - (sum y exp(y)) / S,
 //   dz_v = (1/T) [ sum of g_i over the given tokens i that are v  -  p_v (G + gH (ln p_v + entropy)) ],  G = sum of all g_i, p = exp(logprob).
-// Forward: one pass over the logits. Every thread keeps (m, s, w) = (its maximum, sum e, sum e y) of what it has seen, e = exp(y) with its own m,
-// and the entries that may be among the row's n_top largest go to a small list in shared memory (see `Candidates`).
-// Bound by HBM: 2 or 4 bytes an entry against about 6 issue slots and one exponential.
+// Forward: one pass over the logits. Every thread keeps sums of e = exp(y) and of e y with a reference m in the place of M (see `Running`), and the largest entry
+// of each of a few parts of what it has seen, from which the row's n_top largest are found afterwards (see `Candidates`). Tiles come by asynchronous
+// copies into shared memory, two of them under way a CTA. Copies that go around L1 (.cg), bulk copies of 2 KB and a third tile were all slower (2048 x
+// 151936 fp32 222, 199 and 225 us against 186: L1 holds what is under way, and shared memory is taken from it).
+// Bound: fp32 by HBM (2048 x 151936: 181 us, the measured copy rate); bf16 by the special-function unit besides, one exponential an entry being 91 us of 108 there,
+// and by issue (8 slots an entry). With alternatives the search adds 20 (20 of them) to 35 us (64), when its CTAs' rows end together.
 #include "logprobs.cuh"
 #include "softmax_rows.cuh"
 
@@ -92,6 +95,7 @@ __device__ __forceinline__ void copy_async16(uint32_t smem, const void* gmem) {
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }      // all but the latest N groups have landed
+
 // ---- statistics ----------------------------------------------------------------------------------------------------
 // m: maximum, s: sum of 2^((z - m) c), w: sum of 2^((z - m) c) (z - m) c
 struct Stat {
@@ -249,8 +253,9 @@ constexpr unsigned long long NO_KEY = (unsigned long long)ORDERED_NONE << 32 | 0
 
 __host__ __device__ __forceinline__ int most_of(int n_top) { return n_top + n_top / 4 + 8; }      // entries that a bound on the n_top-th largest may leave
 __host__ __device__ __forceinline__ int capacity_of(int n_top) { return most_of(n_top) + THREADS; }      // of the list: a turn's entries fit behind one that has been cut
-// Cells of a thread: its part of a row in as many runs of tiles. More of them are read again by fewer vectors (8 cells of 3 tiles at 151936 bf16 entries; 2048 rows with
-// 64 alternatives: 154 us with 8), but shared memory is taken from L1 in steps, which the copies under way need: CTAs of more than 48.5 KB leave it too little.
+// Cells of a thread: its part of a row in as many runs of tiles. Of more cells fewer vectors are read again (2048 x 151936 bf16 with 64 alternatives: 140 us with 16,
+// 154 with 8), but shared memory is taken from L1 in steps, which the copies under way need: 16 are worth it where they keep a CTA below 48.5 KB
+// and many candidates are looked for.
 __host__ __device__ __forceinline__ int cells_of(int n_top) { return n_top > 32 && n_top <= 64 ? 16 : 8; }
 static_assert(LP_MAX_TOP + LP_MAX_TOP / 4 + 8 <= THREADS && 16 * THREADS <= 65536, "");
 
@@ -313,8 +318,8 @@ struct Candidates {
     __device__ __forceinline__ static int vector_of(int lo, int per_cell, int cell, int thread, int k) {
         return lo + (cell * per_cell + k) * THREADS + thread;
     }
-    // all threads: a floor that at least n_top of the threads' largest entries lie above, and at most `most`. Found by halving: first between values, and where too many
-    // are equal, between keys. Returns whether this thread's entries may lie above it.
+    // all threads: a floor that at least n_top of the threads' largest entries lie above, and at most `most`. Found between bins of the values' range, then by halving
+    // between values, and where too many are equal, between keys. Returns whether this thread's entries may lie above it.
     template <typename T>
     __device__ bool bound(const Row<T>& row, int lo_j, int hi_j, int per_cell, float top) {
         raise(NO_KEY);
@@ -349,7 +354,7 @@ struct Candidates {
             const bool in_upper = to_upper >= n_top;
             const uint32_t bin = BINS - 1 - 2 * at - !in_upper, from = lo + (bin << shift);
             above = in_upper ? to_upper : to_lower;
-            hi = min(hi, from + (1u << shift));
+            hi = hi - from > 1u << shift ? from + (1u << shift) : hi;      // (their sum may pass 32 bits)
             lo = from;
         }
         if (above <= most) {

@@ -102,6 +102,8 @@ def check_forward(o, z, tokens, T, top):
     (200, 32000, BF16, 1, 5, 1.0, 0, 0),            # two
     (320, 32001, BF16, 0, 20, 1.0, 0, 0),           # one, several tiles, no given token
     (6, 32000, BF16, 4, 0, 1.0, 0, 0),
+    (1300, 3001, BF16, 2, 9, 1.0, 3, 1),            # a CTA goes through several rows, which start differently
+    (1200, 1500, F32, 1, 0, 1.0, 0, 2),
 ])
 def test_matches_the_oracle(lib, n, v, dtype, k, top, T, pad, at):
     z, tokens = logits(n, v, dtype, n + v), given(n, v, k, n + v)
@@ -153,11 +155,13 @@ def row_of(kind, v, dtype, rng):
         z *= 1e30
     elif kind == "one huge":
         z[v // 2] = 3e4
+    elif kind == "far ends":                                   # ties at the top of a range of values that passes 31 bits
+        z = np.where(rng.random(v) < 0.5, 1.5e38, -1.5e38)
     return z
 
 
 KINDS = ["constant", "two values", "rising", "falling", "masked", "all masked", "lowest", "all lowest", "lowest and -inf", "one", "nan", "nan and -inf", "all nan",
-         "inf", "zeros of both signs", "huge", "one huge"]
+         "inf", "zeros of both signs", "huge", "one huge", "far ends"]
 
 
 @pytest.mark.parametrize("v", [50, 5003, 40000])
