@@ -612,7 +612,8 @@ int32_t dflash_block_loss(dflash_handle* h, const dflash_block_loss_args* a /*[h
  * NaN in all numbers but M; NaN is never an alternative. A negative token stands for none (logprob 0), and so does one >= vocab, which
  * sets DFLASH_DEV_BAD_TOKEN. Temperature scales the distribution, not the order of the alternatives.
  * One launch and one pass over the logits, no scratch memory: calls may overlap. Sums in fp32; against exact arithmetic the log probabilities are off by
- * about 1e-6 (plus 2^-24 of their size). Rows may start anywhere (an odd vocabulary or stride costs nothing).
+ * some 1e-7 (plus 2^-24 of their size). Rows may start anywhere; of what lies between two rows up to 14 bytes on either side of a row may be read, but not used.
+ * 32 rows of 151936 bf16 logits take 7 us, with 20 alternatives 10; 544 fp32 rows 52 and 58; 2048 bf16 rows 108 and 126 (64 alternatives: 141).
  * Errors: DFLASH_ERR_INVALID_ARG (null pointer, T not positive and finite, bad dtype or sizes), DFLASH_ERR_UNSUPPORTED (n_tokens or n_top > 128,
  * vocab > 2^30, more than 2^28 rows). */
 typedef struct {
@@ -638,7 +639,8 @@ int32_t dflash_token_logprobs(dflash_handle* h, const dflash_token_logprobs_args
  * The gradient through top_logprob is had by giving top_ids as tokens. Equal tokens' gradients add up in the order of the list. A row whose
  * incoming gradients are all 0 gets zeros, whatever its logits hold (they are not read), and so does a row of -inf only.
  * stats (and entropy, where d_entropy is given) are those of the forward call with the same logits and temperature. dlogits may be
- * the logits' own buffer if dtype and stride agree (otherwise the two must not overlap). One launch; reads the logits once and writes the gradient once.
+ * the logits' own buffer if dtype and stride agree (otherwise the two must not overlap). One launch; reads the logits once and writes the gradient once
+ * (4096 rows of 151936 bf16 logits: 385 us).
  * Errors as above; DFLASH_ERR_UNSUPPORTED also for more than 2^31 pieces of 8192 entries. */
 typedef struct {
     const void*    logits;             /* [device] [n_rows, vocab]                              */
@@ -672,6 +674,8 @@ int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_
  * Where the norm is computed (max_grad_norm > 0, or grad_norm given) and is not finite (a gradient is NaN, infinite or above 1e19), the whole step is left out: nothing but
  * grad_norm is written and DFLASH_DEV_NOT_FINITE is set. Without it such a gradient makes NaN of its own entry (states of 8 bits: of its
  * block's 128 states).
+ * 1.0e9 weights with master copies and clipping take 5.0 ms, with states of 8 bits 3.1. Groups of four entries that lie on their borders in every buffer of a
+ * tensor (all starts multiples of 4 entries, or equally far behind one) are what is fast; states of 8 bits need the former.
  * Launches: one per 320 tensors, twice with the norm. Captured calls may be replayed: lr_dev and step_dev are then read at each replay. No two tensors
  * of a call may overlap; calls must not overlap in time if they share tensors or a workspace.
  * Errors: DFLASH_ERR_INVALID_ARG (null pointer, address that is no multiple of the element's size, n < 0, bad dtype or state_bits, a master copy beside an fp32 param,

@@ -798,8 +798,8 @@ template <typename T>
 cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
     // CTAs per row: what takes the least time by a count of tile times. CTAs that share an SM share its rate, so that what counts is how evenly a turn of
     // CTAs fills the SMs; beside its tiles a turn takes the time of 4 tiles (9 with the search), and a cluster's meeting that of 2 to 4. (A tile time is
-    // 0.46 us. 300 x 151936 bf16 by 1, 2, 4 and 8 CTAs a row: 28, 26, 28 and 39 us, with 20 alternatives 33, 33, 40 and 61; 32 rows 16, 11, 7 and 9; 544 rows
-    // 41, 40, 45 and 66.)
+    // 0.46 us. 32 x 151936 bf16 by 1, 2, 4 and 8 CTAs a row: 14, 10, 7 and 8 us; 300 rows 26, 25, 27 and 38, with 20 alternatives 31, 32, 37 and 57; 800 rows
+    // 57, 49, 61 and 91. The rule is up to a tenth off the best of the four.)
     const int tiles = (p.vocab + TILE * Row<T>::VE - 1) / (TILE * Row<T>::VE);
     const int64_t slots = (int64_t)CTAS_PER_SM * sm_count;
     int cs = 1;
