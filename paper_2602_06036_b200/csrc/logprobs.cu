@@ -536,22 +536,25 @@ __device__ __noinline__ int search_stretch(const T* z, int vocab, int lo_j, int 
     return cand.search(Row<T>(z, vocab), lo_j, hi_j, per_cell, top);
 }
 
-// The tiles of a CTA's rows, in order: its stretch of each
+// A CTA's stretch of a row: vectors [lo, hi)
 template <typename T, int CS>
-struct Cursor {
+struct Stretch {
     Row<T> row;
-    int r, j, lo, hi;
-    __device__ __forceinline__ void to(const ForwardParams& p, int rank, int to_row) {
-        r = to_row;
-        lo = hi = 0;
-        if (r < p.n_rows) {
-            row = Row<T>(reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld, p.vocab);
-            const int per = (row.n_vec + CS - 1) / CS;
-            lo = min(rank * per, row.n_vec);
-            hi = min(row.n_vec, lo + per);
-        }
-        j = lo;
+    int lo, hi;
+    __device__ __forceinline__ Stretch(const ForwardParams& p, int rank, int r) : row(reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld, p.vocab) {
+        const int per = (row.n_vec + CS - 1) / CS;
+        lo = min(rank * per, row.n_vec);
+        hi = min(row.n_vec, lo + per);
     }
+    __device__ __forceinline__ int tiles() const { return (hi - lo + TILE - 1) / TILE; }
+};
+// Tiles [from, from + count) of a stretch, all of whose vectors are among [first, last)
+struct Span {
+    int from;
+    uint32_t count;
+    __device__ __forceinline__ Span() {}
+    __device__ __forceinline__ Span(int lo, int first, int last) : from(lo < first), count((uint32_t)max(0, (last - lo) / TILE - from)) {}      // (first: 0 or 1)
+    __device__ __forceinline__ bool has(int k) const { return (uint32_t)(k - from) < count; }
 };
 
 // A cluster of CS CTAs per row, a CTA per stretch of its vectors. One CTA a row: it goes on with another row, whose first tiles are then already under way;
@@ -576,58 +579,71 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
     const int step = gridDim.x / CS;
     const char* begin = reinterpret_cast<const char*>(p.logits);
     const auto in_memory = [&](const char* a) { return a >= begin && a + 16 <= p.end; };
-    Cursor<T, CS> ahead;
-    ahead.to(p, rank, blockIdx.x / CS);
-    const uint32_t slots = ptx::smem_u32(ring + tid), slots_end = slots + STAGES * TILE_BYTES;
-    uint32_t fill = slots;                                 // the next tile's place in the ring
+    // the next tile to be requested: the k-th of row r's stretch, whose part for this thread begins at `from`; `plain` ones lie inside of the buffer
+    int ahead_r = blockIdx.x / CS, ahead_k = 0, ahead_tiles = 0;
+    const char* ahead_at = nullptr;
+    Span plain;
+    const auto look_ahead = [&]() {                        // at row ahead_r
+        const Stretch<T, CS> n(p, rank, ahead_r);
+        ahead_k = 0;
+        ahead_tiles = n.tiles();
+        ahead_at = n.row.address(n.lo) + tid * 16;
+        plain = Span(n.lo, n.row.base < begin, min(n.hi, n.row.n_vec - (n.row.address(n.row.n_vec) > p.end)));
+    };
+    look_ahead();                                          // (the grid has no more clusters than there are rows)
+    const uint32_t slots = ptx::smem_u32(ring + tid);
+    uint32_t fill = slots;                                 // its place in the ring of two
     const auto request = [&]() {
-        while (ahead.j >= ahead.hi && ahead.r < p.n_rows) ahead.to(p, rank, ahead.r + step);
-        if (ahead.r < p.n_rows) {
-            const char* tile = ahead.row.address(ahead.j);
-            const char* a = tile + tid * 16;
-            static_assert(UNROLL == 4, "");
-            if (ahead.j + TILE <= ahead.hi && tile >= begin && tile + TILE_BYTES <= p.end) {
-                copy_async16<0 * THREADS * 16>(fill, a);
-                copy_async16<1 * THREADS * 16>(fill, a);
-                copy_async16<2 * THREADS * 16>(fill, a);
-                copy_async16<3 * THREADS * 16>(fill, a);
+        while (ahead_k == ahead_tiles && ahead_r < p.n_rows) {
+            ahead_r += step;
+            if (ahead_r < p.n_rows) look_ahead();
+        }
+        if (ahead_r < p.n_rows) {
+            static_assert(UNROLL == 4 && STAGES == 2, "");
+            if (plain.has(ahead_k)) {
+                copy_async16<0 * THREADS * 16>(fill, ahead_at);
+                copy_async16<1 * THREADS * 16>(fill, ahead_at);
+                copy_async16<2 * THREADS * 16>(fill, ahead_at);
+                copy_async16<3 * THREADS * 16>(fill, ahead_at);
             } else {
+                const Stretch<T, CS> n(p, rank, ahead_r);
+                const int j = n.lo + ahead_k * TILE + tid;
 #pragma unroll
                 for (int u = 0; u < UNROLL; ++u)
-                    if (ahead.j + u * THREADS + tid < ahead.hi && in_memory(a + u * THREADS * 16)) copy_async16(fill + u * THREADS * 16, a + u * THREADS * 16);
+                    if (j + u * THREADS < n.hi && in_memory(ahead_at + u * THREADS * 16)) copy_async16(fill + u * THREADS * 16, ahead_at + u * THREADS * 16);
             }
-            ahead.j += TILE;
+            ++ahead_k;
+            ahead_at += TILE_BYTES;
         }
         copy_commit();
-        fill += TILE_BYTES;
-        if (fill == slots_end) fill = slots;
+        fill = 2 * slots + TILE_BYTES - fill;
     };
     for (int i = 0; i < STAGES; ++i) request();
-    const uint4* use = ring + tid;
+    int use = tid;                                         // place of the next tile to be worked on
     for (int r = blockIdx.x / CS; r < p.n_rows; r += step) {
-        Cursor<T, CS> cur;
-        cur.to(p, rank, r);
+        const Stretch<T, CS> cur(p, rank, r);
         const Row<T>& row = cur.row;
         // a given token's logit (every CTA holds the row's result in the end; the first one writes it)
         const int tok = tid < p.n_tokens && rank == 0 ? p.tokens[(int64_t)r * p.n_tokens + tid] : -1;
         Running t;
         t.reset();
         float peak = -CUDART_INF_F, cell_top = -CUDART_INF_F;
-        const int tiles = (cur.hi - cur.lo + TILE - 1) / TILE, tiles_a_cell = (tiles + n_cells - 1) / n_cells, per_cell = tiles_a_cell * UNROLL;
-        int cell = 0, cell_end = cur.lo + tiles_a_cell * TILE;
-        for (int j0 = cur.lo; j0 < cur.hi; j0 += TILE) {
+        const int tiles = cur.tiles(), tiles_a_cell = (tiles + n_cells - 1) / n_cells, per_cell = tiles_a_cell * UNROLL;
+        const Span whole(cur.lo, row.shift > 0, min(cur.hi, (p.vocab + row.shift) / Row<T>::VE));      // tiles inside of the row
+        int cell = 0, in_cell = 0;
+        for (int k = 0; k < tiles; ++k) {
             copy_wait<STAGES - 1>();
             uint4 raw[UNROLL];
-            if (j0 + TILE <= cur.hi && row.whole(j0) && row.whole(j0 + TILE - 1)) {
+            if (whole.has(k)) {
 #pragma unroll
-                for (int u = 0; u < UNROLL; ++u) raw[u] = use[u * THREADS];
+                for (int u = 0; u < UNROLL; ++u) raw[u] = ring[use + u * THREADS];
             } else {
 #pragma unroll
                 for (int u = 0; u < UNROLL; ++u) {
-                    const int j = j0 + u * THREADS + tid;
+                    const int j = cur.lo + k * TILE + u * THREADS + tid;
                     raw[u] = no_entries<T>();
                     if (j < cur.hi) {
-                        raw[u] = use[u * THREADS];
+                        raw[u] = ring[use + u * THREADS];
                         if (!row.whole(j)) raw[u] = edge_of<T>(row.address(j), row.first(j), p.vocab, raw[u], in_memory(row.address(j)));
                     }
                 }
@@ -641,16 +657,14 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
             }
             peak = fmaxf(peak, top);
             if (p.n_top > 0) {
-                if (j0 == cell_end) {
-                    ++cell;
-                    cell_end += tiles_a_cell * TILE;
-                    cell_top = top;
-                } else {
-                    cell_top = fmaxf(cell_top, top);
+                cell_top = fmaxf(cell_top, top);
+                if (++in_cell == tiles_a_cell || k + 1 == tiles) {
+                    set_cell(cells, cell++, cell_top);
+                    cell_top = -CUDART_INF_F;
+                    in_cell = 0;
                 }
-                set_cell(cells, cell, cell_top);
             }
-            use = use + TILE == ring + tid + STAGES * TILE ? ring + tid : use + TILE;
+            use = 2 * tid + TILE - use;
             request();                                     // into the place that has just been read
             if (!t.plain) {
                 t.add<T>(raw, p.c);
@@ -660,7 +674,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
             }
         }
         if (p.n_top > 0)
-            for (int k = tiles == 0 ? 0 : cell + 1; k < n_cells; ++k) set_cell(cells, k, -CUDART_INF_F);
+            for (; cell < n_cells; ++cell) set_cell(cells, cell, -CUDART_INF_F);
         float z_tok = 0.f;
         if (tok >= p.vocab && p.status) atomicOr(p.status, DFLASH_DEV_BAD_TOKEN);
         if (tok >= 0 && tok < p.vocab) z_tok = as_f(reinterpret_cast<const T*>(p.logits)[(int64_t)r * p.ld + tok]);
