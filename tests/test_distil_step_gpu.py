@@ -1,11 +1,15 @@
 """A training step as it is put together: a teacher's alternatives, the student's log probabilities at them, the gradient of their cross entropy, and the
 AdamW step of the weights, against the same in 64 bits."""
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
 
 from oracle import dflash_oracle as orc
 from paper_2602_06036_b200 import binding, synth
+from tests.conftest import ROOT
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +57,45 @@ def test_distilling_a_head_from_a_teacher_s_alternatives(bits):
         w = weight.double().cpu().numpy()                       # each step is judged from the state that it finds
         wide = lambda k: entry[k].double().cpu().numpy() * (np.repeat(entry[k + "_scale"].double().cpu().numpy(), 128) if bits == 8 else 1.0)
         m, root = wide("exp_avg"), wide("exp_avg_sq") if bits == 8 else np.sqrt(wide("exp_avg_sq"))
+
+
+FIRST_CALLS = """
+import torch
+from paper_2602_06036_b200 import binding, synth
+lib = binding.DFlash(synth.TINY)
+f = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt, device="cuda")
+torch.manual_seed(0)
+sets = []
+for n, v in ((3, 50000), (700, 2000)):                        # by clusters, and CTAs that go through several rows
+    z = torch.randn(n, v, device="cuda").bfloat16()
+    t = torch.randint(0, v, (n, 2), device="cuda", dtype=torch.int32)
+    sets.append((z, t, dict(logprob=f(n, 2), stats=f(n, 2), entropy=f(n), top_ids=f(n, 7, dt=torch.int32), top_logprob=f(n, 7)), f(n, 2) + 0.5, torch.zeros_like(z)))
+entry = dict(param=f(5000) + 1, grad=f(5000) + 0.1, exp_avg=f(5000), exp_avg_sq=f(5000))
+plan, norm = lib.adamw_plan([entry]), f(1)
+
+def work():
+    for z, t, out, g, dz in sets:
+        lib.dflash_token_logprobs(z, t, **out)
+        lib.dflash_token_logprobs_bwd(z, t, out["stats"], g, dz)
+    lib.dflash_adamw_step(plan, 1, 0.01, max_grad_norm=1.0, grad_norm=norm)
+
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):                                 # nothing of the library has run in this process
+    work()
+graph.replay()
+torch.cuda.synchronize()
+got = [x.clone() for s in sets for x in (*s[2].values(), s[4])] + [entry["param"].clone(), norm.clone()]
+for k in ("exp_avg", "exp_avg_sq"):
+    entry[k].zero_()
+entry["param"].fill_(1)
+work()
+torch.cuda.synchronize()
+want = [x for s in sets for x in (*s[2].values(), s[4])] + [entry["param"], norm]
+assert all(torch.equal(a, b) for a, b in zip(got, want)) and int(lib.status) == 0 and float(norm) > 0
+print("same")
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    run = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and "same" in run.stdout, run.stderr[-2000:]
