@@ -284,16 +284,10 @@ def _stream(stream) -> C.c_void_p:
     return C.c_void_p(s.cuda_stream)
 
 
-def _current_stream(index: int) -> int:
-    """cudaStream_t of a device's current stream; without the Stream object around it, where torch offers that (1 us less)."""
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
-
-
-def _current_device() -> int:
-    """torch.cuda.current_device() without its look at whether CUDA is initialised, which a handle's tensors have seen to."""
-    get = getattr(torch._C, "_cuda_getDevice", None)
-    return get() if get is not None else torch.cuda.current_device()
+# cudaStream_t of a device's current stream, without the Stream object around it where torch offers that (1 us less)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+# torch.cuda.current_device() without its look at whether CUDA is initialised, which a handle's tensors have seen to
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def launch_count() -> int:
@@ -594,10 +588,11 @@ class DFlash:
         """Address of a contiguous tensor of this handle's device, of the given type and shape; None for None."""
         if t is None:
             return None
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self._index and t.is_contiguous():
+            return t.data_ptr()
         assert t.dtype is dtype, f"{dtype} tensor expected, got {t.dtype}"
         assert t.get_device() == self._index and t.is_contiguous(), f"contiguous tensor on {self.device} expected"
-        assert t.shape == shape, f"shape {shape} expected, got {tuple(t.shape)}"
-        return t.data_ptr()
+        raise AssertionError(f"shape {shape} expected, got {tuple(t.shape)}")
 
     def _pool(self, kv_pool):
         c = self.cfg
