@@ -132,6 +132,35 @@ def test_a_large_tensor(lib):
     run_and_check(lib, [tensor(5_000_003, "mixed", BF16, 8, seed=1), tensor(3_000_001, "bf16", BF16, 32, seed=2)], t=1000, max_norm=1.0)
 
 
+def test_a_tensor_of_more_than_32_bits_of_entries(lib):
+    """Three pieces of it, the last one behind entry 2^31, against the same step of each piece alone."""
+    n, piece = 2 ** 31 + 301, 1024
+    big = {"param": torch.empty(n, dtype=BF16, device="cuda"), "grad": torch.zeros(n, dtype=BF16, device="cuda"), "weight_decay": 0.1}
+    for k in ("exp_avg", "exp_avg_sq"):
+        big[k] = torch.zeros(n, dtype=torch.uint8, device="cuda").view(E4M3)
+        big[k + "_scale"] = torch.zeros(-(-n // 128), device="cuda")
+    big["param"].fill_(1.0)
+    parts = []
+    for i, at in enumerate((0, 2 ** 30, 2 ** 31 - 768)):
+        e = tensor(min(piece, n - at), "bf16", BF16, 8, seed=i)
+        for k in ("param", "grad", "exp_avg", "exp_avg_sq"):
+            big[k].view(torch.uint8 if k[0] == "e" else BF16)[at:at + piece].copy_(e[k].view(torch.uint8 if k[0] == "e" else BF16))
+        for k in ("exp_avg_scale", "exp_avg_sq_scale"):
+            big[k][at // 128:at // 128 + len(e[k])].copy_(e[k])
+        parts.append((at, e))
+    norm, same = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    lib.dflash_adamw_step(lib.adamw_plan([big]), 3, 1e-2, max_grad_norm=0.01, grad_norm=norm)
+    lib.dflash_adamw_step(lib.adamw_plan([e for _, e in parts]), 3, 1e-2, max_grad_norm=0.01, grad_norm=same)
+    torch.cuda.synchronize()
+    assert abs(float(norm) / float(same) - 1) <= 4 * U          # added up in another order
+    for at, e in parts:
+        m = len(e["param"])
+        off = (big["param"][at:at + m].float() - e["param"].float()).abs()
+        assert bool((off <= 2.0 ** -7 * e["param"].float().abs()).all()) and bool((e["param"] != 1).any())      # a rounding either way where the factor is an ulp off
+        same_code = big["exp_avg"].view(torch.uint8)[at:at + m] == e["exp_avg"].view(torch.uint8)
+        assert float(same_code.float().mean()) > 0.98
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("t,beta1,beta2", [(1, 0.9, 0.999), (1, 0.0, 0.0), (100000, 0.95, 0.9999), (2 ** 31 - 1, 0.9, 0.95)])
 def test_first_and_late_steps(lib, bits, t, beta1, beta2):

@@ -104,6 +104,7 @@ def check_forward(o, z, tokens, T, top):
     (6, 32000, BF16, 4, 0, 1.0, 0, 0),
     (1300, 3001, BF16, 2, 9, 1.0, 3, 1),            # a CTA goes through several rows, which start differently
     (1200, 1500, F32, 1, 0, 1.0, 0, 2),
+    (1, 3000001, BF16, 1, 30, 1.0, 0, 3),           # hundreds of tiles
 ])
 def test_matches_the_oracle(lib, n, v, dtype, k, top, T, pad, at):
     z, tokens = logits(n, v, dtype, n + v), given(n, v, k, n + v)
@@ -155,13 +156,17 @@ def row_of(kind, v, dtype, rng):
         z *= 1e30
     elif kind == "one huge":
         z[v // 2] = 3e4
+    elif kind.startswith("few threads"):                       # large entries where few threads look: many are above what bounds those threads' largest
+        per = 16 // torch.empty(0, dtype=dtype).element_size()
+        hot = (np.arange(v) // per * 37) % 256 < int(kind.split()[-1])
+        z = np.where(hot, 20.0 + rng.random(v), z * 0.01)
     elif kind == "far ends":                                   # ties at the top of a range of values that passes 31 bits
         z = np.where(rng.random(v) < 0.5, 1.5e38, -1.5e38)
     return z
 
 
 KINDS = ["constant", "two values", "rising", "falling", "masked", "all masked", "lowest", "all lowest", "lowest and -inf", "one", "nan", "nan and -inf", "all nan",
-         "inf", "zeros of both signs", "huge", "one huge", "far ends"]
+         "inf", "zeros of both signs", "huge", "one huge", "far ends", "few threads 6", "few threads 140"]
 
 
 @pytest.mark.parametrize("v", [50, 5003, 40000])
@@ -320,6 +325,20 @@ def test_gradient_through_the_alternatives(lib):
     d = torch.empty(6, 400, device="cuda")
     lib.dflash_token_logprobs_bwd(z.cuda(), o["top_ids"], o["stats"], g.cuda(), d)
     check_backward(d, z, o["top_ids"].cpu(), g, None, 1.0, F32)
+
+
+def test_rows_beyond_32_bits(lib):
+    """The last row begins 2^31 entries behind the first one, in the logits and in the gradient."""
+    n, v, apart = 9, 5000, 2 ** 28
+    z, tokens = logits(n, v, BF16, 31), given(n, v, 2, 31)
+    zd = torch.empty(8 * apart + v, dtype=BF16, device="cuda").as_strided((n, v), (apart, 1))
+    zd.copy_(z)
+    o = forward(lib, zd, tokens.cuda(), 1.0, 9)
+    torch.cuda.synchronize()
+    check_forward(o, z, tokens, 1.0, 9)
+    g = torch.randn(n, 2)
+    lib.dflash_token_logprobs_bwd(zd, tokens.cuda(), o["stats"], g.cuda(), zd)
+    check_backward(zd, z, tokens, g, None, 1.0, BF16)
 
 
 def test_runs_agree_bit_by_bit(lib):
