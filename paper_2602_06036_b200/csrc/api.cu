@@ -805,12 +805,14 @@ int32_t dflash_block_attention_bwd(dflash_handle* h, const dflash_attn_bwd_args*
 // ---- log probabilities ----
 static bool is_dtype(int32_t d) { return d == DFLASH_F32 || d == DFLASH_BF16; }
 static bool on_elements(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % elem_size(dtype) == 0; }
+// 1 / T and log2(e) / T are factors of the kernels
+static bool is_temperature(float t) { return t > 0.f && std::isfinite(t) && std::isfinite((float)(1.4426950408889634 / (double)t)); }
 constexpr int32_t MAX_VOCAB = 1 << 30, MAX_LOGIT_ROWS = 1 << 28;      // the kernels count entries of a row, and their CTAs, in 32 bits
 
 int32_t dflash_token_logprobs(dflash_handle* h, const dflash_token_logprobs_args* a, void* stream) {
     if (!h || !a) return DFLASH_ERR_INVALID_ARG;
     if (a->n_rows < 0 || a->vocab < 1 || a->n_tokens < 0 || a->n_top < 0 || !is_dtype(a->logits_dtype)) return DFLASH_ERR_INVALID_ARG;
-    if (!(a->temperature > 0.f) || !std::isfinite(a->temperature) || !std::isfinite(1.f / a->temperature)) return DFLASH_ERR_INVALID_ARG;
+    if (!is_temperature(a->temperature)) return DFLASH_ERR_INVALID_ARG;
     if (a->n_tokens > LP_MAX_TOKENS || a->n_top > LP_MAX_TOP || a->vocab > MAX_VOCAB || a->n_rows > MAX_LOGIT_ROWS) return DFLASH_ERR_UNSUPPORTED;
     if (a->n_rows == 0) return DFLASH_OK;
     if (!a->logits || !on_elements(a->logits, a->logits_dtype) || (a->row_stride && a->row_stride < a->vocab)) return DFLASH_ERR_INVALID_ARG;
@@ -824,7 +826,7 @@ int32_t dflash_token_logprobs(dflash_handle* h, const dflash_token_logprobs_args
 int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_bwd_args* a, void* stream) {
     if (!h || !a) return DFLASH_ERR_INVALID_ARG;
     if (a->n_rows < 0 || a->vocab < 1 || a->n_tokens < 0 || !is_dtype(a->logits_dtype) || !is_dtype(a->dlogits_dtype)) return DFLASH_ERR_INVALID_ARG;
-    if (!(a->temperature > 0.f) || !std::isfinite(a->temperature) || !std::isfinite(1.f / a->temperature)) return DFLASH_ERR_INVALID_ARG;
+    if (!is_temperature(a->temperature)) return DFLASH_ERR_INVALID_ARG;
     if (a->n_tokens > LP_MAX_TOKENS || a->vocab > MAX_VOCAB || a->n_rows > MAX_LOGIT_ROWS) return DFLASH_ERR_UNSUPPORTED;
     if ((int64_t)a->n_rows * ((a->vocab + 8191) / 8192) > INT32_MAX) return DFLASH_ERR_UNSUPPORTED;
     if (a->n_rows == 0) return DFLASH_OK;

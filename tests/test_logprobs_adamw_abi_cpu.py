@@ -108,3 +108,12 @@ def test_adamw(lib, h):
     assert lib.dflash_adamw_step(None, C.byref(make()), None) == -1 and lib.dflash_adamw_step(h, None, None) == -1
     w = lib.dflash_adamw_workspace_bytes
     assert 0 < w(h, 0) == w(h, 320) < w(h, 321) and w(h, -1) == -1 and w(None, 1) == -1
+
+
+@pytest.mark.parametrize("temperature", [1e-45, 2.9e-39, 3.5e-39, 4.2e-39])
+def test_temperatures_whose_factors_are_infinite(lib, h, temperature):
+    """log2(e) / T passes fp32's range below 4.24e-39, where 1 / T (from 2.94e-39 on) still fits: 0 times it would make NaN of a row's maximum."""
+    a = binding.TokenLogprobsArgs(P, 0, 0, 4, 1000, temperature, 2, P, P, P, P, 5, P, P, None)
+    assert lib.dflash_token_logprobs(h, C.byref(a), None) == -1
+    b = binding.TokenLogprobsBwdArgs(P, 1, 0, 4, 1000, temperature, 2, P, P, P, P, P, 2 * P, 1, 0, None)
+    assert lib.dflash_token_logprobs_bwd(h, C.byref(b), None) == -1
