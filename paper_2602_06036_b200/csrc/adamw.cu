@@ -23,6 +23,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <limits>
 #include <type_traits>
 
 namespace dflash {
@@ -433,7 +434,7 @@ int launch_tables(const Launch& L, const dflash_adamw_args& a) {
     p.ln_b1 = a.beta1 > 0.0 ? std::log(a.beta1) : -INFINITY;
     p.ln_b2 = a.beta2 > 0.0 ? std::log(a.beta2) : -INFINITY;
     p.b1 = (float)a.beta1; p.b2 = (float)a.beta2; p.one_b1 = (float)(1.0 - a.beta1); p.one_b2 = (float)(1.0 - a.beta2);
-    p.eps = (float)a.eps; p.grad_scale = (float)a.grad_scale; p.max_norm = (float)a.max_grad_norm; p.status = L.status;
+    p.eps = (float)a.eps; p.grad_scale = (float)a.grad_scale; p.max_norm = a.max_grad_norm > 0.0 ? std::max((float)a.max_grad_norm, std::numeric_limits<float>::denorm_min()) : 0.f; p.status = L.status;
     const double bc1 = a.step_dev ? 1.0 : -std::expm1(a.step * p.ln_b1), bc2 = a.step_dev ? 1.0 : -std::expm1(a.step * p.ln_b2);
     p.rsqrt_bc2 = (float)(1.0 / std::sqrt(bc2));
     const double lr = a.lr_dev ? 1.0 : a.lr;

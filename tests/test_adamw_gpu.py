@@ -209,6 +209,15 @@ def test_a_norm_that_is_not_finite_leaves_everything_as_it_was(lib):
     lib.status.zero_()
 
 
+def test_a_clipping_norm_below_fp32s_range_still_clips(lib):
+    """Gradients times 1e-50 / norm are 0 in fp32: new states stay 0, and so do the weights' steps."""
+    e = tensor(300, "fp32", F32, 32, seed=4, wd=0.0, fresh=True)
+    old = e["param"].clone()
+    lib.dflash_adamw_step(lib.adamw_plan([e]), 1, 1e-3, max_grad_norm=1e-50)
+    torch.cuda.synchronize()
+    assert torch.equal(e["param"], old) and not e["exp_avg"].any() and not e["exp_avg_sq"].any()
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_without_the_norm_such_a_gradient_stays_in_its_place(lib, bits):
     e = tensor(400, "fp32", F32, bits, seed=3)
