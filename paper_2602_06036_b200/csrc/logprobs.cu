@@ -17,8 +17,13 @@
 namespace dflash {
 namespace {
 
-constexpr int THREADS = 256, WARPS = THREADS / 32, UNROLL = 4, CTAS_PER_SM = 4;
-constexpr int TILE = THREADS * UNROLL, TILE_BYTES = TILE * 16;      // 16-byte vectors of a tile: UNROLL a thread
+constexpr int UNROLL = 4;
+// A CTA of 256 threads, or of fewer where rows are short and many (see `launch_forward`)
+template <int N>
+struct Cta {
+    static constexpr int THREADS = N, WARPS = N / 32, PER_SM = 1024 / N;
+    static constexpr int TILE = N * UNROLL, TILE_BYTES = TILE * 16;      // 16-byte vectors of a tile: UNROLL a thread
+};
 constexpr int STAGES = 2;                                      // tiles under way
 constexpr int MAX_CLUSTER = 8;
 constexpr float LN2 = 0.6931471805599453f;
@@ -252,12 +257,14 @@ constexpr uint32_t ORDERED_NONE = 0x007fffffu;                 // ordered(-inf)
 constexpr unsigned long long NO_KEY = (unsigned long long)ORDERED_NONE << 32 | 0xffffffffu;      // not below any key of -inf, below all others
 
 __host__ __device__ __forceinline__ int most_of(int n_top) { return n_top + n_top / 4 + 8; }      // entries that a bound on the n_top-th largest may leave
-__host__ __device__ __forceinline__ int capacity_of(int n_top) { return most_of(n_top) + THREADS; }      // of the list: a turn's entries fit behind one that has been cut
+__host__ __device__ __forceinline__ int capacity_of(int n_top, int threads) { return most_of(n_top) + threads; }      // of the list: a turn's entries fit behind one that has been cut
+// what a CTA of so many threads takes: of more than half of its threads' largest entries the bound below is a weak one, and each given token has a thread
+constexpr bool takes(int threads, int n_top, int n_tokens) { return 2 * n_top <= threads && n_tokens <= threads; }
 // Cells of a thread: its part of a row in as many runs of tiles. Of more cells fewer vectors are read again (2048 x 151936 bf16 with 64 alternatives: 140 us with 16,
 // 154 with 8), but shared memory is taken from L1 in steps, which the copies under way need: 16 are worth it where they keep a CTA below 48.5 KB
 // and many candidates are looked for.
 __host__ __device__ __forceinline__ int cells_of(int n_top) { return n_top > 32 && n_top <= 64 ? 16 : 8; }
-static_assert(LP_MAX_TOP + LP_MAX_TOP / 4 + 8 <= THREADS && 16 * THREADS <= 65536, "");
+static_assert(takes(256, LP_MAX_TOP, LP_MAX_TOKENS) && 32 + 32 / 4 + 8 <= 64 && 16 * 256 <= 65536, "the most that a bound leaves has a thread each; cells in 16 bits");
 
 constexpr int BIN_BITS = 6, BINS = 1 << BIN_BITS;                   // of the range of the threads' largest entries
 
@@ -265,7 +272,9 @@ constexpr int BIN_BITS = 6, BINS = 1 << BIN_BITS;                   // of the ra
 // n_top threads' largest entries bound the n_top-th largest of the stretch from below, and little else is above a bound that few of them are (`bound`).
 // What is, lies in a few cells, which are read again (from L2, mostly) by all threads together. The pass itself so needs no barrier and looks at no
 // entry twice; taking candidates out as they come by cost a barrier a tile and more than the reading of the row.
+template <class C>
 struct Candidates {
+    static constexpr int THREADS = C::THREADS, WARPS = C::WARPS;
     unsigned long long* list;      // [capacity] keys
     unsigned long long* few;       // [most]
     uint16_t* cells;               // [n_cells][THREADS] largest entries as bf16, rounded up
@@ -466,6 +475,7 @@ struct Candidates {
     }
 };
 // Lanes that share a key's comparisons: as many as there are threads for
+template <int THREADS>
 __device__ __forceinline__ int lanes_a_key(int n) { return n <= THREADS / 8 ? 8 : n <= THREADS / 4 ? 4 : n <= THREADS / 2 ? 2 : 1; }
 // The place of key `mine` among n keys, largest first: by `lanes` neighbouring lanes, of which this is the part-th; all of them get it
 __device__ __forceinline__ int rank_of(const unsigned long long* list, int n, unsigned long long mine, int part, int lanes) {
@@ -475,6 +485,7 @@ __device__ __forceinline__ int rank_of(const unsigned long long* list, int n, un
     for (int o = lanes >> 1; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
     return above;
 }
+template <int THREADS>
 __device__ __forceinline__ void set_cell(uint16_t* cells, int cell, float top) {
     const uint32_t b = __float_as_uint(top);                   // (towards +inf: of a negative number the rest is cut off; NaN stays NaN in a cell that then counts as none)
     cells[cell * THREADS + threadIdx.x] = (uint16_t)((b & 0x80000000u ? b : b + 0xffffu) >> 16);
@@ -504,12 +515,12 @@ __device__ __forceinline__ void st_cluster_u64(const void* local_smem, uint32_t 
 // Shared memory behind the tiles under way, in 8-byte words: cells, list, few, what the CTAs of a cluster tell each other (twice 8 bytes each) and their keys, found
 struct Layout {
     int cells, list, few, told, keys, found, words;
-    __host__ __device__ Layout(int n_top, int cs) {
+    __host__ __device__ Layout(int n_top, int cs, int threads) {
         const int most = n_top > 0 ? most_of(n_top) : 0, n_cells = n_top > 0 ? cells_of(n_top) : 0;
         cells = 0;
-        told = cells + n_cells * THREADS / 4;
+        told = cells + n_cells * threads / 4;
         list = told + (cs > 1 ? 2 * cs : 0);
-        few = list + (n_top > 0 ? capacity_of(n_top) : 0);
+        few = list + (n_top > 0 ? capacity_of(n_top, threads) : 0);
         keys = few + most;
         found = keys + (cs > 1 ? cs * n_top : 0);
         words = found + most * n_cells / 4;
@@ -517,21 +528,21 @@ struct Layout {
 };
 
 // The search as a call of its own: its registers are not the pass's
-template <typename T>
+template <typename T, class C>
 __device__ __noinline__ int search_stretch(const T* z, int vocab, int lo_j, int hi_j, int per_cell, float top, int n_top, int cs, unsigned long long* words, int* count,
                                            uint32_t* ends) {
-    const Layout at(n_top, cs);
-    Candidates cand;
+    const Layout at(n_top, cs, C::THREADS);
+    Candidates<C> cand;
     cand.list = words + at.list;
     cand.few = words + at.few;
     cand.cells = reinterpret_cast<uint16_t*>(words + at.cells);
     cand.found = reinterpret_cast<uint16_t*>(words + at.found);
     cand.count = count;
     cand.ends = ends;
-    cand.bins = reinterpret_cast<int*>(ends + 2 * WARPS);
+    cand.bins = reinterpret_cast<int*>(ends + 2 * C::WARPS);
     cand.n_top = n_top;
     cand.most = most_of(n_top);
-    cand.capacity = capacity_of(n_top);
+    cand.capacity = capacity_of(n_top, C::THREADS);
     cand.n_cells = cells_of(n_top);
     return cand.search(Row<T>(z, vocab), lo_j, hi_j, per_cell, top);
 }
@@ -546,9 +557,9 @@ struct Stretch {
         lo = min(rank * per, row.n_vec);
         hi = min(row.n_vec, lo + per);
     }
-    __device__ __forceinline__ int tiles() const { return (hi - lo + TILE - 1) / TILE; }
 };
 // Tiles [from, from + count) of a stretch, all of whose vectors are among [first, last)
+template <int TILE>
 struct Span {
     int from;
     uint32_t count;
@@ -559,15 +570,16 @@ struct Span {
 
 // A cluster of CS CTAs per row, a CTA per stretch of its vectors. One CTA a row: it goes on with another row, whose first tiles are then already under way;
 // several: the grid has a cluster for each row.
-template <typename T, int CS>
-__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(const ForwardParams p) {
+template <typename T, int CS, class C>
+__global__ void __launch_bounds__(C::THREADS, C::PER_SM) token_logprobs_kernel(const ForwardParams p) {
+    constexpr int THREADS = C::THREADS, WARPS = C::WARPS, TILE = C::TILE, TILE_BYTES = C::TILE_BYTES;
     extern __shared__ uint4 ring[];                        // [STAGES][TILE]: a thread reads what it has copied itself
     __shared__ Stat sh[WARPS];
     __shared__ uint32_t ends[2 * WARPS + BINS];            // and the search's bins
     __shared__ int count[2];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = CS > 1 ? (int)ptx::cluster_ctarank() : 0;
     unsigned long long* words = reinterpret_cast<unsigned long long*>(ring + STAGES * TILE);
-    const Layout at(p.n_top, CS);
+    const Layout at(p.n_top, CS, THREADS);
     Told* told = reinterpret_cast<Told*>(words + at.told);
     unsigned long long* keys = words + at.keys;
     unsigned long long* list = words + at.list;
@@ -582,13 +594,13 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
     // the next tile to be requested: the k-th of row r's stretch, whose part for this thread begins at `from`; `plain` ones lie inside of the buffer
     int ahead_r = blockIdx.x / CS, ahead_k = 0, ahead_tiles = 0;
     const char* ahead_at = nullptr;
-    Span plain;
+    Span<TILE> plain;
     const auto look_ahead = [&]() {                        // at row ahead_r
         const Stretch<T, CS> n(p, rank, ahead_r);
         ahead_k = 0;
-        ahead_tiles = n.tiles();
+        ahead_tiles = (n.hi - n.lo + TILE - 1) / TILE;
         ahead_at = n.row.address(n.lo) + tid * 16;
-        plain = Span(n.lo, n.row.base < begin, min(n.hi, n.row.n_vec - (n.row.address(n.row.n_vec) > p.end)));
+        plain = Span<TILE>(n.lo, n.row.base < begin, min(n.hi, n.row.n_vec - (n.row.address(n.row.n_vec) > p.end)));
     };
     look_ahead();                                          // (the grid has no more clusters than there are rows)
     const uint32_t slots = ptx::smem_u32(ring + tid);
@@ -628,8 +640,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
         Running t;
         t.reset();
         float peak = -CUDART_INF_F, cell_top = -CUDART_INF_F;
-        const int tiles = cur.tiles(), tiles_a_cell = (tiles + n_cells - 1) / n_cells, per_cell = tiles_a_cell * UNROLL;
-        const Span whole(cur.lo, row.shift > 0, min(cur.hi, (p.vocab + row.shift) / Row<T>::VE));      // tiles inside of the row
+        const int tiles = (cur.hi - cur.lo + TILE - 1) / TILE, tiles_a_cell = (tiles + n_cells - 1) / n_cells, per_cell = tiles_a_cell * UNROLL;
+        const Span<TILE> whole(cur.lo, row.shift > 0, min(cur.hi, (p.vocab + row.shift) / Row<T>::VE));      // tiles inside of the row
         int cell = 0, in_cell = 0;
         for (int k = 0; k < tiles; ++k) {
             copy_wait<STAGES - 1>();
@@ -659,7 +671,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
             if (p.n_top > 0) {
                 cell_top = fmaxf(cell_top, top);
                 if (++in_cell == tiles_a_cell || k + 1 == tiles) {
-                    set_cell(cells, cell++, cell_top);
+                    set_cell<THREADS>(cells, cell++, cell_top);
                     cell_top = -CUDART_INF_F;
                     in_cell = 0;
                 }
@@ -674,7 +686,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
             }
         }
         if (p.n_top > 0)
-            for (; cell < n_cells; ++cell) set_cell(cells, cell, -CUDART_INF_F);
+            for (; cell < n_cells; ++cell) set_cell<THREADS>(cells, cell, -CUDART_INF_F);
         float z_tok = 0.f;
         if (tok >= p.vocab && p.status) atomicOr(p.status, DFLASH_DEV_BAD_TOKEN);
         if (tok >= 0 && tok < p.vocab) z_tok = as_f(reinterpret_cast<const T*>(p.logits)[(int64_t)r * p.ld + tok]);
@@ -682,10 +694,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
         Stat x = lanes_merged<32>(t.total(peak, p.c), p.c);
         if (lane == 0) sh[warp] = x;
         int n_list = 0;
-        if (p.n_top > 0) n_list = search_stretch(reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld, p.vocab, cur.lo, cur.hi, per_cell, peak, p.n_top, CS, words, count, ends);
+        if (p.n_top > 0) n_list = search_stretch<T, C>(reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld, p.vocab, cur.lo, cur.hi, per_cell, peak, p.n_top, CS, words, count, ends);
         else __syncthreads();
         x = lanes_merged<WARPS>(sh[lane % WARPS], p.c);
-        const int lanes = lanes_a_key(n_list), own = tid / lanes;
+        const int lanes = lanes_a_key<THREADS>(n_list), own = tid / lanes;
         const unsigned long long key = own < n_list ? list[own] : 0;
         const int rank_in_list = p.n_top > 0 ? rank_of(list, n_list, key, tid % lanes, lanes) : 0;
         const int place = own < n_list && tid % lanes == 0 ? rank_in_list : p.n_top;
@@ -773,14 +785,14 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) token_logprobs_kernel(co
 
 // The rows by clusters of CS CTAs. Clusters are placed on as few SMs as hold them, while others idle; so a CTA takes a share of
 // the SM's shared memory that leaves room for `per_sm` of them and no more (32 x 151936 bf16, four CTAs a row: 9.8 us with room for four, 6.9 for one).
-template <typename T, int CS>
+template <typename T, int CS, class C>
 cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
     constexpr int SM_SMEM = 228 * 1024, CTA_EXTRA = 2048;      // what an SM has, and what a CTA takes beside its dynamic part, rounded up
     static bool attr_set[MAX_DEVICES] = {};
     static int alone[MAX_DEVICES] = {};                        // clusters that fit at one CTA per SM
-    const int dev = current_device_slot(), words = Layout(p.n_top, CS).words * 8;
+    const int dev = current_device_slot(), words = Layout(p.n_top, CS, C::THREADS).words * 8;
     if (dev < 0) return cudaErrorInvalidDevice;
-    const auto kernel = token_logprobs_kernel<T, CS>;
+    const auto kernel = token_logprobs_kernel<T, CS, C>;
     if (!attr_set[dev]) {
         const int most = SM_SMEM - 1024 - CTA_EXTRA;
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
@@ -789,7 +801,7 @@ cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st
         if (CS > 1) {
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(CS);
-            cfg.blockDim = dim3(THREADS);
+            cfg.blockDim = dim3(C::THREADS);
             cfg.dynamicSmemBytes = most;
             cudaLaunchAttribute attr[1];
             attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -802,14 +814,24 @@ cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st
         alone[dev] = n;
         attr_set[dev] = true;
     }
-    const int per_sm = std::max(1, std::min(CTAS_PER_SM, (p.n_rows + alone[dev] - 1) / alone[dev]));
-    const size_t smem = std::max<size_t>((size_t)STAGES * TILE_BYTES + words, per_sm < CTAS_PER_SM ? SM_SMEM / (per_sm + 1) : 0);
-    if (CS == 1) return launch_pdl(kernel, dim3(std::min(p.n_rows, CTAS_PER_SM * sm_count)), dim3(THREADS), smem, st, p);
-    return launch_pdl_cluster(kernel, dim3(p.n_rows * CS), dim3(THREADS), smem, st, CS, p);
+    const int per_sm = std::max(1, std::min(C::PER_SM, (p.n_rows + alone[dev] - 1) / alone[dev]));
+    const size_t smem = std::max<size_t>((size_t)STAGES * C::TILE_BYTES + words, per_sm < C::PER_SM ? SM_SMEM / (per_sm + 1) : 0);
+    if (CS == 1) return launch_pdl(kernel, dim3(std::min(p.n_rows, C::PER_SM * sm_count)), dim3(C::THREADS), smem, st, p);
+    return launch_pdl_cluster(kernel, dim3(p.n_rows * CS), dim3(C::THREADS), smem, st, CS, p);
 }
 
 template <typename T>
 cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
+    using Wide = Cta<256>;
+    constexpr int TILE = Wide::TILE, CTAS_PER_SM = Wide::PER_SM;
+    // Short rows that are many: smaller CTAs, and so more rows under way an SM. What a row costs beside its tiles (barriers, sums, the search) then overlaps with other rows'
+    // work, and less of its last tile is empty. Worth it once there are rows for all CTAs of the next larger size: bf16, 20 alternatives, 64 x 1024 with 256, 128 and
+    // 64 threads 5.6, 5.5 and 5.9 us, 1200 x 1024 17.4, 11.5 and 8.0. In long rows the bound from fewer threads leaves larger cells to be read again, of fp32
+    // sooner, whose pass HBM holds already: bf16 4096 x 50257 120 and 97 us with 256 and 128, 2048 x 151936 128 and 133 (64 alternatives: 65536 80 and 85,
+    // 32000 105 and 98); fp32 4096 x 14000 70 and 57, 32000 101 and 103; with 128 and 64 bf16 4096 x 5003 40 and 29, 16384 44 and 42, fp32 16384 62 and 67.
+    const int64_t row = (int64_t)p.vocab * (int64_t)sizeof(T), few = (int64_t)(p.n_top <= 32 ? 112 : 64) << (sizeof(T) == 4 ? 9 : 10);
+    if (row <= 32 << 10 && p.n_rows >= Cta<128>::PER_SM * sm_count && takes(64, p.n_top, p.n_tokens)) return launch_forward<T, 1, Cta<64>>(p, sm_count, st);
+    if (row <= few && p.n_rows >= Wide::PER_SM * sm_count && takes(128, p.n_top, p.n_tokens)) return launch_forward<T, 1, Cta<128>>(p, sm_count, st);
     // CTAs per row: what takes the least time by a count of tile times. CTAs that share an SM share its rate, so that what counts is how evenly a turn of
     // CTAs fills the SMs; beside its tiles a turn takes the time of 4 tiles (9 with the search), and a cluster's meeting that of 2 to 4. (A tile time is
     // 0.46 us. 32 x 151936 bf16 by 1, 2, 4 and 8 CTAs a row: 14, 10, 7 and 8 us; 300 rows 26, 25, 27 and 38, with 20 alternatives 31, 32, 37 and 57; 800 rows
@@ -827,10 +849,10 @@ cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st
         }
     }
     switch (cs) {
-        case 1: return launch_forward<T, 1>(p, sm_count, st);
-        case 2: return launch_forward<T, 2>(p, sm_count, st);
-        case 4: return launch_forward<T, 4>(p, sm_count, st);
-        default: return launch_forward<T, 8>(p, sm_count, st);
+        case 1: return launch_forward<T, 1, Wide>(p, sm_count, st);
+        case 2: return launch_forward<T, 2, Wide>(p, sm_count, st);
+        case 4: return launch_forward<T, 4, Wide>(p, sm_count, st);
+        default: return launch_forward<T, 8, Wide>(p, sm_count, st);
     }
 }
 

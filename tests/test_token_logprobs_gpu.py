@@ -185,6 +185,30 @@ def test_rows_where_it_can_go_wrong(lib, v, dtype, top):
             check_forward({k: x[i * len(KINDS):(i + 1) * len(KINDS)] for k, x in o.items()}, z, tokens, 1.0, top)
 
 
+@pytest.mark.parametrize("n,v,dtype,top,k", [
+    (1200, 50, F32, 32, 3), (1200, 5003, BF16, 3, 64), (1200, 8001, F32, 32, 0), (1200, 16000, BF16, 20, 1),      # CTAs of 64 threads
+    (1200, 5003, BF16, 20, 65), (1200, 5003, F32, 33, 1), (600, 14300, F32, 32, 2), (600, 32000, BF16, 64, 128),   # of 128
+    (600, 57000, BF16, 8, 1),
+    (600, 5003, F32, 65, 1), (600, 33000, BF16, 40, 1),                                                             # of 256
+])
+def test_such_rows_by_the_hundred(lib, n, v, dtype, top, k):
+    """Short rows that are many go to smaller CTAs."""
+    rng = np.random.default_rng(v + top)
+    z = torch.from_numpy(np.stack([row_of(kind, v, dtype, rng) for kind in KINDS])).to(dtype)
+    tokens = given(len(KINDS), v, k, 5)
+    copies = n // len(KINDS)
+    zz = placed(z.repeat(copies, 1), 5 if v < 10000 else 0, 3)
+    o = forward(lib, zz, tokens.repeat(copies, 1).cuda(), 1.0, top)
+    torch.cuda.synchronize()
+    some = {}
+    for i in range(copies):                                    # (copies differ in the last bits where they start elsewhere between two borders)
+        part = {key: x[i * len(KINDS):(i + 1) * len(KINDS)] for key, x in o.items()}
+        some.setdefault(tuple(x.cpu().numpy().tobytes() for x in part.values()), part)
+    assert len(some) <= 8
+    for part in some.values():
+        check_forward(part, z, tokens, 1.0, top)
+
+
 def test_tiny_and_large_temperatures(lib):
     z, tokens = logits(4, 3001, F32, 9), given(4, 3001, 4, 9)
     for T in (1e-30, 1e-3, 1e6):
