@@ -857,7 +857,7 @@ cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st
 }
 
 // ---- gradient ----------------------------------------------------------------------------------------------------------
-constexpr int B_THREADS = 256, GROUP = 8;                      // groups of 8 entries a thread
+constexpr int GROUP = 8;                                       // groups of 8 entries a thread
 
 struct BackwardParams {
     const void* logits;
@@ -923,10 +923,12 @@ __device__ __forceinline__ void store_entry(float* dst, float g) { *dst = g; }
 __device__ __forceinline__ void store_entry(__nv_bfloat16* dst, float g) { *dst = __float2bfloat16_rn(g); }
 
 // CTA (row, piece of the row)
-template <typename T, typename O>
+template <typename T, typename O, int B_THREADS>
 __global__ void __launch_bounds__(B_THREADS) token_logprobs_bwd_kernel(const BackwardParams p) {
-    __shared__ int s_tok[LP_MAX_TOKENS];
-    __shared__ float s_g[LP_MAX_TOKENS], s_sum[B_THREADS / 32];
+    constexpr int MOST = B_THREADS < LP_MAX_TOKENS ? B_THREADS : LP_MAX_TOKENS;      // given tokens: a thread each
+    __shared__ int4 s_tok[MOST / 4];                           // -1 for none
+    __shared__ float4 s_g[MOST / 4];
+    __shared__ float s_sum[B_THREADS / 32];
     ptx::pdl_trigger();
     ptx::pdl_wait();
     const int tid = threadIdx.x;
@@ -934,19 +936,24 @@ __global__ void __launch_bounds__(B_THREADS) token_logprobs_bwd_kernel(const Bac
     const int lo = piece * p.per_piece, hi = min(p.vocab, lo + p.per_piece);
     const T* z = reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld;
     O* dz = reinterpret_cast<O*>(p.dlogits) + (int64_t)r * p.d_ld;
-    // ---- the row's numbers
+    // ---- the row's numbers, all of them requested before any is waited for
     int tok = -1;
     float g = 0.f, z_tok = 0.f;
+    const float top = p.stats[2 * (int64_t)r], log_sum = p.stats[2 * (int64_t)r + 1];
+    const float gh = p.d_entropy ? p.d_entropy[r] : 0.f, h = p.d_entropy ? p.entropy[r] : 0.f;
     if (tid < p.n_tokens) {
         tok = p.tokens[(int64_t)r * p.n_tokens + tid];
+        g = p.d_logprob[(int64_t)r * p.n_tokens + tid];
+        if (tok >= lo && tok < hi) z_tok = as_f(z[tok]);       // before any store: dlogits may be the logits
         if (tok >= p.vocab) {
             if (p.status && piece == 0) atomicOr(p.status, DFLASH_DEV_BAD_TOKEN);
             tok = -1;
         }
-        if (tok >= 0) g = p.d_logprob[(int64_t)r * p.n_tokens + tid];
-        if (tok >= lo && tok < hi) z_tok = as_f(z[tok]);       // before any store: dlogits may be the logits
-        s_tok[tid] = tok;
-        s_g[tid] = g;
+        if (tok < 0) g = 0.f;
+    }
+    if (tid < MOST) {
+        reinterpret_cast<int*>(s_tok)[tid] = tok;
+        reinterpret_cast<float*>(s_g)[tid] = g;
     }
     float sum = g;
 #pragma unroll
@@ -955,9 +962,7 @@ __global__ void __launch_bounds__(B_THREADS) token_logprobs_bwd_kernel(const Bac
     const int any = __syncthreads_or(g != 0.f);
     sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < LP_MAX_TOKENS / 32; ++w) sum += s_sum[w];
-    const float top = p.stats[2 * (int64_t)r], log_sum = p.stats[2 * (int64_t)r + 1];
-    const float gh = p.d_entropy ? p.d_entropy[r] : 0.f, h = p.d_entropy ? p.entropy[r] : 0.f;
+    for (int w = 0; w < MOST / 32; ++w) sum += s_sum[w];
     const bool off_row = (!any && gh == 0.f) || (top == -CUDART_INF_F && log_sum == 0.f);      // nothing comes in, or a row of -inf
     // with y = log2 p = (z - top) c - log_sum / ln 2:  dz = p (a + b y)
     const float sub = log_sum * LOG2E, a = -(sum + gh * h) * p.inv_t, b = -gh * LN2 * p.inv_t;
@@ -1006,17 +1011,20 @@ __global__ void __launch_bounds__(B_THREADS) token_logprobs_bwd_kernel(const Bac
     if (!off_row && tok >= lo && tok < hi) {
         float own = 0.f;
         bool earlier = false;
-        for (int i = 0; i < p.n_tokens; ++i) {
-            if (s_tok[i] == tok) {
-                earlier |= i < tid;
-                own += s_g[i];
-            }
+        for (int i = 0; i < p.n_tokens; i += 4) {
+            const int4 t = s_tok[i / 4];
+            const float4 d = s_g[i / 4];
+            own += t.x == tok ? d.x : 0.f;
+            own += t.y == tok ? d.y : 0.f;
+            own += t.z == tok ? d.z : 0.f;
+            own += t.w == tok ? d.w : 0.f;
+            earlier |= (t.x == tok && i < tid) || (t.y == tok && i + 1 < tid) || (t.z == tok && i + 2 < tid) || (t.w == tok && i + 3 < tid);
         }
         if (!earlier) store_entry(dz + tok, fmaf(own, p.inv_t, grad(z_tok)));
     }
 }
 
-template <typename T, typename O>
+template <typename T, typename O, int B_THREADS>
 cudaError_t launch_backward(BackwardParams p, int rows, int sm_count, cudaStream_t st) {
     // pieces of a row: whole tiles, few enough that a CTA's start is little beside its work, enough to fill the GPU
     constexpr int TILE = B_THREADS * 4 * GROUP;
@@ -1025,7 +1033,18 @@ cudaError_t launch_backward(BackwardParams p, int rows, int sm_count, cudaStream
     while (per > 1 && (int64_t)rows * ((tiles + per - 1) / per) < 8ll * sm_count) --per;
     p.per_piece = per * TILE;
     p.pieces = (p.vocab + p.per_piece - 1) / p.per_piece;
-    return launch_pdl(token_logprobs_bwd_kernel<T, O>, dim3((unsigned)((int64_t)rows * p.pieces)), dim3(B_THREADS), 0, st, p);
+    return launch_pdl(token_logprobs_bwd_kernel<T, O, B_THREADS>, dim3((unsigned)((int64_t)rows * p.pieces)), dim3(B_THREADS), 0, st, p);
+}
+
+template <typename T, typename O>
+cudaError_t launch_backward(const BackwardParams& p, int rows, int sm_count, cudaStream_t st) {
+    // With many rows smaller CTAs overlap what a row costs before its first load and after its last store with other rows' work (64 given tokens, 4096 x 1024 bf16
+    // with 256, 128 and 64 threads 22, 14 and 12 us, x 8192 36, 29 and 27; x 151936 with 256 and 128 449 and 428). fp32 gradients of long rows are better
+    // off in larger ones (4096 x 151936 750 and 803 us, x 2049 20 and 14).
+    constexpr bool O16 = sizeof(O) == 2;
+    if (O16 && p.vocab <= 8192 && rows >= 16 * sm_count && p.n_tokens <= 64) return launch_backward<T, O, 64>(p, rows, sm_count, st);
+    if ((O16 || p.vocab <= 4096) && rows >= 8 * sm_count) return launch_backward<T, O, 128>(p, rows, sm_count, st);
+    return launch_backward<T, O, 256>(p, rows, sm_count, st);
 }
 
 }  // namespace

@@ -322,6 +322,35 @@ def test_gradient_of_rows_where_it_can_go_wrong(lib, dtype, v):
     assert not d.any()
 
 
+@pytest.mark.parametrize("v,dtype,out,k,pad,at", [
+    (1000, F32, F32, 64, 0, 0), (1000, BF16, BF16, 64, 3, 1), (5003, BF16, BF16, 3, 0, 0), (8192, F32, BF16, 1, 0, 1),      # CTAs of 64 and of 128 threads
+    (5003, BF16, BF16, 65, 0, 2), (9001, BF16, BF16, 128, 0, 0), (4096, F32, F32, 128, 5, 0), (4099, F32, F32, 2, 0, 0),     # of 128 and 256
+])
+def test_gradients_of_rows_by_the_thousand(lib, v, dtype, out, k, pad, at):
+    """Many rows go to smaller CTAs. An entry's gradient is worked out alike in all of them, so a few rows on their own (checked against the oracle) have the same."""
+    n = 2400
+    z = torch.from_numpy(np.random.default_rng(v).normal(size=(n, v)).astype(np.float32) * 3).to(dtype)
+    tokens = given(n, v, k, v)
+    tokens[:, k // 2] = tokens[:, 0]
+    rng = np.random.default_rng(v)
+    g, gh = torch.from_numpy(rng.normal(size=(n, k))).float(), torch.from_numpy(rng.normal(size=n)).float()
+    zd, td, gd, ghd = placed(z, pad, at), tokens.cuda(), g.cuda(), gh.cuda()
+    o = forward(lib, zd, td, 1.3)
+    whole = torch.full((n, v), 5.0, dtype=out, device="cuda")
+    lib.dflash_token_logprobs_bwd(zd, td, o["stats"], gd, whole, temperature=1.3, entropy=o["entropy"], d_entropy=ghd)
+    for from_, to in ((0, 40), (1184, 1224), (2360, 2400)):
+        part = torch.full((n, v), 5.0, dtype=out, device="cuda")[from_:to]
+        lib.dflash_token_logprobs_bwd(zd[from_:to], td[from_:to], o["stats"][from_:to].contiguous(), gd[from_:to].contiguous(), part, temperature=1.3,
+                                      entropy=o["entropy"][from_:to].contiguous(), d_entropy=ghd[from_:to].contiguous())
+        torch.cuda.synchronize()
+        assert torch.equal(part, whole[from_:to])
+        check_backward(part, z[from_:to], tokens[from_:to], g[from_:to], gh[from_:to], 1.3, out)
+    some = torch.empty(1300, v, dtype=out, device="cuda")
+    lib.dflash_token_logprobs_bwd(zd[:1300], td[:1300], o["stats"][:1300], gd[:1300], some, temperature=1.3, entropy=o["entropy"][:1300], d_entropy=ghd[:1300])
+    torch.cuda.synchronize()
+    assert torch.equal(some[:1184], whole[:1184]) and torch.equal(some, whole[:1300])
+
+
 @pytest.mark.parametrize("dtype,v,pad", [(BF16, 20000, 0), (F32, 5003, 5)])
 def test_gradient_in_the_logits_own_place(lib, dtype, v, pad):
     z, tokens = logits(9, v, dtype, 3), given(9, v, 40, 3)
