@@ -613,7 +613,8 @@ int32_t dflash_block_loss(dflash_handle* h, const dflash_block_loss_args* a /*[h
  * sets DFLASH_DEV_BAD_TOKEN. Temperature scales the distribution, not the order of the alternatives.
  * One launch and one pass over the logits, no scratch memory: calls may overlap. Sums in fp32; against exact arithmetic the log probabilities are off by
  * some 1e-7 (plus 2^-24 of their size). Rows may start anywhere; of what lies between two rows up to 14 bytes on either side of a row may be read, but not used.
- * 32 rows of 151936 bf16 logits take 7 us, with 20 alternatives 10; 544 fp32 rows 52 and 58; 2048 bf16 rows 108 and 126 (64 alternatives: 141).
+ * 32 rows of 151936 bf16 logits take 7 us, with 20 alternatives 10; 544 fp32 rows 52 and 57; 2048 bf16 rows 108 and 122 (64 alternatives: 139);
+ * 4096 rows of 32000 52 and 69.
  * Errors: DFLASH_ERR_INVALID_ARG (null pointer, T below 4.3e-39 or not finite, bad dtype or sizes), DFLASH_ERR_UNSUPPORTED (n_tokens or n_top > 128,
  * vocab > 2^30, more than 2^28 rows). */
 typedef struct {

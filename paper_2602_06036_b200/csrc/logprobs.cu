@@ -5,9 +5,9 @@
 // Forward: one pass over the logits. Every thread keeps sums of e = exp(y) and of e y with a reference m in the place of M (see `Running`), and the largest entry
 // of each of a few parts of what it has seen, from which the row's n_top largest are found afterwards (see `Candidates`). Tiles come by asynchronous
 // copies into shared memory, two of them under way a CTA. Copies that go around L1 (.cg), bulk copies of 2 KB and a third tile were all slower (2048 x
-// 151936 fp32 222, 199 and 225 us against 186: L1 holds what is under way, and shared memory is taken from it).
+// 151936 fp32 222, 199 and 225 us against 186 at the time: L1 holds what is under way, and shared memory is taken from it).
 // Bound: fp32 by HBM (2048 x 151936: 181 us, the measured copy rate); bf16 by the special-function unit besides, one exponential an entry being 91 us of 108 there,
-// and by issue (8 slots an entry). With alternatives the search adds 20 (20 of them) to 35 us (64), when its CTAs' rows end together.
+// and by issue (7 slots an entry). With alternatives the search adds 14 (20 of them) to 31 us (64), when its CTAs' rows end together.
 #include "logprobs.cuh"
 #include "softmax_rows.cuh"
 
@@ -260,7 +260,7 @@ __host__ __device__ __forceinline__ int most_of(int n_top) { return n_top + n_to
 __host__ __device__ __forceinline__ int capacity_of(int n_top, int threads) { return most_of(n_top) + threads; }      // of the list: a turn's entries fit behind one that has been cut
 // what a CTA of so many threads takes: of more than half of its threads' largest entries the bound below is a weak one, and each given token has a thread
 constexpr bool takes(int threads, int n_top, int n_tokens) { return 2 * n_top <= threads && n_tokens <= threads; }
-// Cells of a thread: its part of a row in as many runs of tiles. Of more cells fewer vectors are read again (2048 x 151936 bf16 with 64 alternatives: 140 us with 16,
+// Cells of a thread: its part of a row in as many runs of tiles. Of more cells fewer vectors are read again (2048 x 151936 bf16 with 64 alternatives: 139 us with 16,
 // 154 with 8), but shared memory is taken from L1 in steps, which the copies under way need: 16 are worth it where they keep a CTA below 48.5 KB
 // and many candidates are looked for.
 __host__ __device__ __forceinline__ int cells_of(int n_top) { return n_top > 32 && n_top <= 64 ? 16 : 8; }
