@@ -300,6 +300,7 @@ class AdamwPlan:
     def __init__(self, entries, index: int):
         self.tensors = [dict(e) for e in entries]
         self.n = len(self.tensors)
+        self.index = index
         self.table = (AdamwTensor * max(self.n, 1))()
         written = []
         for i, e in enumerate(self.tensors):
@@ -743,6 +744,7 @@ class DFlash:
     def dflash_adamw_step(self, plan: AdamwPlan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, max_grad_norm=0.0, grad_norm=None, stream=None):
         """One AdamW step of all tensors of the plan. step (from 1) and lr: numbers, or int32 / fp32 tensors of one entry on the device (for captured
         calls). max_grad_norm > 0 clips by the norm of all gradients; grad_norm fp32 [1] receives it."""
+        assert plan.index == self._index, f"plan of tensors on device {plan.index} given to a handle on device {self._index}"
         on_device = lambda x: isinstance(x, torch.Tensor)  # noqa: E731
         ws, ws_bytes = None, 0
         if max_grad_norm > 0 or grad_norm is not None:
