@@ -677,8 +677,8 @@ int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_
  * block's 128 states).
  * 1.0e9 weights with master copies and clipping take 5.0 ms, with states of 8 bits 3.1. Groups of four entries that lie on their borders in every buffer of a
  * tensor (all starts multiples of 4 entries, or equally far behind one) are what is fast; states of 8 bits need the former.
- * Launches: one per 320 tensors, twice with the norm. Captured calls may be replayed: lr_dev and step_dev are then read at each replay. No two tensors
- * of a call may overlap; calls must not overlap in time if they share tensors or a workspace.
+ * Launches: one per 320 tensors, twice with the norm. Captured calls may be replayed: lr_dev and step_dev are then read at each replay. No buffer that a
+ * call writes may overlap another one of its buffers (gradients may be shared by tensors); calls must not overlap in time if they share tensors or a workspace.
  * Errors: DFLASH_ERR_INVALID_ARG (null pointer, address that is no multiple of the element's size, n < 0, bad dtype or state_bits, a master copy beside an fp32 param,
  * step < 1, betas outside [0, 1), eps below 2^-126, grad_scale not positive), DFLASH_ERR_WORKSPACE (only where the norm is computed). */
 typedef struct {

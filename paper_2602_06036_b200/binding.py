@@ -302,7 +302,7 @@ class AdamwPlan:
         self.n = len(self.tensors)
         self.index = index
         self.table = (AdamwTensor * max(self.n, 1))()
-        written = []
+        spans = []                                            # (start, end, tensor, name) of every buffer
         for i, e in enumerate(self.tensors):
             unknown = set(e) - {"param", "grad", "exp_avg", "exp_avg_sq", "master", "exp_avg_scale", "exp_avg_sq_scale", "weight_decay", "lr_scale"}
             assert not unknown, f"tensor {i}: unknown {sorted(unknown)}"
@@ -319,8 +319,8 @@ class AdamwPlan:
                 assert t.dtype in types, f"tensor {i}: {name} has type {t.dtype}, expected {types}"
                 assert t.get_device() == index and t.is_contiguous(), f"tensor {i}: {name} has to be contiguous and on device {index}"
                 assert t.numel() == size, f"tensor {i}: {name} has {t.numel()} entries, expected {size}"
-                if name != "grad" and size:
-                    written.append((t.data_ptr(), t.data_ptr() + size * t.element_size(), i, name))
+                if size:
+                    spans.append((t.data_ptr(), t.data_ptr() + size * t.element_size(), i, name))
                 return t.data_ptr()
 
             assert e.get("master") is None or param.dtype is torch.bfloat16, f"tensor {i}: a master copy goes with a bf16 param"
@@ -330,9 +330,16 @@ class AdamwPlan:
                 address("exp_avg_sq", state, n), *((address(k, (torch.float32,), scales) if bits == 8 else None) for k in ("exp_avg_scale", "exp_avg_sq_scale")),
                 n, F32 if param.dtype is torch.float32 else BF16, F32 if e["grad"].dtype is torch.float32 else BF16, bits,
                 float(e.get("weight_decay", 0.0)), float(e.get("lr_scale", 1.0)))
-        written.sort()
-        for a, b in zip(written, written[1:]):
-            assert a[1] <= b[0], f"{a[3]} of tensor {a[2]} and {b[3]} of tensor {b[2]} overlap"
+        # what is written lies apart from everything else; gradients are only read, so that tensors may share them
+        last_read = last_written = (0, 0, 0, "")                # of the spans before, those that reach furthest
+        for s in sorted(spans):
+            reads = s[3] == "grad"
+            for a in (last_written,) if reads else (last_written, last_read):
+                assert a[1] <= s[0], f"{a[3]} of tensor {a[2]} and {s[3]} of tensor {s[2]} overlap"
+            if reads:
+                last_read = max(last_read, s, key=lambda x: x[1])
+            else:
+                last_written = s
 
 
 class DFlash:

@@ -38,3 +38,24 @@ def test_a_plan_of_another_device_is_refused(clip):
     assert not other.calls
     own.dflash_adamw_step(plan, 1, 1e-3, max_grad_norm=clip)
     assert len(own.calls) == 1 and own.calls[0].n_tensors == 1
+
+
+def test_a_gradient_over_what_the_step_writes_is_refused():
+    """Written buffers lie apart from all others; gradients may be shared."""
+    flat = torch.zeros(1000)
+    four = lambda k, n=300: flat[k:k + n]
+    e = lambda param, grad, **over: {"param": param, "grad": grad, "exp_avg": torch.zeros(len(param)), "exp_avg_sq": torch.zeros(len(param)), **over}
+    g = torch.zeros(300)
+    for bad in ([e(four(0), four(0))],                                            # its own weights
+                [e(four(0), four(299))], [e(four(299), four(0))],                 # one entry of them
+                [e(four(0), g), e(torch.zeros(100), four(100, 100))],              # inside of another tensor's
+                [e(four(100, 100), torch.zeros(100)), e(torch.zeros(1000), flat)],  # around them
+                [e(torch.zeros(1000), flat), e(torch.zeros(10), four(0, 10)), e(four(500, 100), torch.zeros(100))],      # behind a shorter gradient
+                [e(four(0), g, exp_avg=g)], [e(four(0), g, exp_avg_sq=g)],
+                [entry(grad=flat.view(BF16)[:300], master=four(0))]):
+        with pytest.raises(AssertionError, match="overlap"):
+            binding.AdamwPlan(bad, HOST)
+    for good in ([e(four(0), four(300)), e(four(600), four(300))],                # one gradient for two tensors, in between them
+                 [e(torch.zeros(1000), flat), e(torch.zeros(10), four(3, 10)), e(torch.zeros(300), four(0))],
+                 [entry(0, grad=torch.zeros(0)), entry(3)]):
+        assert binding.AdamwPlan([{**x, "grad": x["grad"].to(BF16) if x["param"].dtype is BF16 else x["grad"]} for x in good], HOST).n == len(good)
