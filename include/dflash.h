@@ -672,7 +672,7 @@ int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_
  * States: state_bits 32: exp_avg and exp_avg_sq hold m and v in fp32. state_bits 8: they hold e4m3 codes of m and of sqrt(v), with one
  * fp32 scale for each 128 entries (value = code * scale, scale = largest magnitude / 448, rounded to nearest; 0 where that magnitude is below 2^-117). The step itself uses m and v before
  * that rounding. Zeroed buffers are states of 0 in either form.
- * Where the norm is computed (max_grad_norm > 0, or grad_norm given) and is not finite (a gradient is NaN, infinite or above 1e19), the whole step is left out: nothing but
+ * Where the norm is computed (max_grad_norm > 0, or grad_norm given) and is not finite (a gradient is NaN, infinite or above 1.8e19, whose square fp32 does not hold), the whole step is left out: nothing but
  * grad_norm is written and DFLASH_DEV_NOT_FINITE is set. Without it such a gradient makes NaN of its own entry (states of 8 bits: of its
  * block's 128 states).
  * 1.0e9 weights with master copies and clipping take 5.0 ms, with states of 8 bits 3.1. Groups of four entries that lie on their borders in every buffer of a

@@ -361,11 +361,16 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) adamw_kernel(const __gri
     }
 }
 
-// sum of the squares of the entries [from, to) of 16-byte vectors at p, NORM_UNROLL a thread and THREADS apart
-template <typename G, bool WIDE>
-__device__ __forceinline__ float squares(const G* p, int64_t from, int64_t to) {
+__device__ __forceinline__ void add_square(float& s, float x) { s = fmaf(x, x, s); }
+__device__ __forceinline__ void add_square(double& s, float x) {
+    const float q = x * x;                                  // (one that fp32 does not hold stays infinite: nor could the second moment hold it)
+    s += q < CUDART_INF_F ? (double)x * (double)x : (double)q;
+}
+// sum, in S, of the squares of the entries [from, to) of 16-byte vectors at p, NORM_UNROLL a thread and THREADS apart
+template <typename S, typename G, bool WIDE>
+__device__ __forceinline__ S squares(const G* p, int64_t from, int64_t to) {
     constexpr int VE = 16 / (int)sizeof(G);
-    float s = 0.f;
+    S s = 0;
     uint4 raw[NORM_UNROLL];
 #pragma unroll
     for (int u = 0; u < NORM_UNROLL; ++u) {
@@ -377,8 +382,7 @@ __device__ __forceinline__ float squares(const G* p, int64_t from, int64_t to) {
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
                 if (i + e < from || i + e >= to) continue;
-                const float x = (float)p[i + e];
-                s = fmaf(x, x, s);
+                add_square(s, (float)p[i + e]);
             }
         }
     }
@@ -388,24 +392,19 @@ __device__ __forceinline__ float squares(const G* p, int64_t from, int64_t to) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if constexpr (sizeof(G) == 4) {
-                s = fmaf(__uint_as_float(w[k]), __uint_as_float(w[k]), s);
+                add_square(s, __uint_as_float(w[k]));
             } else {
-                const float x = __uint_as_float(w[k] << 16), y = __uint_as_float(w[k] & 0xffff0000u);
-                s = fmaf(x, x, s);
-                s = fmaf(y, y, s);
+                add_square(s, __uint_as_float(w[k] << 16));
+                add_square(s, __uint_as_float(w[k] & 0xffff0000u));
             }
         }
     }
     return s;
 }
 
-// partial[blockIdx.x] = sum of the squares of the gradients in this CTA's chunks. In the table a chunk has NORM_BYTES, and `lead` entries lie between
-// a gradient's start and the 16-byte border in front of it. The few squares of a thread and chunk are added up in fp32, those sums in double.
-template <int N>
-__global__ void __launch_bounds__(THREADS, NORM_CTAS_PER_SM) adamw_norm_kernel(const __grid_constant__ Table<N> tab, double* __restrict__ partial) {
-    __shared__ double sh[WARPS];
-    ptx::pdl_trigger();
-    ptx::pdl_wait();
+// sum of the squares of the gradients in this CTA's chunks, each thread's and chunk's added up in S, those sums in double
+template <typename S, int N>
+__device__ __forceinline__ double cta_squares(const Table<N>& tab, double* sh) {
     double sum = 0.0;
     const int64_t chunks = tab.first[tab.n];
     int k = 0;
@@ -416,12 +415,27 @@ __global__ void __launch_bounds__(THREADS, NORM_CTAS_PER_SM) adamw_norm_kernel(c
         const int64_t at = (c - tab.first[k]) * size - t.lead, from = -at, to = t.n - at;
         const bool wide = from <= 0 && to >= size;
         const char* p = reinterpret_cast<const char*>(t.grad) + at * es;
-        float s;
-        if (t.kind & 2) s = wide ? squares<__nv_bfloat16, true>(reinterpret_cast<const __nv_bfloat16*>(p), from, to) : squares<__nv_bfloat16, false>(reinterpret_cast<const __nv_bfloat16*>(p), from, to);
-        else s = wide ? squares<float, true>(reinterpret_cast<const float*>(p), from, to) : squares<float, false>(reinterpret_cast<const float*>(p), from, to);
+        S s;
+        if (t.kind & 2) s = wide ? squares<S, __nv_bfloat16, true>(reinterpret_cast<const __nv_bfloat16*>(p), from, to) : squares<S, __nv_bfloat16, false>(reinterpret_cast<const __nv_bfloat16*>(p), from, to);
+        else s = wide ? squares<S, float, true>(reinterpret_cast<const float*>(p), from, to) : squares<S, float, false>(reinterpret_cast<const float*>(p), from, to);
         sum += (double)s;
     }
-    sum = cta_sum(sum, sh);
+    return cta_sum(sum, sh);
+}
+
+// partial[blockIdx.x] = sum of the squares of the gradients in this CTA's chunks. In the table a chunk has NORM_BYTES, and `lead` entries lie between
+// a gradient's start and the 16-byte border in front of it. The 16 or 32 squares of a thread and chunk are added up in fp32, whose range they may pass together
+// (32 of 5e18) and below which squares vanish: of a sum of 2^-90 on, that is nothing. Where the sum is none such, all of them are taken in double.
+template <int N>
+__global__ void __launch_bounds__(THREADS, NORM_CTAS_PER_SM) adamw_norm_kernel(const __grid_constant__ Table<N> tab, double* __restrict__ partial) {
+    __shared__ double sh[WARPS];
+    ptx::pdl_trigger();
+    ptx::pdl_wait();
+    double sum = cta_squares<float>(tab, sh);
+    if (!(sum >= 8.0779357e-28 && sum < CUDART_INF)) {      // (all threads have the same sum)
+        __syncthreads();
+        sum = cta_squares<double>(tab, sh);
+    }
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
