@@ -615,8 +615,8 @@ int32_t dflash_block_loss(dflash_handle* h, const dflash_block_loss_args* a /*[h
  * some 1e-7 (plus 2^-24 of their size). Rows may start anywhere; of what lies between two rows up to 14 bytes on either side of a row may be read, but not used.
  * 32 rows of 151936 bf16 logits take 7 us, with 20 alternatives 10; 544 fp32 rows 52 and 57; 2048 bf16 rows 108 and 122 (64 alternatives: 139);
  * 4096 rows of 32000 52 and 69.
- * Errors: DFLASH_ERR_INVALID_ARG (null pointer, T below 4.3e-39 or not finite, bad dtype or sizes), DFLASH_ERR_UNSUPPORTED (n_tokens or n_top > 128,
- * vocab > 2^30, more than 2^28 rows). */
+ * Errors: DFLASH_ERR_INVALID_ARG (null pointer, address that is no multiple of the element's size, of 8 for stats; T below 4.3e-39 or not finite, bad dtype or
+ * sizes), DFLASH_ERR_UNSUPPORTED (n_tokens or n_top > 128, vocab > 2^30, more than 2^28 rows). */
 typedef struct {
     const void*    logits;        /* [device] [n_rows, vocab]                                   */
     int32_t        logits_dtype;  /* DFLASH_F32 | DFLASH_BF16                                   */
@@ -642,7 +642,7 @@ int32_t dflash_token_logprobs(dflash_handle* h, const dflash_token_logprobs_args
  * stats (and entropy, where d_entropy is given) are those of the forward call with the same logits and temperature. dlogits may be
  * the logits' own buffer if dtype and stride agree (otherwise the two must not overlap). One launch; reads the logits once and writes the gradient once
  * (4096 rows of 151936 bf16 logits: 385 us).
- * Errors as above; DFLASH_ERR_UNSUPPORTED also for more than 2^31 pieces of 8192 entries. */
+ * Errors as above (stats: 4); DFLASH_ERR_UNSUPPORTED also for more than 2^31 pieces of 8192 entries. */
 typedef struct {
     const void*    logits;             /* [device] [n_rows, vocab]                              */
     int32_t        logits_dtype;       /* DFLASH_F32 | DFLASH_BF16                              */
@@ -679,8 +679,8 @@ int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_
  * tensor (all starts multiples of 4 entries, or equally far behind one) are what is fast; states of 8 bits need the former.
  * Launches: one per 320 tensors, twice with the norm. Captured calls may be replayed: lr_dev and step_dev are then read at each replay. No buffer that a
  * call writes may overlap another one of its buffers (gradients may be shared by tensors); calls must not overlap in time if they share tensors or a workspace.
- * Errors: DFLASH_ERR_INVALID_ARG (null pointer, address that is no multiple of the element's size, n < 0, bad dtype or state_bits, a master copy beside an fp32 param,
- * step < 1, betas outside [0, 1), eps below 2^-126, grad_scale not positive), DFLASH_ERR_WORKSPACE (only where the norm is computed). */
+ * Errors: DFLASH_ERR_INVALID_ARG (null pointer, address of any argument that is no multiple of the element's size, n < 0, bad dtype or state_bits, a master
+ * copy beside an fp32 param, step < 1, betas outside [0, 1), eps below 2^-126, grad_scale not positive), DFLASH_ERR_WORKSPACE (only where the norm is computed). */
 typedef struct {
     void*       param;             /* [device] in/out [n] (out only with `master`)              */
     const void* grad;              /* [device] [n]                                              */

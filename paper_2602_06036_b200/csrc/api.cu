@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 
 using namespace dflash;
@@ -805,6 +806,12 @@ int32_t dflash_block_attention_bwd(dflash_handle* h, const dflash_attn_bwd_args*
 // ---- log probabilities ----
 static bool is_dtype(int32_t d) { return d == DFLASH_F32 || d == DFLASH_BF16; }
 static bool on_elements(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % elem_size(dtype) == 0; }
+// addresses of 32-bit numbers
+static bool on_words(std::initializer_list<const void*> all) {
+    uintptr_t bits = 0;
+    for (const void* p : all) bits |= reinterpret_cast<uintptr_t>(p);
+    return (bits & 3) == 0;
+}
 // 1 / T and log2(e) / T are factors of the kernels
 static bool is_temperature(float t) { return t > 0.f && std::isfinite(t) && std::isfinite((float)(1.4426950408889634 / (double)t)); }
 constexpr int32_t MAX_VOCAB = 1 << 30, MAX_LOGIT_ROWS = 1 << 28;      // the kernels count entries of a row, and their CTAs, in 32 bits
@@ -817,7 +824,7 @@ int32_t dflash_token_logprobs(dflash_handle* h, const dflash_token_logprobs_args
     if (a->n_rows == 0) return DFLASH_OK;
     if (!a->logits || !on_elements(a->logits, a->logits_dtype) || (a->row_stride && a->row_stride < a->vocab)) return DFLASH_ERR_INVALID_ARG;
     if ((a->n_tokens > 0 && (!a->tokens || !a->logprob)) || (a->n_top > 0 && (!a->top_ids || !a->top_logprob))) return DFLASH_ERR_INVALID_ARG;
-    if (reinterpret_cast<uintptr_t>(a->stats) & 7) return DFLASH_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(a->stats) & 7) || !on_words({a->tokens, a->logprob, a->entropy, a->top_ids, a->top_logprob, a->dev_status})) return DFLASH_ERR_INVALID_ARG;
     Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
     RUN(FAM_MISC, launch_token_logprobs(L, *a));
     return DFLASH_OK;
@@ -834,6 +841,7 @@ int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_
     if (!a->logits || !a->dlogits || !a->stats || (a->n_tokens > 0 && (!a->tokens || !a->d_logprob)) || (a->d_entropy && !a->entropy) || ld < a->vocab ||
         d_ld < a->vocab || !on_elements(a->logits, a->logits_dtype) || !on_elements(a->dlogits, a->dlogits_dtype))
         return DFLASH_ERR_INVALID_ARG;
+    if (!on_words({a->tokens, a->stats, a->entropy, a->d_logprob, a->d_entropy, a->dev_status})) return DFLASH_ERR_INVALID_ARG;
     if (a->logits == a->dlogits && (a->logits_dtype != a->dlogits_dtype || ld != d_ld)) return DFLASH_ERR_INVALID_ARG;
     Launch L{h, (cudaStream_t)stream, a->dev_status, nullptr};
     RUN(FAM_MISC, launch_token_logprobs_bwd(L, *a));
@@ -851,6 +859,7 @@ int32_t dflash_adamw_step(dflash_handle* h, const dflash_adamw_args* a, void* st
     if (!(a->beta1 >= 0.0 && a->beta1 < 1.0 && a->beta2 >= 0.0 && a->beta2 < 1.0) || !((float)a->eps >= 1.17549435e-38f) || !std::isfinite((float)a->eps) || !((float)a->grad_scale > 0.f) ||
         !std::isfinite((float)a->grad_scale) || std::isnan(a->max_grad_norm))
         return DFLASH_ERR_INVALID_ARG;
+    if (!on_words({a->step_dev, a->lr_dev, a->grad_norm, a->dev_status})) return DFLASH_ERR_INVALID_ARG;
     if ((!a->step_dev && a->step < 1) || (!a->lr_dev && !std::isfinite((float)a->lr))) return DFLASH_ERR_INVALID_ARG;
     for (int i = 0; i < a->n_tensors; ++i) {
         const dflash_adamw_tensor& t = a->tensors[i];
