@@ -11,6 +11,7 @@
 #include "logprobs.cuh"
 #include "softmax_rows.cuh"
 
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -788,16 +789,16 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) token_logprobs_kernel(c
 template <typename T, int CS, class C>
 cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
     constexpr int SM_SMEM = 228 * 1024, CTA_EXTRA = 2048;      // what an SM has, and what a CTA takes beside its dynamic part, rounded up
-    static bool attr_set[MAX_DEVICES] = {};
-    static int alone[MAX_DEVICES] = {};                        // clusters that fit at one CTA per SM
+    static std::atomic<int> fits[MAX_DEVICES] = {};            // clusters that fit at one CTA per SM; 0: not asked yet. (One variable: two handles may ask at once.)
     const int dev = current_device_slot(), words = Layout(p.n_top, CS, C::THREADS).words * 8;
     if (dev < 0) return cudaErrorInvalidDevice;
     const auto kernel = token_logprobs_kernel<T, CS, C>;
-    if (!attr_set[dev]) {
+    int alone = fits[dev].load(std::memory_order_acquire);
+    if (alone == 0) {
         const int most = SM_SMEM - 1024 - CTA_EXTRA;
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
         if (e != cudaSuccess) return e;
-        int n = sm_count;
+        alone = sm_count;
         if (CS > 1) {
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(CS);
@@ -809,12 +810,11 @@ cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st
             attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
             cfg.attrs = attr;
             cfg.numAttrs = 1;
-            if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) n = std::max(1, sm_count / CS);
+            if (cudaOccupancyMaxActiveClusters(&alone, kernel, &cfg) != cudaSuccess || alone < 1) alone = std::max(1, sm_count / CS);
         }
-        alone[dev] = n;
-        attr_set[dev] = true;
+        fits[dev].store(alone, std::memory_order_release);
     }
-    const int per_sm = std::max(1, std::min(C::PER_SM, (p.n_rows + alone[dev] - 1) / alone[dev]));
+    const int per_sm = std::max(1, std::min(C::PER_SM, (p.n_rows + alone - 1) / alone));
     const size_t smem = std::max<size_t>((size_t)STAGES * C::TILE_BYTES + words, per_sm < C::PER_SM ? SM_SMEM / (per_sm + 1) : 0);
     if (CS == 1) return launch_pdl(kernel, dim3(std::min(p.n_rows, C::PER_SM * sm_count)), dim3(C::THREADS), smem, st, p);
     return launch_pdl_cluster(kernel, dim3(p.n_rows * CS), dim3(C::THREADS), smem, st, CS, p);
