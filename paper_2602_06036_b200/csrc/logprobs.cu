@@ -9,7 +9,7 @@
 // Bound: fp32 by HBM (2048 x 151936: 181 us, the measured copy rate); bf16 by the special-function unit besides, one exponential an entry being 91 us of 108 there,
 // and by issue (7 slots an entry). With alternatives the search adds 14 (20 of them) to 31 us (64), when its CTAs' rows end together.
 #include "logprobs.cuh"
-#include "softmax_rows.cuh"
+#include "logit_math.cuh"
 
 #include <atomic>
 #include <cmath>

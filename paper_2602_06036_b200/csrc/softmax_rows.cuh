@@ -3,28 +3,13 @@
 // and the merge of a row's segments by a group of lanes.
 #pragma once
 
-#include "dflash_internal.h"
-#include "ptx_sm100.cuh"
-
-#include <math_constants.h>
-
-#include <algorithm>
+#include "logit_math.cuh"
 
 namespace dflash {
 namespace {
 
 constexpr int MAX_STAT_SEG = 16;   // segments of a row's softmax statistics
-constexpr float LOG2E = 1.4426950408889634f;
 
-// 2^x by the special-function unit alone (2 ulp, results below 2^-126 flush to zero): for sums of many
-// exponentials, where the library routine's extra range handling is most of a term's cost
-__device__ __forceinline__ float fast_exp2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float as_f(float v) { return v; }
-__device__ __forceinline__ float as_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float ld_logit(const void* row, int bf16, int i) {
     return bf16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[i]) : reinterpret_cast<const float*>(row)[i];
 }
@@ -48,18 +33,6 @@ __device__ __forceinline__ void stat_raise(float2& t, float m_new, float c) {   
     if (m_new > t.x) {
         t.y = t.x > -CUDART_INF_F ? t.y * exp2f((t.x - m_new) * c) : 0.f;
         t.x = m_new;
-    }
-}
-
-__device__ __forceinline__ void unpack16(const uint4& v, float (&f)[4], float) {
-    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
-}
-__device__ __forceinline__ void unpack16(const uint4& v, float (&f)[8], __nv_bfloat16) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        f[2 * k] = __uint_as_float(w[k] << 16);
-        f[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
     }
 }
 
