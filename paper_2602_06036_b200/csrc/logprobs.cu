@@ -858,6 +858,7 @@ cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st
 
 // ---- gradient ----------------------------------------------------------------------------------------------------------
 constexpr int GROUP = 8;                                       // groups of 8 entries a thread
+constexpr float GONE = -150.f;                                 // p = 2^y is 0 below, and its factor, which grows with -y, has to stay finite
 
 struct BackwardParams {
     const void* logits;
@@ -867,7 +868,8 @@ struct BackwardParams {
     int32_t* status;
     int64_t ld, d_ld;
     int32_t vocab, n_tokens, pieces, per_piece;                // entries of a piece: a multiple of GROUP
-    float inv_t, c;
+    float c;
+    float scale, inv_t;            // gradients are added up times `scale`, a power of two; inv_t = 1 / (T scale)
 };
 
 // A group's 16-byte vectors from the border in front of it on: `off` entries lie between the two (OFF: which is not 0, and takes one vector more)
@@ -940,7 +942,7 @@ __global__ void __launch_bounds__(B_THREADS) token_logprobs_bwd_kernel(const Bac
     int tok = -1;
     float g = 0.f, z_tok = 0.f;
     const float top = p.stats[2 * (int64_t)r], log_sum = p.stats[2 * (int64_t)r + 1];
-    const float gh = p.d_entropy ? p.d_entropy[r] : 0.f, h = p.d_entropy ? p.entropy[r] : 0.f;
+    const float gh_in = p.d_entropy ? p.d_entropy[r] : 0.f, h = p.d_entropy ? p.entropy[r] : 0.f;
     if (tid < p.n_tokens) {
         tok = p.tokens[(int64_t)r * p.n_tokens + tid];
         g = p.d_logprob[(int64_t)r * p.n_tokens + tid];
@@ -951,6 +953,8 @@ __global__ void __launch_bounds__(B_THREADS) token_logprobs_bwd_kernel(const Bac
         }
         if (tok < 0) g = 0.f;
     }
+    const bool some = g != 0.f;
+    g *= p.scale;
     if (tid < MOST) {
         reinterpret_cast<int*>(s_tok)[tid] = tok;
         reinterpret_cast<float*>(s_g)[tid] = g;
@@ -959,16 +963,16 @@ __global__ void __launch_bounds__(B_THREADS) token_logprobs_bwd_kernel(const Bac
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if ((tid & 31) == 0) s_sum[tid >> 5] = sum;
-    const int any = __syncthreads_or(g != 0.f);
+    const int any = __syncthreads_or(some);
     sum = 0.f;
 #pragma unroll
     for (int w = 0; w < MOST / 32; ++w) sum += s_sum[w];
-    const bool off_row = (!any && gh == 0.f) || (top == -CUDART_INF_F && log_sum == 0.f);      // nothing comes in, or a row of -inf
+    const bool off_row = (!any && gh_in == 0.f) || (top == -CUDART_INF_F && log_sum == 0.f);      // nothing comes in, or a row of -inf
     // with y = log2 p = (z - top) c - log_sum / ln 2:  dz = p (a + b y)
-    const float sub = log_sum * LOG2E, a = -(sum + gh * h) * p.inv_t, b = -gh * LN2 * p.inv_t;
+    const float gh = gh_in * p.scale, sub = log_sum * LOG2E, a = -(sum + gh * h) * p.inv_t, b = -gh * LN2 * p.inv_t;
     auto grad = [&](float v) {
         const float y = fmaf(v - top, p.c, -sub);
-        return fast_exp2(y) * fmaf(b, fmaxf(y, FAR), a);
+        return fast_exp2(y) * fmaf(b, fmaxf(y, GONE), a);
     };
     // ---- the piece: groups whose stores lie on 16-byte borders; their loads begin `off` entries behind one, and their vectors have to lie inside of the row
     constexpr int AZ = 16 / (int)sizeof(T), AO = 16 / (int)sizeof(O);
@@ -1068,7 +1072,11 @@ int launch_token_logprobs_bwd(const Launch& L, const dflash_token_logprobs_bwd_a
     p.dlogits = a.dlogits; p.status = L.status;
     p.ld = a.row_stride ? a.row_stride : a.vocab; p.d_ld = a.dlogits_row_stride ? a.dlogits_row_stride : a.vocab;
     p.vocab = a.vocab; p.n_tokens = a.n_tokens;
-    p.inv_t = (float)(1.0 / (double)a.temperature); p.c = (float)(1.4426950408889634 / (double)a.temperature);
+    p.c = (float)(1.4426950408889634 / (double)a.temperature);
+    // The sum of a row's gradients may pass fp32's range where 1 / T brings it back. 2^-8 does for the most of them and the largest entropy; a factor that is not
+    // below 1 / T takes nothing from those whose share is a normal number.
+    p.scale = std::ldexp(1.f, -std::min(8, std::max(0, std::ilogb(a.temperature))));
+    p.inv_t = (float)(1.0 / ((double)a.temperature * (double)p.scale));
     const bool in16 = a.logits_dtype == DFLASH_BF16, out16 = a.dlogits_dtype == DFLASH_BF16;
     cudaError_t e;
     if (in16) e = out16 ? launch_backward<__nv_bfloat16, __nv_bfloat16>(p, a.n_rows, L.h->sm_count, L.st) : launch_backward<__nv_bfloat16, float>(p, a.n_rows, L.h->sm_count, L.st);
