@@ -103,6 +103,10 @@ template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }      // all but the latest N groups have landed
 
 // ---- statistics ----------------------------------------------------------------------------------------------------
+// (z - m) c and (z - m) / T by way of half the difference, which is the same but for numbers below 2^-125: the difference of two logits may pass fp32's
+// range where c or 1 / T brings it back.
+__device__ __forceinline__ float difference_times(float z, float m, float c) { return 2.f * (fmaf(z, 0.5f, -0.5f * m) * c); }
+__device__ __forceinline__ float difference_over(float z, float m, float t) { return 2.f * (fmaf(z, 0.5f, -0.5f * m) / t); }
 // m: maximum, s: sum of 2^((z - m) c), w: sum of 2^((z - m) c) (z - m) c
 struct Stat {
     float m, s, w;
@@ -110,7 +114,7 @@ struct Stat {
 // to a maximum `to` that is not smaller
 __device__ __forceinline__ Stat raised(const Stat& a, float to, float c) {
     if (a.m == to) return a;
-    const float d = a.m == -CUDART_INF_F ? FAR : fmaxf((a.m - to) * c, FAR), f = fast_exp2(d);
+    const float d = a.m == -CUDART_INF_F ? FAR : fmaxf(difference_times(a.m, to, c), FAR), f = fast_exp2(d);
     return Stat{to, a.s * f, (a.w + a.s * d) * f};
 }
 __device__ __forceinline__ Stat merged(const Stat& a, const Stat& b, float c) {
@@ -193,7 +197,7 @@ struct Running {
         plain = !(fabsf(r) < 1048576.f && c < 1.0e8f && c > 1.0e-20f);
         neg_r = -r;
         rest = plain ? 0.f : fmaf(to, c, -r);
-        const float d = old == -CUDART_INF_F ? FAR : fmaxf((old - to) * c, FAR) - old_rest + rest, f = fast_exp2(d);
+        const float d = old == -CUDART_INF_F ? FAR : fmaxf(difference_times(old, to, c), FAR) - old_rest + rest, f = fast_exp2(d);
         const float2 a = halves(s), b = halves(w);
         s = pair(a.x * f, a.y * f);
         w = pair((b.x + a.x * d) * f, (b.y + a.y * d) * f);
@@ -228,7 +232,7 @@ struct Running {
         const float base = m == -CUDART_INF_F ? 0.f : m;       // every term is 0 then
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float y = (f[e] - base) * c, x = fast_exp2(y);
+            const float y = difference_times(f[e], base, c), x = fast_exp2(y);
             a.x += x;
             b.x = fmaf(x, fmaxf(y, FAR), b.x);
         }
@@ -734,7 +738,7 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) token_logprobs_kernel(c
             }
             if (tid < p.n_tokens) {
                 float lp = 0.f;
-                if (tok >= 0 && tok < p.vocab) lp = empty ? -CUDART_INF_F : (z_tok - x.m) / p.temperature - log_sum;
+                if (tok >= 0 && tok < p.vocab) lp = empty ? -CUDART_INF_F : difference_over(z_tok, x.m, p.temperature) - log_sum;
                 p.logprob[(int64_t)r * p.n_tokens + tid] = lp;
             }
         }
@@ -745,7 +749,7 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) token_logprobs_kernel(c
             if constexpr (CS == 1) {
                 if (place < p.n_top) {
                     ids[place] = index_of(key);
-                    lps[place] = (value_of(key) - x.m) / p.temperature - log_sum;
+                    lps[place] = difference_over(value_of(key), x.m, p.temperature) - log_sum;
                 }
             } else {
                 // a key's place in the row: its place in the CTA's own list and the number of larger ones in each other list, one lane a list
@@ -771,7 +775,7 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) token_logprobs_kernel(c
                     for (int o = CS / 2; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
                     if (q == 0 && i < n_list && above < p.n_top) {
                         ids[above] = index_of(k);
-                        lps[above] = (value_of(k) - x.m) / p.temperature - log_sum;
+                        lps[above] = difference_over(value_of(k), x.m, p.temperature) - log_sum;
                     }
                 }
             }
@@ -868,7 +872,7 @@ struct BackwardParams {
     int32_t* status;
     int64_t ld, d_ld;
     int32_t vocab, n_tokens, pieces, per_piece;                // entries of a piece: a multiple of GROUP
-    float c;
+    float part, c;                 // (z - M) log2(e) / T = (part z - part M) c: halves, whose difference stays in range, where T > 1; the whole elsewhere
     float scale, inv_t;            // gradients are added up times `scale`, a power of two; inv_t = 1 / (T scale)
 };
 
@@ -969,9 +973,9 @@ __global__ void __launch_bounds__(B_THREADS) token_logprobs_bwd_kernel(const Bac
     for (int w = 0; w < MOST / 32; ++w) sum += s_sum[w];
     const bool off_row = (!any && gh_in == 0.f) || (top == -CUDART_INF_F && log_sum == 0.f);      // nothing comes in, or a row of -inf
     // with y = log2 p = (z - top) c - log_sum / ln 2:  dz = p (a + b y)
-    const float gh = gh_in * p.scale, sub = log_sum * LOG2E, a = -(sum + gh * h) * p.inv_t, b = -gh * LN2 * p.inv_t;
+    const float part = p.part, part_top = top * part, gh = gh_in * p.scale, sub = log_sum * LOG2E, a = -(sum + gh * h) * p.inv_t, b = -gh * LN2 * p.inv_t;
     auto grad = [&](float v) {
-        const float y = fmaf(v - top, p.c, -sub);
+        const float y = fmaf(fmaf(v, part, -part_top), p.c, -sub);
         return fast_exp2(y) * fmaf(b, fmaxf(y, GONE), a);
     };
     // ---- the piece: groups whose stores lie on 16-byte borders; their loads begin `off` entries behind one, and their vectors have to lie inside of the row
@@ -1072,7 +1076,8 @@ int launch_token_logprobs_bwd(const Launch& L, const dflash_token_logprobs_bwd_a
     p.dlogits = a.dlogits; p.status = L.status;
     p.ld = a.row_stride ? a.row_stride : a.vocab; p.d_ld = a.dlogits_row_stride ? a.dlogits_row_stride : a.vocab;
     p.vocab = a.vocab; p.n_tokens = a.n_tokens;
-    p.c = (float)(1.4426950408889634 / (double)a.temperature);
+    p.part = a.temperature > 1.f ? 0.5f : 1.f;
+    p.c = (float)(1.4426950408889634 / (double)a.temperature / (double)p.part);
     // The sum of a row's gradients may pass fp32's range where 1 / T brings it back. 2^-8 does for the most of them and the largest entropy; a factor that is not
     // below 1 / T takes nothing from those whose share is a normal number.
     p.scale = std::ldexp(1.f, -std::min(8, std::max(0, std::ilogb(a.temperature))));
