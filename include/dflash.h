@@ -760,6 +760,11 @@ int32_t dflash_gemm_plan_check(int32_t M, int32_t N, int32_t K, int32_t n_groups
 int32_t dflash_prefix_plan_check(const dflash_handle* h, int32_t batch, int32_t rows, int32_t n_groups, const int32_t* group_start,
                                  const int32_t* prefix_len, const int32_t* ctx_len, int32_t max_ctx_len, int64_t* info /*[host] [6] or NULL*/);
 
+/* How dflash_token_logprobs cuts up a call of such sizes (no CUDA work). info: threads of a CTA, CTAs of a row, CTAs in all; where those are fewer than the
+ * rows' a CTA goes through several rows. The paper has no counterpart: a test aid. */
+int32_t dflash_token_logprobs_plan(const dflash_handle* h, int32_t logits_dtype, int32_t n_rows, int32_t vocab, int32_t n_tokens, int32_t n_top,
+                                   int32_t* info /*[host] [3]*/);
+
 /* Static description of a return code. */
 const char* dflash_status_string(int32_t code);
 

@@ -34,7 +34,7 @@ EXPORTS = (
     "dflash_block_attention_bwd", "dflash_gemm_plan_check", "dflash_prefix_attention",
     "dflash_prefix_attention_workspace_bytes", "dflash_prefix_plan_check", "dflash_pages_copy", "dflash_pages_fork",
     "dflash_pages_resize", "dflash_pages_compact", "dflash_pages_workspace_bytes", "dflash_token_logprobs",
-    "dflash_token_logprobs_bwd", "dflash_adamw_step", "dflash_adamw_workspace_bytes",
+    "dflash_token_logprobs_bwd", "dflash_token_logprobs_plan", "dflash_adamw_step", "dflash_adamw_workspace_bytes",
 )
 N_FAMILIES = 15
 
@@ -243,6 +243,8 @@ def load():
     i32p = C.POINTER(C.c_int32)
     lib.dflash_prefix_plan_check.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, i32p, i32p, i32p, C.c_int32, C.POINTER(C.c_int64)]
     lib.dflash_prefix_plan_check.restype = C.c_int32
+    lib.dflash_token_logprobs_plan.argtypes = [C.c_void_p] + [C.c_int32] * 5 + [i32p]
+    lib.dflash_token_logprobs_plan.restype = C.c_int32
     lib.dflash_status_string.argtypes = [C.c_int32]
     lib.dflash_status_string.restype = C.c_char_p
     lib.dflash_launch_count.argtypes = []

@@ -883,6 +883,13 @@ int32_t dflash_adamw_step(dflash_handle* h, const dflash_adamw_args* a, void* st
     return DFLASH_OK;
 }
 
+int32_t dflash_token_logprobs_plan(const dflash_handle* h, int32_t logits_dtype, int32_t n_rows, int32_t vocab, int32_t n_tokens, int32_t n_top, int32_t* info) {
+    if (!h || !info || !is_dtype(logits_dtype) || n_rows < 1 || vocab < 1 || n_tokens < 0 || n_top < 0) return DFLASH_ERR_INVALID_ARG;
+    if (n_tokens > LP_MAX_TOKENS || n_top > LP_MAX_TOP || vocab > MAX_VOCAB || n_rows > MAX_LOGIT_ROWS) return DFLASH_ERR_UNSUPPORTED;
+    token_logprobs_plan(elem_size(logits_dtype), n_rows, vocab, n_tokens, n_top, h->sm_count, info);
+    return DFLASH_OK;
+}
+
 int32_t dflash_gemm_plan_check(int32_t M, int32_t N, int32_t K, int32_t n_groups, int32_t sm_count, int32_t pair_cap,
                                int32_t cluster_cap, int32_t* info) {
     return dflash::gemm_plan_check(M, N, K, n_groups, sm_count, pair_cap, cluster_cap, info);

@@ -791,7 +791,7 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) token_logprobs_kernel(c
 // The rows by clusters of CS CTAs. Clusters are placed on as few SMs as hold them, while others idle; so a CTA takes a share of
 // the SM's shared memory that leaves room for `per_sm` of them and no more (32 x 151936 bf16, four CTAs a row: 9.8 us with room for four, 6.9 for one).
 template <typename T, int CS, class C>
-cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
+cudaError_t launch_forward(const ForwardParams& p, int grid, int sm_count, cudaStream_t st) {
     constexpr int SM_SMEM = 228 * 1024, CTA_EXTRA = 2048;      // what an SM has, and what a CTA takes beside its dynamic part, rounded up
     static std::atomic<int> fits[MAX_DEVICES] = {};            // clusters that fit at one CTA per SM; 0: not asked yet. (One variable: two handles may ask at once.)
     const int dev = current_device_slot(), words = Layout(p.n_top, CS, C::THREADS).words * 8;
@@ -820,43 +820,54 @@ cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st
     }
     const int per_sm = std::max(1, std::min(C::PER_SM, (p.n_rows + alone - 1) / alone));
     const size_t smem = std::max<size_t>((size_t)STAGES * C::TILE_BYTES + words, per_sm < C::PER_SM ? SM_SMEM / (per_sm + 1) : 0);
-    if (CS == 1) return launch_pdl(kernel, dim3(std::min(p.n_rows, C::PER_SM * sm_count)), dim3(C::THREADS), smem, st, p);
-    return launch_pdl_cluster(kernel, dim3(p.n_rows * CS), dim3(C::THREADS), smem, st, CS, p);
+    if (CS == 1) return launch_pdl(kernel, dim3(grid), dim3(C::THREADS), smem, st, p);
+    return launch_pdl_cluster(kernel, dim3(grid), dim3(C::THREADS), smem, st, CS, p);
 }
 
-template <typename T>
-cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
+// How a call is cut up: threads of a CTA, CTAs of a row, CTAs
+struct Form {
+    int threads, cs, grid;
+};
+Form forward_form(int es, int n_rows, int vocab, int n_tokens, int n_top, int sm_count) {
     using Wide = Cta<256>;
-    constexpr int TILE = Wide::TILE, CTAS_PER_SM = Wide::PER_SM;
     // Short rows that are many: smaller CTAs, and so more rows under way an SM. What a row costs beside its tiles (barriers, sums, the search) then overlaps with other rows'
     // work, and less of its last tile is empty. Worth it once there are rows for all CTAs of the next larger size: bf16, 20 alternatives, 64 x 1024 with 256, 128 and
     // 64 threads 5.6, 5.5 and 5.9 us, 1200 x 1024 17.4, 11.5 and 8.0. In long rows the bound from fewer threads leaves larger cells to be read again, of fp32
     // sooner, whose pass HBM holds already: bf16 4096 x 50257 120 and 97 us with 256 and 128, 2048 x 151936 128 and 133 (64 alternatives: 65536 80 and 85,
     // 32000 105 and 98); fp32 4096 x 14000 70 and 57, 32000 101 and 103; with 128 and 64 bf16 4096 x 5003 40 and 29, 16384 44 and 42, fp32 16384 62 and 67.
-    const int64_t row = (int64_t)p.vocab * (int64_t)sizeof(T), few = (int64_t)(p.n_top <= 32 ? 112 : 64) << (sizeof(T) == 4 ? 9 : 10);
-    if (row <= 32 << 10 && p.n_rows >= Cta<128>::PER_SM * sm_count && takes(64, p.n_top, p.n_tokens)) return launch_forward<T, 1, Cta<64>>(p, sm_count, st);
-    if (row <= few && p.n_rows >= Wide::PER_SM * sm_count && takes(128, p.n_top, p.n_tokens)) return launch_forward<T, 1, Cta<128>>(p, sm_count, st);
+    const int64_t row = (int64_t)vocab * es, few = (int64_t)(n_top <= 32 ? 112 : 64) << (es == 4 ? 9 : 10);
+    const auto alone = [&](int threads, int per_sm) { return Form{threads, 1, std::min(n_rows, per_sm * sm_count)}; };
+    if (row <= 32 << 10 && n_rows >= Cta<128>::PER_SM * sm_count && takes(64, n_top, n_tokens)) return alone(64, Cta<64>::PER_SM);
+    if (row <= few && n_rows >= Wide::PER_SM * sm_count && takes(128, n_top, n_tokens)) return alone(128, Cta<128>::PER_SM);
     // CTAs per row: what takes the least time by a count of tile times. CTAs that share an SM share its rate, so that what counts is how evenly a turn of
     // CTAs fills the SMs; beside its tiles a turn takes the time of 4 tiles (9 with the search), and a cluster's meeting that of 2 to 4. (A tile time is
     // 0.46 us. 32 x 151936 bf16 by 1, 2, 4 and 8 CTAs a row: 14, 10, 7 and 8 us; 300 rows 26, 25, 27 and 38, with 20 alternatives 31, 32, 37 and 57; 800 rows
     // 57, 49, 61 and 91. The rule is up to a tenth off the best of the four.)
-    const int tiles = (p.vocab + TILE * Row<T>::VE - 1) / (TILE * Row<T>::VE);
-    const int64_t slots = (int64_t)CTAS_PER_SM * sm_count;
+    const int tile = Wide::TILE_BYTES / es, tiles = (vocab + tile - 1) / tile;
+    const int64_t slots = (int64_t)Wide::PER_SM * sm_count;
     int cs = 1;
     int64_t least = INT64_MAX;
     for (int s = 1; s <= MAX_CLUSTER && s / 2 < tiles; s *= 2) {
-        const int64_t n = (int64_t)p.n_rows * s, full = n / slots, last = (n % slots + sm_count - 1) / sm_count, each = (tiles + s - 1) / s;
-        const int64_t time = (full * CTAS_PER_SM + last) * each + (full + (last > 0)) * (p.n_top > 0 ? 9 : 4) + (s == 1 ? 0 : s == 8 ? 4 : 2);
+        const int64_t n = (int64_t)n_rows * s, full = n / slots, last = (n % slots + sm_count - 1) / sm_count, each = (tiles + s - 1) / s;
+        const int64_t time = (full * Wide::PER_SM + last) * each + (full + (last > 0)) * (n_top > 0 ? 9 : 4) + (s == 1 ? 0 : s == 8 ? 4 : 2);
         if (time < least) {
             least = time;
             cs = s;
         }
     }
-    switch (cs) {
-        case 1: return launch_forward<T, 1, Wide>(p, sm_count, st);
-        case 2: return launch_forward<T, 2, Wide>(p, sm_count, st);
-        case 4: return launch_forward<T, 4, Wide>(p, sm_count, st);
-        default: return launch_forward<T, 8, Wide>(p, sm_count, st);
+    return cs == 1 ? alone(256, Wide::PER_SM) : Form{256, cs, n_rows * cs};
+}
+
+template <typename T>
+cudaError_t launch_forward(const ForwardParams& p, int sm_count, cudaStream_t st) {
+    const Form f = forward_form((int)sizeof(T), p.n_rows, p.vocab, p.n_tokens, p.n_top, sm_count);
+    switch (f.threads * f.cs) {
+        case 64: return launch_forward<T, 1, Cta<64>>(p, f.grid, sm_count, st);
+        case 128: return launch_forward<T, 1, Cta<128>>(p, f.grid, sm_count, st);
+        case 256: return launch_forward<T, 1, Cta<256>>(p, f.grid, sm_count, st);
+        case 512: return launch_forward<T, 2, Cta<256>>(p, f.grid, sm_count, st);
+        case 1024: return launch_forward<T, 4, Cta<256>>(p, f.grid, sm_count, st);
+        default: return launch_forward<T, 8, Cta<256>>(p, f.grid, sm_count, st);
     }
 }
 
@@ -1056,6 +1067,11 @@ cudaError_t launch_backward(const BackwardParams& p, int rows, int sm_count, cud
 }
 
 }  // namespace
+
+void token_logprobs_plan(int es, int n_rows, int vocab, int n_tokens, int n_top, int sm_count, int32_t* info) {
+    const Form f = forward_form(es, n_rows, vocab, n_tokens, n_top, sm_count);
+    info[0] = f.threads; info[1] = f.cs; info[2] = f.grid;
+}
 
 int launch_token_logprobs(const Launch& L, const dflash_token_logprobs_args& a) {
     ForwardParams p{};
