@@ -379,7 +379,8 @@ class DFlash:
 
     # ---- set-up -------------------------------------------------------------------------
     def set_weights(self, packed: Dict, rope_cos: torch.Tensor, rope_sin: torch.Tensor):
-        """`packed` = synth.pack_device_weights(...) moved to the device (any mapping with the same keys)."""
+        """`packed` = synth.pack_device_weights(...) moved to the device (any mapping with the same keys). Contiguous tensors of the handle's device are
+        held as they are, without a copy: what changes them in place (dflash_adamw_step) holds for the calls behind it on the stream."""
         dev = self.device
         keep = {k: packed[k].to(dev).contiguous() for k in ("embed", "W_c", "g_c", "g_f", "W_lm")}
         keep["layers"] = [{k: v.to(dev).contiguous() for k, v in lw.items()} for lw in packed["layers"]]
