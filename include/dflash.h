@@ -677,6 +677,8 @@ int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_
  * block's 128 states).
  * 1.0e9 weights with master copies and clipping take 5.0 ms, with states of 8 bits 3.1. Groups of four entries that lie on their borders in every buffer of a
  * tensor (all starts multiples of 4 entries, or equally far behind one) are what is fast; states of 8 bits need the former.
+ * The table names addresses: gradients have to be written where it says, a new backward pass's too (a program that frees them and lets them be made anew
+ * makes its table anew).
  * Launches: one per 320 tensors, twice with the norm. Captured calls may be replayed: lr_dev and step_dev are then read at each replay. No buffer that a
  * call writes may overlap another one of its buffers (gradients may be shared by tensors); calls must not overlap in time if they share tensors or a workspace.
  * Errors: DFLASH_ERR_INVALID_ARG (null pointer, address of any argument that is no multiple of the element's size, n < 0, bad dtype or state_bits, a master

@@ -297,7 +297,9 @@ def launch_count() -> int:
 
 
 class AdamwPlan:
-    """The tensors of an optimiser step as the library takes them (see DFlash.adamw_plan). Keeps them alive; their addresses are those of the plan."""
+    """The tensors of an optimiser step as the library takes them (see DFlash.adamw_plan). Keeps them alive; their addresses are those of the plan. So a
+    gradient has to stay where it is: after `p.grad = None` (zero_grad's default) the next backward pass makes another tensor, of which the plan knows
+    nothing. Clear gradients in place (zero_grad(set_to_none=False)), or make a new plan."""
 
     def __init__(self, entries, index: int):
         self.tensors = [dict(e) for e in entries]
