@@ -265,10 +265,9 @@ __host__ __device__ __forceinline__ int most_of(int n_top) { return n_top + n_to
 __host__ __device__ __forceinline__ int capacity_of(int n_top, int threads) { return most_of(n_top) + threads; }      // of the list: a turn's entries fit behind one that has been cut
 // what a CTA of so many threads takes: of more than half of its threads' largest entries the bound below is a weak one, and each given token has a thread
 constexpr bool takes(int threads, int n_top, int n_tokens) { return 2 * n_top <= threads && n_tokens <= threads; }
-// Cells of a thread: its part of a row in as many runs of tiles. Of more cells fewer vectors are read again (2048 x 151936 bf16 with 64 alternatives: 139 us with 16,
-// 154 with 8), but shared memory is taken from L1 in steps, which the copies under way need: 16 are worth it where they keep a CTA below 48.5 KB
-// and many candidates are looked for.
-__host__ __device__ __forceinline__ int cells_of(int n_top) { return n_top > 32 && n_top <= 64 ? 16 : 8; }
+// Cells of a thread: its part of a row in as many runs of tiles. Of more cells fewer vectors are read again, but a cell has a tile at least, and shared memory
+// is taken from L1, which the copies under way need (see `many_cells`).
+__host__ __device__ __forceinline__ int cells_of(bool many) { return many ? 16 : 8; }
 static_assert(takes(256, LP_MAX_TOP, LP_MAX_TOKENS) && 32 + 32 / 4 + 8 <= 64 && 16 * 256 <= 65536, "the most that a bound leaves has a thread each; cells in 16 bits");
 
 constexpr int BIN_BITS = 6, BINS = 1 << BIN_BITS;                   // of the range of the threads' largest entries
@@ -505,6 +504,7 @@ struct ForwardParams {
     int64_t ld;
     int32_t n_rows, vocab, n_tokens, n_top;
     float temperature, c;          // c = log2(e) / T
+    bool many;                     // cells
 };
 
 // What a CTA of a cluster tells the others about its stretch of the row
@@ -520,8 +520,8 @@ __device__ __forceinline__ void st_cluster_u64(const void* local_smem, uint32_t 
 // Shared memory behind the tiles under way, in 8-byte words: cells, list, few, what the CTAs of a cluster tell each other (twice 8 bytes each) and their keys, found
 struct Layout {
     int cells, list, few, told, keys, found, words;
-    __host__ __device__ Layout(int n_top, int cs, int threads) {
-        const int most = n_top > 0 ? most_of(n_top) : 0, n_cells = n_top > 0 ? cells_of(n_top) : 0;
+    __host__ __device__ Layout(int n_top, bool many, int cs, int threads) {
+        const int most = n_top > 0 ? most_of(n_top) : 0, n_cells = n_top > 0 ? cells_of(many) : 0;
         cells = 0;
         told = cells + n_cells * threads / 4;
         list = told + (cs > 1 ? 2 * cs : 0);
@@ -534,9 +534,9 @@ struct Layout {
 
 // The search as a call of its own: its registers are not the pass's
 template <typename T, class C>
-__device__ __noinline__ int search_stretch(const T* z, int vocab, int lo_j, int hi_j, int per_cell, float top, int n_top, int cs, unsigned long long* words, int* count,
-                                           uint32_t* ends) {
-    const Layout at(n_top, cs, C::THREADS);
+__device__ __noinline__ int search_stretch(const T* z, int vocab, int lo_j, int hi_j, int per_cell, float top, int n_top, bool many, int cs, unsigned long long* words,
+                                           int* count, uint32_t* ends) {
+    const Layout at(n_top, many, cs, C::THREADS);
     Candidates<C> cand;
     cand.list = words + at.list;
     cand.few = words + at.few;
@@ -548,7 +548,7 @@ __device__ __noinline__ int search_stretch(const T* z, int vocab, int lo_j, int 
     cand.n_top = n_top;
     cand.most = most_of(n_top);
     cand.capacity = capacity_of(n_top, C::THREADS);
-    cand.n_cells = cells_of(n_top);
+    cand.n_cells = cells_of(many);
     return cand.search(Row<T>(z, vocab), lo_j, hi_j, per_cell, top);
 }
 
@@ -584,12 +584,12 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) token_logprobs_kernel(c
     __shared__ int count[2];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = CS > 1 ? (int)ptx::cluster_ctarank() : 0;
     unsigned long long* words = reinterpret_cast<unsigned long long*>(ring + STAGES * TILE);
-    const Layout at(p.n_top, CS, THREADS);
+    const Layout at(p.n_top, p.many, CS, THREADS);
     Told* told = reinterpret_cast<Told*>(words + at.told);
     unsigned long long* keys = words + at.keys;
     unsigned long long* list = words + at.list;
     uint16_t* cells = reinterpret_cast<uint16_t*>(words + at.cells);
-    const int n_cells = cells_of(p.n_top);
+    const int n_cells = cells_of(p.many);
     ptx::pdl_trigger();
     ptx::pdl_wait();
     if constexpr (CS > 1) ptx::cluster_arrive();           // (waited for before the first store into another CTA)
@@ -699,7 +699,7 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) token_logprobs_kernel(c
         Stat x = lanes_merged<32>(t.total(peak, p.c), p.c);
         if (lane == 0) sh[warp] = x;
         int n_list = 0;
-        if (p.n_top > 0) n_list = search_stretch<T, C>(reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld, p.vocab, cur.lo, cur.hi, per_cell, peak, p.n_top, CS, words, count, ends);
+        if (p.n_top > 0) n_list = search_stretch<T, C>(reinterpret_cast<const T*>(p.logits) + (int64_t)r * p.ld, p.vocab, cur.lo, cur.hi, per_cell, peak, p.n_top, p.many, CS, words, count, ends);
         else __syncthreads();
         x = lanes_merged<WARPS>(sh[lane % WARPS], p.c);
         const int lanes = lanes_a_key<THREADS>(n_list), own = tid / lanes;
@@ -788,13 +788,23 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) token_logprobs_kernel(c
     }
 }
 
+// Whether a CTA keeps 16 cells a thread instead of 8: where its part of a row has more than 8 tiles, more than 32 alternatives are looked for, and a full SM's CTAs
+// stay within 196 KB of shared memory, the last step that leaves L1 more than a few. 2048 x 151936 bf16 (10 tiles) with 33, 48, 64, 80 and 100 alternatives, 8 cells 124, 133, 140,
+// 148 and 161 us, 16 cells 126, 132, 138, 143 and 202 (the last passes 196 KB); 544 x 151936 fp32 with 64 68 and 64; 2 tiles, 4096 x 32000 bf16 with 64, 87 and 98.
+template <class C>
+bool many_cells(int tiles, int n_top, int cs) {
+    constexpr int STATIC = 512, PER_CTA = 1024, STEP = 196 * 1024;      // static shared memory, what the system takes of each CTA
+    return tiles > 8 && n_top > 32 && C::PER_SM * (STAGES * C::TILE_BYTES + Layout(n_top, true, cs, C::THREADS).words * 8 + STATIC + PER_CTA) <= STEP;
+}
+
 // The rows by clusters of CS CTAs. Clusters are placed on as few SMs as hold them, while others idle; so a CTA takes a share of
 // the SM's shared memory that leaves room for `per_sm` of them and no more (32 x 151936 bf16, four CTAs a row: 9.8 us with room for four, 6.9 for one).
 template <typename T, int CS, class C>
-cudaError_t launch_forward(const ForwardParams& p, int grid, int sm_count, cudaStream_t st) {
+cudaError_t launch_forward(ForwardParams p, int grid, int sm_count, cudaStream_t st) {
     constexpr int SM_SMEM = 228 * 1024, CTA_EXTRA = 2048;      // what an SM has, and what a CTA takes beside its dynamic part, rounded up
     static std::atomic<int> fits[MAX_DEVICES] = {};            // clusters that fit at one CTA per SM; 0: not asked yet. (One variable: two handles may ask at once.)
-    const int dev = current_device_slot(), words = Layout(p.n_top, CS, C::THREADS).words * 8;
+    p.many = many_cells<C>((p.vocab / Row<T>::VE + C::TILE * CS - 1) / (C::TILE * CS), p.n_top, CS);
+    const int dev = current_device_slot(), words = Layout(p.n_top, p.many, CS, C::THREADS).words * 8;
     if (dev < 0) return cudaErrorInvalidDevice;
     const auto kernel = token_logprobs_kernel<T, CS, C>;
     int alone = fits[dev].load(std::memory_order_acquire);
