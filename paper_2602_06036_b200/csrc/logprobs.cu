@@ -6,8 +6,10 @@
 // of each of a few parts of what it has seen, from which the row's n_top largest are found afterwards (see `Candidates`). Tiles come by asynchronous
 // copies into shared memory, two of them under way a CTA. Copies that go around L1 (.cg), bulk copies of 2 KB and a third tile were all slower (2048 x
 // 151936 fp32 222, 199 and 225 us against 186 at the time: L1 holds what is under way, and shared memory is taken from it).
-// Bound: fp32 by HBM (2048 x 151936: 181 us, the measured copy rate); bf16 by the special-function unit besides, one exponential an entry being 91 us of 108 there,
-// and by issue (7 slots an entry). With alternatives the search adds 14 (20 of them) to 31 us (64), when its CTAs' rows end together.
+// Bound: fp32 by HBM (2048 x 151936: 187 us, 181 being the measured copy rate). bf16 (107 us) by no single unit: 95 us of bytes, 67 of exponentials (16 a clock and SM at the
+// 1965 MHz of short runs), 70 of issue (8 slots an entry); a long run's power limit lowers the clock to some 1640 MHz and all but the first with it (125 us). With alternatives the
+// search adds 14 (20 of them) to 31 us (64), when its CTAs' rows end together. Rows of equal values cost it most (no bound keeps entries out, and they are cut down turn by turn):
+// 2048 x 151936 bf16 171 us with 20 alternatives (121 otherwise) and 355 with 64 (138), 4096 x 32000 186 with 20 (70), 32 x 151936 18 (10.5).
 #include "logprobs.cuh"
 #include "logit_math.cuh"
 
@@ -1068,8 +1070,9 @@ cudaError_t launch_backward(BackwardParams p, int rows, int sm_count, cudaStream
 template <typename T, typename O>
 cudaError_t launch_backward(const BackwardParams& p, int rows, int sm_count, cudaStream_t st) {
     // With many rows smaller CTAs overlap what a row costs before its first load and after its last store with other rows' work (64 given tokens, 4096 x 1024 bf16
-    // with 256, 128 and 64 threads 22, 14 and 12 us, x 8192 36, 29 and 27; x 151936 with 256 and 128 449 and 428). fp32 gradients of long rows are better
-    // off in larger ones (4096 x 151936 750 and 803 us, x 2049 20 and 14).
+    // with 256, 128 and 64 threads 22, 14 and 12 us, x 8192 36, 29 and 27; x 151936 with 256 and 128 449 and 428). fp32 gradients of the longest rows are
+    // better off in larger ones: one given token, 256 and 128 threads, fp32 logits 4096 x 151936 797 and 829 us, x 32000 177 and 181, x 8192 54 and 48, x 4096 31 and 27,
+    // x 2049 24 and 17; bf16 ones 650 and 652, 163 and 159, 50 and 43, 30 and 25, 24 and 16.
     constexpr bool O16 = sizeof(O) == 2;
     if (O16 && p.vocab <= 8192 && rows >= 16 * sm_count && p.n_tokens <= 64) return launch_backward<T, O, 64>(p, rows, sm_count, st);
     if ((O16 || p.vocab <= 4096) && rows >= 8 * sm_count) return launch_backward<T, O, 128>(p, rows, sm_count, st);
