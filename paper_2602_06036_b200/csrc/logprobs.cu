@@ -402,6 +402,8 @@ struct Candidates {
                         if (f[e] == top) at = row.first(j) + e;
                 }
             }
+            // (not there any more: a row that another stream writes to meanwhile. The keys have to differ all the same, or the halving would not end)
+            if (at < 0) at = max(0, row.first(vector_of(lo_j, per_cell, 0, threadIdx.x, 0)));
             best = key_of(top, at);
         }
         unsigned long long l = (unsigned long long)lo << 32 | 0xffffffffu, h = (unsigned long long)hi << 32 | 0xffffffffu;
