@@ -612,7 +612,7 @@ int32_t dflash_block_loss(dflash_handle* h, const dflash_block_loss_args* a /*[h
  * NaN in all numbers but M; NaN is never an alternative. A negative token stands for none (logprob 0), and so does one >= vocab, which
  * sets DFLASH_DEV_BAD_TOKEN. Temperature scales the distribution, not the order of the alternatives.
  * One launch and one pass over the logits, no scratch memory: calls may overlap. Sums in fp32; against exact arithmetic the log probabilities are off by
- * some 1e-7 (plus 2^-24 of their size). Rows may start anywhere; of what lies between two rows up to 14 bytes on either side of a row may be read, but not used.
+ * some 1e-7 (plus 2^-24 of their size), that of a token that is all but certain, and such a row's entropy, by some 1e-6 of themselves: 0 where no other is left. Rows may start anywhere; of what lies between two rows up to 14 bytes on either side of a row may be read, but not used.
  * 32 rows of 151936 bf16 logits take 7 us, with 20 alternatives 10.5; 544 fp32 rows 53 and 58; 2048 bf16 rows 107 and 121 (64 alternatives: 138);
  * 4096 rows of 32000 53 and 70: short runs, from a graph. Calls that follow each other for long are slower where the power limit lowers the clock (154 with 64
  * alternatives), and rows in which very many entries are equal to the n_top-th largest are searched longer (those of one value: 171 instead of 121).
