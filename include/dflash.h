@@ -613,9 +613,9 @@ int32_t dflash_block_loss(dflash_handle* h, const dflash_block_loss_args* a /*[h
  * sets DFLASH_DEV_BAD_TOKEN. Temperature scales the distribution, not the order of the alternatives.
  * One launch and one pass over the logits, no scratch memory: calls may overlap. Sums in fp32; against exact arithmetic the log probabilities are off by
  * some 1e-7 (plus 2^-24 of their size), that of a token that is all but certain, and such a row's entropy, by some 1e-6 of themselves: 0 where no other is left. Rows may start anywhere; of what lies between two rows up to 14 bytes on either side of a row may be read, but not used.
- * 32 rows of 151936 bf16 logits take 7 us, with 20 alternatives 10.5; 544 fp32 rows 53 and 58; 2048 bf16 rows 107 and 121 (64 alternatives: 138);
- * 4096 rows of 32000 53 and 70: short runs, from a graph. Calls that follow each other for long are slower where the power limit lowers the clock (154 with 64
- * alternatives), and rows in which very many entries are equal to the n_top-th largest are searched longer (those of one value: 171 instead of 121).
+ * 32 rows of 151936 bf16 logits take 7.7 us, with 20 alternatives 11; 544 fp32 rows 53 and 58; 2048 bf16 rows 108 and 122 (64 alternatives: 138);
+ * 4096 rows of 32000 53 and 71: short runs, from a graph. Calls that follow each other for long are slower where the power limit lowers the clock (149 to 155 with
+ * 64 alternatives), and rows in which very many entries are equal to the n_top-th largest are searched longer (those of one value: 172 instead of 122).
  * Errors: DFLASH_ERR_INVALID_ARG (null pointer, address that is no multiple of the element's size, of 8 for stats; T below 4.3e-39 or not finite, bad dtype or
  * sizes), DFLASH_ERR_UNSUPPORTED (n_tokens or n_top > 128, vocab > 2^30, more than 2^28 rows). */
 typedef struct {
@@ -642,7 +642,7 @@ int32_t dflash_token_logprobs(dflash_handle* h, const dflash_token_logprobs_args
  * incoming gradients are all 0 gets zeros, whatever its logits hold (they are not read), and so does a row of -inf only.
  * stats (and entropy, where d_entropy is given) are those of the forward call with the same logits and temperature. dlogits may be
  * the logits' own buffer if dtype and stride agree (otherwise the two must not overlap). One launch; reads the logits once and writes the gradient once
- * (4096 rows of 151936 logits, bf16 to bf16 395 us, to fp32 650; fp32 to bf16 544, to fp32 797).
+ * (4096 rows of 151936 logits, bf16 to bf16 385 to 395 us, to fp32 650; fp32 to bf16 544, to fp32 776 to 797).
  * Errors as above (stats: 4); DFLASH_ERR_UNSUPPORTED also for more than 2^31 pieces of 8192 entries. */
 typedef struct {
     const void*    logits;             /* [device] [n_rows, vocab]                              */

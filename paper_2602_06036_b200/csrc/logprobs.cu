@@ -6,10 +6,10 @@
 // of each of a few parts of what it has seen, from which the row's n_top largest are found afterwards (see `Candidates`). Tiles come by asynchronous
 // copies into shared memory, two of them under way a CTA. Copies that go around L1 (.cg), bulk copies of 2 KB and a third tile were all slower (2048 x
 // 151936 fp32 222, 199 and 225 us against 186 at the time: L1 holds what is under way, and shared memory is taken from it).
-// Bound: fp32 by HBM (2048 x 151936: 187 us, 181 being the measured copy rate). bf16 (107 us) by no single unit: 95 us of bytes, 67 of exponentials (16 a clock and SM at the
-// 1965 MHz of short runs), 70 of issue (8 slots an entry); a long run's power limit lowers the clock to some 1640 MHz and all but the first with it (125 us). With alternatives the
+// Bound: fp32 by HBM (2048 x 151936: 187 us, 181 being the measured copy rate). bf16 (108 us) by no single unit: 95 us of bytes, 67 of exponentials (16 a clock and SM at the
+// 1965 MHz of short runs), 70 of issue (8 slots an entry); a long run's power limit lowers the clock to some 1640 to 1720 MHz and all but the first with it (120 to 125 us). With alternatives the
 // search adds 14 (20 of them) to 31 us (64), when its CTAs' rows end together. Rows of equal values cost it most (no bound keeps entries out, and they are cut down turn by turn):
-// 2048 x 151936 bf16 171 us with 20 alternatives (121 otherwise) and 355 with 64 (138), 4096 x 32000 186 with 20 (70), 32 x 151936 18 (10.5).
+// 2048 x 151936 bf16 172 us with 20 alternatives (122 otherwise) and 358 with 64 (138), 4096 x 32000 183 with 20 (71), 32 x 151936 18 (11).
 #include "logprobs.cuh"
 #include "logit_math.cuh"
 
