@@ -845,8 +845,8 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) token_logprobs_kernel(c
 }
 
 // Whether a CTA keeps 16 cells a thread instead of 8: where its part of a row has more than 8 tiles, more than 32 alternatives are looked for, and a full SM's CTAs
-// stay within 196 KB of shared memory, the last step that leaves L1 more than a few. 2048 x 151936 bf16 (10 tiles) with 33, 48, 64, 80 and 100 alternatives, 8 cells 124, 133, 140,
-// 148 and 161 us, 16 cells 126, 132, 138, 143 and 202 (the last passes 196 KB); 544 x 151936 fp32 with 64 68 and 64; 2 tiles, 4096 x 32000 bf16 with 64, 87 and 98.
+// stay within 196 KB of shared memory, the last step that leaves L1 more than a few. 2048 x 151936 bf16 (19 tiles) with 33, 48, 64, 80 and 100 alternatives, 8 cells 124, 133, 140,
+// 148 and 161 us, 16 cells 126, 132, 138, 143 and 202 (the last passes 196 KB); 544 x 151936 fp32 with 64 68 and 64; 8 tiles, 4096 x 32000 bf16 with 64 in CTAs of 128 threads, 87 and 98.
 template <class C>
 bool many_cells(int tiles, int n_top, int cs) {
     constexpr int STATIC = 512, PER_CTA = 1024, STEP = 196 * 1024;      // static shared memory, what the system takes of each CTA

@@ -83,9 +83,9 @@ def test_ctas_that_go_through_several_rows(lib, threads, v, dtype, top, k):
 
 
 @pytest.mark.parametrize("n,v,dtype,top", [(50, 151936, BF16, 33), (444, 151936, BF16, 64), (444, 151936, F32, 80), (444, 151936, F32, 90), (1, 2000003, BF16, 40), (1, 2000003, F32, 64),
-                                           (444, 131072, BF16, 64), (444, 131073, BF16, 64), (444, 131088, BF16, 64), (444, 147456, BF16, 64)])
+                                           (444, 65536, BF16, 64), (444, 65537, BF16, 64), (444, 65544, BF16, 64), (444, 73728, BF16, 64), (444, 131072, BF16, 64), (444, 147456, BF16, 64)])
 def test_parts_of_more_than_eight_tiles(lib, n, v, dtype, top):
-    """Where a thread's part of a row is kept in 16 cells, on either side of the rule (131072 bf16 entries are 8 tiles, 147456 nine)."""
+    """Where a thread's part of a row is kept in 16 cells, on either side of the rule (65536 bf16 entries are 8 tiles)."""
     kinds = (KINDS + PARTS)[:max(1, min(n, 24))] if n > 1 else ["a value in each part"]
     z, tokens = rows_of(kinds, v, dtype, v + top), given(len(kinds), v, 2, 5)
     copies = -(-n // len(kinds))
