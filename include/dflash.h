@@ -612,7 +612,8 @@ int32_t dflash_block_loss(dflash_handle* h, const dflash_block_loss_args* a /*[h
  * NaN in all numbers but M; NaN is never an alternative. A negative token stands for none (logprob 0), and so does one >= vocab, which
  * sets DFLASH_DEV_BAD_TOKEN. Temperature scales the distribution, not the order of the alternatives.
  * One launch and one pass over the logits, no scratch memory: calls may overlap. Sums in fp32; against exact arithmetic the log probabilities are off by
- * some 1e-7 (plus 2^-24 of their size), that of a token that is all but certain, and such a row's entropy, by some 1e-6 of themselves: 0 where no other is left. Rows may start anywhere; of what lies between two rows up to 14 bytes on either side of a row may be read, but not used.
+ * some 1e-7 (plus 2^-24 of their size), that of a token that is all but certain, and such a row's entropy, by some 1e-6 of themselves: 0 where no other is
+ * left. Rows may start anywhere; of what lies between two rows up to 14 bytes on either side of a row may be read, but not used.
  * 32 rows of 151936 bf16 logits take 7.7 us, with 20 alternatives 11; 544 fp32 rows 53 and 58; 2048 bf16 rows 108 and 122 (64 alternatives: 138);
  * 4096 rows of 32000 53 and 71: short runs, from a graph. Calls that follow each other for long are slower where the power limit lowers the clock (149 to 155 with
  * 64 alternatives), and rows in which very many entries are equal to the n_top-th largest are searched longer (those of one value: 172 instead of 122).
@@ -671,11 +672,11 @@ int32_t dflash_token_logprobs_bwd(dflash_handle* h, const dflash_token_logprobs_
  * Arithmetic is fp32, the norm is added up in double in a fixed order. The weights w are `param` (fp32; or bf16, to which
  * every step is rounded to nearest, so that steps below 2^-9 of a weight are lost), or an fp32 `master` copy, which `param` (bf16) then receives rounded.
  * States: state_bits 32: exp_avg and exp_avg_sq hold m and v in fp32. state_bits 8: they hold e4m3 codes of m and of sqrt(v), with one
- * fp32 scale for each 128 entries (value = code * scale; scale = largest magnitude times 1/448, 1/448 and the product rounded to fp32; 0 where that magnitude is below 2^-117; codes rounded to nearest). The step itself uses m and v before
- * that rounding. Zeroed buffers are states of 0 in either form.
- * Where the norm is computed (max_grad_norm > 0, or grad_norm given) and is not finite (a gradient is NaN, infinite or above 1.8e19, whose square fp32 does not hold), the whole step is left out: nothing but
- * grad_norm is written and DFLASH_DEV_NOT_FINITE is set. Without it such a gradient makes NaN of its own entry (states of 8 bits: of its
- * block's 128 states).
+ * fp32 scale for each 128 entries (value = code * scale; scale = largest magnitude times 1/448, 1/448 and the product rounded to fp32; 0 where that magnitude
+ * is below 2^-117; codes rounded to nearest). The step itself uses m and v before that rounding. Zeroed buffers are states of 0 in either form.
+ * Where the norm is computed (max_grad_norm > 0, or grad_norm given) and is not finite (a gradient is NaN, infinite or above 1.8e19, whose square fp32 does
+ * not hold), the whole step is left out: nothing but grad_norm is written and DFLASH_DEV_NOT_FINITE is set. Without it such a gradient makes NaN or infinities
+ * of its own entry (states of 8 bits: NaN of its block's 128 states).
  * 1.0e9 weights with master copies and clipping take 5.0 ms, with states of 8 bits 3.3 (short runs: 3.1). Groups of four entries that lie on their borders in every buffer of a
  * tensor (all starts multiples of 4 entries, or equally far behind one) are what is fast; states of 8 bits need the former.
  * The table names addresses: gradients have to be written where it says, a new backward pass's too (a program that frees them and lets them be made anew

@@ -3,7 +3,7 @@
 //   w = w - lr wd w - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps).
 // The tensors are described in the launch's parameters (no table in device memory to keep), as many as fit one launch. A launch cuts them into
 // chunks of CHUNK entries and every CTA takes chunks in turn. Bound by HBM: 2 to 4 bytes of gradient, 4 to 10 of weights and 16 (or 4.1) of states an entry.
-// Measured without clipping for 2.5e8 weights, share of the copy rate: 32-bit states 0.94 to 0.97, 8-bit ones 0.90 beside master copies, 0.68 without (65
+// Measured without clipping for 2.5e8 weights, share of the copy rate: 32-bit states 0.94 to 0.97, 8-bit ones 0.90 beside master copies, 0.67 without (65
 // instructions an entry, a third of them roots, divisions and roundings that have to be exact, hold it then). What is under way decides: four blocks
 // of a warp and two CTAs an SM against two and four: 0.95 and 0.92, 8 bits 0.90 and 0.77. Clipping adds the reading of the gradients: 2.0e9 bytes 400 us.
 // Norm: a launch in front adds the squares up, a partial sum a CTA; each CTA of the step adds the partial sums up itself, in their order, which
